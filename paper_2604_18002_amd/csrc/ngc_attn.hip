@@ -72,6 +72,7 @@
 
 #include "../../include/ngc.h"
 #include "ngc_device.h"
+#include "ngc_workspace.h"
 
 namespace ngc {
 
@@ -613,8 +614,6 @@ void decode_kernel(AttnArgs a)
 using namespace ngc;
 
 namespace {
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-constexpr size_t STATUS_BYTES = NGC_STATUS_WORDS * sizeof(int32_t);
 // How many workgroups share a segment.  Microseconds per launch (MI355X, one launch per layer of 28 from a HIP graph, D = 128)
 // against S, best in brackets:
 //     segments x rows      S=1    2     3     4     5     6     7     8    10    12    16    24    32
@@ -705,18 +704,6 @@ bool first_tile_early(int nseg_launch, int S, int max_len, int max_len_hint)
     return max_len_hint > ATT_WAVES * ATT_TILE;
 }
 
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-// workspace layout: [status][per segment of the cache: 2 int32 of the paged layout's pool bookkeeping]
-//                   [per segment of the cache: ticket][partial O][partial (max, sum)]
-size_t ticket_offset(const ngc_cache *c)
-{
-    return STATUS_BYTES + (size_t)c->L * c->B * c->Hkv * 2 * sizeof(int32_t);
-}
-size_t attn_offset(const ngc_cache *c)
-{
-    return align256(ticket_offset(c) + (size_t)c->L * c->B * c->Hkv * sizeof(int32_t));
-}
 size_t partial_o_bytes(const ngc_cache *c, int nseg_launch, int S)
 {
     return align256((size_t)nseg_launch * S * (c->Hq / c->Hkv) * c->D * sizeof(float));
@@ -798,7 +785,7 @@ extern "C" size_t ngc_workspace_bytes(const ngc_cache *c, int32_t max_keep)
     const size_t one = attn_partial_bytes(c, per_layer, most_splits(per_layer, c->cap));
     const size_t all = attn_partial_bytes(c, per_layer * c->L, most_splits(per_layer * c->L, c->cap));
     const size_t most = one > all ? one : all;
-    return attn_offset(c) + most;
+    return scratch_offset(c) + most;
 }
 
 namespace {
@@ -834,7 +821,7 @@ int launch_decode(const ngc_cache *c, const ngc_paged_cache *pc, int32_t layer, 
     const bool static_ok = fits_static(c, nseg, static_limit_splits(nseg, max_len, c->D * 2));
     if (fixed_layout && !static_ok) return NGC_ENOSPC;
     while (static_ok && S > 1 && !fits_static(c, nseg, S)) --S;
-    const size_t off = fixed_layout ? FIXED_PARTIAL_OFFSET : attn_offset(c);
+    const size_t off = fixed_layout ? FIXED_PARTIAL_OFFSET : scratch_offset(c);
     if (ws_bytes < off) return NGC_ENOSPC;
     while (S > 1 && ws_bytes < off + attn_partial_bytes(c, nseg, S)) --S;   // fewer splits: same result, less scratch
     if ((long long)nseg * S > 0x7FFFFFFFLL) return NGC_EUNSUPPORTED;
@@ -953,9 +940,6 @@ extern "C" int ngc_paged_decode_attn(const ngc_paged_cache *pc, int32_t layer, c
     if (pc->page_rows < ATT_TILE || (pc->page_rows & (pc->page_rows - 1)) != 0) return NGC_EINVAL;
     if (pc->max_pages <= 0 || pc->num_pages <= 0) return NGC_EINVAL;
     if ((long long)pc->max_pages * pc->page_rows > 0x7FFFFFFFLL / 256) return NGC_EUNSUPPORTED;
-    ngc_cache c{};
-    c.k = pc->k_pool; c.v = pc->v_pool; c.len = pc->len; c.pos = nullptr;
-    c.L = pc->L; c.B = pc->B; c.Hkv = pc->Hkv; c.Hq = pc->Hq; c.D = pc->D;
-    c.cap = pc->max_pages * pc->page_rows;
+    const ngc_cache c = logical_geometry(pc);
     return launch_decode(&c, pc, layer, nullptr, q, scale, max_len_hint, out, lse_out, nullptr, ws, ws_bytes, stream);
 }

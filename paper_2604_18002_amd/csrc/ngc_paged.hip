@@ -14,6 +14,7 @@
 #include "../../include/ngc.h"
 #include "ngc_device.h"
 #include "ngc_select.h"
+#include "ngc_workspace.h"
 
 namespace ngc {
 
@@ -306,34 +307,6 @@ using namespace ngc;
 
 namespace {
 
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-constexpr size_t STATUS_BYTES = NGC_STATUS_WORDS * sizeof(int32_t);
-
-int check_paged(const ngc_paged_cache *pc)
-{
-    if (!pc || !pc->k_pool || !pc->v_pool || !pc->table || !pc->len || !pc->free_stack || !pc->free_count)
-        return NGC_EINVAL;
-    if (!aligned16(pc->k_pool) || !aligned16(pc->v_pool)) return NGC_EINVAL;
-    if (pc->L <= 0 || pc->B <= 0 || pc->Hkv <= 0 || pc->Hq <= 0 || pc->max_pages <= 0 || pc->num_pages <= 0)
-        return NGC_EINVAL;
-    if (pc->D != 64 && pc->D != 128) return NGC_EINVAL;
-    if (pc->Hq % pc->Hkv != 0 || pc->Hq / pc->Hkv > 16) return NGC_EINVAL;
-    if (pc->L > 65535 || pc->Hkv > 65534) return NGC_EINVAL;
-    if (pc->page_rows < 32 || (pc->page_rows & (pc->page_rows - 1)) != 0) return NGC_EINVAL;
-    if (pc->max_pages > 16384) return NGC_EUNSUPPORTED;
-    if ((long long)pc->max_pages * pc->page_rows > 0x7FFFFFFFLL / 256) return NGC_EUNSUPPORTED;
-    return NGC_OK;
-}
-
-int paged_layer_range(const ngc_paged_cache *pc, int layer, int *seg0, int *nseg)
-{
-    if (layer < -1 || layer >= pc->L) return NGC_EINVAL;
-    const int per_layer = pc->B * pc->Hkv;
-    *seg0 = layer < 0 ? 0 : layer * per_layer;
-    *nseg = layer < 0 ? pc->L * per_layer : per_layer;
-    return NGC_OK;
-}
-
 PagedArgs paged_args(const ngc_paged_cache *pc, void *ws, int seg0, int nseg)
 {
     PagedArgs pa;
@@ -356,9 +329,7 @@ extern "C" size_t ngc_paged_workspace_bytes(const ngc_paged_cache *pc)
     if (!pc || pc->max_pages <= 0 || pc->page_rows <= 0) return 0;
     // same layout as the contiguous cache of the same logical geometry:
     // [status][2 int32 per segment][split partials of decode attention]
-    ngc_cache c{};
-    c.L = pc->L; c.B = pc->B; c.Hkv = pc->Hkv; c.Hq = pc->Hq; c.D = pc->D;
-    c.cap = pc->max_pages * pc->page_rows;
+    const ngc_cache c = logical_geometry(pc);
     return ngc_workspace_bytes(&c, 0);
 }
 
