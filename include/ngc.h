@@ -25,6 +25,17 @@
  *                        Sec. 4.2 are pages and eviction edits a page table
  *                        instead of moving rows
  *
+ * and, for rollouts that draft several tokens at a time and for groups of
+ * rollouts of one prompt:
+ *
+ *   ngc_tree_attn        attention of a tree of drafted tokens over the cache
+ *   ngc_tree_verify      which of them stand, and the token behind them, from the
+ *                        target's probabilities and given random numbers
+ *   ngc_tree_commit      the accepted ones become rows of the cache
+ *   ngc_paged_tree_attn, ngc_paged_tree_commit  over the paged layout
+ *   ngc_paged_fork, ngc_paged_free, ngc_paged_compact  copies of sequences, ended
+ *                        sequences, and a pool with its pages in use at the front
+ *
  * General conventions
  *   - Every pointer is a DEVICE pointer unless a comment says "host".  The
  *     structs themselves (ngc_cache, ngc_evict_params) live in HOST memory and
@@ -66,9 +77,10 @@ extern "C" {
 
 /* Status words: int32 counters at the start of the workspace, one per kind of
  * device-detected anomaly.  The caller zeroes the workspace once; kernels only
- * add to them.  NGC_STATUS_WORDS words are reserved; the last two are the
- * library's own (the work counter of the eviction kernel and a count of its
- * finished workgroups: both zero again when a launch has ended). */
+ * add to them.  NGC_STATUS_WORDS words are reserved; those from word 8 on are
+ * the library's own (tickets of ngc_tree_verify; the last two: the work counter
+ * of the eviction kernel and a count of its finished workgroups): all zero again
+ * when a launch has ended. */
 #define NGC_STATUS_WORDS        64
 #define NGC_STATUS_KEEP_CLAMPED  0  /* keep[seg] > items (or < 0): clamped                  */
 #define NGC_STATUS_LEN_CLAMPED   1  /* len[seg] > cap (or < 0): clamped                     */
@@ -77,6 +89,9 @@ extern "C" {
 #define NGC_STATUS_BAD_SIGMA     4  /* ngc_subset_logprob: index out of range or repeated   */
 #define NGC_STATUS_POOL_BOUNDS   5  /* paged cache: free stack would overflow, or a page id
                                        in a table is outside the pool: ignored              */
+#define NGC_STATUS_BAD_TREE      6  /* drafted tokens: a parent, token, path entry or count out
+                                       of range, or a row of probabilities without any     */
+#define NGC_STATUS_BAD_FORK      7  /* ngc_paged_fork: a source that is none: left as it is */
 
 /* Non-owning view of a KV cache in device memory.
  *   k, v : bf16, dense [L][B][Hkv][cap][D], 16-byte aligned.  Rows [0, len) of
@@ -441,7 +456,8 @@ typedef struct ngc_paged_cache {
     int32_t  L, B, Hkv, Hq, D, page_rows, max_pages, num_pages;
 } ngc_paged_cache;
 
-/* Bytes of workspace that make every ngc_paged_* call succeed. */
+/* Bytes of workspace that make every ngc_paged_* call succeed, other than
+ * ngc_paged_fork and ngc_paged_compact (ngc_paged_pool_workspace_bytes). */
 size_t ngc_paged_workspace_bytes(const ngc_paged_cache *pc);
 
 /* One eviction round over pages (Sec. 4.1-4.3 with block = page_rows): the
@@ -485,6 +501,140 @@ int ngc_paged_score_keys(const ngc_paged_cache *pc, int32_t layer, const void *q
                          const float *lse_recent, int32_t w,
                          float scale, uint32_t flags, int32_t block, float *scores_out,
                          void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Drafted tokens.  A sequence has up to W drafted tokens ("nodes") behind its
+ * cache, which form trees:
+ *   parent   int32 [B][W]: the node that comes before, -1 for none.  A parent comes
+ *            before its children: parent[b][i] < i.  Anything else is counted
+ *            (NGC_STATUS_BAD_TREE) and taken for -1.
+ *   n_draft  int32 [B] or NULL: nodes of each sequence, 0 .. W (NULL: all W).
+ *            Others are clamped and counted.
+ * Their rows are not in the cache: they lie in buffers of their own, as a
+ * projection writes them, and enter the cache when they are accepted:
+ *   k_draft, v_draft  bf16 [B][W][Hkv][D] (or [L][B][W][Hkv][D] for layer = -1),
+ *            16-byte aligned.
+ * Nothing is read or written at nodes >= n_draft[b].  W <= 64 (NGC_EUNSUPPORTED
+ * beyond). */
+
+/* Attention of the drafted tokens of `layer` (-1 = all layers): for every node i
+ * of sequence b and query head g, with h = g / (Hq / Hkv),
+ *     out[b][i][g][:] = sum_j softmax_j( scale * <q[b][i][g], K_j> ) V_j
+ *     over the cached rows j < len[layer][b][h] and the drafted rows j in
+ *     { i, parent(i), parent(parent(i)), .. }.
+ *   q        bf16 [B][W][Hq][D] (or [L][B][W][Hq][D]), 16-byte aligned
+ *   out      fp32, same shape, 16-byte aligned
+ *   lse_out  optional fp32 [B][W][Hq] (or [L][B][W][Hq]): the log of the sum of the
+ *            exponentials (natural log), as from ngc_decode_attn, or NULL
+ *   scale    positive and finite (NGC_EINVAL otherwise)
+ *   max_len_hint  as in ngc_decode_attn: steers how the work is split, never what
+ *            is computed
+ * The cache is only read.  A chain (parent[i] = i - 1) gives what W calls of
+ * ngc_decode_step would, one after the other.  What a node does not see never
+ * reaches its output, values that are not finite included.  Scores, soft-max and
+ * accumulation are fp32.
+ * ws must hold ngc_workspace_bytes(); with ngc_tree_workspace_bytes(), which is
+ * not less, few segments are shared by as many workgroups as pays. */
+size_t ngc_tree_workspace_bytes(const ngc_cache *c, int32_t W);
+int ngc_tree_attn(const ngc_cache *c, int32_t layer, const void *k_draft, const void *v_draft,
+                  const int32_t *parent, const int32_t *n_draft, int32_t W, const void *q, float scale,
+                  int32_t max_len_hint, float *out, float *lse_out,
+                  void *ws, size_t ws_bytes, void *stream);
+
+/* Which drafted tokens stand, and the token that follows them, such that what is
+ * emitted has the target's distribution.  Node 0 is the pending token (it has been
+ * emitted already); the others are proposals.  From node 0 on, at every node the
+ * children are tried in ascending order:
+ *     drafts sampled independently from draft[node] (draft != NULL), S = 1, c = 0:
+ *         accept x  if  u S q(x) < max(p(x) - c q(x), 0);
+ *         else c = c + S, S = sum_t max(p(t) - c q(t), 0)
+ *     drafts chosen in any other way (draft == NULL), S = 1:
+ *         accept x  if  u S < r(x),  r = p without the tokens refused at this node;
+ *         else S = max(S - r(x), 0)
+ * with p = target[b][node], q = draft[b][node], u = u_accept[b][child].  The walk
+ * goes on from an accepted child; where nobody is accepted (or there is no child)
+ * the next token is drawn from what is left, r = max(p - c q, 0) or p without the
+ * refused tokens (p itself if that is zero everywhere):
+ *     next = min { t : r(0) + .. + r(t) > u_sample[b] * (r(0) + .. + r(V - 1)) }.
+ *   target, draft  fp32, row of node i at [(b * W + i) * prob_stride], V values that
+ *            add up to 1 (rows of nodes the walk does not reach are not read); 4-byte
+ *            aligned.  Values below 0 and NaN count as 0.  One-hot rows give greedy
+ *            verification.
+ *   token    int32 [B][W]; token[b][0] is not looked at.  A token outside [0, V)
+ *            is counted and never accepted.
+ *   u_accept, u_sample  fp32 [B][W], [B], in [0, 1)
+ *   path_out int32 [B][W]: node 0 and the accepted nodes in order, -1 behind them
+ *   n_path_out  int32 [B]: how many they are (0 where n_draft is 0)
+ *   next_out int32 [B]: the token that follows; -1 where n_draft is 0, and, counted,
+ *            where p has no positive value
+ * Sums are 64-bit, in a fixed order.  ws must hold ngc_verify_workspace_bytes();
+ * it may be a workspace of a cache: it is left as it was found. */
+size_t ngc_verify_workspace_bytes(int32_t B, int32_t V);
+int ngc_tree_verify(const float *target, const float *draft, int64_t prob_stride,
+                    const int32_t *token, const int32_t *parent, const int32_t *n_draft,
+                    int32_t B, int32_t W, int32_t V, const float *u_accept, const float *u_sample,
+                    int32_t *path_out, int32_t *n_path_out, int32_t *next_out,
+                    void *ws, size_t ws_bytes, void *stream);
+
+/* The first n_path[b] nodes of path[b] become rows of the cache, in that order,
+ * behind the rows of every segment of `layer` (-1 = all layers); len grows.
+ *   path, n_path  int32 [B][W], [B], as ngc_tree_verify writes them.  A count outside
+ *            0 .. W is clamped and counted, a node outside 0 .. W - 1 counted (which
+ *            drafted row stands in is unspecified).
+ *   draft_pos  int32 [B][W]: what is stored into pos for each node, or NULL
+ * Rows that a segment has no room for are left out, the last first, and counted
+ * one by one (NGC_STATUS_APPEND_FULL).  Dense: ws needs NGC_STATUS_WORDS * 4 bytes.
+ * Paged: the pages that are missing are granted to the segments in ascending id,
+ * to each as many as it needs from the top of the stack downwards; a segment that
+ * finds fewer gets those that are left. */
+int ngc_tree_commit(const ngc_cache *c, int32_t layer, const void *k_draft, const void *v_draft,
+                    const int32_t *draft_pos, const int32_t *path, const int32_t *n_path, int32_t W,
+                    void *ws, size_t ws_bytes, void *stream);
+
+/* ngc_tree_attn and ngc_tree_commit over the paged layout. */
+size_t ngc_paged_tree_workspace_bytes(const ngc_paged_cache *pc, int32_t W);
+int ngc_paged_tree_attn(const ngc_paged_cache *pc, int32_t layer, const void *k_draft, const void *v_draft,
+                        const int32_t *parent, const int32_t *n_draft, int32_t W, const void *q, float scale,
+                        int32_t max_len_hint, float *out, float *lse_out,
+                        void *ws, size_t ws_bytes, void *stream);
+int ngc_paged_tree_commit(const ngc_paged_cache *pc, int32_t layer, const void *k_draft, const void *v_draft,
+                          const int32_t *draft_pos, const int32_t *path, const int32_t *n_path, int32_t W,
+                          void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Sequences of a paged cache.  Every page stays in exactly one place, so a copy
+ * of a sequence has pages of its own (its rollout evicts others than the
+ * original's). */
+
+/* Bytes of workspace that make every ngc_paged_* call succeed. */
+size_t ngc_paged_pool_workspace_bytes(const ngc_paged_cache *pc);
+
+/* Sequences become copies of others, in every segment of `layer` (-1 = all): where
+ * source[b] >= 0 and != b, sequence b gives its pages back, is granted as many as
+ * sequence source[b] has, and receives its rows (K, V and pos) and length.  Other
+ * sequences are untouched.
+ *   source   int32 [B].  A sequence that is copied must not be replaced in the same
+ *            call; where source[b] names one that is, or none, b is left as it is and
+ *            counted once per call (NGC_STATUS_BAD_FORK).
+ * Pages are released (segments in ascending id, pages in ascending logical index)
+ * before any is granted (segments in ascending id, pages from the top of the stack
+ * downwards).  Where the stack does not hold all pages of a segment, it and the
+ * segments behind it that need pages are left with length 0 and counted
+ * (NGC_STATUS_APPEND_FULL).  ws must hold ngc_paged_pool_workspace_bytes(). */
+int ngc_paged_fork(const ngc_paged_cache *pc, int32_t layer, const int32_t *source,
+                   void *ws, size_t ws_bytes, void *stream);
+
+/* Sequences end: where drop[b] != 0, every segment of `layer` (-1 = all) of
+ * sequence b gives its pages back (order above) and has length 0.  drop: int32 [B]. */
+int ngc_paged_free(const ngc_paged_cache *pc, int32_t layer, const int32_t *drop,
+                   void *ws, size_t ws_bytes, void *stream);
+
+/* The pages in use become pages 0 .. U - 1 of the pools, U = num_pages - *free_count:
+ * the i-th page in use at or beyond U moves to the i-th free page below U (both
+ * ascending), rows, pos and table entries with it.  The free stack then holds the
+ * pages num_pages - 1 down to U, U on top: the pools' ends can be given back.
+ * Takes the whole cache; ws must hold ngc_paged_pool_workspace_bytes(). */
+int ngc_paged_compact(const ngc_paged_cache *pc, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

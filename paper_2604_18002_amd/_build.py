@@ -28,6 +28,9 @@ _UNITS = (
     ("ngc_attn.hip", []),
     ("ngc_score.hip", []),
     ("ngc_replay.hip", []),
+    ("ngc_tree.hip", []),
+    ("ngc_verify.hip", ["-ffp-contract=off"]),      # what is compared is defined product by product
+    ("ngc_pool.hip", []),
 )
 _PROBE_UNITS = (("ngc_probe.hip", []),)
 

@@ -32,6 +32,8 @@ STATUS_EMPTY_ATTN = 2
 STATUS_APPEND_FULL = 3
 STATUS_BAD_SIGMA = 4
 STATUS_POOL_BOUNDS = 5
+STATUS_BAD_TREE = 6
+STATUS_BAD_FORK = 7
 
 EVICT_SELECT_ONLY = 1
 EVICT_UNORDERED = 2
@@ -43,7 +45,10 @@ EXPORTS = ("ngc_version", "ngc_strerror", "ngc_workspace_bytes", "ngc_perturbed_
            "ngc_subset_logprob", "ngc_cache_append", "ngc_decode_attn", "ngc_score_keys",
            "ngc_subset_logprob_backward", "ngc_replay_attn", "ngc_replay_workspace_bytes",
            "ngc_paged_workspace_bytes", "ngc_paged_evict", "ngc_paged_append", "ngc_paged_decode_attn",
-           "ngc_paged_score_keys", "ngc_lmem", "ngc_keep_counts", "ngc_decode_attn_static", "ngc_decode_step")
+           "ngc_paged_score_keys", "ngc_lmem", "ngc_keep_counts", "ngc_decode_attn_static", "ngc_decode_step",
+           "ngc_tree_workspace_bytes", "ngc_tree_attn", "ngc_verify_workspace_bytes", "ngc_tree_verify", "ngc_tree_commit",
+           "ngc_paged_tree_workspace_bytes", "ngc_paged_tree_attn", "ngc_paged_tree_commit",
+           "ngc_paged_pool_workspace_bytes", "ngc_paged_fork", "ngc_paged_free", "ngc_paged_compact")
 STATIC_SCRATCH_BYTES = 2 << 20
 
 
@@ -142,6 +147,21 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.ngc_lmem.restype = C.c_int
     lib.ngc_keep_counts.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, vp, vp]
     lib.ngc_keep_counts.restype = C.c_int
+    for cache, prefix in ((cp, "ngc_"), (gp, "ngc_paged_")):
+        size, attn, commit = (getattr(lib, prefix + name) for name in ("tree_workspace_bytes", "tree_attn", "tree_commit"))
+        size.argtypes, size.restype = [cache, i32], sz
+        attn.argtypes, attn.restype = [cache, i32, vp, vp, vp, vp, i32, vp, f32, i32, vp, vp, vp, sz, vp], C.c_int
+        commit.argtypes, commit.restype = [cache, i32, vp, vp, vp, vp, vp, i32, vp, sz, vp], C.c_int
+    lib.ngc_verify_workspace_bytes.argtypes = [i32, i32]
+    lib.ngc_verify_workspace_bytes.restype = sz
+    lib.ngc_tree_verify.argtypes = [vp, vp, i64, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.ngc_tree_verify.restype = C.c_int
+    lib.ngc_paged_pool_workspace_bytes.argtypes = [gp]
+    lib.ngc_paged_pool_workspace_bytes.restype = sz
+    for fn in (lib.ngc_paged_fork, lib.ngc_paged_free):
+        fn.argtypes, fn.restype = [gp, i32, vp, vp, sz, vp], C.c_int
+    lib.ngc_paged_compact.argtypes = [gp, vp, sz, vp]
+    lib.ngc_paged_compact.restype = C.c_int
     if path == LIB_PATH:
         if not os.path.exists(HOST_LIB_PATH):
             raise RuntimeError(f"{HOST_LIB_PATH} is missing: build it first (python -m paper_2604_18002_amd._build); "
@@ -440,3 +460,81 @@ def ngc_keep_counts(len_t, seg0: int, nseg: int, cap: int, block: int, num: int,
                     stream=None):
     _check(_front().keep_counts(len_t, seg0, nseg, cap, block, num, den, min_keep, keep_out, _stream(stream)),
            "ngc_keep_counts")
+
+
+# ----------------------------------------------------------- drafted tokens ---
+
+def ngc_tree_workspace_bytes(cache: Cache, W: int) -> int:
+    v = cache.view()
+    return int(load_library().ngc_tree_workspace_bytes(C.byref(v), W))
+
+
+def ngc_paged_tree_workspace_bytes(pc: PagedCache, W: int) -> int:
+    v = pc.view()
+    return int(load_library().ngc_paged_tree_workspace_bytes(C.byref(v), W))
+
+
+def ngc_verify_workspace_bytes(B: int, V: int) -> int:
+    return int(load_library().ngc_verify_workspace_bytes(B, V))
+
+
+def allocate_tree_workspace(cache, W: int, V: int = 1):
+    """A zeroed workspace tensor (uint8) for everything a program that drafts does with this cache (either layout):
+    attention and commits of W drafted tokens, their verification over a vocabulary of V, and the calls of the cache itself."""
+    import torch
+    if isinstance(cache, PagedCache):
+        size = max(ngc_paged_tree_workspace_bytes(cache, W), ngc_paged_pool_workspace_bytes(cache))
+        like, B = cache.k_pool, cache.table.shape[1]
+    else:
+        size, like, B = ngc_tree_workspace_bytes(cache, W), cache.k, cache.k.shape[1]
+    return torch.zeros(max(size, ngc_verify_workspace_bytes(B, V)), dtype=torch.uint8, device=like.device)
+
+
+def ngc_tree_attn(cache: Cache, layer: int, k_draft, v_draft, parent, n_draft, W: int, q, scale: float, max_len_hint: int,
+                  out, ws, stream=None, lse_out=None):
+    _check(_front().tree_attn(cache, layer, k_draft, v_draft, parent, n_draft, W, q, scale, max_len_hint, out, lse_out, ws,
+                              _stream(stream)),
+           "ngc_tree_attn")
+
+
+def ngc_paged_tree_attn(pc: PagedCache, layer: int, k_draft, v_draft, parent, n_draft, W: int, q, scale: float,
+                        max_len_hint: int, out, ws, stream=None, lse_out=None):
+    _check(_front().paged_tree_attn(pc, layer, k_draft, v_draft, parent, n_draft, W, q, scale, max_len_hint, out, lse_out, ws,
+                                    _stream(stream)),
+           "ngc_paged_tree_attn")
+
+
+def ngc_tree_verify(target, draft, prob_stride: int, token, parent, n_draft, B: int, W: int, V: int, u_accept, u_sample,
+                    path_out, n_path_out, next_out, ws, stream=None):
+    _check(_front().tree_verify(target, draft, prob_stride, token, parent, n_draft, B, W, V, u_accept, u_sample, path_out,
+                                n_path_out, next_out, ws, _stream(stream)),
+           "ngc_tree_verify")
+
+
+def ngc_tree_commit(cache: Cache, layer: int, k_draft, v_draft, draft_pos, path, n_path, W: int, ws, stream=None):
+    _check(_front().tree_commit(cache, layer, k_draft, v_draft, draft_pos, path, n_path, W, ws, _stream(stream)),
+           "ngc_tree_commit")
+
+
+def ngc_paged_tree_commit(pc: PagedCache, layer: int, k_draft, v_draft, draft_pos, path, n_path, W: int, ws, stream=None):
+    _check(_front().paged_tree_commit(pc, layer, k_draft, v_draft, draft_pos, path, n_path, W, ws, _stream(stream)),
+           "ngc_paged_tree_commit")
+
+
+# ------------------------------------------- sequences of the paged layout ---
+
+def ngc_paged_pool_workspace_bytes(pc: PagedCache) -> int:
+    v = pc.view()
+    return int(load_library().ngc_paged_pool_workspace_bytes(C.byref(v)))
+
+
+def ngc_paged_fork(pc: PagedCache, layer: int, source, ws, stream=None):
+    _check(_front().paged_fork(pc, layer, source, ws, _stream(stream)), "ngc_paged_fork")
+
+
+def ngc_paged_free(pc: PagedCache, layer: int, drop, ws, stream=None):
+    _check(_front().paged_free(pc, layer, drop, ws, _stream(stream)), "ngc_paged_free")
+
+
+def ngc_paged_compact(pc: PagedCache, ws, stream=None):
+    _check(_front().paged_compact(pc, ws, _stream(stream)), "ngc_paged_compact")

@@ -19,7 +19,8 @@ namespace {
 #define NGC_HOST_ENTRIES(X) \
     X(perturbed_keys) X(keep_counts) X(evict) X(subset_logprob) X(subset_logprob_backward) X(lmem) X(cache_append) \
     X(decode_attn) X(decode_step) X(decode_attn_static) X(score_keys) X(replay_attn) X(paged_evict) X(paged_append) \
-    X(paged_decode_attn) X(paged_score_keys)
+    X(paged_decode_attn) X(paged_score_keys) X(tree_attn) X(paged_tree_attn) X(tree_verify) X(tree_commit) \
+    X(paged_tree_commit) X(paged_fork) X(paged_free) X(paged_compact)
 
 // the library's entry points, looked up once by open()
 struct Entries {
@@ -346,6 +347,39 @@ ENTRY(paged_score_keys, 11)
     return call(lib.paged_score_keys, &c, i32(a[1]), ptr(a[2]), as<float>(a[3]), i32(a[4]), f32(a[5]), i32(a[6]),
                 i32(a[7]), as<float>(a[8]), ptr(a[9]), bytes(a[9]), stream(a[10]));
 END
+#define TREE_ATTN(name, view) \
+ENTRY(name, 14) \
+    const auto c = view(a[0]); \
+    return call(lib.name, &c, i32(a[1]), ptr(a[2]), ptr(a[3]), as<int32_t>(a[4]), as<int32_t>(a[5]), i32(a[6]), ptr(a[7]), \
+                f32(a[8]), i32(a[9]), as<float>(a[10]), as<float>(a[11]), ptr(a[12]), bytes(a[12]), stream(a[13])); \
+END
+TREE_ATTN(tree_attn, cache_of)
+TREE_ATTN(paged_tree_attn, paged_of)
+#define TREE_COMMIT(name, view) \
+ENTRY(name, 10) \
+    const auto c = view(a[0]); \
+    return call(lib.name, &c, i32(a[1]), ptr(a[2]), ptr(a[3]), as<int32_t>(a[4]), as<int32_t>(a[5]), as<int32_t>(a[6]), \
+                i32(a[7]), ptr(a[8]), bytes(a[8]), stream(a[9])); \
+END
+TREE_COMMIT(tree_commit, cache_of)
+TREE_COMMIT(paged_tree_commit, paged_of)
+ENTRY(tree_verify, 16)
+    return call(lib.tree_verify, as<float>(a[0]), as<float>(a[1]), i64(a[2]), as<int32_t>(a[3]), as<int32_t>(a[4]),
+                as<int32_t>(a[5]), i32(a[6]), i32(a[7]), i32(a[8]), as<float>(a[9]), as<float>(a[10]), as<int32_t>(a[11]),
+                as<int32_t>(a[12]), as<int32_t>(a[13]), ptr(a[14]), bytes(a[14]), stream(a[15]));
+END
+ENTRY(paged_fork, 5)
+    const ngc_paged_cache c = paged_of(a[0]);
+    return call(lib.paged_fork, &c, i32(a[1]), as<int32_t>(a[2]), ptr(a[3]), bytes(a[3]), stream(a[4]));
+END
+ENTRY(paged_free, 5)
+    const ngc_paged_cache c = paged_of(a[0]);
+    return call(lib.paged_free, &c, i32(a[1]), as<int32_t>(a[2]), ptr(a[3]), bytes(a[3]), stream(a[4]));
+END
+ENTRY(paged_compact, 3)
+    const ngc_paged_cache c = paged_of(a[0]);
+    return call(lib.paged_compact, &c, ptr(a[1]), bytes(a[1]), stream(a[2]));
+END
 
 // open(path): the library the calls go to (already loaded by the binding, so this only finds its entry points)
 PyObject *open_(PyObject *, PyObject *path)
@@ -424,6 +458,8 @@ PyMethodDef methods[] = {
     FAST(perturbed_keys), FAST(keep_counts), FAST(evict), FAST(subset_logprob), FAST(subset_logprob_backward), FAST(lmem),
     FAST(cache_append), FAST(decode_attn), FAST(decode_step), FAST(decode_attn_static), FAST(score_keys),
     FAST(replay_attn), FAST(paged_evict), FAST(paged_append), FAST(paged_decode_attn), FAST(paged_score_keys),
+    FAST(tree_attn), FAST(paged_tree_attn), FAST(tree_verify), FAST(tree_commit), FAST(paged_tree_commit),
+    FAST(paged_fork), FAST(paged_free), FAST(paged_compact),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ngc_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,638 @@
+// Attention for a tree of drafted tokens over the surviving cache rows on gfx950.
+//
+// A sequence has W drafted tokens (nodes) behind its cache; node i attends to all n cached rows and to those drafted
+// nodes that lie on its way from the root, itself included:
+//
+//     out_i = softmax_j( scale <q_i, k_j> ) v_j   over   j in cache  and  j in anc(i) = {i, parent(i), ..}.
+//
+// The drafted rows live in buffers of their own, as a projection writes them ([B][W][Hkv][D]): nothing that may be
+// rejected enters the cache.  A KV head serves R = W G query rows (G query heads per node), so a segment's K and V are
+// read once for all of them and the products, 4 D R flops for 4 D bytes, range from memory bound (R below ~64) to bound
+// by the matrix cores.
+//
+// A workgroup = 4 waves; wave (wq, wk) holds 32 query rows (row block wq of WQ) and takes 32 of a tile's keys (part wk of
+// WK = 4 / WQ; both halves of the 64 where WQ = 4).  Tiles go from memory straight into double-buffered LDS and are
+// shared by the waves.  S^T = K Q^T and O^T = V^T P by 32x32x16 matrix instructions: one query row per lane % 32, so all
+// soft-max state is lane local and crosses lanes once, between the two halves; one pass with a running maximum and sum.
+// The drafted rows are one more tile behind those of the cache, masked by a word of ancestor bits per lane.
+//
+// P enters the second product as three bf16 parts (24 bits): with two (2^-17 of an entry lost at most) the output is
+// 2-3 times further from the 64-bit result than products in 32 bits are.
+//
+// Few segments are shared by S workgroups that take tiles in turn; each leaves an unnormalised partial (max, sum, O) and
+// a second launch joins them.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/ngc.h"
+#include "ngc_device.h"
+#include "ngc_workspace.h"
+
+namespace ngc {
+
+constexpr int TREE_WAVES = 4;
+constexpr int TREE_QW = 32;                 // query rows per wave
+constexpr int TREE_MT = 32;                 // keys per step of the math
+constexpr int TREE_PARTS = 3;               // bf16 parts of P
+// Start of the running max: finite and below every real score, so that 2^(x - m) is 0 for x = -inf without a special case.
+constexpr float TREE_M_INIT = -1.0e30f;
+// The reference of the exponents moves only when a maximum has outgrown it by 2^8.
+constexpr float TREE_LAZY = 8.0f;
+
+struct TreeArgs {
+    const unsigned char *k, *v;         // the cache's rows, or the pools
+    const int32_t *len;
+    const unsigned char *k_draft, *v_draft;   // bf16 [launch layers][B][W][Hkv][D]
+    const int32_t *parent;              // [B][W]
+    const int32_t *n_draft;             // [B] or nullptr
+    const unsigned char *q;             // bf16 [launch layers][B][W][Hq][D]
+    float *out;                         // fp32, as q
+    float *lse_out;                     // fp32 [launch layers][B][W][Hq] or nullptr
+    float *part_o;                      // [segments of the launch][S][R][D]
+    float *part_ml;                     // [segments of the launch][S][R][2]
+    int32_t *status;
+    int seg0, S, W, G, B, Hkv, cap;
+    float scale_log2e;
+    const int32_t *table;               // paged layout only
+    int max_pages, num_pages, page_shift;
+};
+
+// What a workgroup has to know about its segment.
+struct TreeSegment {
+    int seg_local, b, h, n, nd;         // rows in the cache, drafted nodes
+    size_t seq;                         // launch layer * B + sequence
+};
+
+__device__ __forceinline__ TreeSegment tree_segment(const TreeArgs &a, bool counts)
+{
+    TreeSegment s;
+    s.seg_local = (int)blockIdx.x;
+    const int seg = a.seg0 + s.seg_local;
+    s.seq = (size_t)(s.seg_local / a.Hkv);
+    s.h = s.seg_local % a.Hkv;
+    s.b = (int)(s.seq % a.B);
+    s.n = a.len[seg];
+    s.nd = a.n_draft ? a.n_draft[s.b] : a.W;
+    if (s.n < 0 || s.n > a.cap) {
+        if (counts) atomicAdd(&a.status[NGC_STATUS_LEN_CLAMPED], 1);
+        s.n = s.n < 0 ? 0 : a.cap;
+    }
+    if (s.nd < 0 || s.nd > a.W) {
+        if (counts && s.h == 0) atomicAdd(&a.status[NGC_STATUS_BAD_TREE], 1);
+        s.nd = s.nd < 0 ? 0 : a.W;
+    }
+    return s;
+}
+
+template <int WQ> constexpr int tree_tile_keys() { return WQ == 1 ? 128 : 64; }
+
+// The bits of a node's ancestors, itself included, in lane = node; steps of 1, 2, 4, .. up the tree.  A parent that does
+// not come before its child is taken for none.
+__device__ __forceinline__ uint64_t tree_ancestors(const TreeArgs &a, int b, int nd, bool counts)
+{
+    const int lane = lane_id();
+    int up = lane < nd ? a.parent[(size_t)b * a.W + lane] : -1;
+    const bool bad = up < -1 || up >= lane;
+    const uint64_t bad_nodes = __ballot(bad && lane < nd);
+    if (counts && lane == 0 && bad_nodes) atomicAdd(&a.status[NGC_STATUS_BAD_TREE], __popcll(bad_nodes));
+    up = bad ? -1 : up;
+    uint32_t lo = lane < 32 ? 1u << lane : 0u, hi = lane < 32 ? 0u : 1u << (lane - 32);
+#pragma unroll
+    for (int step = 0; step < 6; ++step) {
+        const int from = up < 0 ? lane : up;
+        lo |= (uint32_t)__shfl((int)lo, from);
+        hi |= (uint32_t)__shfl((int)hi, from);
+        const int next = __shfl(up, from);
+        up = up < 0 ? -1 : next;
+    }
+    return (uint64_t)hi << 32 | lo;
+}
+
+template <int D, int WQ, bool PAGED>
+__global__ __launch_bounds__(TREE_WAVES * 64) __attribute__((amdgpu_waves_per_eu(WQ == 1 ? 1 : 2)))
+void tree_attn_kernel(TreeArgs a)
+{
+    constexpr int WK = TREE_WAVES / WQ;
+    constexpr int KT = tree_tile_keys<WQ>();               // keys per LDS tile
+    constexpr int STEPS = KT / (TREE_MT * WK);             // steps of a wave per tile
+    constexpr int ROW_BYTES = D * 2;
+    constexpr int DT = D / 32;                             // 32-wide d tiles of the second product
+    constexpr int KCH = D / 16;                            // 16-wide d chunks of the first product
+    constexpr int TILE_LDS = KT * ROW_BYTES;
+    constexpr int PIECES = ROW_BYTES / 16;                 // 16-byte pieces per row
+    constexpr int LOAD_ROWS = 64 / PIECES;                 // rows one wave-wide load brings
+    constexpr int WAVE_ROWS = KT / TREE_WAVES;             // rows of a tile that a wave loads: inside one page
+    constexpr int LOADS = WAVE_ROWS / LOAD_ROWS;
+    constexpr int RB = TREE_QW * WQ;                       // query rows of the workgroup
+
+    __shared__ __align__(16) unsigned char lds_k0[TILE_LDS], lds_k1[TILE_LDS], lds_v0[TILE_LDS], lds_v1[TILE_LDS];
+    __shared__ float red_m[TREE_WAVES][TREE_QW], red_l[TREE_WAVES][TREE_QW];
+
+    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
+    const int wq = wv % WQ, wk = wv / WQ;
+    const int li = lane & 31, half = lane >> 5;
+    const int split = (int)blockIdx.y, block = (int)blockIdx.z;
+    const TreeSegment s = tree_segment(a, threadIdx.x == 0 && split == 0 && block == 0);
+    const int G = a.G, Hq = a.G * a.Hkv;
+    const int R = s.nd * G;                                // query rows that there are
+    const int row_base = block * RB;
+    if (row_base >= R) return;                             // (uniform; also where nothing is drafted)
+    const int n = s.n, nd = s.nd;
+    const int cache_tiles = (n + KT - 1) / KT;
+    const int tiles = cache_tiles + 1;                     // the last one: the drafted rows
+    if (split >= tiles) return;                            // no partial: the merge counts tiles too
+
+    const int wave_row0 = row_base + wq * TREE_QW;
+    const bool active = wave_row0 < R;                     // (a last block may have waves without query rows)
+    const int my_row = wave_row0 + li < R ? wave_row0 + li : R - 1;
+    const int node = my_row / G, head = s.h * G + my_row % G;
+
+    // ---- where rows lie ---------------------------------------------------------
+    const unsigned char *kseg = PAGED ? a.k : a.k + (size_t)(a.seg0 + s.seg_local) * a.cap * ROW_BYTES;
+    const unsigned char *vseg = PAGED ? a.v : a.v + (size_t)(a.seg0 + s.seg_local) * a.cap * ROW_BYTES;
+    const int32_t *tab = PAGED ? a.table + (size_t)(a.seg0 + s.seg_local) * a.max_pages : nullptr;
+    const size_t draft_at = ((s.seq * a.W) * a.Hkv + s.h) * ROW_BYTES;
+    const uint32_t draft_row = (uint32_t)a.Hkv * ROW_BYTES;
+    // First of the wave's rows in cache tile t, the segment's last row where there are none; paged: its place in the pools.
+    auto first_row = [&](int t) {
+        const int r0 = t * KT + wv * WAVE_ROWS;
+        return r0 < n ? r0 : n - 1;
+    };
+    auto tile_base = [&](int t) -> size_t {                // of the wave's first row, in bytes
+        if (t >= cache_tiles) return draft_at;
+        const int r0 = first_row(t);
+        if constexpr (!PAGED) return (size_t)r0 * ROW_BYTES;
+        int page = tab[r0 >> a.page_shift];
+        page = (page < 0 || page >= a.num_pages) ? 0 : page;          // never leave the pool
+        return (((size_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1))) * ROW_BYTES;
+    };
+
+    // Rows of a tile go straight from memory to LDS: a wave-wide load brings LOAD_ROWS whole rows, lane after lane.  The K
+    // pieces of row r are stored at slot (piece ^ (r & SWZ)), so that reading one piece of 32 consecutive rows meets every
+    // bank; the V pieces at (piece ^ v_swizzle(r)), so that reading 32 bytes of 4 consecutive rows does.
+    constexpr int SWZ = PIECES - 1;
+    auto v_swizzle = [](int r) { return (2 * r) & (PIECES < 16 ? SWZ : 7); };
+    const int lrow = lane / PIECES, lslot = lane % PIECES;
+    auto load_tile = [&](int t, size_t base, unsigned char *dk, unsigned char *dv) {
+        const bool drafted = t >= cache_tiles;
+        const unsigned char *ks = drafted ? a.k_draft + base : kseg + base;
+        const unsigned char *vs = drafted ? a.v_draft + base : vseg + base;
+        const uint32_t stride = drafted ? draft_row : (uint32_t)ROW_BYTES;
+        const int first = drafted ? 0 : first_row(t);                  // what `base` names
+        const int last = drafted ? nd - 1 : n - 1;
+        const int start = drafted ? wv * WAVE_ROWS : first;
+#pragma unroll
+        for (int r = 0; r < LOADS; ++r) {
+            const int row0 = r * LOAD_ROWS;                            // of the wave's rows
+            int row = start + row0 + lrow;
+            row = row < last ? row : last;
+            const uint32_t at = (uint32_t)(row - first) * stride;
+            const int slot_row = wv * WAVE_ROWS + row0;
+            load_to_lds16(ks + (at + (uint32_t)(lslot ^ ((slot_row + lrow) & SWZ)) * 16u), dk + slot_row * ROW_BYTES);
+            load_to_lds16(vs + (at + (uint32_t)(lslot ^ v_swizzle(slot_row + lrow)) * 16u), dv + slot_row * ROW_BYTES);
+        }
+    };
+
+    int t = split;
+    size_t base_next;
+    load_tile(t, tile_base(t), lds_k0, lds_v0);
+    base_next = tile_base(t + a.S);
+
+    // ---- query operands: 32 rows per wave, lane % 32 = row ------------------------
+    bf16x8 qop[KCH];
+    {
+        const unsigned char *qrow = a.q + ((s.seq * a.W + node) * Hq + head) * ROW_BYTES;
+#pragma unroll
+        for (int c = 0; c < KCH; ++c)
+            qop[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qrow + c * 32 + half * 16));
+    }
+    uint32_t sees_lo, sees_hi;             // drafted nodes that this lane's row sees
+    {
+        const uint64_t anc = tree_ancestors(a, s.b, nd, wv == 0 && split == 0 && block == 0 && s.h == 0);
+        sees_lo = (uint32_t)__shfl((int)(uint32_t)anc, node);
+        sees_hi = (uint32_t)__shfl((int)(uint32_t)(anc >> 32), node);
+    }
+
+    f32x16 oacc[DT];
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[c][r] = 0.f;
+    float m_run = TREE_M_INIT, l_run = 0.f;
+
+    // LDS offsets of this lane's operands.  K: piece 2c + half of row li.  V: a transposing read gives lane x of 16 the
+    // column d0 + x of 4 rows if lane x points at the 4 values from d0 + 4 (x % 4) of row x / 4; the rows are the keys
+    // its half contracts over in a 16-key chunk (4 half .. +3 and 8 + 4 half .. +3: the order the scores come in).
+    uint32_t koff[KCH];
+#pragma unroll
+    for (int c = 0; c < KCH; ++c) koff[c] = (uint32_t)(li * ROW_BYTES + (((2 * c + half) ^ (li & SWZ)) * 16));
+    uint32_t vrd[DT];
+    {
+        const int row = 4 * half + (lane & 15) / 4;       // + 16 kc + 8 g: the same row modulo 8 for every g, kc
+#pragma unroll
+        for (int c = 0; c < DT; ++c) {
+            const int d0 = 32 * c + (lane & 16) + 4 * (lane & 3);
+            vrd[c] = (uint32_t)(row * ROW_BYTES + (((d0 / 8) ^ v_swizzle(row)) * 16) + (d0 % 8) * 2);
+        }
+    }
+
+    // The sums are rescaled only when a maximum has outgrown the reference: any reference gives the same quotients, and
+    // probabilities up to 2^TREE_LAZY lose nothing in fp32 or in their bf16 parts.  `top`: of the row, in the scaled domain.
+    auto raise_reference = [&](float top) {
+        if (__ballot(top > m_run + TREE_LAZY)) {
+            const float m_new = max_no_nan(m_run, top);
+            const float alpha = (m_new == m_run) ? 1.0f : fast_exp2(m_run - m_new);
+            l_run *= alpha;
+#pragma unroll
+            for (int c = 0; c < DT; ++c) oacc[c] *= alpha;
+            m_run = m_new;
+        }
+    };
+
+    // 32 keys; `sees`: bit i = whether this lane's row sees the i-th of them
+    auto compute_step = [&](const unsigned char *lk, const unsigned char *lv, uint32_t sees, bool full) {
+        f32x16 sc;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+        u32x4 kop[KCH];
+#pragma unroll
+        for (int c = 0; c < KCH; ++c) kop[c] = *reinterpret_cast<const u32x4 *>(lk + koff[c]);
+        __builtin_amdgcn_sched_barrier(0);     // all requests first: the products then wait for one after the other
+#pragma unroll
+        for (int c = 0; c < KCH; ++c)
+            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kop[c]), qop[c], sc, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);     // the V rows arrive while the soft-max arithmetic runs
+        u32x2 vop[2][DT][2];      // [16-key chunk][d tile][keys 4 half .. +3, 8 + 4 half .. +3]
+#pragma unroll
+        for (int kc = 0; kc < 2; ++kc)
+#pragma unroll
+            for (int c = 0; c < DT; ++c)
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+                    vop[kc][c][g] = read_transposed16(lv + vrd[c] + (16 * kc + 8 * g) * ROW_BYTES);
+        __builtin_amdgcn_sched_barrier(0);
+        // lane (row = li, half), register r: key 8 (r / 4) + 4 half + r % 4 of this step, raw scores; the (positive) scale
+        // is applied inside the exponent's multiply-add
+        if (!full) {
+            const uint32_t w = sees >> (4 * half);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[r] = (w >> (8 * (r / 4) + r % 4)) & 1u ? sc[r] : -INFINITY;
+        }
+        float tmx = sc[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) tmx = max_no_nan(tmx, sc[r]);
+        raise_reference(half_rows_max(tmx) * a.scale_log2e);
+        const float neg_m = -m_run;
+        uint32_t part[TREE_PARTS][8];
+        float psum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            f32x2 p = {fast_exp2(__builtin_fmaf(sc[2 * e], a.scale_log2e, neg_m)),       // -inf gives 0
+                       fast_exp2(__builtin_fmaf(sc[2 * e + 1], a.scale_log2e, neg_m))};
+            psum += p[0] + p[1];
+#pragma unroll
+            for (int i = 0; i < TREE_PARTS; ++i) {        // rounded to bf16; the remainder is exact
+                const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+                part[i][e] = w;
+                if (i + 1 < TREE_PARTS) p = f32x2{p[0] - __uint_as_float(w << 16), p[1] - __uint_as_float(w & 0xFFFF0000u)};
+            }
+        }
+        l_run += psum;
+#pragma unroll
+        for (int kc = 0; kc < 2; ++kc) {
+            bf16x8 v[DT];
+#pragma unroll
+            for (int c = 0; c < DT; ++c)
+                v[c] = __builtin_bit_cast(bf16x8, u32x4{vop[kc][c][0][0], vop[kc][c][0][1], vop[kc][c][1][0], vop[kc][c][1][1]});
+#pragma unroll
+            for (int i = 0; i < TREE_PARTS; ++i) {
+                const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{part[i][4 * kc], part[i][4 * kc + 1], part[i][4 * kc + 2],
+                                                                  part[i][4 * kc + 3]});
+#pragma unroll
+                for (int c = 0; c < DT; ++c) oacc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c], p, oacc[c], 0, 0, 0);
+            }
+        }
+    };
+
+    // Key by key on the vector ALU, for drafted rows with values that are not finite: a product with P = 0 would carry them
+    // into rows that do not see them.
+    auto compute_drafts_singly = [&](const unsigned char *lk, const unsigned char *lv) {
+        for (int j = wk; j < nd; j += WK) {
+            const bool seen = ((j < 32 ? sees_lo >> j : sees_hi >> (j - 32)) & 1u) != 0;
+            float dot = 0.f;
+#pragma unroll
+            for (int c = 0; c < KCH; ++c) {
+                const bf16x8 kp = *reinterpret_cast<const bf16x8 *>(lk + j * ROW_BYTES + (((2 * c + half) ^ (j & SWZ)) * 16));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dot = __builtin_fmaf((float)kp[e], (float)qop[c][e], dot);
+            }
+            dot = half_rows_sum(dot);
+            raise_reference(seen ? dot * a.scale_log2e : -INFINITY);
+            const float p = fast_exp2(__builtin_fmaf(dot, a.scale_log2e, -m_run));
+            l_run += seen && half == 0 ? p : 0.f;
+#pragma unroll
+            for (int c = 0; c < DT; ++c)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int d = 32 * c + 8 * (r / 4) + 4 * half + r % 4;
+                    const __bf16 x = *reinterpret_cast<const __bf16 *>(lv + j * ROW_BYTES + (((d / 8) ^ v_swizzle(j)) * 16) + (d % 8) * 2);
+                    oacc[c][r] = seen ? __builtin_fmaf(p, (float)x, oacc[c][r]) : oacc[c][r];
+                }
+        }
+    };
+
+    auto compute_tile = [&](int t, const unsigned char *lk, const unsigned char *lv) {
+        if (t >= cache_tiles) {
+            bool odd = false;                              // a value that is infinite or NaN among the drafted V rows
+            for (int i = threadIdx.x; i < nd * PIECES; i += TREE_WAVES * 64) {
+                const u32x4 x = *reinterpret_cast<const u32x4 *>(lv + i * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    odd |= (x[e] & 0x7F80u) == 0x7F80u || (x[e] & 0x7F800000u) == 0x7F800000u;
+            }
+            if (__syncthreads_or(odd)) {
+                if (active) compute_drafts_singly(lk, lv);
+                return;
+            }
+        }
+        if (!active) return;
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+            const int at = (wk * STEPS + st) * TREE_MT;    // first key of the step in the tile
+            uint32_t sees;
+            bool full = false;
+            if (t >= cache_tiles) {
+                if (at >= nd) break;
+                sees = at == 0 ? sees_lo : sees_hi;
+            } else {
+                const int left = n - (t * KT + at);
+                if (left <= 0) break;
+                full = left >= TREE_MT;
+                sees = full ? 0xFFFFFFFFu : (1u << left) - 1u;
+            }
+            compute_step(lk + at * ROW_BYTES, lv + at * ROW_BYTES, sees, full);
+        }
+    };
+
+    // Tile t is computed from one pair of LDS buffers while the rows of the next one travel into the other.
+    lds_loads_done();
+    while (true) {
+        if (t + a.S < tiles) {
+            load_tile(t + a.S, base_next, lds_k1, lds_v1);
+            base_next = tile_base(t + 2 * a.S);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        compute_tile(t, lds_k0, lds_v0);
+        __builtin_amdgcn_sched_barrier(0);
+        if ((t += a.S) >= tiles) break;
+        lds_loads_done();
+        if (t + a.S < tiles) {
+            load_tile(t + a.S, base_next, lds_k0, lds_v0);
+            base_next = tile_base(t + 2 * a.S);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        compute_tile(t, lds_k1, lds_v1);
+        __builtin_amdgcn_sched_barrier(0);
+        if ((t += a.S) >= tiles) break;
+        lds_loads_done();
+    }
+
+    // ---- join the waves of a row block, normalise, write --------------------------
+    // O goes through LDS, so that a row's D values leave as whole cache lines: a wave's own 32 rows in its part of the tile
+    // buffers, 16-byte piece p of row r at slot p ^ r.
+    constexpr int OP = D / 4;                              // 16-byte pieces per output row
+    constexpr int O_LDS = TREE_QW * D * 4;
+    static_assert(O_LDS <= TILE_LDS, "a wave's output rows fit a tile buffer");
+    __syncthreads();                                       // every wave is done with the tiles
+    auto rows_of = [&](int w) { return w == 0 ? lds_k0 : w == 1 ? lds_k1 : w == 2 ? lds_v0 : lds_v1; };
+    {
+        const float l = half_rows_sum(l_run);
+        if (half == 0) { red_m[wv][li] = active ? m_run : TREE_M_INIT; red_l[wv][li] = active ? l : 0.f; }
+        unsigned char *mine = rows_of(wv);
+#pragma unroll
+        for (int c = 0; c < DT; ++c)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {   // register (c, 4g + i) holds d = 32 c + 8 g + 4 half + i
+                const int piece = 8 * c + 2 * g + half;
+                *reinterpret_cast<f32x4 *>(mine + li * (D * 4) + ((piece ^ li) & (OP - 1)) * 16) =
+                    f32x4{oacc[c][4 * g], oacc[c][4 * g + 1], oacc[c][4 * g + 2], oacc[c][4 * g + 3]};
+            }
+    }
+    __syncthreads();
+    constexpr int ROWS = TREE_WAVES * 64 / OP;             // rows per workgroup-wide store
+    const int piece = threadIdx.x % OP;
+    for (int r0 = threadIdx.x / OP; r0 < RB; r0 += ROWS) {
+        const int row = row_base + r0;
+        if (row >= R) break;
+        const int q = r0 / TREE_QW, i = r0 % TREE_QW;
+        float f[WK], m_all = TREE_M_INIT, l_all = 0.f;
+#pragma unroll
+        for (int w = 0; w < WK; ++w) m_all = fmaxf(m_all, red_m[w * WQ + q][i]);
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WK; ++w) {
+            f[w] = WK == 1 ? 1.f : fast_exp2(red_m[w * WQ + q][i] - m_all);
+            l_all += red_l[w * WQ + q][i] * f[w];
+            o += *reinterpret_cast<const f32x4 *>(rows_of(w * WQ + q) + i * (D * 4) + ((piece ^ i) & (OP - 1)) * 16) * f[w];
+        }
+        if (a.S == 1) {
+            const size_t at = (s.seq * a.W + row / G) * Hq + s.h * G + row % G;
+            __builtin_nontemporal_store(o / l_all, reinterpret_cast<f32x4 *>(a.out + at * D) + piece);
+            if (a.lse_out && piece == 0) a.lse_out[at] = (m_all + __log2f(l_all)) * 0.6931471805599453f;
+        } else {
+            const size_t at = ((size_t)s.seg_local * a.S + split) * (size_t)(a.W * G) + row;
+            *(reinterpret_cast<f32x4 *>(a.part_o + at * D) + piece) = o;
+            if (piece == 0) *reinterpret_cast<f32x2 *>(a.part_ml + at * 2) = f32x2{m_all, l_all};
+        }
+    }
+}
+
+// Joins the partials of a segment: out = sum_s O_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).  D / 4 threads per query row.
+constexpr int TREE_MERGE_THREADS = 256;
+template <int D>
+__global__ __launch_bounds__(TREE_MERGE_THREADS) void tree_merge_kernel(TreeArgs a, int tile_keys)
+{
+    constexpr int OP = D / 4;
+    const TreeSegment s = tree_segment(a, false);
+    const int row = (int)blockIdx.y * (TREE_MERGE_THREADS / OP) + (int)threadIdx.x / OP;
+    const int piece = (int)threadIdx.x % OP;
+    if (row >= s.nd * a.G) return;
+    const int tiles = (s.n + tile_keys - 1) / tile_keys + 1;
+    const int parts = tiles < a.S ? tiles : a.S;
+    const size_t rows = (size_t)a.W * a.G;
+    const size_t first = (size_t)s.seg_local * a.S * rows + row;
+    constexpr int BATCH = 8;
+    float M = TREE_M_INIT, den = 0.f;
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = 0; p0 < parts; p0 += BATCH) {
+        f32x4 o[BATCH];
+        f32x2 ml[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const size_t at = first + (size_t)(p0 + u < parts ? p0 + u : parts - 1) * rows;
+            o[u] = *(reinterpret_cast<const f32x4 *>(a.part_o + at * D) + piece);
+            ml[u] = *reinterpret_cast<const f32x2 *>(a.part_ml + at * 2);
+        }
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) top = fmaxf(top, ml[u][0]);
+        const float old = fast_exp2(M - top);
+        den *= old;
+        num *= old;
+        M = top;
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const float f = p0 + u < parts ? fast_exp2(ml[u][0] - top) : 0.f;
+            den += ml[u][1] * f;
+            num += o[u] * f;
+        }
+    }
+    const size_t at = (s.seq * a.W + row / a.G) * (a.G * a.Hkv) + s.h * a.G + row % a.G;
+    *(reinterpret_cast<f32x4 *>(a.out + at * D) + piece) = num / den;
+    if (a.lse_out && piece == 0) a.lse_out[at] = (M + __log2f(den)) * 0.6931471805599453f;
+}
+
+}  // namespace ngc
+
+// ============================================================ host side ====
+
+using namespace ngc;
+
+namespace {
+constexpr int TREE_MAX_NODES = 64;          // a word of ancestor bits
+constexpr int TREE_MAX_SPLITS = 64;
+constexpr int TREE_RESIDENT = 512;          // workgroups that the chip holds at once
+
+struct TreeShape {
+    int wq, blocks, tile_keys, splits;
+};
+
+size_t tree_partial_bytes(const ngc_cache *c, int nseg, int W, int S)
+{
+    const size_t rows = (size_t)nseg * S * W * (c->Hq / c->Hkv);
+    return S > 1 ? align256(rows * c->D * sizeof(float)) + align256(rows * 2 * sizeof(float)) : 0;
+}
+
+TreeShape tree_shape(const ngc_cache *c, int nseg, int W, int max_len)
+{
+    const int R = W * (c->Hq / c->Hkv);
+    TreeShape s;
+    s.wq = R <= TREE_QW ? 1 : R <= 2 * TREE_QW ? 2 : 4;
+    s.blocks = (R + s.wq * TREE_QW - 1) / (s.wq * TREE_QW);
+    s.tile_keys = s.wq == 1 ? 128 : 64;
+    const int tiles = (max_len + s.tile_keys - 1) / s.tile_keys + 1;
+    long long most = TREE_RESIDENT / ((long long)nseg * s.blocks);
+    most = most < tiles ? most : tiles;
+    most = most < TREE_MAX_SPLITS ? most : TREE_MAX_SPLITS;
+    s.splits = most > 1 ? (int)most : 1;
+    return s;
+}
+
+bool tree_geometry_ok(const ngc_cache *c, int32_t W)
+{
+    return c && c->L > 0 && c->B > 0 && c->Hkv > 0 && c->Hq > 0 && c->cap > 0 && c->Hq % c->Hkv == 0 && W >= 1 && W <= TREE_MAX_NODES;
+}
+
+int launch_tree(const ngc_cache *c, const ngc_paged_cache *pc, int32_t layer, const void *k_draft, const void *v_draft,
+                const int32_t *parent, const int32_t *n_draft, int32_t W, const void *q, float scale, int32_t max_len_hint,
+                float *out, float *lse_out, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!c->k || !c->v || !c->len || !k_draft || !v_draft || !parent || !q || !out || !ws) return NGC_EINVAL;
+    if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(k_draft) || !aligned16(v_draft) || !aligned16(q) || !aligned16(out) ||
+        !aligned16(ws))
+        return NGC_EINVAL;
+    if (c->L <= 0 || c->B <= 0 || c->Hkv <= 0 || c->Hq <= 0 || c->cap <= 0 || W < 1) return NGC_EINVAL;
+    if (c->D != 64 && c->D != 128) return NGC_EINVAL;
+    if (c->Hq % c->Hkv != 0 || c->Hq / c->Hkv > 16) return NGC_EINVAL;
+    if (layer < -1 || layer >= c->L || max_len_hint < 0) return NGC_EINVAL;
+    if (!(scale > 0.f) || scale > 3.0e38f) return NGC_EINVAL;       // positive and finite: maxima are taken before scaling
+    if (W > TREE_MAX_NODES) return NGC_EUNSUPPORTED;
+    if ((long long)c->cap * c->D * 2 > 0x7FFFFFFFLL) return NGC_EUNSUPPORTED;                       // 32-bit byte offsets
+    if ((long long)W * c->Hkv * c->D * 2 > 0x7FFFFFFFLL) return NGC_EUNSUPPORTED;
+    const int per_layer = c->B * c->Hkv;
+    const int nseg = layer < 0 ? c->L * per_layer : per_layer;
+    const int max_len = (max_len_hint > 0 && max_len_hint < c->cap) ? max_len_hint : c->cap;
+    const size_t off = scratch_offset(c);
+    if (ws_bytes < off) return NGC_ENOSPC;
+    const TreeShape shape = tree_shape(c, nseg, W, max_len);
+    int S = shape.splits;
+    while (S > 1 && ws_bytes < off + tree_partial_bytes(c, nseg, W, S)) --S;      // fewer workgroups: less scratch
+
+    const int G = c->Hq / c->Hkv;
+    TreeArgs a{};
+    a.k = reinterpret_cast<const unsigned char *>(c->k);
+    a.v = reinterpret_cast<const unsigned char *>(c->v);
+    a.len = c->len;
+    a.k_draft = reinterpret_cast<const unsigned char *>(k_draft);
+    a.v_draft = reinterpret_cast<const unsigned char *>(v_draft);
+    a.parent = parent;
+    a.n_draft = n_draft;
+    a.q = reinterpret_cast<const unsigned char *>(q);
+    a.out = out;
+    a.lse_out = lse_out;
+    a.part_o = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(ws) + off);
+    a.part_ml = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(ws) + off +
+                                          align256((size_t)nseg * S * W * G * c->D * sizeof(float)));
+    a.status = reinterpret_cast<int32_t *>(ws);
+    a.seg0 = layer < 0 ? 0 : layer * per_layer;
+    a.S = S; a.W = W; a.G = G; a.B = c->B; a.Hkv = c->Hkv; a.cap = c->cap;
+    a.scale_log2e = scale * 1.4426950408889634f;
+    if (pc) {
+        a.table = pc->table; a.max_pages = pc->max_pages; a.num_pages = pc->num_pages;
+        a.page_shift = __builtin_ctz((unsigned)pc->page_rows);
+    }
+    hipStream_t st = (hipStream_t)stream;
+#define NGC_TREE(D, WQ) (pc ? reinterpret_cast<const void *>(&tree_attn_kernel<D, WQ, true>) \
+                            : reinterpret_cast<const void *>(&tree_attn_kernel<D, WQ, false>))
+#define NGC_TREE_D(D) (shape.wq == 1 ? NGC_TREE(D, 1) : shape.wq == 2 ? NGC_TREE(D, 2) : NGC_TREE(D, 4))
+    const void *fn = c->D == 128 ? NGC_TREE_D(128) : NGC_TREE_D(64);
+#undef NGC_TREE_D
+#undef NGC_TREE
+    const int rc = launch(fn, dim3(nseg, S, shape.blocks), dim3(TREE_WAVES * 64), 0, st, a);
+    if (rc || S == 1) return rc;
+    const int rows_per = TREE_MERGE_THREADS / (c->D / 4);
+    const dim3 grid(nseg, (W * G + rows_per - 1) / rows_per);
+    if (c->D == 128) hipLaunchKernelGGL(tree_merge_kernel<128>, grid, dim3(TREE_MERGE_THREADS), 0, st, a, shape.tile_keys);
+    else hipLaunchKernelGGL(tree_merge_kernel<64>, grid, dim3(TREE_MERGE_THREADS), 0, st, a, shape.tile_keys);
+    NGC_HIP_CHECK(hipGetLastError());
+    return NGC_OK;
+}
+}  // namespace
+
+extern "C" size_t ngc_tree_workspace_bytes(const ngc_cache *c, int32_t W)
+{
+    if (!tree_geometry_ok(c, W)) return 0;
+    const int per_layer = c->B * c->Hkv;
+    // one layer or all layers, any length hint: the most workgroups a segment can be shared by
+    const size_t one = tree_partial_bytes(c, per_layer, W, tree_shape(c, per_layer, W, c->cap).splits);
+    const size_t all = tree_partial_bytes(c, per_layer * c->L, W, tree_shape(c, per_layer * c->L, W, c->cap).splits);
+    const size_t own = scratch_offset(c) + (one > all ? one : all), others = ngc_workspace_bytes(c, 0);
+    return own > others ? own : others;
+}
+
+extern "C" size_t ngc_paged_tree_workspace_bytes(const ngc_paged_cache *pc, int32_t W)
+{
+    if (check_paged(pc) != NGC_OK) return 0;
+    const ngc_cache c = logical_geometry(pc);
+    return ngc_tree_workspace_bytes(&c, W);
+}
+
+extern "C" int ngc_tree_attn(const ngc_cache *c, int32_t layer, const void *k_draft, const void *v_draft,
+                             const int32_t *parent, const int32_t *n_draft, int32_t W, const void *q, float scale,
+                             int32_t max_len_hint, float *out, float *lse_out, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!c) return NGC_EINVAL;
+    return launch_tree(c, nullptr, layer, k_draft, v_draft, parent, n_draft, W, q, scale, max_len_hint, out, lse_out, ws, ws_bytes,
+                       stream);
+}
+
+extern "C" int ngc_paged_tree_attn(const ngc_paged_cache *pc, int32_t layer, const void *k_draft, const void *v_draft,
+                                   const int32_t *parent, const int32_t *n_draft, int32_t W, const void *q, float scale,
+                                   int32_t max_len_hint, float *out, float *lse_out, void *ws, size_t ws_bytes, void *stream)
+{
+    const int rc = check_paged(pc);
+    if (rc) return rc;
+    const ngc_cache c = logical_geometry(pc);
+    return launch_tree(&c, pc, layer, k_draft, v_draft, parent, n_draft, W, q, scale, max_len_hint, out, lse_out, ws, ws_bytes, stream);
+}
