@@ -25,6 +25,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/ngc.h"
 #include "ngc_device.h"
 #include "ngc_workspace.h"
@@ -52,10 +54,21 @@ struct TreeArgs {
     float *part_o;                      // [segments of the launch][S][R][D]
     float *part_ml;                     // [segments of the launch][S][R][2]
     int32_t *status;
+    int32_t *ticket;                    // [segments of the launch][ticket_step]: 0 between launches; nullptr: joined by a launch
+    int ticket_step;
     int seg0, S, W, G, B, Hkv, cap;
     float scale_log2e;
     const int32_t *table;               // paged layout only
     int max_pages, num_pages, page_shift;
+};
+
+// How a segment's keys are dealt out: tiles of `keys`, the drafted rows in tiles of their own, `waves` tiles to a workgroup at a time.
+struct TreeTiles {
+    int keys, waves;
+    __host__ __device__ int groups(int n, int nd) const
+    {
+        return ((n + keys - 1) / keys + (nd + keys - 1) / keys + waves - 1) / waves;
+    }
 };
 
 // What a workgroup has to know about its segment.
@@ -85,14 +98,12 @@ __device__ __forceinline__ TreeSegment tree_segment(const TreeArgs &a, bool coun
     return s;
 }
 
-template <int WQ> constexpr int tree_tile_keys() { return WQ == 1 ? 128 : 64; }
-
 // The bits of a node's ancestors, itself included, in lane = node; steps of 1, 2, 4, .. up the tree.  A parent that does
 // not come before its child is taken for none.
-__device__ __forceinline__ uint64_t tree_ancestors(const TreeArgs &a, int b, int nd, bool counts)
+__device__ __forceinline__ uint64_t tree_ancestors(const TreeArgs &a, int up, int nd, bool counts)      // up: of node = lane
 {
     const int lane = lane_id();
-    int up = lane < nd ? a.parent[(size_t)b * a.W + lane] : -1;
+    up = lane < nd ? up : -1;
     const bool bad = up < -1 || up >= lane;
     const uint64_t bad_nodes = __ballot(bad && lane < nd);
     if (counts && lane == 0 && bad_nodes) atomicAdd(&a.status[NGC_STATUS_BAD_TREE], __popcll(bad_nodes));
@@ -109,12 +120,12 @@ __device__ __forceinline__ uint64_t tree_ancestors(const TreeArgs &a, int b, int
     return (uint64_t)hi << 32 | lo;
 }
 
-template <int D, int WQ, bool PAGED>
-__global__ __launch_bounds__(TREE_WAVES * 64) __attribute__((amdgpu_waves_per_eu(WQ == 1 ? 1 : 2)))
+template <int D, int WQ, bool ONCE, bool PAGED>
+__global__ __launch_bounds__(TREE_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void tree_attn_kernel(TreeArgs a)
 {
     constexpr int WK = TREE_WAVES / WQ;
-    constexpr int KT = tree_tile_keys<WQ>();               // keys per LDS tile
+    constexpr int KT = 64;                                 // keys per LDS tile
     constexpr int STEPS = KT / (TREE_MT * WK);             // steps of a wave per tile
     constexpr int ROW_BYTES = D * 2;
     constexpr int DT = D / 32;                             // 32-wide d tiles of the second product
@@ -148,6 +159,14 @@ void tree_attn_kernel(TreeArgs a)
     const int my_row = wave_row0 + li < R ? wave_row0 + li : R - 1;
     const int node = my_row / G, head = s.h * G + my_row % G;
 
+    // ---- query operands: 32 rows per wave, lane % 32 = row ------------------------
+    bf16x8 qop[KCH];
+    {
+        const unsigned char *qrow = a.q + ((s.seq * a.W + node) * Hq + head) * ROW_BYTES;
+#pragma unroll
+        for (int c = 0; c < KCH; ++c)
+            qop[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qrow + c * 32 + half * 16));
+    }
     // ---- where rows lie ---------------------------------------------------------
     const unsigned char *kseg = PAGED ? a.k : a.k + (size_t)(a.seg0 + s.seg_local) * a.cap * ROW_BYTES;
     const unsigned char *vseg = PAGED ? a.v : a.v + (size_t)(a.seg0 + s.seg_local) * a.cap * ROW_BYTES;
@@ -174,42 +193,43 @@ void tree_attn_kernel(TreeArgs a)
     constexpr int SWZ = PIECES - 1;
     auto v_swizzle = [](int r) { return (2 * r) & (PIECES < 16 ? SWZ : 7); };
     const int lrow = lane / PIECES, lslot = lane % PIECES;
-    auto load_tile = [&](int t, size_t base, unsigned char *dk, unsigned char *dv) {
+    auto load = [&](int t, size_t base, const unsigned char *cached, const unsigned char *drafts, unsigned char *to, auto swizzle) {
         const bool drafted = t >= cache_tiles;
-        const unsigned char *ks = drafted ? a.k_draft + base : kseg + base;
-        const unsigned char *vs = drafted ? a.v_draft + base : vseg + base;
+        const unsigned char *src = drafted ? drafts + base : cached + base;
         const uint32_t stride = drafted ? draft_row : (uint32_t)ROW_BYTES;
         const int first = drafted ? 0 : first_row(t);                  // what `base` names
         const int last = drafted ? nd - 1 : n - 1;
         const int start = drafted ? wv * WAVE_ROWS : first;
 #pragma unroll
         for (int r = 0; r < LOADS; ++r) {
-            const int row0 = r * LOAD_ROWS;                            // of the wave's rows
-            int row = start + row0 + lrow;
+            const int slot_row = wv * WAVE_ROWS + r * LOAD_ROWS;
+            int row = start + r * LOAD_ROWS + lrow;
             row = row < last ? row : last;
-            const uint32_t at = (uint32_t)(row - first) * stride;
-            const int slot_row = wv * WAVE_ROWS + row0;
-            load_to_lds16(ks + (at + (uint32_t)(lslot ^ ((slot_row + lrow) & SWZ)) * 16u), dk + slot_row * ROW_BYTES);
-            load_to_lds16(vs + (at + (uint32_t)(lslot ^ v_swizzle(slot_row + lrow)) * 16u), dv + slot_row * ROW_BYTES);
+            const unsigned char *at = src + ((uint32_t)(row - first) * stride + (uint32_t)(lslot ^ swizzle(slot_row + lrow)) * 16u);
+            if constexpr (ONCE) load_once_to_lds16(at, to + slot_row * ROW_BYTES);
+            else load_to_lds16(at, to + slot_row * ROW_BYTES);
         }
     };
+    auto load_k = [&](int t, size_t base, unsigned char *to) { load(t, base, kseg, a.k_draft, to, [&](int r) { return r & SWZ; }); };
+    auto load_v = [&](int t, size_t base, unsigned char *to) { load(t, base, vseg, a.v_draft, to, v_swizzle); };
 
+    // Asked for in this order, now and in the loop: K of a tile, its V, K of the next tile, its V, ..
     int t = split;
-    size_t base_next;
-    load_tile(t, tile_base(t), lds_k0, lds_v0);
-    base_next = tile_base(t + a.S);
-
-    // ---- query operands: 32 rows per wave, lane % 32 = row ------------------------
-    bf16x8 qop[KCH];
+    const int S = a.S;
+    int up = lane < a.W ? a.parent[(size_t)s.b * a.W + lane] : -1;
+    __asm__ volatile("" : "+v"(up));                       // waited for here, not behind the first tile
+    size_t base1, base2;                                   // of the next tile and the one after it
     {
-        const unsigned char *qrow = a.q + ((s.seq * a.W + node) * Hq + head) * ROW_BYTES;
-#pragma unroll
-        for (int c = 0; c < KCH; ++c)
-            qop[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qrow + c * 32 + half * 16));
+        const size_t base0 = tile_base(t);
+        base1 = tile_base(t + S);
+        load_k(t, base0, lds_k0);
+        load_v(t, base0, lds_v0);
+        base2 = tile_base(t + 2 * S);
     }
+
     uint32_t sees_lo, sees_hi;             // drafted nodes that this lane's row sees
     {
-        const uint64_t anc = tree_ancestors(a, s.b, nd, wv == 0 && split == 0 && block == 0 && s.h == 0);
+        const uint64_t anc = tree_ancestors(a, up, nd, wv == 0 && split == 0 && block == 0 && s.h == 0);
         sees_lo = (uint32_t)__shfl((int)(uint32_t)anc, node);
         sees_hi = (uint32_t)__shfl((int)(uint32_t)(anc >> 32), node);
     }
@@ -250,19 +270,21 @@ void tree_attn_kernel(TreeArgs a)
         }
     };
 
-    // 32 keys; `sees`: bit i = whether this lane's row sees the i-th of them
-    auto compute_step = [&](const unsigned char *lk, const unsigned char *lv, uint32_t sees, bool full) {
+    // Raw scores of 32 keys with this lane's row: register r holds key 8 (r / 4) + 4 half + r % 4 of them.
+    auto scores = [&](const unsigned char *lk) {
         f32x16 sc;
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] = 0.f;
         u32x4 kop[KCH];
 #pragma unroll
         for (int c = 0; c < KCH; ++c) kop[c] = *reinterpret_cast<const u32x4 *>(lk + koff[c]);
-        __builtin_amdgcn_sched_barrier(0);     // all requests first: the products then wait for one after the other
 #pragma unroll
         for (int c = 0; c < KCH; ++c)
             sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kop[c]), qop[c], sc, 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);     // the V rows arrive while the soft-max arithmetic runs
+        return sc;
+    };
+    // O += P V for 32 keys and their raw scores; the (positive) scale is applied inside the exponent's multiply-add.
+    auto add_values = [&](const unsigned char *lv, const f32x16 &sc) {
         u32x2 vop[2][DT][2];      // [16-key chunk][d tile][keys 4 half .. +3, 8 + 4 half .. +3]
 #pragma unroll
         for (int kc = 0; kc < 2; ++kc)
@@ -271,18 +293,7 @@ void tree_attn_kernel(TreeArgs a)
 #pragma unroll
                 for (int g = 0; g < 2; ++g)
                     vop[kc][c][g] = read_transposed16(lv + vrd[c] + (16 * kc + 8 * g) * ROW_BYTES);
-        __builtin_amdgcn_sched_barrier(0);
-        // lane (row = li, half), register r: key 8 (r / 4) + 4 half + r % 4 of this step, raw scores; the (positive) scale
-        // is applied inside the exponent's multiply-add
-        if (!full) {
-            const uint32_t w = sees >> (4 * half);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sc[r] = (w >> (8 * (r / 4) + r % 4)) & 1u ? sc[r] : -INFINITY;
-        }
-        float tmx = sc[0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) tmx = max_no_nan(tmx, sc[r]);
-        raise_reference(half_rows_max(tmx) * a.scale_log2e);
+        __builtin_amdgcn_sched_barrier(0);     // the V rows arrive while the exponentials are made
         const float neg_m = -m_run;
         uint32_t part[TREE_PARTS][8];
         float psum = 0.f;
@@ -315,88 +326,121 @@ void tree_attn_kernel(TreeArgs a)
         }
     };
 
-    // Key by key on the vector ALU, for drafted rows with values that are not finite: a product with P = 0 would carry them
-    // into rows that do not see them.
-    auto compute_drafts_singly = [&](const unsigned char *lk, const unsigned char *lv) {
-        for (int j = wk; j < nd; j += WK) {
-            const bool seen = ((j < 32 ? sees_lo >> j : sees_hi >> (j - 32)) & 1u) != 0;
-            float dot = 0.f;
+    // The drafted V rows: values that are not finite would reach rows that do not see them, through a product with P = 0.  They
+    // become 0 in LDS and are added, by themselves, to the rows that see them.  Returns whether there are any.
+    auto take_out_odd_values = [&](unsigned char *lv) {
+        bool any = false;
+        for (int i = threadIdx.x; i < nd * PIECES; i += TREE_WAVES * 64) {
+            u32x4 x = *reinterpret_cast<const u32x4 *>(lv + i * 16);
+            bool odd = false;
 #pragma unroll
-            for (int c = 0; c < KCH; ++c) {
-                const bf16x8 kp = *reinterpret_cast<const bf16x8 *>(lk + j * ROW_BYTES + (((2 * c + half) ^ (j & SWZ)) * 16));
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dot = __builtin_fmaf((float)kp[e], (float)qop[c][e], dot);
+            for (int e = 0; e < 4; ++e) {
+                if ((x[e] & 0x7F80u) == 0x7F80u) { odd = true; x[e] &= 0xFFFF0000u; }
+                if ((x[e] & 0x7F800000u) == 0x7F800000u) { odd = true; x[e] &= 0xFFFFu; }
             }
-            dot = half_rows_sum(dot);
-            raise_reference(seen ? dot * a.scale_log2e : -INFINITY);
-            const float p = fast_exp2(__builtin_fmaf(dot, a.scale_log2e, -m_run));
-            l_run += seen && half == 0 ? p : 0.f;
+            if (odd) *reinterpret_cast<u32x4 *>(lv + i * 16) = x;
+            any |= odd;
+        }
+        return __syncthreads_or(any) != 0;
+    };
+    auto add_odd_values = [&]() {
+        for (int j = 0; j < nd; ++j) {
+            const bool seen = ((j < 32 ? sees_lo >> j : sees_hi >> (j - 32)) & 1u) != 0;
+            // of lane half: d = 32 c + 8 g + 4 half + i.  (The address is made opaque: nothing of it is kept over the loop.)
+            const unsigned char *row = a.v_draft + draft_at + (size_t)j * draft_row + half * 8;
+            __asm__ volatile("" : "+v"(row));
 #pragma unroll
             for (int c = 0; c < DT; ++c)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int d = 32 * c + 8 * (r / 4) + 4 * half + r % 4;
-                    const __bf16 x = *reinterpret_cast<const __bf16 *>(lv + j * ROW_BYTES + (((d / 8) ^ v_swizzle(j)) * 16) + (d % 8) * 2);
-                    oacc[c][r] = seen ? __builtin_fmaf(p, (float)x, oacc[c][r]) : oacc[c][r];
+                for (int g = 0; g < 4; ++g) {
+                    const u32x2 x = *reinterpret_cast<const u32x2 *>(row + (32 * c + 8 * g) * 2);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t bits = i & 1 ? x[i / 2] & 0xFFFF0000u : x[i / 2] << 16;
+                        if (seen && (bits & 0x7F800000u) == 0x7F800000u) oacc[c][4 * g + i] += __uint_as_float(bits);
+                    }
                 }
         }
     };
 
-    auto compute_tile = [&](int t, const unsigned char *lk, const unsigned char *lv) {
-        if (t >= cache_tiles) {
-            bool odd = false;                              // a value that is infinite or NaN among the drafted V rows
-            for (int i = threadIdx.x; i < nd * PIECES; i += TREE_WAVES * 64) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(lv + i * 16);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    odd |= (x[e] & 0x7F80u) == 0x7F80u || (x[e] & 0x7F800000u) == 0x7F800000u;
+    // One tile, in two parts with a barrier in front of each.  In front of the first: everybody's K rows are there, and the V
+    // buffer of the tile before is read out, so the next tile's V is asked for.  In front of the second: everybody's V rows
+    // are there, and the K buffer is read out, so K of the tile after the next is asked for.  Each wait is for all but the
+    // newest two halves of a tile (48 KB of a workgroup's 64 are on their way or waited for at any time), except in a
+    // workgroup's last two tiles, where less follows.
+    constexpr int WAIT_OLDER = 0x0070 | (2 * LOADS);       // vmcnt(2 LOADS); lgkmcnt(0): what this wave has read has arrived
+    constexpr int WAIT_ALL = 0x0070;                       // vmcnt(0) lgkmcnt(0)
+    auto tile_step = [&](auto main, unsigned char *lk, unsigned char *lv, unsigned char *next_v) {
+        constexpr bool MAIN = decltype(main)::value;       // two more tiles follow: this one is a full tile of the cache
+        __builtin_amdgcn_s_waitcnt(MAIN ? WAIT_OLDER : WAIT_ALL);
+        __asm__ volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        __asm__ volatile("" ::: "memory");
+        if (MAIN || t + S < tiles) load_v(t + S, base1, next_v);
+        __builtin_amdgcn_sched_barrier(0);
+        const bool drafted = !MAIN && t >= cache_tiles;
+        f32x16 sc[STEPS];
+        int steps = STEPS;                                 // of this wave that have keys
+        if (active) {
+            if (!MAIN) {
+                const int keys = (drafted ? nd : n - t * KT) - wk * STEPS * TREE_MT;
+                steps = keys <= 0 ? 0 : keys <= TREE_MT ? 1 : STEPS;
             }
-            if (__syncthreads_or(odd)) {
-                if (active) compute_drafts_singly(lk, lv);
-                return;
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) {
+                if (!MAIN && st >= steps) break;
+                sc[st] = scores(lk + (wk * STEPS + st) * TREE_MT * ROW_BYTES);
             }
         }
-        if (!active) return;
+        __builtin_amdgcn_sched_barrier(0);
+        bool odd = false;
+        __builtin_amdgcn_s_waitcnt(MAIN ? WAIT_OLDER : WAIT_ALL);
+        __asm__ volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        __asm__ volatile("" ::: "memory");
+        if (MAIN || t + 2 * S < tiles) load_k(t + 2 * S, base2, lk);
+        base1 = base2;
+        base2 = tile_base(t + 3 * S);
+        if (drafted) odd = take_out_odd_values(lv);
+        if (!active || steps == 0) return;
+        __builtin_amdgcn_sched_barrier(0);
+        float top = -INFINITY;
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
-            const int at = (wk * STEPS + st) * TREE_MT;    // first key of the step in the tile
-            uint32_t sees;
-            bool full = false;
-            if (t >= cache_tiles) {
-                if (at >= nd) break;
-                sees = at == 0 ? sees_lo : sees_hi;
-            } else {
-                const int left = n - (t * KT + at);
-                if (left <= 0) break;
-                full = left >= TREE_MT;
-                sees = full ? 0xFFFFFFFFu : (1u << left) - 1u;
+            if (!MAIN && st >= steps) break;
+            if constexpr (!MAIN) {
+                const int at = (wk * STEPS + st) * TREE_MT, left = n - (t * KT + at);
+                const uint32_t sees = drafted ? (at == 0 ? sees_lo : sees_hi) : left >= TREE_MT ? 0xFFFFFFFFu : (1u << left) - 1u;
+                const uint32_t w = sees >> (4 * half);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sc[st][r] = (w >> (8 * (r / 4) + r % 4)) & 1u ? sc[st][r] : -INFINITY;
             }
-            compute_step(lk + at * ROW_BYTES, lv + at * ROW_BYTES, sees, full);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = max_no_nan(top, sc[st][r]);
         }
+        raise_reference(half_rows_max(top) * a.scale_log2e);
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+            if (!MAIN && st >= steps) break;
+            add_values(lv + (wk * STEPS + st) * TREE_MT * ROW_BYTES, sc[st]);
+        }
+        if (odd && wk == 0) add_odd_values();
     };
-
-    // Tile t is computed from one pair of LDS buffers while the rows of the next one travel into the other.
-    lds_loads_done();
-    while (true) {
-        if (t + a.S < tiles) {
-            load_tile(t + a.S, base_next, lds_k1, lds_v1);
-            base_next = tile_base(t + 2 * a.S);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        compute_tile(t, lds_k0, lds_v0);
-        __builtin_amdgcn_sched_barrier(0);
-        if ((t += a.S) >= tiles) break;
-        lds_loads_done();
-        if (t + a.S < tiles) {
-            load_tile(t + a.S, base_next, lds_k0, lds_v0);
-            base_next = tile_base(t + 2 * a.S);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        compute_tile(t, lds_k1, lds_v1);
-        __builtin_amdgcn_sched_barrier(0);
-        if ((t += a.S) >= tiles) break;
-        lds_loads_done();
+    // (The compiler keeps account of what is on its way and makes a read of a buffer wait for it: it must find the same order on
+    // every way into the loop, or it has everything waited for.  The waits above are its builtin for the same reason.)
+    if (t + 3 * S < tiles) {
+        load_k(t + S, base1, lds_k1);
+        do {
+            tile_step(std::true_type{}, lds_k0, lds_v0, lds_v1);
+            t += S;
+            tile_step(std::true_type{}, lds_k1, lds_v1, lds_v0);
+            t += S;
+        } while (t + 3 * S < tiles);
+    } else if (t + S < tiles) {
+        load_k(t + S, base1, lds_k1);
     }
+    for (bool even = true; t < tiles; t += S, even = !even)
+        tile_step(std::false_type{}, even ? lds_k0 : lds_k1, even ? lds_v0 : lds_v1, even ? lds_v1 : lds_v0);
 
     // ---- join the waves of a row block, normalise, write --------------------------
     // O goes through LDS, so that a row's D values leave as whole cache lines: a wave's own 32 rows in its part of the tile
@@ -436,7 +480,7 @@ void tree_attn_kernel(TreeArgs a)
             l_all += red_l[w * WQ + q][i] * f[w];
             o += *reinterpret_cast<const f32x4 *>(rows_of(w * WQ + q) + i * (D * 4) + ((piece ^ i) & (OP - 1)) * 16) * f[w];
         }
-        if (a.S == 1) {
+        if (a.S == 1 || tiles == 1) {
             const size_t at = (s.seq * a.W + row / G) * Hq + s.h * G + row % G;
             __builtin_nontemporal_store(o / l_all, reinterpret_cast<f32x4 *>(a.out + at * D) + piece);
             if (a.lse_out && piece == 0) a.lse_out[at] = (m_all + __log2f(l_all)) * 0.6931471805599453f;
@@ -448,18 +492,384 @@ void tree_attn_kernel(TreeArgs a)
     }
 }
 
+// Up to 32 query rows.  Every wave walks key tiles of its own, 32 keys each (tile t belongs to wave t % 4 of workgroup
+// (t / 4) % S), through its own part of LDS: no barrier until the end.  A tile's K and V have one buffer each; the next
+// tile's K is requested as soon as this one's has been read into registers, its V likewise, so that 8 to 16 KB of every
+// wave are on their way, two workgroups a CU.  The drafted rows are the last one or two tiles.
+template <int D, bool PAGED>
+__global__ __launch_bounds__(TREE_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
+void tree_narrow_kernel(TreeArgs a)
+{
+    constexpr int ROW_BYTES = D * 2;
+    constexpr int DT = D / 32, KCH = D / 16;
+    constexpr int TILE_LDS = TREE_MT * ROW_BYTES;
+    constexpr int PIECES = ROW_BYTES / 16;
+    constexpr int LOAD_ROWS = 64 / PIECES;
+    constexpr int LOADS = TREE_MT / LOAD_ROWS;
+    constexpr int OP = D / 4;                              // 16-byte pieces per output row
+
+    __shared__ __align__(16) unsigned char lds_k[TREE_WAVES * TILE_LDS], lds_v[TREE_WAVES * TILE_LDS];
+    __shared__ float red_m[TREE_WAVES][TREE_QW], red_l[TREE_WAVES][TREE_QW];
+    __shared__ int is_last;
+
+    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
+    const int li = lane & 31, half = lane >> 5;
+    const int split = (int)blockIdx.y;
+    const int G = a.G, Hq = a.G * a.Hkv;
+    const TreeSegment s = tree_segment(a, threadIdx.x == 0 && split == 0);
+
+    // ---- queries and parents: neither the length nor the number of drafts is waited for ----
+    const int my_row = li < a.W * G ? li : a.W * G - 1;
+    const int node = my_row / G, head = s.h * G + my_row % G;
+    bf16x8 qop[KCH];
+    {
+        const unsigned char *qrow = a.q + ((s.seq * a.W + node) * Hq + head) * ROW_BYTES;
+#pragma unroll
+        for (int c = 0; c < KCH; ++c)
+            qop[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qrow + c * 32 + half * 16));
+    }
+    int up = lane < a.W ? a.parent[(size_t)s.b * a.W + lane] : -1;
+    const int n = s.n, nd = s.nd, R = nd * G;
+    if (nd == 0) return;
+    const int cache_tiles = (n + TREE_MT - 1) / TREE_MT;
+    const int tiles = cache_tiles + (nd + TREE_MT - 1) / TREE_MT;
+    const int parts = (tiles + TREE_WAVES - 1) / TREE_WAVES < a.S ? (tiles + TREE_WAVES - 1) / TREE_WAVES : a.S;   // with tiles
+    if (split >= parts) return;                            // (they take no ticket)
+
+    const unsigned char *kseg = PAGED ? a.k : a.k + (size_t)(a.seg0 + s.seg_local) * a.cap * ROW_BYTES;
+    const unsigned char *vseg = PAGED ? a.v : a.v + (size_t)(a.seg0 + s.seg_local) * a.cap * ROW_BYTES;
+    const int32_t *tab = PAGED ? a.table + (size_t)(a.seg0 + s.seg_local) * a.max_pages : nullptr;
+    const size_t draft_at = ((s.seq * a.W) * a.Hkv + s.h) * ROW_BYTES;
+    const uint32_t draft_row = (uint32_t)a.Hkv * ROW_BYTES;
+    auto tile_base = [&](int t) -> size_t {                // of a cache tile, in bytes; a tile lies inside one page
+        t = t < cache_tiles ? t : cache_tiles - 1;
+        if (t < 0) return 0;
+        const int r0 = t * TREE_MT;
+        if constexpr (!PAGED) return (size_t)r0 * ROW_BYTES;
+        int page = tab[r0 >> a.page_shift];
+        page = (page < 0 || page >= a.num_pages) ? 0 : page;          // never leave the pool
+        return (((size_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1))) * ROW_BYTES;
+    };
+
+    constexpr int SWZ = PIECES - 1;
+    auto v_swizzle = [](int r) { return (2 * r) & (PIECES < 16 ? SWZ : 7); };
+    const int lrow = lane / PIECES, lslot = lane % PIECES;
+    unsigned char *const wk = lds_k + wv * TILE_LDS, *const wvl = lds_v + wv * TILE_LDS;
+    // K (or V) rows of a tile, straight to LDS; rows behind the last are the last one again
+    auto load = [&](int t, size_t base, const unsigned char *cached, const unsigned char *drafts, unsigned char *to, auto swizzle) {
+        const bool drafted = t >= cache_tiles;
+        const int first = (drafted ? t - cache_tiles : t) * TREE_MT;
+        const int last = (drafted ? nd : n) - 1 - first;
+        const uint32_t stride = drafted ? draft_row : (uint32_t)ROW_BYTES;
+        const unsigned char *src = drafted ? drafts + draft_at + (size_t)first * draft_row : cached + base;
+#pragma unroll
+        for (int r = 0; r < LOADS; ++r) {
+            const int slot_row = r * LOAD_ROWS + lrow;
+            const int row = slot_row < last ? slot_row : last;
+            load_once_to_lds16(src + ((uint32_t)row * stride + (uint32_t)(lslot ^ swizzle(slot_row)) * 16u), to + r * LOAD_ROWS * ROW_BYTES);
+        }
+    };
+    auto load_k = [&](int t, size_t base) { load(t, base, kseg, a.k_draft, wk, [&](int r) { return r & SWZ; }); };
+    auto load_v = [&](int t, size_t base) { load(t, base, vseg, a.v_draft, wvl, v_swizzle); };
+
+    const int step = a.S * TREE_WAVES;
+    int t = split * TREE_WAVES + wv;
+    size_t base1 = 0;
+    __asm__ volatile("" : "+v"(up));       // waited for here (it was asked for with the length), not behind the first tile
+    if (t < tiles) {
+        const size_t base0 = tile_base(t);
+        load_k(t, base0);
+        load_v(t, base0);
+        base1 = tile_base(t + step);
+    }
+    uint32_t sees_lo, sees_hi;             // drafted nodes that this lane's row sees
+    {
+        const uint64_t anc = tree_ancestors(a, up, nd, wv == 0 && split == 0 && s.h == 0);
+        sees_lo = (uint32_t)__shfl((int)(uint32_t)anc, node);
+        sees_hi = (uint32_t)__shfl((int)(uint32_t)(anc >> 32), node);
+    }
+
+    f32x16 oacc[DT];
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[c][r] = 0.f;
+    float m_run = TREE_M_INIT, l_run = 0.f;
+    uint32_t koff[KCH];
+#pragma unroll
+    for (int c = 0; c < KCH; ++c) koff[c] = (uint32_t)(li * ROW_BYTES + (((2 * c + half) ^ (li & SWZ)) * 16));
+    uint32_t vrd[DT];
+    {
+        const int row = 4 * half + (lane & 15) / 4;
+#pragma unroll
+        for (int c = 0; c < DT; ++c) {
+            const int d0 = 32 * c + (lane & 16) + 4 * (lane & 3);
+            vrd[c] = (uint32_t)(row * ROW_BYTES + (((d0 / 8) ^ v_swizzle(row)) * 16) + (d0 % 8) * 2);
+        }
+    }
+
+    // as in tree_attn_kernel: values of drafted V rows that are not finite become 0 and are added to the rows that see them
+    auto take_out_odd_values = [&]() {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < TILE_LDS / 16 / 64; ++i) {
+            u32x4 x = *reinterpret_cast<const u32x4 *>(wvl + (i * 64 + lane) * 16);
+            bool odd = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if ((x[e] & 0x7F80u) == 0x7F80u) { odd = true; x[e] &= 0xFFFF0000u; }
+                if ((x[e] & 0x7F800000u) == 0x7F800000u) { odd = true; x[e] &= 0xFFFFu; }
+            }
+            if (odd) *reinterpret_cast<u32x4 *>(wvl + (i * 64 + lane) * 16) = x;
+            any |= odd;
+        }
+        return __ballot(any) != 0;
+    };
+    auto add_odd_values = [&](int chunk, uint32_t sees) {
+        for (int j = chunk * TREE_MT; j < nd && j < (chunk + 1) * TREE_MT; ++j) {
+            const bool seen = ((sees >> (j - chunk * TREE_MT)) & 1u) != 0;
+            const unsigned char *row = a.v_draft + draft_at + (size_t)j * draft_row + half * 8;
+            __asm__ volatile("" : "+v"(row));
+#pragma unroll
+            for (int c = 0; c < DT; ++c)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const u32x2 x = *reinterpret_cast<const u32x2 *>(row + (32 * c + 8 * g) * 2);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t bits = i & 1 ? x[i / 2] & 0xFFFF0000u : x[i / 2] << 16;
+                        if (seen && (bits & 0x7F800000u) == 0x7F800000u) oacc[c][4 * g + i] += __uint_as_float(bits);
+                    }
+                }
+        }
+    };
+
+    constexpr int WAIT_LDS = 0xC07F;                       // lgkmcnt(0)
+    constexpr int WAIT_OLDER = 0x0F70 | LOADS;             // vmcnt(LOADS): all but the newest tile half is there
+    auto tile_step = [&](int t, auto next) {
+        // (a tile that is not full, or drafted, is a wave's last: what comes after it is less than a step of the deal)
+        constexpr bool NEXT = decltype(next)::value;
+        const bool drafted = !NEXT && t >= cache_tiles;
+        const int chunk = t - cache_tiles;
+        const int left = n - t * TREE_MT;
+        const bool full = NEXT || (!drafted && left >= TREE_MT);
+        const uint32_t sees = drafted ? (chunk == 0 ? sees_lo : sees_hi) : full ? 0xFFFFFFFFu : (1u << left) - 1u;
+        __builtin_amdgcn_s_waitcnt(WAIT_OLDER);            // K; V is still on its way
+        __asm__ volatile("" ::: "memory");
+        u32x4 kop[KCH];
+#pragma unroll
+        for (int c = 0; c < KCH; ++c) kop[c] = *reinterpret_cast<const u32x4 *>(wk + koff[c]);
+        __builtin_amdgcn_s_waitcnt(WAIT_LDS);
+        __builtin_amdgcn_sched_barrier(0);
+        if (NEXT) load_k(t + step, base1);                 // into the buffer that has just been read
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 sc;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < KCH; ++c)
+            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kop[c]), qop[c], sc, 0, 0, 0);
+        if (!full) {
+            const uint32_t w = sees >> (4 * half);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[r] = (w >> (8 * (r / 4) + r % 4)) & 1u ? sc[r] : -INFINITY;
+        }
+        float tmx = sc[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) tmx = max_no_nan(tmx, sc[r]);
+        tmx = half_rows_max(tmx) * a.scale_log2e;
+        if (__ballot(tmx > m_run + TREE_LAZY)) {
+            const float m_new = max_no_nan(m_run, tmx);
+            const float alpha = (m_new == m_run) ? 1.0f : fast_exp2(m_run - m_new);
+            l_run *= alpha;
+#pragma unroll
+            for (int c = 0; c < DT; ++c) oacc[c] *= alpha;
+            m_run = m_new;
+        }
+        const float neg_m = -m_run;
+        uint32_t part[TREE_PARTS][8];
+        float psum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            f32x2 p = {fast_exp2(__builtin_fmaf(sc[2 * e], a.scale_log2e, neg_m)),
+                       fast_exp2(__builtin_fmaf(sc[2 * e + 1], a.scale_log2e, neg_m))};
+            psum += p[0] + p[1];
+#pragma unroll
+            for (int i = 0; i < TREE_PARTS; ++i) {
+                const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+                part[i][e] = w;
+                if (i + 1 < TREE_PARTS) p = f32x2{p[0] - __uint_as_float(w << 16), p[1] - __uint_as_float(w & 0xFFFF0000u)};
+            }
+        }
+        l_run += psum;
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(NEXT ? WAIT_OLDER : 0x0F70);        // V
+        __asm__ volatile("" ::: "memory");
+        const bool odd = drafted && take_out_odd_values();
+        u32x2 vop[2][DT][2];
+#pragma unroll
+        for (int kc = 0; kc < 2; ++kc)
+#pragma unroll
+            for (int c = 0; c < DT; ++c)
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+                    vop[kc][c][g] = read_transposed16(wvl + vrd[c] + (16 * kc + 8 * g) * ROW_BYTES);
+        __builtin_amdgcn_s_waitcnt(WAIT_LDS);
+        __builtin_amdgcn_sched_barrier(0);
+        if (NEXT) {
+            load_v(t + step, base1);
+            base1 = tile_base(t + 2 * step);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kc = 0; kc < 2; ++kc) {
+            bf16x8 v[DT];
+#pragma unroll
+            for (int c = 0; c < DT; ++c)
+                v[c] = __builtin_bit_cast(bf16x8, u32x4{vop[kc][c][0][0], vop[kc][c][0][1], vop[kc][c][1][0], vop[kc][c][1][1]});
+#pragma unroll
+            for (int i = 0; i < TREE_PARTS; ++i) {
+                const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{part[i][4 * kc], part[i][4 * kc + 1], part[i][4 * kc + 2],
+                                                                  part[i][4 * kc + 3]});
+#pragma unroll
+                for (int c = 0; c < DT; ++c) oacc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c], p, oacc[c], 0, 0, 0);
+            }
+        }
+        if (odd) add_odd_values(chunk, sees);
+    };
+    if (t < tiles) {
+        while (t + step < tiles) {
+            tile_step(t, std::true_type{});
+            t += step;
+        }
+        tile_step(t, std::false_type{});
+    }
+
+    // ---- join the waves: O of every wave in its own part of the buffers, 16-byte piece p of row r at slot p ^ r, rows 0-15 where
+    // K was, the others where V was ----
+    {
+        const float l = half_rows_sum(l_run);
+        if (half == 0) { red_m[wv][li] = m_run; red_l[wv][li] = l; }
+        unsigned char *mine = (li < 16 ? wk : wvl) + (li & 15) * (D * 4);
+#pragma unroll
+        for (int c = 0; c < DT; ++c)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {   // register (c, 4g + i) holds d = 32 c + 8 g + 4 half + i
+                const int piece = 8 * c + 2 * g + half;
+                *reinterpret_cast<f32x4 *>(mine + ((piece ^ li) & (OP - 1)) * 16) =
+                    f32x4{oacc[c][4 * g], oacc[c][4 * g + 1], oacc[c][4 * g + 2], oacc[c][4 * g + 3]};
+            }
+    }
+    __syncthreads();
+    constexpr int ROWS = TREE_WAVES * 64 / OP;             // rows per workgroup-wide store
+    const int piece = threadIdx.x % OP;
+    auto joined = [&](int i, float &m_all, float &l_all) {
+        m_all = red_m[0][i];
+#pragma unroll
+        for (int w = 1; w < TREE_WAVES; ++w) m_all = fmaxf(m_all, red_m[w][i]);
+        l_all = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < TREE_WAVES; ++w) {
+            const float f = fast_exp2(red_m[w][i] - m_all);
+            l_all += red_l[w][i] * f;
+            o += *reinterpret_cast<const f32x4 *>((i < 16 ? lds_k : lds_v) + w * TILE_LDS + (i & 15) * (D * 4) +
+                                                  ((piece ^ i) & (OP - 1)) * 16) * f;
+        }
+        return o;
+    };
+    auto write = [&](int row, f32x4 o, float m_all, float l_all) {
+        const size_t at = (s.seq * a.W + row / G) * Hq + s.h * G + row % G;
+        *(reinterpret_cast<f32x4 *>(a.out + at * D) + piece) = o / l_all;
+        if (a.lse_out && piece == 0) a.lse_out[at] = (m_all + __log2f(l_all)) * 0.6931471805599453f;
+    };
+    float m_all, l_all;
+    if (parts == 1) {
+        for (int row = threadIdx.x / OP; row < R; row += ROWS) {
+            const f32x4 o = joined(row, m_all, l_all);
+            write(row, o, m_all, l_all);
+        }
+        return;
+    }
+    const size_t rows = (size_t)a.W * G;
+    const size_t first = ((size_t)s.seg_local * a.S + split) * rows;
+    if (!a.ticket) {                                       // a second launch joins the partials
+        for (int row = threadIdx.x / OP; row < R; row += ROWS) {
+            const f32x4 o = joined(row, m_all, l_all);
+            *(reinterpret_cast<f32x4 *>(a.part_o + (first + row) * D) + piece) = o;
+            if (piece == 0) *reinterpret_cast<f32x2 *>(a.part_ml + (first + row) * 2) = f32x2{m_all, l_all};
+        }
+        return;
+    }
+    // The partials cross workgroups (and the L2 caches of different XCDs) through device-scope stores and loads; the workgroup
+    // that takes the segment's last ticket joins them.
+    {
+        const __amdgpu_buffer_rsrc_t po = device_span(a.part_o + first * D, (uint32_t)(rows * D * sizeof(float)));
+        const __amdgpu_buffer_rsrc_t pml = device_span(a.part_ml + first * 2, (uint32_t)(rows * 2 * sizeof(float)));
+        for (int row = threadIdx.x / OP; row < R; row += ROWS) {
+            const f32x4 o = joined(row, m_all, l_all);
+            st_device16(po, (uint32_t)((row * D + piece * 4) * sizeof(float)), o);
+            if (piece == 0) st_device8(pml, (uint32_t)(row * 2 * sizeof(float)), f32x2{m_all, l_all});
+        }
+    }
+    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this thread's partial stores have reached memory
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int32_t *ticket = a.ticket + (size_t)s.seg_local * a.ticket_step;
+        const int old = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        is_last = old == parts - 1;
+        if (is_last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!is_last) return;
+    __asm__ volatile("" ::: "memory");
+    const size_t all = (size_t)s.seg_local * a.S * rows;
+    const __amdgpu_buffer_rsrc_t po = device_span(a.part_o + all * D, (uint32_t)(parts * rows * D * sizeof(float)));
+    const __amdgpu_buffer_rsrc_t pml = device_span(a.part_ml + all * 2, (uint32_t)(parts * rows * 2 * sizeof(float)));
+    constexpr int BATCH = 8;
+    for (int row = threadIdx.x / OP; row < R; row += ROWS) {
+        float M = TREE_M_INIT, den = 0.f;
+        f32x4 num = {0.f, 0.f, 0.f, 0.f};
+        for (int p0 = 0; p0 < parts; p0 += BATCH) {
+            f32x4 o[BATCH];
+            f32x2 ml[BATCH];
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                const uint32_t at = (uint32_t)((p0 + u < parts ? p0 + u : parts - 1) * (int)rows + row);
+                o[u] = ld_device16(po, (uint32_t)((at * D + piece * 4) * sizeof(float)));
+                ml[u] = ld_device8(pml, (uint32_t)(at * 2 * sizeof(float)));
+            }
+            float top = M;
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) top = fmaxf(top, ml[u][0]);
+            const float old = fast_exp2(M - top);
+            den *= old;
+            num *= old;
+            M = top;
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                const float f = p0 + u < parts ? fast_exp2(ml[u][0] - top) : 0.f;
+                den += ml[u][1] * f;
+                num += o[u] * f;
+            }
+        }
+        write(row, num, M, den);
+    }
+}
+
 // Joins the partials of a segment: out = sum_s O_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).  D / 4 threads per query row.
 constexpr int TREE_MERGE_THREADS = 256;
 template <int D>
-__global__ __launch_bounds__(TREE_MERGE_THREADS) void tree_merge_kernel(TreeArgs a, int tile_keys)
+__global__ __launch_bounds__(TREE_MERGE_THREADS) void tree_merge_kernel(TreeArgs a, TreeTiles tl)
 {
     constexpr int OP = D / 4;
     const TreeSegment s = tree_segment(a, false);
     const int row = (int)blockIdx.y * (TREE_MERGE_THREADS / OP) + (int)threadIdx.x / OP;
     const int piece = (int)threadIdx.x % OP;
     if (row >= s.nd * a.G) return;
-    const int tiles = (s.n + tile_keys - 1) / tile_keys + 1;
+    const int tiles = tl.groups(s.n, s.nd);
     const int parts = tiles < a.S ? tiles : a.S;
+    if (parts == 1) return;                                // the only workgroup with tiles has written the output
     const size_t rows = (size_t)a.W * a.G;
     const size_t first = (size_t)s.seg_local * a.S * rows + row;
     constexpr int BATCH = 8;
@@ -503,9 +913,12 @@ namespace {
 constexpr int TREE_MAX_NODES = 64;          // a word of ancestor bits
 constexpr int TREE_MAX_SPLITS = 64;
 constexpr int TREE_RESIDENT = 512;          // workgroups that the chip holds at once
+constexpr size_t TREE_TICKET_BYTES = 128 * 1024;
 
 struct TreeShape {
-    int wq, blocks, tile_keys, splits;
+    bool narrow;
+    int wq, blocks, splits;             // row blocks of 32 in a workgroup, workgroups for the rows, and for the keys
+    TreeTiles tiles;
 };
 
 size_t tree_partial_bytes(const ngc_cache *c, int nseg, int W, int S)
@@ -518,10 +931,11 @@ TreeShape tree_shape(const ngc_cache *c, int nseg, int W, int max_len)
 {
     const int R = W * (c->Hq / c->Hkv);
     TreeShape s;
+    s.narrow = R <= TREE_QW;
     s.wq = R <= TREE_QW ? 1 : R <= 2 * TREE_QW ? 2 : 4;
     s.blocks = (R + s.wq * TREE_QW - 1) / (s.wq * TREE_QW);
-    s.tile_keys = s.wq == 1 ? 128 : 64;
-    const int tiles = (max_len + s.tile_keys - 1) / s.tile_keys + 1;
+    s.tiles = s.narrow ? TreeTiles{TREE_MT, TREE_WAVES} : TreeTiles{64, 1};
+    const int tiles = s.tiles.groups(max_len, W);
     long long most = TREE_RESIDENT / ((long long)nseg * s.blocks);
     most = most < tiles ? most : tiles;
     most = most < TREE_MAX_SPLITS ? most : TREE_MAX_SPLITS;
@@ -583,18 +997,24 @@ int launch_tree(const ngc_cache *c, const ngc_paged_cache *pc, int32_t layer, co
         a.page_shift = __builtin_ctz((unsigned)pc->page_rows);
     }
     hipStream_t st = (hipStream_t)stream;
-#define NGC_TREE(D, WQ) (pc ? reinterpret_cast<const void *>(&tree_attn_kernel<D, WQ, true>) \
-                            : reinterpret_cast<const void *>(&tree_attn_kernel<D, WQ, false>))
-#define NGC_TREE_D(D) (shape.wq == 1 ? NGC_TREE(D, 1) : shape.wq == 2 ? NGC_TREE(D, 2) : NGC_TREE(D, 4))
+#define NGC_TREE(KERNEL, ...) (pc ? reinterpret_cast<const void *>(&KERNEL<__VA_ARGS__, true>) \
+                                  : reinterpret_cast<const void *>(&KERNEL<__VA_ARGS__, false>))
+#define NGC_TREE_D(D) (shape.narrow ? NGC_TREE(tree_narrow_kernel, D) : shape.wq == 2 ? NGC_TREE(tree_attn_kernel, D, 2, true) \
+                       : shape.blocks == 1 ? NGC_TREE(tree_attn_kernel, D, 4, true) : NGC_TREE(tree_attn_kernel, D, 4, false))
     const void *fn = c->D == 128 ? NGC_TREE_D(128) : NGC_TREE_D(64);
 #undef NGC_TREE_D
 #undef NGC_TREE
+    const bool tickets = shape.narrow && (size_t)S * W * G * c->D * sizeof(float) <= TREE_TICKET_BYTES;
+    if (tickets) {
+        a.ticket = reinterpret_cast<int32_t *>(reinterpret_cast<unsigned char *>(ws) + ticket_offset(c));
+        a.ticket_step = ticket_step((size_t)c->L * per_layer, nseg);
+    }
     const int rc = launch(fn, dim3(nseg, S, shape.blocks), dim3(TREE_WAVES * 64), 0, st, a);
-    if (rc || S == 1) return rc;
+    if (rc || S == 1 || tickets) return rc;
     const int rows_per = TREE_MERGE_THREADS / (c->D / 4);
     const dim3 grid(nseg, (W * G + rows_per - 1) / rows_per);
-    if (c->D == 128) hipLaunchKernelGGL(tree_merge_kernel<128>, grid, dim3(TREE_MERGE_THREADS), 0, st, a, shape.tile_keys);
-    else hipLaunchKernelGGL(tree_merge_kernel<64>, grid, dim3(TREE_MERGE_THREADS), 0, st, a, shape.tile_keys);
+    if (c->D == 128) hipLaunchKernelGGL(tree_merge_kernel<128>, grid, dim3(TREE_MERGE_THREADS), 0, st, a, shape.tiles);
+    else hipLaunchKernelGGL(tree_merge_kernel<64>, grid, dim3(TREE_MERGE_THREADS), 0, st, a, shape.tiles);
     NGC_HIP_CHECK(hipGetLastError());
     return NGC_OK;
 }
