@@ -620,7 +620,8 @@ size_t ngc_paged_pool_workspace_bytes(const ngc_paged_cache *pc);
  * before any is granted (segments in ascending id, pages from the top of the stack
  * downwards).  Where the stack does not hold all pages of a segment, it and the
  * segments behind it that need pages are left with length 0 and counted
- * (NGC_STATUS_APPEND_FULL).  ws must hold ngc_paged_pool_workspace_bytes(). */
+ * (NGC_STATUS_APPEND_FULL).  B <= 8192 (NGC_EUNSUPPORTED beyond).  ws must hold
+ * ngc_paged_pool_workspace_bytes(). */
 int ngc_paged_fork(const ngc_paged_cache *pc, int32_t layer, const int32_t *source,
                    void *ws, size_t ws_bytes, void *stream);
 

@@ -140,164 +140,287 @@ __global__ __launch_bounds__(COMMIT_THREADS) void commit_kernel(CommitArgs a)
 
 // ------------------------------------------------------------ fork, free ------
 
+constexpr int FORK_COPIES = 4;              // copies of a page that are written from one read of it
+constexpr int FORK_SEQUENCES = 8192;        // whose sources fit in LDS
+
 struct PoolArgs {
     unsigned char *k_pool, *v_pool;
     int32_t *pos_pool;
     int32_t *table, *len, *free_stack, *free_count;
     const int32_t *mark;                    // [B]: fork: the sequence to copy, or below 0; free: whether it goes
     int32_t *freed, *push_base;             // workspace, per segment
-    int32_t *first;                         // workspace, per segment: pages granted before it
-    int32_t *head;                          // workspace: [0] pages granted, [1] height of the stack when they were
+    // fork: workspace.  head: [0] pages to move, [1] height of the stack when pages were granted, [2] whether all were, [3] whether
+    // pages are read more than once
+    int32_t *head;
+    int32_t *first, *work;                  // per segment: pages granted before it; pieces of work before it
+    int32_t *copies, *rank;                 // per sequence: copies of it; which of its source's copies it is
+    int32_t *from, *to;                     // per piece of work: a page, and FORK_COPIES places (-1: none)
     int32_t *status;
     int seg0, nseg, B, Hkv;
     int page_rows, page_shift, max_pages, num_pages;
 };
 
-// The segment that launch segment i is to become a copy of, -1 if none; *invalid: its sequence names one that is none or
-// is itself replaced.
-__device__ __forceinline__ int fork_source(const PoolArgs &a, int i, bool *invalid)
+constexpr int FORK_NONE = -1, FORK_INVALID = -2;
+// The sequence that b is to become a copy of; it must be one, and must not be replaced itself.
+__device__ __forceinline__ int fork_source(const PoolArgs &a, int b)
 {
-    const int b = (i / a.Hkv) % a.B;
     const int s = a.mark[b];
-    *invalid = false;
-    if (s < 0 || s == b) return -1;
-    if (s < a.B) {
-        const int ss = a.mark[s];
-        if (ss < 0 || ss == s) return i + (s - b) * a.Hkv;
-    }
-    *invalid = true;
-    return -1;
+    if (s < 0 || s == b) return FORK_NONE;
+    if (s >= a.B) return FORK_INVALID;
+    const int ss = a.mark[s];
+    return ss < 0 || ss == s ? s : FORK_INVALID;
 }
 
+// Exclusive prefix sums of three numbers at once.
+template <int THREADS>
+__device__ __forceinline__ void block_excl_scan3(int (&v)[3], int (*tmp)[THREADS / NGC_WAVE], int (&total)[3])
+{
+    int incl[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        incl[k] = wave_incl_scan_i(v[k]);
+        if (lane_id() == NGC_WAVE - 1) tmp[k][wave_id()] = incl[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 3; ++k) v[k] = below_waves<THREADS / NGC_WAVE, 1>(tmp[k], &total[k]) + incl[k] - v[k];
+    __syncthreads();
+}
+
+// What every segment gives back, is granted and is copied to; the new lengths and the new height of the stack.  One workgroup;
+// consecutive segments per thread, four at a time so that their lengths are asked for together.
 template <bool FORK>
 __global__ __launch_bounds__(POOL_THREADS) void pool_plan_kernel(PoolArgs a)
 {
-    __shared__ int tmp[32];
+    __shared__ int tmp[3][POOL_THREADS / NGC_WAVE];
+    __shared__ int copies[FORK ? FORK_SEQUENCES : 1];
+    __shared__ short source[FORK ? FORK_SEQUENCES : 1];
     const int count_raw = *a.free_count;
     const int count = count_raw < 0 ? 0 : (count_raw > a.num_pages ? a.num_pages : count_raw);
     const int per = (a.nseg + POOL_THREADS - 1) / POOL_THREADS;
     const int lo = (int)threadIdx.x * per, hi = lo + per < a.nseg ? lo + per : a.nseg;
     const int cap = a.page_rows * a.max_pages;
-    auto rows_of = [&](int i) {
-        const int n = a.len[a.seg0 + i];
-        return n < 0 ? 0 : n > cap ? cap : n;
-    };
     auto pages = [&](int rows) { return (rows + a.page_rows - 1) >> a.page_shift; };
-    // pages that the segment gives back and takes
-    auto plan = [&](int i, int &back, int &rows, bool &invalid) {
-        invalid = false;
-        back = 0;
-        rows = -1;
-        if constexpr (FORK) {
-            const int src = fork_source(a, i, &invalid);
-            if (src < 0) return;
-            rows = rows_of(src);
-        } else {
-            if (a.mark[(i / a.Hkv) % a.B] == 0) return;
-            rows = 0;
+    [[maybe_unused]] bool shared = false;   // whether a page is read for more than one piece of work
+    if constexpr (FORK) {
+        int invalid = 0;
+        for (int b = threadIdx.x; b < a.B; b += POOL_THREADS) {
+            copies[b] = 0;
+            const int s = fork_source(a, b);
+            source[b] = (short)s;
+            invalid += s == FORK_INVALID;
         }
-        back = pages(rows_of(i));
+        if (invalid) atomicAdd(&a.status[NGC_STATUS_BAD_FORK], invalid);
+        __syncthreads();
+        for (int b = threadIdx.x; b < a.B; b += POOL_THREADS)
+            if (source[b] >= 0) a.rank[b] = atomicAdd(&copies[source[b]], 1);
+        __syncthreads();
+        for (int b = threadIdx.x; b < a.B; b += POOL_THREADS) {
+            a.copies[b] = copies[b];
+            shared |= copies[b] > FORK_COPIES;
+        }
+        shared = __syncthreads_or(shared) != 0;
+    }
+    struct Plan {
+        int back, rows, take, work;         // pages given back; new length (-1: stays), pages granted; pieces of work as a source
+        bool clamped;
     };
-    int back, rows, sum_back = 0, sum_take = 0;
-    bool invalid;
-    for (int i = lo; i < hi; ++i) {
-        plan(i, back, rows, invalid);
-        sum_back += back;
-        sum_take += rows > 0 ? pages(rows) : 0;
-    }
-    int total_back, total_take = 0, take_at = 0;
-    int back_at = block_excl_scan_i<POOL_THREADS>(sum_back, tmp, &total_back);
-    if constexpr (FORK) take_at = block_excl_scan_i<POOL_THREADS>(sum_take, tmp, &total_take);
-    int height = count + total_back;
-    if (height > a.num_pages) height = a.num_pages;
-    // Nobody's length has been stored yet; a thread's sources belong to others, but no source is stored to.
-    __syncthreads();
-    int granted = 0;
-    for (int i = lo; i < hi; ++i) {
-        const int n = a.len[a.seg0 + i];
-        plan(i, back, rows, invalid);
-        if (FORK && invalid && i < a.B * a.Hkv && i % a.Hkv == 0) atomicAdd(&a.status[NGC_STATUS_BAD_FORK], 1);
-        a.freed[a.seg0 + i] = back;
-        a.push_base[a.seg0 + i] = count + back_at;
-        back_at += back;
-        if constexpr (FORK) a.first[i] = take_at < height ? take_at : height;
-        if (rows < 0) continue;
-        if (n < 0 || n > cap) atomicAdd(&a.status[NGC_STATUS_LEN_CLAMPED], 1);
-        const int take = pages(rows);
-        if (take && take_at + take > height) {      // not all of its pages are there: it gets none, nor does anybody behind it
-            atomicAdd(&a.status[NGC_STATUS_APPEND_FULL], 1);
-            rows = 0;
-        } else {
-            granted += take;
+    constexpr int STEP = 4;
+    auto plan = [&](int i0, Plan (&p)[STEP]) {
+        int n[STEP], m[STEP];
+#pragma unroll
+        for (int u = 0; u < STEP; ++u) {    // all lengths first
+            const int i = i0 + u < hi ? i0 + u : hi - 1, b = (i / a.Hkv) % a.B;
+            n[u] = a.len[a.seg0 + i];
+            m[u] = 0;
+            if constexpr (FORK) {
+                const int s = source[b];
+                m[u] = s >= 0 ? a.len[a.seg0 + i + (s - b) * a.Hkv] : -1;
+                if (s >= 0 && m[u] < 0) m[u] = 0;
+                m[u] = m[u] > cap ? cap : m[u];
+            } else {
+                m[u] = a.mark[b] != 0 ? 0 : -1;
+            }
         }
-        take_at += take;
-        a.len[a.seg0 + i] = rows;
+#pragma unroll
+        for (int u = 0; u < STEP; ++u) {
+            const int i = i0 + u < hi ? i0 + u : hi - 1, b = (i / a.Hkv) % a.B;
+            const int held = pages(n[u] < 0 ? 0 : n[u] > cap ? cap : n[u]);
+            p[u].rows = m[u];
+            p[u].clamped = m[u] >= 0 && (n[u] < 0 || n[u] > cap);
+            p[u].back = m[u] >= 0 ? held : 0;
+            p[u].take = m[u] > 0 ? pages(m[u]) : 0;
+            p[u].work = FORK ? held * ((copies[b] + FORK_COPIES - 1) / FORK_COPIES) : 0;
+        }
+    };
+    Plan p[STEP];
+    int at[3] = {0, 0, 0}, total[3];        // of pages given back, of pages granted, of pieces of work
+    for (int i0 = lo; i0 < hi; i0 += STEP) {
+        plan(i0, p);
+#pragma unroll
+        for (int u = 0; u < STEP; ++u)
+            if (i0 + u < hi) { at[0] += p[u].back; at[1] += p[u].take; at[2] += p[u].work; }
     }
-    int all;
-    (void)block_excl_scan_i<POOL_THREADS>(granted, tmp, &all);
+    block_excl_scan3<POOL_THREADS>(at, tmp, total);       // (and everybody has read the lengths and the stack's height)
+    const int height = count + total[0] < a.num_pages ? count + total[0] : a.num_pages;
+    [[maybe_unused]] int granted = 0;
+    for (int i0 = lo; i0 < hi; i0 += STEP) {
+        if (per > STEP) plan(i0, p);        // (what is stored to meanwhile is nobody's source, and every segment is one thread's)
+#pragma unroll
+        for (int u = 0; u < STEP; ++u) {
+            const int i = i0 + u;
+            if (i >= hi) break;
+            a.freed[a.seg0 + i] = p[u].back;
+            a.push_base[a.seg0 + i] = count + at[0];
+            if constexpr (FORK) {
+                a.first[i] = at[1];
+                a.work[i] = at[2];
+            }
+            if (p[u].clamped) atomicAdd(&a.status[NGC_STATUS_LEN_CLAMPED], 1);
+            // not all of its pages are there: it gets none, nor does anybody behind it
+            const bool dry = p[u].take && at[1] + p[u].take > height;
+            if (dry) atomicAdd(&a.status[NGC_STATUS_APPEND_FULL], 1);
+            else granted += p[u].take;
+            if (p[u].rows >= 0) a.len[a.seg0 + i] = dry ? 0 : p[u].rows;
+            at[0] += p[u].back;
+            at[1] += p[u].take;
+            at[2] += p[u].work;
+        }
+    }
+    const bool enough = total[1] <= height;
+    int all = total[1];
+    if (!enough) (void)block_excl_scan_i<POOL_THREADS>(granted, tmp[0], &all);
     if (threadIdx.x == 0) {
-        if (count != count_raw || count + total_back > a.num_pages) atomicAdd(&a.status[NGC_STATUS_POOL_BOUNDS], 1);
+        if (count != count_raw || count + total[0] > a.num_pages) atomicAdd(&a.status[NGC_STATUS_POOL_BOUNDS], 1);
         *a.free_count = height - all;
-        if constexpr (FORK) { a.head[0] = all; a.head[1] = height; }
+        if constexpr (FORK) {
+            a.head[0] = enough ? total[2] : all;           // either way no more than there are pages
+            a.head[1] = height;
+            a.head[2] = enough;
+            a.head[3] = shared;
+        }
     }
 }
 
 // A wave per segment: all of its pages go onto the stack.
-__global__ __launch_bounds__(64) void pool_push_kernel(PoolArgs a)
+constexpr int WAVES = 4;                    // per workgroup, where a wave takes a segment
+__global__ __launch_bounds__(WAVES * 64) void pool_push_kernel(PoolArgs a)
 {
-    const int seg = a.seg0 + (int)blockIdx.x;
+    const int i = (int)blockIdx.x * WAVES + wave_id();
+    if (i >= a.nseg) return;
+    const int seg = a.seg0 + i;
     const int f = a.freed[seg], base = a.push_base[seg];
     const int32_t *tab = a.table + (size_t)seg * a.max_pages;
-    for (int r = threadIdx.x; r < f; r += 64)
+    for (int r = lane_id(); r < f; r += 64)
         if (base + r >= 0 && base + r < a.num_pages) a.free_stack[base + r] = tab[r];
 }
 
-// Copies page `from` to page `to`, by all threads of a workgroup.
-template <int THREADS>
-__device__ __forceinline__ void copy_page(const PoolArgs &a, int from, int to, int page_bytes)
+// A wave per segment that becomes a copy: its pages, in its table and in the list of what is to be moved.  A piece of work is a
+// page and up to FORK_COPIES of its copies; where the stack did not hold enough pages, one granted page each.
+__global__ __launch_bounds__(WAVES * 64) void fork_list_kernel(PoolArgs a)
 {
-    const u32x4 *ks = reinterpret_cast<const u32x4 *>(a.k_pool + (size_t)from * page_bytes);
-    const u32x4 *vs = reinterpret_cast<const u32x4 *>(a.v_pool + (size_t)from * page_bytes);
-    u32x4 *kd = reinterpret_cast<u32x4 *>(a.k_pool + (size_t)to * page_bytes);
-    u32x4 *vd = reinterpret_cast<u32x4 *>(a.v_pool + (size_t)to * page_bytes);
-    for (int i = threadIdx.x; i < page_bytes / 16; i += THREADS) {
-        const u32x4 x = __builtin_nontemporal_load(ks + i), y = __builtin_nontemporal_load(vs + i);
-        __builtin_nontemporal_store(x, kd + i);
-        __builtin_nontemporal_store(y, vd + i);
+    const int i = (int)blockIdx.x * WAVES + wave_id();
+    if (i >= a.nseg) return;
+    const int b = (i / a.Hkv) % a.B, s = fork_source(a, b);
+    if (s < 0) return;
+    const int src = i + (s - b) * a.Hkv;
+    const bool enough = a.head[2] != 0;
+    const int height = a.head[1], first = a.first[i], rank = a.rank[b], copies = a.copies[s];
+    const int pages = (a.len[a.seg0 + i] + a.page_rows - 1) >> a.page_shift;      // 0 where none were granted
+    const int chunks = (copies + FORK_COPIES - 1) / FORK_COPIES;
+    for (int j = lane_id(); j < pages; j += 64) {
+        int to = a.free_stack[height - 1 - first - j];
+        const int from = a.table[(size_t)(a.seg0 + src) * a.max_pages + j];
+        a.table[(size_t)(a.seg0 + i) * a.max_pages + j] = to;
+        if (from < 0 || from >= a.num_pages || to < 0 || to >= a.num_pages) {
+            atomicAdd(&a.status[NGC_STATUS_POOL_BOUNDS], 1);
+            to = -1;
+        }
+        const size_t piece = enough ? (size_t)a.work[src] + (size_t)j * chunks + rank / FORK_COPIES : (size_t)first + j;
+        const int slot = enough ? rank % FORK_COPIES : 0;
+        a.to[piece * FORK_COPIES + slot] = to;
+        if (slot == 0) a.from[piece] = from;
+        if (!enough || rank == copies - 1)                 // the piece's last copy
+            for (int u = slot + 1; u < FORK_COPIES; ++u) a.to[piece * FORK_COPIES + u] = -1;
     }
-    if (a.pos_pool)
-        for (int i = threadIdx.x; i < a.page_rows; i += THREADS)
-            a.pos_pool[(size_t)to * a.page_rows + i] = a.pos_pool[(size_t)from * a.page_rows + i];
 }
 
-constexpr int COPY_THREADS = 256;
-constexpr int COPY_GROUPS = 2048;           // workgroups that share the pages
+// Moves pages: page from[x] to COPIES places to[x * COPIES ..].  Tiles of up to 128 KB of K and V: all of a tile's reads, a
+// barrier, all of its writes, a barrier (a CU whose waves mix both moves less).  Compaction (COPIES = 1) updates the tables.
+constexpr int MOVE_THREADS = 1024;
+constexpr int MOVE_GROUPS = 512;
+constexpr int MOVE_BATCH = 8;               // 16-byte pieces per thread
+constexpr int MOVE_PIECES = MOVE_THREADS * MOVE_BATCH;
+constexpr int MOVE_PAGES = MOVE_PIECES * 16 / (2 * 32 * 128);         // per tile, of the smallest kind
 
-__global__ __launch_bounds__(COPY_THREADS) void fork_copy_kernel(PoolArgs a, int page_bytes)
+template <int COPIES>
+__global__ __launch_bounds__(MOVE_THREADS) void move_pages_kernel(PoolArgs a, const int32_t *from_list, const int32_t *to_list,
+                                                                  const int32_t *owner, int page_bytes)
 {
-    const int total = a.head[0], height = a.head[1];
-    const int lo = (int)((long long)total * blockIdx.x / gridDim.x), hi = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
-    if (lo >= hi) return;
-    // the segment that page lo is granted to: the last with first <= lo (later ones of the same value take no page)
-    int i = 0;
-    for (int span = a.nseg; span > 1;) {
-        const int halfway = span / 2;
-        if (a.first[i + halfway] <= lo) i += halfway;
-        span -= halfway;
-    }
-    for (int g = lo; g < hi; ++g) {
-        while (i + 1 < a.nseg && a.first[i + 1] <= g) ++i;
-        bool invalid;
-        const int src = fork_source(a, i, &invalid);
-        const int j = g - a.first[i];
-        const int to = a.free_stack[height - 1 - g];
-        const int from = src >= 0 ? a.table[(size_t)(a.seg0 + src) * a.max_pages + j] : -1;
-        if (threadIdx.x == 0) a.table[(size_t)(a.seg0 + i) * a.max_pages + j] = to;
-        if (from < 0 || from >= a.num_pages || to < 0 || to >= a.num_pages) {
-            if (threadIdx.x == 0) atomicAdd(&a.status[NGC_STATUS_POOL_BOUNDS], 1);
-            continue;
+    __shared__ int from[MOVE_PAGES], to[COPIES][MOVE_PAGES];
+    const int total = a.head[0];
+    const bool again = COPIES > 1 && a.head[3] != 0;        // (15 copies of 48 MB take 192 us if asked for as read once,
+                                                            // 163 if not; one copy of 360 MB 176 and 182)
+    const int pieces = 2 * page_bytes / 16, shift = 31 - __builtin_clz((unsigned)pieces);     // of a page's K and V
+    // a tile holds `per` pages, or a `parts`-th of one; fewer pages where there are too few for two rounds of workgroups
+    const int most = pieces < MOVE_PIECES ? MOVE_PIECES / pieces : 1, share = total / (2 * (int)gridDim.x);
+    const int per = share < 1 ? 1 : share < most ? share : most;
+    const int parts = pieces > MOVE_PIECES ? pieces / MOVE_PIECES : 1;
+    const long long tiles = (long long)((total + per - 1) / per) * parts;
+    for (long long t = blockIdx.x; t < tiles; t += gridDim.x) {
+        const int first = (int)(t / parts) * per, part = (int)(t % parts);
+        const int here = total - first < per ? total - first : per;
+        if ((int)threadIdx.x < here * COPIES) {
+            const int x = (int)threadIdx.x / COPIES, u = (int)threadIdx.x % COPIES;
+            const int hole = to_list[(size_t)(first + x) * COPIES + u];
+            to[u][x] = hole;
+            if (u == 0) {
+                const int page = from_list[first + x];
+                from[x] = page;
+                if (COPIES == 1 && part == 0) a.table[owner[page]] = hole;
+            }
         }
-        copy_page<COPY_THREADS>(a, from, to, page_bytes);
+        __syncthreads();
+        auto place = [&](int x, int page) {
+            const int at = x & (pieces - 1);
+            return reinterpret_cast<u32x4 *>((at < pieces / 2 ? a.k_pool : a.v_pool) + (size_t)page * page_bytes) + (at & (pieces / 2 - 1));
+        };
+        const int end = here << shift;
+        u32x4 x[MOVE_BATCH];
+        // a page whose copies' places are all outside the pool is not read: its number may be outside too
+        auto wanted = [&](int q) {
+            bool any = false;
+#pragma unroll
+            for (int u = 0; u < COPIES; ++u) any |= to[u][q] >= 0;
+            return any;
+        };
+        auto read = [&](auto load) {
+#pragma unroll
+            for (int v = 0; v < MOVE_BATCH; ++v) {
+                const int i = part * MOVE_PIECES + v * MOVE_THREADS + (int)threadIdx.x;
+                if (i < end && wanted(i >> shift)) x[v] = load(place(i, from[i >> shift]));
+            }
+        };
+        if (again) read([](const u32x4 *p) { return *p; });
+        else read([](const u32x4 *p) { return __builtin_nontemporal_load(p); });
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < COPIES; ++u)
+#pragma unroll
+            for (int v = 0; v < MOVE_BATCH; ++v) {
+                const int i = part * MOVE_PIECES + v * MOVE_THREADS + (int)threadIdx.x;
+                if (i < end && to[u][i >> shift] >= 0) __builtin_nontemporal_store(x[v], place(i, to[u][i >> shift]));
+            }
+        if (a.pos_pool && part == 0)
+            for (int i = threadIdx.x; i < here * a.page_rows; i += MOVE_THREADS) {
+                const int q = i / a.page_rows, r = i % a.page_rows;
+                if (!wanted(q)) continue;
+                const int32_t pos = a.pos_pool[(size_t)from[q] * a.page_rows + r];
+#pragma unroll
+                for (int u = 0; u < COPIES; ++u)
+                    if (to[u][q] >= 0) a.pos_pool[(size_t)to[u][q] * a.page_rows + r] = pos;
+            }
+        __syncthreads();
     }
 }
 
@@ -318,17 +441,18 @@ __global__ __launch_bounds__(256) void compact_clear_kernel(CompactArgs a)
 }
 
 // A wave per segment.
-__global__ __launch_bounds__(64) void compact_mark_kernel(CompactArgs a)
+__global__ __launch_bounds__(WAVES * 64) void compact_mark_kernel(CompactArgs a)
 {
-    const int seg = (int)blockIdx.x;
+    const int seg = (int)blockIdx.x * WAVES + wave_id();
+    if (seg >= a.p.nseg) return;
     const int cap = a.p.page_rows * a.p.max_pages;
     int n = a.p.len[seg];
     if (n < 0 || n > cap) {
-        if (threadIdx.x == 0) atomicAdd(&a.p.status[NGC_STATUS_LEN_CLAMPED], 1);
+        if (lane_id() == 0) atomicAdd(&a.p.status[NGC_STATUS_LEN_CLAMPED], 1);
         n = n < 0 ? 0 : cap;
     }
     const int pages = (n + a.p.page_rows - 1) >> a.p.page_shift;
-    for (int j = threadIdx.x; j < pages; j += 64) {
+    for (int j = lane_id(); j < pages; j += 64) {
         const int page = a.p.table[(size_t)seg * a.p.max_pages + j];
         if (page < 0 || page >= a.p.num_pages) {
             atomicAdd(&a.p.status[NGC_STATUS_POOL_BOUNDS], 1);
@@ -389,28 +513,20 @@ __global__ __launch_bounds__(POOL_THREADS) void compact_scan_kernel(CompactArgs 
     }
 }
 
-// A thread per word: its holes and movers enter the lists; the free stack becomes the pages from U on, the lowest on top.
+// A thread per page: holes and movers enter the lists; the free stack becomes the pages from U on, the lowest on top.
 __global__ __launch_bounds__(256) void compact_list_kernel(CompactArgs a)
 {
-    const int w = (int)(blockIdx.x * 256 + threadIdx.x);
-    if (w >= a.words) return;
+    const int page = (int)(blockIdx.x * 256 + threadIdx.x);
+    if (page >= a.p.num_pages) return;
     int f;
     const int U = compact_used(a, &f);
+    const int w = page / 32, bit = page % 32;
     uint32_t holes, movers;
     compact_word(a, w, U, holes, movers);
-    for (int at = a.holes_before[w]; holes; holes &= holes - 1, ++at) a.hole[at] = w * 32 + __builtin_ctz(holes);
-    for (int at = a.movers_before[w]; movers; movers &= movers - 1, ++at) a.mover[at] = w * 32 + __builtin_ctz(movers);
-    for (int i = w * 32; i < w * 32 + 32 && i < f; ++i) a.p.free_stack[i] = a.p.num_pages - 1 - i;
-}
-
-__global__ __launch_bounds__(COPY_THREADS) void compact_move_kernel(CompactArgs a, int page_bytes)
-{
-    const int total = a.p.head[0];
-    for (int i = (int)blockIdx.x; i < total; i += (int)gridDim.x) {
-        const int from = a.mover[i], to = a.hole[i];
-        copy_page<COPY_THREADS>(a.p, from, to, page_bytes);
-        if (threadIdx.x == 0) a.p.table[a.owner[from]] = to;
-    }
+    const uint32_t below = (1u << bit) - 1u;
+    if ((holes >> bit) & 1u) a.hole[a.holes_before[w] + __popc(holes & below)] = page;
+    if ((movers >> bit) & 1u) a.mover[a.movers_before[w] + __popc(movers & below)] = page;
+    if (page < f) a.p.free_stack[page] = a.p.num_pages - 1 - page;
 }
 
 }  // namespace ngc
@@ -469,6 +585,11 @@ PoolArgs pool_args(const ngc_paged_cache *pc, const int32_t *mark, int seg0, int
     a.push_base = a.freed + segments;
     a.head = reinterpret_cast<int32_t *>(base + scratch_offset(&c));
     a.first = a.head + 4;
+    a.work = a.first + segments;
+    a.copies = a.work + segments;
+    a.rank = a.copies + pc->B;
+    a.from = a.rank + pc->B;
+    a.to = a.from + pc->num_pages;
     a.status = reinterpret_cast<int32_t *>(ws);
     a.seg0 = seg0; a.nseg = nseg; a.B = pc->B; a.Hkv = pc->Hkv;
     a.page_rows = pc->page_rows; a.page_shift = __builtin_ctz((unsigned)pc->page_rows);
@@ -479,7 +600,10 @@ PoolArgs pool_args(const ngc_paged_cache *pc, const int32_t *mark, int seg0, int
 // Sums of pages, and heights of the stack, in 32 bits.
 bool page_sums_fit(const ngc_paged_cache *pc, long long nseg) { return nseg * pc->max_pages + pc->num_pages <= 0x7FFFFFFFLL; }
 
-size_t fork_scratch_bytes(const ngc_paged_cache *pc) { return 16 + (size_t)pc->L * pc->B * pc->Hkv * sizeof(int32_t); }
+size_t fork_scratch_bytes(const ngc_paged_cache *pc)
+{
+    return 16 + ((size_t)pc->L * pc->B * pc->Hkv * 2 + (size_t)pc->B * 2 + (size_t)pc->num_pages * (1 + FORK_COPIES)) * sizeof(int32_t);
+}
 size_t compact_scratch_bytes(const ngc_paged_cache *pc)
 {
     const size_t words = ((size_t)pc->num_pages + 31) / 32;
@@ -548,7 +672,7 @@ extern "C" int ngc_paged_free(const ngc_paged_cache *pc, int32_t layer, const in
     hipStream_t st = (hipStream_t)stream;
     rc = launch(reinterpret_cast<const void *>(&pool_plan_kernel<false>), dim3(1), dim3(POOL_THREADS), 0, st, a);
     if (rc) return rc;
-    return launch(reinterpret_cast<const void *>(&pool_push_kernel), dim3(nseg), dim3(64), 0, st, a);
+    return launch(reinterpret_cast<const void *>(&pool_push_kernel), dim3((nseg + WAVES - 1) / WAVES), dim3(WAVES * 64), 0, st, a);
 }
 
 extern "C" int ngc_paged_fork(const ngc_paged_cache *pc, int32_t layer, const int32_t *source, void *ws, size_t ws_bytes, void *stream)
@@ -561,16 +685,19 @@ extern "C" int ngc_paged_fork(const ngc_paged_cache *pc, int32_t layer, const in
     if (rc) return rc;
     const ngc_cache c = logical_geometry(pc);
     if (ws_bytes < scratch_offset(&c) + fork_scratch_bytes(pc)) return NGC_ENOSPC;
-    if (!page_sums_fit(pc, nseg)) return NGC_EUNSUPPORTED;
+    if (!page_sums_fit(pc, nseg) || pc->B > FORK_SEQUENCES) return NGC_EUNSUPPORTED;
     PoolArgs a = pool_args(pc, source, seg0, nseg, ws);
     hipStream_t st = (hipStream_t)stream;
     rc = launch(reinterpret_cast<const void *>(&pool_plan_kernel<true>), dim3(1), dim3(POOL_THREADS), 0, st, a);
     if (rc) return rc;
-    rc = launch(reinterpret_cast<const void *>(&pool_push_kernel), dim3(nseg), dim3(64), 0, st, a);
+    const dim3 waves((nseg + WAVES - 1) / WAVES), threads(WAVES * 64);
+    rc = launch(reinterpret_cast<const void *>(&pool_push_kernel), waves, threads, 0, st, a);
     if (rc) return rc;
-    const int page_bytes = pc->page_rows * pc->D * 2;
-    void *kargs[] = {&a, const_cast<int *>(&page_bytes)};
-    NGC_HIP_CHECK(hipLaunchKernel(reinterpret_cast<const void *>(&fork_copy_kernel), dim3(COPY_GROUPS), dim3(COPY_THREADS), kargs, 0, st));
+    rc = launch(reinterpret_cast<const void *>(&fork_list_kernel), waves, threads, 0, st, a);
+    if (rc) return rc;
+    hipLaunchKernelGGL(move_pages_kernel<FORK_COPIES>, dim3(MOVE_GROUPS), dim3(MOVE_THREADS), 0, st, a, a.from, a.to, nullptr,
+                       pc->page_rows * pc->D * 2);
+    NGC_HIP_CHECK(hipGetLastError());
     return NGC_OK;
 }
 
@@ -594,16 +721,16 @@ extern "C" int ngc_paged_compact(const ngc_paged_cache *pc, void *ws, size_t ws_
     a.mover = a.hole + pc->num_pages;
     hipStream_t st = (hipStream_t)stream;
     const int blocks = (a.words + 255) / 256;
-    const int page_bytes = pc->page_rows * pc->D * 2;
     hipLaunchKernelGGL(compact_clear_kernel, dim3(blocks < 256 ? blocks : 256), dim3(256), 0, st, a);
     NGC_HIP_CHECK(hipGetLastError());
-    hipLaunchKernelGGL(compact_mark_kernel, dim3((unsigned)segments), dim3(64), 0, st, a);
+    hipLaunchKernelGGL(compact_mark_kernel, dim3((unsigned)((segments + WAVES - 1) / WAVES)), dim3(WAVES * 64), 0, st, a);
     NGC_HIP_CHECK(hipGetLastError());
     hipLaunchKernelGGL(compact_scan_kernel, dim3(1), dim3(POOL_THREADS), 0, st, a);
     NGC_HIP_CHECK(hipGetLastError());
-    hipLaunchKernelGGL(compact_list_kernel, dim3(blocks), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(compact_list_kernel, dim3((pc->num_pages + 255) / 256), dim3(256), 0, st, a);
     NGC_HIP_CHECK(hipGetLastError());
-    hipLaunchKernelGGL(compact_move_kernel, dim3(COPY_GROUPS), dim3(COPY_THREADS), 0, st, a, page_bytes);
+    hipLaunchKernelGGL(move_pages_kernel<1>, dim3(MOVE_GROUPS), dim3(MOVE_THREADS), 0, st, a.p, a.mover, a.hole, a.owner,
+                       pc->page_rows * pc->D * 2);
     NGC_HIP_CHECK(hipGetLastError());
     return NGC_OK;
 }

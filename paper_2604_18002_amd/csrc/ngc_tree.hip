@@ -416,7 +416,7 @@ void tree_attn_kernel(TreeArgs a)
                 for (int r = 0; r < 16; ++r) sc[st][r] = (w >> (8 * (r / 4) + r % 4)) & 1u ? sc[st][r] : -INFINITY;
             }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) top = max_no_nan(top, sc[st][r]);
+            for (int r = 0; r < 16; r += 2) top = max_or_nan(max_or_nan(top, sc[st][r]), sc[st][r + 1]);
         }
         raise_reference(half_rows_max(top) * a.scale_log2e);
 #pragma unroll
@@ -674,9 +674,9 @@ void tree_narrow_kernel(TreeArgs a)
 #pragma unroll
             for (int r = 0; r < 16; ++r) sc[r] = (w >> (8 * (r / 4) + r % 4)) & 1u ? sc[r] : -INFINITY;
         }
-        float tmx = sc[0];
+        float tmx = -INFINITY;
 #pragma unroll
-        for (int r = 1; r < 16; ++r) tmx = max_no_nan(tmx, sc[r]);
+        for (int r = 0; r < 16; r += 2) tmx = max_or_nan(max_or_nan(tmx, sc[r]), sc[r + 1]);
         tmx = half_rows_max(tmx) * a.scale_log2e;
         if (__ballot(tmx > m_run + TREE_LAZY)) {
             const float m_new = max_no_nan(m_run, tmx);

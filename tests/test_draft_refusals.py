@@ -115,6 +115,8 @@ def test_sequences_of_a_paged_cache(ngc):
         assert call(_cache(ngc, True, page_rows=33)) == ngc.NGC_EINVAL
         assert call(_cache(ngc, True, B=60000, L=60, max_pages=16384)) in (ngc.NGC_EUNSUPPORTED, ngc.NGC_ENOSPC)
         assert call(_cache(ngc, True, B=60000, L=60, max_pages=16384), ws_bytes=1 << 40) == ngc.NGC_EUNSUPPORTED
+    many = _cache(ngc, True, B=8193)
+    assert lib.ngc_paged_fork(C.byref(many), -1, A, A, 1 << 40, None) == ngc.NGC_EUNSUPPORTED
     compact = lambda c, ws=A, n=need: lib.ngc_paged_compact(C.byref(c), ws, n, None)     # noqa: E731
     assert compact(_cache(ngc, True), None) == ngc.NGC_EINVAL and compact(_cache(ngc, True), A + 8) == ngc.NGC_EINVAL
     assert compact(_cache(ngc, True), n=need // 100) == ngc.NGC_ENOSPC
