@@ -54,8 +54,6 @@ struct TreeArgs {
     float *part_o;                      // [segments of the launch][S][R][D]
     float *part_ml;                     // [segments of the launch][S][R][2]
     int32_t *status;
-    int32_t *ticket;                    // [segments of the launch][ticket_step]: 0 between launches; nullptr: joined by a launch
-    int ticket_step;
     int seg0, S, W, G, B, Hkv, cap;
     float scale_log2e;
     const int32_t *table;               // paged layout only
@@ -510,7 +508,6 @@ void tree_narrow_kernel(TreeArgs a)
 
     __shared__ __align__(16) unsigned char lds_k[TREE_WAVES * TILE_LDS], lds_v[TREE_WAVES * TILE_LDS];
     __shared__ float red_m[TREE_WAVES][TREE_QW], red_l[TREE_WAVES][TREE_QW];
-    __shared__ int is_last;
 
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
     const int li = lane & 31, half = lane >> 5;
@@ -534,7 +531,7 @@ void tree_narrow_kernel(TreeArgs a)
     const int cache_tiles = (n + TREE_MT - 1) / TREE_MT;
     const int tiles = cache_tiles + (nd + TREE_MT - 1) / TREE_MT;
     const int parts = (tiles + TREE_WAVES - 1) / TREE_WAVES < a.S ? (tiles + TREE_WAVES - 1) / TREE_WAVES : a.S;   // with tiles
-    if (split >= parts) return;                            // (they take no ticket)
+    if (split >= parts) return;
 
     const unsigned char *kseg = PAGED ? a.k : a.k + (size_t)(a.seg0 + s.seg_local) * a.cap * ROW_BYTES;
     const unsigned char *vseg = PAGED ? a.v : a.v + (size_t)(a.seg0 + s.seg_local) * a.cap * ROW_BYTES;
@@ -791,69 +788,11 @@ void tree_narrow_kernel(TreeArgs a)
         }
         return;
     }
-    const size_t rows = (size_t)a.W * G;
-    const size_t first = ((size_t)s.seg_local * a.S + split) * rows;
-    if (!a.ticket) {                                       // a second launch joins the partials
-        for (int row = threadIdx.x / OP; row < R; row += ROWS) {
-            const f32x4 o = joined(row, m_all, l_all);
-            *(reinterpret_cast<f32x4 *>(a.part_o + (first + row) * D) + piece) = o;
-            if (piece == 0) *reinterpret_cast<f32x2 *>(a.part_ml + (first + row) * 2) = f32x2{m_all, l_all};
-        }
-        return;
-    }
-    // The partials cross workgroups (and the L2 caches of different XCDs) through device-scope stores and loads; the workgroup
-    // that takes the segment's last ticket joins them.
-    {
-        const __amdgpu_buffer_rsrc_t po = device_span(a.part_o + first * D, (uint32_t)(rows * D * sizeof(float)));
-        const __amdgpu_buffer_rsrc_t pml = device_span(a.part_ml + first * 2, (uint32_t)(rows * 2 * sizeof(float)));
-        for (int row = threadIdx.x / OP; row < R; row += ROWS) {
-            const f32x4 o = joined(row, m_all, l_all);
-            st_device16(po, (uint32_t)((row * D + piece * 4) * sizeof(float)), o);
-            if (piece == 0) st_device8(pml, (uint32_t)(row * 2 * sizeof(float)), f32x2{m_all, l_all});
-        }
-    }
-    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this thread's partial stores have reached memory
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        int32_t *ticket = a.ticket + (size_t)s.seg_local * a.ticket_step;
-        const int old = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        is_last = old == parts - 1;
-        if (is_last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __syncthreads();
-    if (!is_last) return;
-    __asm__ volatile("" ::: "memory");
-    const size_t all = (size_t)s.seg_local * a.S * rows;
-    const __amdgpu_buffer_rsrc_t po = device_span(a.part_o + all * D, (uint32_t)(parts * rows * D * sizeof(float)));
-    const __amdgpu_buffer_rsrc_t pml = device_span(a.part_ml + all * 2, (uint32_t)(parts * rows * 2 * sizeof(float)));
-    constexpr int BATCH = 8;
-    for (int row = threadIdx.x / OP; row < R; row += ROWS) {
-        float M = TREE_M_INIT, den = 0.f;
-        f32x4 num = {0.f, 0.f, 0.f, 0.f};
-        for (int p0 = 0; p0 < parts; p0 += BATCH) {
-            f32x4 o[BATCH];
-            f32x2 ml[BATCH];
-#pragma unroll
-            for (int u = 0; u < BATCH; ++u) {
-                const uint32_t at = (uint32_t)((p0 + u < parts ? p0 + u : parts - 1) * (int)rows + row);
-                o[u] = ld_device16(po, (uint32_t)((at * D + piece * 4) * sizeof(float)));
-                ml[u] = ld_device8(pml, (uint32_t)(at * 2 * sizeof(float)));
-            }
-            float top = M;
-#pragma unroll
-            for (int u = 0; u < BATCH; ++u) top = fmaxf(top, ml[u][0]);
-            const float old = fast_exp2(M - top);
-            den *= old;
-            num *= old;
-            M = top;
-#pragma unroll
-            for (int u = 0; u < BATCH; ++u) {
-                const float f = p0 + u < parts ? fast_exp2(ml[u][0] - top) : 0.f;
-                den += ml[u][1] * f;
-                num += o[u] * f;
-            }
-        }
-        write(row, num, M, den);
+    const size_t first = ((size_t)s.seg_local * a.S + split) * (size_t)(a.W * G);
+    for (int row = threadIdx.x / OP; row < R; row += ROWS) {           // a second launch joins the partials
+        const f32x4 o = joined(row, m_all, l_all);
+        *(reinterpret_cast<f32x4 *>(a.part_o + (first + row) * D) + piece) = o;
+        if (piece == 0) *reinterpret_cast<f32x2 *>(a.part_ml + (first + row) * 2) = f32x2{m_all, l_all};
     }
 }
 
@@ -913,11 +852,10 @@ namespace {
 constexpr int TREE_MAX_NODES = 64;          // a word of ancestor bits
 constexpr int TREE_MAX_SPLITS = 64;
 constexpr int TREE_RESIDENT = 512;          // workgroups that the chip holds at once
-constexpr size_t TREE_TICKET_BYTES = 128 * 1024;
+constexpr int TREE_CUS = 256;
 
 struct TreeShape {
-    bool narrow;
-    int wq, blocks, splits;             // row blocks of 32 in a workgroup, workgroups for the rows, and for the keys
+    int wq, blocks, splits;             // row blocks of 32 in a workgroup (1: tree_narrow_kernel), workgroups for the rows, and for the keys
     TreeTiles tiles;
 };
 
@@ -927,19 +865,60 @@ size_t tree_partial_bytes(const ngc_cache *c, int nseg, int W, int S)
     return S > 1 ? align256(rows * c->D * sizeof(float)) + align256(rows * 2 * sizeof(float)) : 0;
 }
 
+int tree_most_splits(int nseg, int blocks, int groups)
+{
+    long long most = TREE_RESIDENT / ((long long)nseg * blocks);
+    most = most < groups ? most : groups;
+    most = most < TREE_MAX_SPLITS ? most : TREE_MAX_SPLITS;
+    return most > 1 ? (int)most : 1;
+}
+
+// How many workgroups share a segment's keys.  A workgroup works through rounds of tiles, 256 keys of four waves' (narrow) or 64
+// of one tile: 1.2 us (narrow, and two row blocks) or 1.6 us (four) a round at D = 128, half of that at D = 64.  Two workgroups on
+// a CU take 1.3 times as long as one (narrow) or no longer.  The rows come at 4.5 TB/s while it lasts, less where the last
+// workgroups have a CU to themselves; of the two the longer counts whole, the other by 0.64.  Sharing costs a launch that
+// joins the partials and their way to memory and back.  Microseconds per launch at S workgroups (HIP graph), best in brackets,
+// * what the rule takes (1.01 times the best on average):
+//     segments x rows, query rows     S=1     2      3      4       6      8      12     16     24     32     48
+//         8 x 4000,  32              42.4   27.1   21.5   18.4    16.1   14.0   13.6  [12.6]* 13.4   12.7
+//        64 x  800,  24              15.1   14.1   13.4  [12.6]*  13.1   13.2
+//        80 x 4000,  30              48.9   37.3  [36.1]* 42.7    38.7   40.5
+//       128 x 1493,  48              35.9   33.7   32.2  [30.7]*  39.6   40.2
+//        16 x  700,  56              20.8   16.4   14.5   14.2    12.5   12.6  [11.9]*
+//        32 x  525,  96              32.9   23.4   19.6   18.7   [16.4]  16.9                              (* 5: 18.6)
+//        32 x 2000, 128              67.7   43.2   33.2   30.0   [25.4]* 28.0   28.6   29.0
+//         8 x 6000, 112             175.0   94.3   67.0   53.2    39.3   32.5   26.5   23.3  [21.2]* 22.0   25.9
+//       128 x 2000, 128             117.5   74.1   70.6  [64.7]*  75.8   76.6
+//       512 x 2713,  28 and 63    [113, 131]* 126, 152
+int tree_splits(int nseg, int rows, int blocks, int row_bytes, int max_len, int groups, int wq)
+{
+    const int most = tree_most_splits(nseg, blocks, groups);
+    const float round = (wq == 4 ? 1.6f : 1.2f) * (row_bytes == 256 ? 1.f : 0.5f);
+    const float read = (float)nseg * (float)max_len * 2.f * (float)row_bytes / 4.5e6f;
+    int best = 1;
+    float best_us = 3.0e38f;
+    for (int s = 1; s <= most; ++s) {
+        const int rounds = (groups + s - 1) / s;
+        if (s > 1 && (groups + s - 2) / (s - 1) == rounds) continue;       // one fewer does as well
+        const int wg = nseg * blocks * s, per_cu = (wg + TREE_CUS - 1) / TREE_CUS;
+        const float work = round * (float)rounds * (per_cu == 1 ? 1.f : (float)per_cu * (wq == 1 ? 0.66f : 0.5f));
+        const float wait = read * (per_cu == 1 ? 1.f : sqrtf((float)(per_cu * TREE_CUS) / (float)wg));
+        const float shared = s == 1 ? 0.f : 1.27f * (float)per_cu + (float)wg * (float)rows * (float)row_bytes * 4.f / 5.0e6f;
+        const float us = (work > wait ? work + 0.64f * wait : wait + 0.64f * work) + shared;
+        if (us < best_us) { best_us = us; best = s; }
+    }
+    return best;
+}
+
 TreeShape tree_shape(const ngc_cache *c, int nseg, int W, int max_len)
 {
     const int R = W * (c->Hq / c->Hkv);
     TreeShape s;
-    s.narrow = R <= TREE_QW;
     s.wq = R <= TREE_QW ? 1 : R <= 2 * TREE_QW ? 2 : 4;
-    s.blocks = (R + s.wq * TREE_QW - 1) / (s.wq * TREE_QW);
-    s.tiles = s.narrow ? TreeTiles{TREE_MT, TREE_WAVES} : TreeTiles{64, 1};
-    const int tiles = s.tiles.groups(max_len, W);
-    long long most = TREE_RESIDENT / ((long long)nseg * s.blocks);
-    most = most < tiles ? most : tiles;
-    most = most < TREE_MAX_SPLITS ? most : TREE_MAX_SPLITS;
-    s.splits = most > 1 ? (int)most : 1;
+    const int rows = s.wq * TREE_QW;
+    s.blocks = (R + rows - 1) / rows;
+    s.tiles = s.wq == 1 ? TreeTiles{TREE_MT, TREE_WAVES} : TreeTiles{64, 1};
+    s.splits = tree_splits(nseg, R < rows ? R : rows, s.blocks, c->D * 2, max_len, s.tiles.groups(max_len, W), s.wq);
     return s;
 }
 
@@ -999,18 +978,13 @@ int launch_tree(const ngc_cache *c, const ngc_paged_cache *pc, int32_t layer, co
     hipStream_t st = (hipStream_t)stream;
 #define NGC_TREE(KERNEL, ...) (pc ? reinterpret_cast<const void *>(&KERNEL<__VA_ARGS__, true>) \
                                   : reinterpret_cast<const void *>(&KERNEL<__VA_ARGS__, false>))
-#define NGC_TREE_D(D) (shape.narrow ? NGC_TREE(tree_narrow_kernel, D) : shape.wq == 2 ? NGC_TREE(tree_attn_kernel, D, 2, true) \
+#define NGC_TREE_D(D) (shape.wq == 1 ? NGC_TREE(tree_narrow_kernel, D) : shape.wq == 2 ? NGC_TREE(tree_attn_kernel, D, 2, true) \
                        : shape.blocks == 1 ? NGC_TREE(tree_attn_kernel, D, 4, true) : NGC_TREE(tree_attn_kernel, D, 4, false))
     const void *fn = c->D == 128 ? NGC_TREE_D(128) : NGC_TREE_D(64);
 #undef NGC_TREE_D
 #undef NGC_TREE
-    const bool tickets = shape.narrow && (size_t)S * W * G * c->D * sizeof(float) <= TREE_TICKET_BYTES;
-    if (tickets) {
-        a.ticket = reinterpret_cast<int32_t *>(reinterpret_cast<unsigned char *>(ws) + ticket_offset(c));
-        a.ticket_step = ticket_step((size_t)c->L * per_layer, nseg);
-    }
     const int rc = launch(fn, dim3(nseg, S, shape.blocks), dim3(TREE_WAVES * 64), 0, st, a);
-    if (rc || S == 1 || tickets) return rc;
+    if (rc || S == 1) return rc;
     const int rows_per = TREE_MERGE_THREADS / (c->D / 4);
     const dim3 grid(nseg, (W * G + rows_per - 1) / rows_per);
     if (c->D == 128) hipLaunchKernelGGL(tree_merge_kernel<128>, grid, dim3(TREE_MERGE_THREADS), 0, st, a, shape.tiles);
@@ -1025,8 +999,11 @@ extern "C" size_t ngc_tree_workspace_bytes(const ngc_cache *c, int32_t W)
     if (!tree_geometry_ok(c, W)) return 0;
     const int per_layer = c->B * c->Hkv;
     // one layer or all layers, any length hint: the most workgroups a segment can be shared by
-    const size_t one = tree_partial_bytes(c, per_layer, W, tree_shape(c, per_layer, W, c->cap).splits);
-    const size_t all = tree_partial_bytes(c, per_layer * c->L, W, tree_shape(c, per_layer * c->L, W, c->cap).splits);
+    auto most = [&](int nseg) {
+        const TreeShape s = tree_shape(c, nseg, W, c->cap);
+        return tree_partial_bytes(c, nseg, W, tree_most_splits(nseg, s.blocks, s.tiles.groups(c->cap, W)));
+    };
+    const size_t one = most(per_layer), all = most(per_layer * c->L);
     const size_t own = scratch_offset(c) + (one > all ? one : all), others = ngc_workspace_bytes(c, 0);
     return own > others ? own : others;
 }
