@@ -69,32 +69,38 @@ struct TreeTiles {
     }
 };
 
+// A word that nobody writes during the launch, at a wave-uniform address: through the scalar unit.  (Behind a load to LDS the
+// compiler takes any memory for changed, loads the word into a vector register and waits for everything in front of it.)
+__device__ __forceinline__ int32_t constant_word(const int32_t *p)
+{
+    return *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>((uintptr_t)p);
+}
+
 // What a workgroup has to know about its segment.
 struct TreeSegment {
-    int seg_local, b, h, n, nd;         // rows in the cache, drafted nodes
+    int seg_local, h;
     size_t seq;                         // launch layer * B + sequence
-};
+    int b;
+    int n, nd;                          // rows in the cache, drafted nodes; as they are in memory until clamp()
 
-__device__ __forceinline__ TreeSegment tree_segment(const TreeArgs &a, bool counts)
-{
-    TreeSegment s;
-    s.seg_local = (int)blockIdx.x;
-    const int seg = a.seg0 + s.seg_local;
-    s.seq = (size_t)(s.seg_local / a.Hkv);
-    s.h = s.seg_local % a.Hkv;
-    s.b = (int)(s.seq % a.B);
-    s.n = a.len[seg];
-    s.nd = a.n_draft ? a.n_draft[s.b] : a.W;
-    if (s.n < 0 || s.n > a.cap) {
-        if (counts) atomicAdd(&a.status[NGC_STATUS_LEN_CLAMPED], 1);
-        s.n = s.n < 0 ? 0 : a.cap;
+    __device__ __forceinline__ TreeSegment(const TreeArgs &a)
+        : seg_local((int)blockIdx.x), h(seg_local % a.Hkv), seq((size_t)(seg_local / a.Hkv)),
+          b((int)(seq % a.B)), n(constant_word(a.len + a.seg0 + seg_local)),
+          nd(a.n_draft ? constant_word(a.n_draft + b) : a.W)
+    {
     }
-    if (s.nd < 0 || s.nd > a.W) {
-        if (counts && s.h == 0) atomicAdd(&a.status[NGC_STATUS_BAD_TREE], 1);
-        s.nd = s.nd < 0 ? 0 : a.W;
+    __device__ __forceinline__ void clamp(const TreeArgs &a, bool counts)
+    {
+        if (n < 0 || n > a.cap) {
+            if (counts) atomicAdd(&a.status[NGC_STATUS_LEN_CLAMPED], 1);
+            n = n < 0 ? 0 : a.cap;
+        }
+        if (nd < 0 || nd > a.W) {
+            if (counts && h == 0) atomicAdd(&a.status[NGC_STATUS_BAD_TREE], 1);
+            nd = nd < 0 ? 0 : a.W;
+        }
     }
-    return s;
-}
+};
 
 // The bits of a node's ancestors, itself included, in lane = node; steps of 1, 2, 4, .. up the tree.  A parent that does
 // not come before its child is taken for none.
@@ -142,33 +148,72 @@ void tree_attn_kernel(TreeArgs a)
     const int wq = wv % WQ, wk = wv / WQ;
     const int li = lane & 31, half = lane >> 5;
     const int split = (int)blockIdx.y, block = (int)blockIdx.z;
-    const TreeSegment s = tree_segment(a, threadIdx.x == 0 && split == 0 && block == 0);
+    TreeSegment s(a);
     const int G = a.G, Hq = a.G * a.Hkv;
-    const int R = s.nd * G;                                // query rows that there are
-    const int row_base = block * RB;
-    if (row_base >= R) return;                             // (uniform; also where nothing is drafted)
-    const int n = s.n, nd = s.nd;
-    const int cache_tiles = (n + KT - 1) / KT;
-    const int tiles = cache_tiles + 1;                     // the last one: the drafted rows
-    if (split >= tiles) return;                            // no partial: the merge counts tiles too
+    const int row_base = block * RB, wave_row0 = row_base + wq * TREE_QW;
 
-    const int wave_row0 = row_base + wq * TREE_QW;
-    const bool active = wave_row0 < R;                     // (a last block may have waves without query rows)
-    const int my_row = wave_row0 + li < R ? wave_row0 + li : R - 1;
-    const int node = my_row / G, head = s.h * G + my_row % G;
-
-    // ---- query operands: 32 rows per wave, lane % 32 = row ------------------------
+    // ---- asked for before the lengths have arrived: parents, queries (32 rows per wave, lane % 32 = row) and the first tile ----
+    const int up = a.parent[(size_t)s.b * a.W + (lane < a.W ? lane : a.W - 1)];      // (of lanes that are no node it is not looked at)
+    const int my_row = wave_row0 + li < a.W * G ? wave_row0 + li : a.W * G - 1;
+    const int node = my_row / G;
     bf16x8 qop[KCH];
     {
-        const unsigned char *qrow = a.q + ((s.seq * a.W + node) * Hq + head) * ROW_BYTES;
+        const unsigned char *qrow = a.q + ((s.seq * a.W + node) * Hq + s.h * G + my_row % G) * ROW_BYTES;
 #pragma unroll
         for (int c = 0; c < KCH; ++c)
             qop[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qrow + c * 32 + half * 16));
     }
-    // ---- where rows lie ---------------------------------------------------------
     const unsigned char *kseg = PAGED ? a.k : a.k + (size_t)(a.seg0 + s.seg_local) * a.cap * ROW_BYTES;
     const unsigned char *vseg = PAGED ? a.v : a.v + (size_t)(a.seg0 + s.seg_local) * a.cap * ROW_BYTES;
     const int32_t *tab = PAGED ? a.table + (size_t)(a.seg0 + s.seg_local) * a.max_pages : nullptr;
+    auto row_base_of = [&](int r0) -> size_t {             // of a cached row, in bytes
+        if constexpr (!PAGED) return (size_t)r0 * ROW_BYTES;
+        int page = constant_word(tab + (r0 >> a.page_shift));
+        page = (page < 0 || page >= a.num_pages) ? 0 : page;          // never leave the pool
+        return (((size_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1))) * ROW_BYTES;
+    };
+    // Rows of a tile go straight from memory to LDS: a wave-wide load brings LOAD_ROWS whole rows, lane after lane.  The K
+    // pieces of row r are stored at slot (piece ^ (r & SWZ)), so that reading one piece of 32 consecutive rows meets every
+    // bank; the V pieces at (piece ^ v_swizzle(r)), so that reading 32 bytes of 4 consecutive rows does.
+    constexpr int SWZ = PIECES - 1;
+    auto v_swizzle = [](int r) { return (2 * r) & (PIECES < 16 ? SWZ : 7); };
+    auto k_swizzle = [](int r) { return r & SWZ; };
+    const int lrow = lane / PIECES, lslot = lane % PIECES;
+    auto load_row = [&](const unsigned char *row, int slot_row, unsigned char *to, auto swizzle) {
+        const unsigned char *at = row + (uint32_t)(lslot ^ swizzle(slot_row + lrow)) * 16u;
+        if constexpr (ONCE) load_once_to_lds16(at, to + slot_row * ROW_BYTES);
+        else load_to_lds16(at, to + slot_row * ROW_BYTES);
+    };
+    int t = split;
+    const int S = a.S;
+    {   // the first tile as if it were full (rows behind the capacity are the last one again): where it is not, it is asked for again
+        int r0 = t * KT + wv * WAVE_ROWS;
+        r0 = r0 < a.cap ? r0 : a.cap - 1;
+        const size_t base0 = row_base_of(r0);
+        const int most = a.cap - 1 - r0;
+#pragma unroll
+        for (int r = 0; r < LOADS; ++r) {
+            const int row = r * LOAD_ROWS + lrow < most ? r * LOAD_ROWS + lrow : most;
+            load_row(kseg + base0 + (uint32_t)row * ROW_BYTES, wv * WAVE_ROWS + r * LOAD_ROWS, lds_k0, k_swizzle);
+        }
+        __builtin_amdgcn_sched_barrier(0);                 // in this order: it is waited for in this order
+#pragma unroll
+        for (int r = 0; r < LOADS; ++r) {
+            const int row = r * LOAD_ROWS + lrow < most ? r * LOAD_ROWS + lrow : most;
+            load_row(vseg + base0 + (uint32_t)row * ROW_BYTES, wv * WAVE_ROWS + r * LOAD_ROWS, lds_v0, v_swizzle);
+        }
+        __asm__ volatile("" ::: "memory");
+    }
+    s.clamp(a, threadIdx.x == 0 && split == 0 && block == 0);
+    const int R = s.nd * G;                                // query rows that there are
+    const int n = s.n, nd = s.nd;
+    const int cache_tiles = (n + KT - 1) / KT;
+    const int tiles = cache_tiles + 1;                     // the last one: the drafted rows
+    if (row_base >= R || split >= tiles) {                 // (uniform; the merge counts tiles too)
+        __builtin_amdgcn_s_waitcnt(0x0F70);                // nothing may be on its way to LDS that is not this workgroup's any more
+        return;
+    }
+    const bool active = wave_row0 < R;                     // (a last block may have waves without query rows)
     const size_t draft_at = ((s.seq * a.W) * a.Hkv + s.h) * ROW_BYTES;
     const uint32_t draft_row = (uint32_t)a.Hkv * ROW_BYTES;
     // First of the wave's rows in cache tile t, the segment's last row where there are none; paged: its place in the pools.
@@ -177,20 +222,8 @@ void tree_attn_kernel(TreeArgs a)
         return r0 < n ? r0 : n - 1;
     };
     auto tile_base = [&](int t) -> size_t {                // of the wave's first row, in bytes
-        if (t >= cache_tiles) return draft_at;
-        const int r0 = first_row(t);
-        if constexpr (!PAGED) return (size_t)r0 * ROW_BYTES;
-        int page = tab[r0 >> a.page_shift];
-        page = (page < 0 || page >= a.num_pages) ? 0 : page;          // never leave the pool
-        return (((size_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1))) * ROW_BYTES;
+        return t >= cache_tiles ? draft_at : row_base_of(first_row(t));
     };
-
-    // Rows of a tile go straight from memory to LDS: a wave-wide load brings LOAD_ROWS whole rows, lane after lane.  The K
-    // pieces of row r are stored at slot (piece ^ (r & SWZ)), so that reading one piece of 32 consecutive rows meets every
-    // bank; the V pieces at (piece ^ v_swizzle(r)), so that reading 32 bytes of 4 consecutive rows does.
-    constexpr int SWZ = PIECES - 1;
-    auto v_swizzle = [](int r) { return (2 * r) & (PIECES < 16 ? SWZ : 7); };
-    const int lrow = lane / PIECES, lslot = lane % PIECES;
     auto load = [&](int t, size_t base, const unsigned char *cached, const unsigned char *drafts, unsigned char *to, auto swizzle) {
         const bool drafted = t >= cache_tiles;
         const unsigned char *src = drafted ? drafts + base : cached + base;
@@ -200,30 +233,23 @@ void tree_attn_kernel(TreeArgs a)
         const int start = drafted ? wv * WAVE_ROWS : first;
 #pragma unroll
         for (int r = 0; r < LOADS; ++r) {
-            const int slot_row = wv * WAVE_ROWS + r * LOAD_ROWS;
             int row = start + r * LOAD_ROWS + lrow;
             row = row < last ? row : last;
-            const unsigned char *at = src + ((uint32_t)(row - first) * stride + (uint32_t)(lslot ^ swizzle(slot_row + lrow)) * 16u);
-            if constexpr (ONCE) load_once_to_lds16(at, to + slot_row * ROW_BYTES);
-            else load_to_lds16(at, to + slot_row * ROW_BYTES);
+            load_row(src + (uint32_t)(row - first) * stride, wv * WAVE_ROWS + r * LOAD_ROWS, to, swizzle);
         }
     };
-    auto load_k = [&](int t, size_t base, unsigned char *to) { load(t, base, kseg, a.k_draft, to, [&](int r) { return r & SWZ; }); };
+    auto load_k = [&](int t, size_t base, unsigned char *to) { load(t, base, kseg, a.k_draft, to, k_swizzle); };
     auto load_v = [&](int t, size_t base, unsigned char *to) { load(t, base, vseg, a.v_draft, to, v_swizzle); };
 
-    // Asked for in this order, now and in the loop: K of a tile, its V, K of the next tile, its V, ..
-    int t = split;
-    const int S = a.S;
-    int up = lane < a.W ? a.parent[(size_t)s.b * a.W + lane] : -1;
-    __asm__ volatile("" : "+v"(up));                       // waited for here, not behind the first tile
-    size_t base1, base2;                                   // of the next tile and the one after it
-    {
+    // Asked for in this order, here and in the loop: K of a tile, its V, K of the next tile, its V, ..
+    if ((t + 1) * KT > n) {
         const size_t base0 = tile_base(t);
-        base1 = tile_base(t + S);
+        __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): not before what was asked for in vain has arrived
+        __asm__ volatile("" ::: "memory");
         load_k(t, base0, lds_k0);
         load_v(t, base0, lds_v0);
-        base2 = tile_base(t + 2 * S);
     }
+    size_t base1 = tile_base(t + S), base2 = tile_base(t + 2 * S);     // of the next tile and the one after it
 
     uint32_t sees_lo, sees_hi;             // drafted nodes that this lane's row sees
     {
@@ -513,45 +539,68 @@ void tree_narrow_kernel(TreeArgs a)
     const int li = lane & 31, half = lane >> 5;
     const int split = (int)blockIdx.y;
     const int G = a.G, Hq = a.G * a.Hkv;
-    const TreeSegment s = tree_segment(a, threadIdx.x == 0 && split == 0);
+    TreeSegment s(a);
 
-    // ---- queries and parents: neither the length nor the number of drafts is waited for ----
+    // ---- asked for before the lengths have arrived: parents, queries and the wave's first tile ----
+    const int up = a.parent[(size_t)s.b * a.W + (lane < a.W ? lane : a.W - 1)];      // (of lanes that are no node it is not looked at)
     const int my_row = li < a.W * G ? li : a.W * G - 1;
-    const int node = my_row / G, head = s.h * G + my_row % G;
+    const int node = my_row / G;
     bf16x8 qop[KCH];
     {
-        const unsigned char *qrow = a.q + ((s.seq * a.W + node) * Hq + head) * ROW_BYTES;
+        const unsigned char *qrow = a.q + ((s.seq * a.W + node) * Hq + s.h * G + my_row % G) * ROW_BYTES;
 #pragma unroll
         for (int c = 0; c < KCH; ++c)
             qop[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qrow + c * 32 + half * 16));
     }
-    int up = lane < a.W ? a.parent[(size_t)s.b * a.W + lane] : -1;
-    const int n = s.n, nd = s.nd, R = nd * G;
-    if (nd == 0) return;
-    const int cache_tiles = (n + TREE_MT - 1) / TREE_MT;
-    const int tiles = cache_tiles + (nd + TREE_MT - 1) / TREE_MT;
-    const int parts = (tiles + TREE_WAVES - 1) / TREE_WAVES < a.S ? (tiles + TREE_WAVES - 1) / TREE_WAVES : a.S;   // with tiles
-    if (split >= parts) return;
-
     const unsigned char *kseg = PAGED ? a.k : a.k + (size_t)(a.seg0 + s.seg_local) * a.cap * ROW_BYTES;
     const unsigned char *vseg = PAGED ? a.v : a.v + (size_t)(a.seg0 + s.seg_local) * a.cap * ROW_BYTES;
     const int32_t *tab = PAGED ? a.table + (size_t)(a.seg0 + s.seg_local) * a.max_pages : nullptr;
+    auto row_base_of = [&](int r0) -> size_t {             // of a cached row, in bytes
+        if constexpr (!PAGED) return (size_t)r0 * ROW_BYTES;
+        int page = constant_word(tab + (r0 >> a.page_shift));
+        page = (page < 0 || page >= a.num_pages) ? 0 : page;          // never leave the pool
+        return (((size_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1))) * ROW_BYTES;
+    };
+    constexpr int SWZ = PIECES - 1;
+    auto v_swizzle = [](int r) { return (2 * r) & (PIECES < 16 ? SWZ : 7); };
+    auto k_swizzle = [](int r) { return r & SWZ; };
+    const int lrow = lane / PIECES, lslot = lane % PIECES;
+    unsigned char *const wk = lds_k + wv * TILE_LDS, *const wvl = lds_v + wv * TILE_LDS;
+    const int step = a.S * TREE_WAVES;
+    int t = split * TREE_WAVES + wv;
+    {   // the tile as if it were full (rows behind the capacity are the last one again): where it is not, it is asked for again
+        int r0 = t * TREE_MT;
+        r0 = r0 < a.cap ? r0 : a.cap - 1;
+        const size_t base0 = row_base_of(r0);
+        const int most = a.cap - 1 - r0;
+        auto whole = [&](const unsigned char *rows, unsigned char *to, auto swizzle) {
+#pragma unroll
+            for (int r = 0; r < LOADS; ++r) {
+                const int slot_row = r * LOAD_ROWS + lrow, row = slot_row < most ? slot_row : most;
+                load_once_to_lds16(rows + base0 + (uint32_t)row * ROW_BYTES + (uint32_t)(lslot ^ swizzle(slot_row)) * 16u,
+                                   to + r * LOAD_ROWS * ROW_BYTES);
+            }
+        };
+        whole(kseg, wk, k_swizzle);
+        __builtin_amdgcn_sched_barrier(0);                 // K first: it is waited for first
+        whole(vseg, wvl, v_swizzle);
+        __asm__ volatile("" ::: "memory");
+    }
+    s.clamp(a, threadIdx.x == 0 && split == 0);
+    const int n = s.n, nd = s.nd, R = nd * G;
+    const int cache_tiles = (n + TREE_MT - 1) / TREE_MT;
+    const int tiles = cache_tiles + (nd + TREE_MT - 1) / TREE_MT;
+    const int parts = (tiles + TREE_WAVES - 1) / TREE_WAVES < a.S ? (tiles + TREE_WAVES - 1) / TREE_WAVES : a.S;   // with tiles
+    if (nd == 0 || split >= parts) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);                // nothing may be on its way to LDS that is not this workgroup's any more
+        return;
+    }
     const size_t draft_at = ((s.seq * a.W) * a.Hkv + s.h) * ROW_BYTES;
     const uint32_t draft_row = (uint32_t)a.Hkv * ROW_BYTES;
     auto tile_base = [&](int t) -> size_t {                // of a cache tile, in bytes; a tile lies inside one page
         t = t < cache_tiles ? t : cache_tiles - 1;
-        if (t < 0) return 0;
-        const int r0 = t * TREE_MT;
-        if constexpr (!PAGED) return (size_t)r0 * ROW_BYTES;
-        int page = tab[r0 >> a.page_shift];
-        page = (page < 0 || page >= a.num_pages) ? 0 : page;          // never leave the pool
-        return (((size_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1))) * ROW_BYTES;
+        return t < 0 ? 0 : row_base_of(t * TREE_MT);
     };
-
-    constexpr int SWZ = PIECES - 1;
-    auto v_swizzle = [](int r) { return (2 * r) & (PIECES < 16 ? SWZ : 7); };
-    const int lrow = lane / PIECES, lslot = lane % PIECES;
-    unsigned char *const wk = lds_k + wv * TILE_LDS, *const wvl = lds_v + wv * TILE_LDS;
     // K (or V) rows of a tile, straight to LDS; rows behind the last are the last one again
     auto load = [&](int t, size_t base, const unsigned char *cached, const unsigned char *drafts, unsigned char *to, auto swizzle) {
         const bool drafted = t >= cache_tiles;
@@ -566,18 +615,23 @@ void tree_narrow_kernel(TreeArgs a)
             load_once_to_lds16(src + ((uint32_t)row * stride + (uint32_t)(lslot ^ swizzle(slot_row)) * 16u), to + r * LOAD_ROWS * ROW_BYTES);
         }
     };
-    auto load_k = [&](int t, size_t base) { load(t, base, kseg, a.k_draft, wk, [&](int r) { return r & SWZ; }); };
+    auto load_k = [&](int t, size_t base) { load(t, base, kseg, a.k_draft, wk, k_swizzle); };
     auto load_v = [&](int t, size_t base) { load(t, base, vseg, a.v_draft, wvl, v_swizzle); };
 
-    const int step = a.S * TREE_WAVES;
-    int t = split * TREE_WAVES + wv;
     size_t base1 = 0;
-    __asm__ volatile("" : "+v"(up));       // waited for here (it was asked for with the length), not behind the first tile
     if (t < tiles) {
-        const size_t base0 = tile_base(t);
-        load_k(t, base0);
-        load_v(t, base0);
+        if ((t + 1) * TREE_MT > n) {
+            const size_t base0 = tile_base(t);
+            __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt(0): not before what was asked for in vain has arrived
+            __asm__ volatile("" ::: "memory");
+            load_k(t, base0);
+            __builtin_amdgcn_sched_barrier(0);
+            load_v(t, base0);
+        }
         base1 = tile_base(t + step);
+    } else {
+        __builtin_amdgcn_s_waitcnt(0x0F70);                // (its part of LDS takes the wave's output)
+        __asm__ volatile("" ::: "memory");
     }
     uint32_t sees_lo, sees_hi;             // drafted nodes that this lane's row sees
     {
@@ -802,7 +856,8 @@ template <int D>
 __global__ __launch_bounds__(TREE_MERGE_THREADS) void tree_merge_kernel(TreeArgs a, TreeTiles tl)
 {
     constexpr int OP = D / 4;
-    const TreeSegment s = tree_segment(a, false);
+    TreeSegment s(a);
+    s.clamp(a, false);
     const int row = (int)blockIdx.y * (TREE_MERGE_THREADS / OP) + (int)threadIdx.x / OP;
     const int piece = (int)threadIdx.x % OP;
     if (row >= s.nd * a.G) return;
