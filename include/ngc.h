@@ -514,8 +514,8 @@ int ngc_paged_score_keys(const ngc_paged_cache *pc, int32_t layer, const void *q
  * projection writes them, and enter the cache when they are accepted:
  *   k_draft, v_draft  bf16 [B][W][Hkv][D] (or [L][B][W][Hkv][D] for layer = -1),
  *            16-byte aligned.
- * Nothing is read or written at nodes >= n_draft[b].  W <= 64 (NGC_EUNSUPPORTED
- * beyond). */
+ * What the buffers hold at nodes >= n_draft[b] does not matter, and nothing is
+ * written there.  W <= 64 (NGC_EUNSUPPORTED beyond). */
 
 /* Attention of the drafted tokens of `layer` (-1 = all layers): for every node i
  * of sequence b and query head g, with h = g / (Hq / Hkv),

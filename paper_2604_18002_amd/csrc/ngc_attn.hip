@@ -721,7 +721,7 @@ bool fits_static(const ngc_cache *c, int nseg_launch, int S)
 }
 }  // namespace
 
-extern "C" int ngc_version(void) { return 220; }
+extern "C" int ngc_version(void) { return 230; }
 
 extern "C" const char *ngc_strerror(int code)
 {

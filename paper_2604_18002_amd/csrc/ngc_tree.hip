@@ -7,20 +7,33 @@
 //
 // The drafted rows live in buffers of their own, as a projection writes them ([B][W][Hkv][D]): nothing that may be
 // rejected enters the cache.  A KV head serves R = W G query rows (G query heads per node), so a segment's K and V are
-// read once for all of them and the products, 4 D R flops for 4 D bytes, range from memory bound (R below ~64) to bound
-// by the matrix cores.
+// read once for all of them: 4 D R flops for 4 D bytes, memory bound below ~64 rows, bound by the products beyond.
 //
-// A workgroup = 4 waves; wave (wq, wk) holds 32 query rows (row block wq of WQ) and takes 32 of a tile's keys (part wk of
-// WK = 4 / WQ; both halves of the 64 where WQ = 4).  Tiles go from memory straight into double-buffered LDS and are
-// shared by the waves.  S^T = K Q^T and O^T = V^T P by 32x32x16 matrix instructions: one query row per lane % 32, so all
-// soft-max state is lane local and crosses lanes once, between the two halves; one pass with a running maximum and sum.
+// S^T = K Q^T and O^T = V^T P by 32x32x16 matrix instructions: one query row per lane % 32, so all soft-max state is lane
+// local and crosses lanes once, between the two halves; one pass over the keys with a running maximum and sum.  K and V go
+// from memory straight into LDS, V is read transposed from there.  Two kernels:
+//   tree_narrow_kernel  R <= 32: every wave has all query rows and walks key tiles of its own, without a barrier;
+//   tree_attn_kernel    beyond: 4 waves share tiles of 64 keys, wave (wq, wk) has row block wq of WQ = 2 or 4 and part wk of
+//                       the keys; more than 128 rows are several workgroups.
 // The drafted rows are one more tile behind those of the cache, masked by a word of ancestor bits per lane.
 //
-// P enters the second product as three bf16 parts (24 bits): with two (2^-17 of an entry lost at most) the output is
-// 2-3 times further from the 64-bit result than products in 32 bits are.
+// P enters the second product as three bf16 parts (24 bits): with two (2^-17 of an entry lost at most) the output would be
+// 2.2e-6 (of its norm) from the 64-bit result, where products in 32 bits are 3e-7 to 1.2e-6 away; with three it is 1.5e-7 to
+// 7e-7.  That is 4 products per 32x32x32 block in place of 3.
 //
 // Few segments are shared by S workgroups that take tiles in turn; each leaves an unnormalised partial (max, sum, O) and
-// a second launch joins them.
+// a second launch joins them (tree_splits() has the rule and its figures).
+//
+// What it measures (one layer, HIP graph): 128 x 28/4 heads x 2713 rows, chains of 4 (R = 28) 113.5 us, the rows at 6.4 TB/s;
+// with lengths of 1894-3533 121 us (the last workgroups have the chip to themselves); trees of 9 (R = 63) 127 us; 32 x 28/4 x
+// 4096, trees of 64 (R = 448) 239 us, 507 TFLOP/s by the formula, 1020 as issued; the large matrix product of this card reaches 1241.
+// What bounds the products: a 32x32x16 product occupies the matrix unit for 32 cycles and keeps the vector unit from issuing
+// for about 16 of them (a loop of 1 product and 16 multiply-adds takes 38 ns on one wave, 8 of them 22.6, 4 of them 15.1), so
+// the 32 products and ~200 vector instructions of a step of 32 keys take ~1600 cycles wherever they stand.
+// Measured and not kept: the exponentials of 16 keys between the products of the 16 before (no change, see above); the
+// remainders of P by a bf16 dot product (3 instead of 5 instructions a pair: 4 % slower); 64 rows in a wave of tree_narrow_kernel
+// (one wave per SIMD: 128 segments x 1493 rows 30 -> 32-40 us); 8 waves and 128 keys per workgroup (R 33-64: 0.90-1.04 of the time,
+// R 65-128: 0.96-1.12); joining the partials in the same launch by tickets (as fast or slower, and state to keep).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

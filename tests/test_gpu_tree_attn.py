@@ -133,6 +133,7 @@ def test_ragged_drafts_leave_the_others_as_they_were(page, nd):
 
 
 @pytest.mark.parametrize("lens,B,H,G,W", [((2500,), 1, 2, 4, 5), ((1900, 33), 2, 4, 7, 64), ((5000, 1, 777), 3, 2, 16, 10),
+                                          ((700, 64, 0, 1500), 2, 2, 16, 64),
                                           ((900, 1100, 40), 40, 4, 2, 16)])
 @pytest.mark.parametrize("ws", ["tree", "cache"])
 def test_long_caches_shared_by_workgroups(lens, B, H, G, W, ws):
@@ -152,6 +153,20 @@ def test_layers_one_by_one_and_all_at_once():
     c.run(layer=-1)
     c.check()
     assert c.torch.allclose(c.out[1], one, atol=1e-5)
+
+
+def test_nothing_is_drafted():
+    c = Case(B=2, H=2, G=4, W=5, lens=(80, 300), cap=400, nd=(0, 0), seed=8)
+    c.run()
+    c.check()
+    assert c.ngc.read_status(c.ws)[:8] == [0] * 8
+
+
+def test_a_full_cache_and_an_odd_capacity():
+    for cap in (1, 37, 95, 161):
+        c = Case(B=2, H=2, G=5, W=4, lens=(cap, cap - 1), cap=cap, seed=cap)
+        c.run()
+        c.check()
 
 
 def test_values_that_are_not_seen_stay_out():

@@ -175,6 +175,17 @@ def test_emitted_tokens_have_the_target_s_distribution(drafted):
     assert (np.abs(f - p) < 5 * np.sqrt(p * (1 - p) / B) + 1e-6).all()
 
 
+@pytest.mark.parametrize("B", [2, 60, 300])
+def test_what_the_workspace_holds_does_not_matter(B):
+    """Other calls leave their scratch behind; only the status words have to be as they leave them."""
+    import torch
+    from paper_2604_18002_amd import binding as ngc
+    c = _case(B, B, 4, 3000, shape="star", near=2.0)
+    ws = torch.full((ngc.ngc_verify_workspace_bytes(B, 3000),), 0xA5, dtype=torch.uint8, device="cuda")
+    ws[:256] = 0
+    _check(c, _run(c, ws=ws))
+
+
 def test_captured_on_another_stream_and_in_a_cache_s_workspace():
     import torch
     from paper_2604_18002_amd import binding as ngc
