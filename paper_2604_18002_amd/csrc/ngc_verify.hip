@@ -50,7 +50,11 @@ struct VerifyArgs {
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));    // rows begin at any multiple of 4 bytes
 
-__device__ __forceinline__ double residual(float p, float q, double c) { return __builtin_fmax((double)p - c * (double)q, 0.0); }
+// (A q below 0 or NaN counts as 0, as such a p does.)
+__device__ __forceinline__ double residual(float p, float q, double c)
+{
+    return __builtin_fmax((double)p - c * (double)__builtin_fmaxf(q, 0.f), 0.0);
+}
 
 // Sum over this lane and those below it.
 __device__ __forceinline__ double wave_incl_scan_d(double v)
@@ -251,7 +255,7 @@ __global__ __launch_bounds__(VF_THREADS) void verify_kernel(VerifyArgs a)
                 bool take;
                 double r;
                 if (draft) {
-                    const double q = (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(qv), x));
+                    const double q = (double)__builtin_fmaxf(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(qv), x)), 0.f);
                     r = __builtin_fmax(p - c * q, 0.0);
                     take = ux * S * q < r;
                 } else {

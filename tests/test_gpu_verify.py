@@ -144,6 +144,21 @@ def test_rows_without_probability():
     assert got[3][6] == 2
 
 
+@pytest.mark.parametrize("shape", ["chain", "star", "tree"])
+def test_draft_values_below_zero_and_nan_count_as_zero(shape):
+    c = _case(29, 24, 9, 300, shape=shape, near=1.0)
+    rng = np.random.default_rng(30)
+    raw = c["draft"].copy()
+    odd = rng.random(raw.shape)
+    raw[odd < 0.1] = -0.25
+    raw[odd > 0.9] = np.nan
+    for b in range(0, 24, 3):               # proposed tokens among them
+        raw[b, np.maximum(c["parent"][b], 0), c["token"][b]] = -1.0 if b % 2 else np.nan
+    got = _run(dict(c, draft=raw))
+    _check(dict(c, draft=np.maximum(np.nan_to_num(raw, nan=0.0), 0.0)), got)
+    assert got[3][:8] == [0] * 8
+
+
 def test_what_is_out_of_range_is_counted():
     c = _case(9, 3, 6, 100, shape="chain", drafted=False)
     c["token"][0, 2], c["token"][1, 3], c["token"][2, 0] = 100, -1, -50     # the last is the pending token: not looked at
