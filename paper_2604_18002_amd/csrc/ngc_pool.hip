@@ -367,7 +367,7 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_pages_kernel(PoolArgs a, co
     const int total = a.head[0];
     const bool again = COPIES > 1 && a.head[3] != 0;        // (15 copies of 48 MB take 192 us if asked for as read once,
                                                             // 163 if not; one copy of 360 MB 176 and 182)
-    const int pieces = 2 * page_bytes / 16, shift = 31 - __builtin_clz((unsigned)pieces);     // of a page's K and V
+    const int pieces = page_bytes / 8, shift = 31 - __builtin_clz((unsigned)pieces);     // of a page's K and V
     // a tile holds `per` pages, or a `parts`-th of one; fewer pages where there are too few for two rounds of workgroups
     const int most = pieces < MOVE_PIECES ? MOVE_PIECES / pieces : 1, share = total / (2 * (int)gridDim.x);
     const int per = share < 1 ? 1 : share < most ? share : most;

@@ -250,6 +250,34 @@ def test_packing_a_table_that_names_no_page():
     assert s[ngc.STATUS_POOL_BOUNDS] == 2 + 3 + 1 and s[ngc.STATUS_LEN_CLAMPED] == 1
 
 
+def test_pages_of_a_gibibyte():
+    import torch
+    from paper_2604_18002_amd import binding as ngc
+    P = 1 << 22                             # 256 bytes each: K and V of a page are 2^31 bytes
+    cache = ngc.PagedCache.allocate(1, 2, 1, 1, 128, P, 1, 3, with_pos=True)
+    for pool in (cache.k_pool, cache.v_pool):
+        pool.random_(-100, 100)
+    cache.pos_pool.random_(0, 1000)
+    cache.table.copy_(torch.tensor([2, 0]).view(1, 2, 1, 1))
+    cache.len.copy_(torch.tensor([P - 1, 0]).view(1, 2, 1))
+    cache.free_stack.copy_(torch.tensor([1, 0, -9]))
+    cache.free_count.fill_(2)
+    pools = (cache.k_pool, cache.v_pool, cache.pos_pool)
+    was = [t[2].clone() for t in pools]
+    ws = ngc.allocate_tree_workspace(cache, 1)
+    ngc.ngc_paged_fork(cache, -1, torch.tensor([0, 0], dtype=torch.int32, device="cuda"), ws)
+    torch.cuda.synchronize()
+    assert cache.table.flatten().tolist() == [2, 0] and cache.len.flatten().tolist() == [P - 1, P - 1]
+    assert all(torch.equal(t[0], w) and torch.equal(t[2], w) for t, w in zip(pools, was))
+    ngc.ngc_paged_free(cache, -1, torch.tensor([0, 1], dtype=torch.int32, device="cuda"), ws)
+    for t in pools:
+        t[0].zero_()
+    ngc.ngc_paged_compact(cache, ws)
+    torch.cuda.synchronize()
+    assert cache.table.flatten().tolist()[0] == 0 and cache.free_stack.tolist()[:2] == [2, 1] and int(cache.free_count) == 2
+    assert all(torch.equal(t[0], w) for t, w in zip(pools, was)) and sum(ngc.read_status(ws)) == 0
+
+
 def test_captured_page_operations():
     import torch
     rng = np.random.default_rng(6)
