@@ -96,9 +96,23 @@ __global__ __launch_bounds__(COMMIT_THREADS) void commit_kernel(CommitArgs a)
     constexpr int ROWS = COMMIT_THREADS / (2 * PIECES);     // rows (K and V) per step
     const int seg = a.seg0 + (int)blockIdx.x;
     const int seq = (int)blockIdx.x / a.Hkv, h = (int)blockIdx.x % a.Hkv, b = seq % a.B;
+    const int sub = (int)threadIdx.x / (2 * PIECES), lane = (int)threadIdx.x % (2 * PIECES);
+    const bool is_v = lane >= PIECES;
+    const int piece = is_v ? lane - PIECES : lane;
     const int n = a.len[seg];
     const int asked = a.n_path[b];
     const int wanted = path_length(a, b);
+    // The first rows are asked for before it is known how many there are: a path has W entries, and node 0 stands in for those
+    // that name none.
+    const unsigned char *drafts = (is_v ? a.v_draft : a.k_draft) + ((size_t)seq * a.W * a.Hkv + h) * ROW_BYTES + piece * 16;
+    int node, named;
+    u32x4 x;
+    auto ask = [&](int i) {
+        named = a.path[(size_t)b * a.W + i];
+        node = named < 0 || named >= a.W ? 0 : named;
+        x = *reinterpret_cast<const u32x4 *>(drafts + (size_t)node * a.Hkv * ROW_BYTES);
+    };
+    ask(sub < a.W ? sub : 0);
     const bool valid = n >= 0 && n <= a.cap;
     int m = PAGED ? a.rows[seg] : wanted;
     m = !valid || m < 0 ? 0 : m < a.cap - n ? m : a.cap - n;
@@ -112,17 +126,10 @@ __global__ __launch_bounds__(COMMIT_THREADS) void commit_kernel(CommitArgs a)
             if (threadIdx.x == 0) atomicAdd(&a.status[NGC_STATUS_POOL_BOUNDS], 1);
         }
     }
-    const int sub = (int)threadIdx.x / (2 * PIECES), lane = (int)threadIdx.x % (2 * PIECES);
-    const bool is_v = lane >= PIECES;
-    const int piece = is_v ? lane - PIECES : lane;
     int bad = 0;
     for (int i = sub; i < m; i += ROWS) {
-        int node = a.path[(size_t)b * a.W + i];
-        if (node < 0 || node >= a.W) {      // counted; some drafted row stands in
-            node = 0;
-            bad += lane == 0;
-        }
-        const size_t from = (((size_t)seq * a.W + node) * a.Hkv + h) * ROW_BYTES + piece * 16;
+        if (i != sub) ask(i);
+        bad += lane == 0 && named != node;
         size_t row;
         if constexpr (PAGED) {
             const int at = n + i;
@@ -130,8 +137,7 @@ __global__ __launch_bounds__(COMMIT_THREADS) void commit_kernel(CommitArgs a)
         } else {
             row = (size_t)seg * a.cap + n + i;
         }
-        *reinterpret_cast<u32x4 *>((is_v ? a.v : a.k) + row * ROW_BYTES + piece * 16) =
-            *reinterpret_cast<const u32x4 *>((is_v ? a.v_draft : a.k_draft) + from);
+        *reinterpret_cast<u32x4 *>((is_v ? a.v : a.k) + row * ROW_BYTES + piece * 16) = x;
         if (lane == 0 && a.pos && a.draft_pos) a.pos[row] = a.draft_pos[(size_t)b * a.W + node];
     }
     if (bad && h == 0) atomicAdd(&a.status[NGC_STATUS_BAD_TREE], bad);

@@ -202,7 +202,12 @@ __global__ __launch_bounds__(VF_THREADS) void verify_kernel(VerifyArgs a)
     const int W = a.W, V = a.V;
     const bool counts = share == 0 && wv == 0;
 
+    // A node per lane (every wave for itself: the refused tokens are looked up by lane later on); asked for together.
+    const size_t at_lane = (size_t)b * W + (lane < W ? lane : W - 1);
     int nd = a.n_draft ? a.n_draft[b] : W;
+    int up = a.parent[at_lane], token = a.token[at_lane];
+    const float u = a.u_accept[at_lane];
+    const double us = (double)a.u_sample[b];
     if (nd < 0 || nd > W) {
         if (counts && lane == 0) atomicAdd(&a.status[NGC_STATUS_BAD_TREE], 1);
         nd = nd < 0 ? 0 : W;
@@ -218,14 +223,7 @@ __global__ __launch_bounds__(VF_THREADS) void verify_kernel(VerifyArgs a)
     const float *target = a.target + (size_t)b * W * a.stride;
     const float *draft = a.draft ? a.draft + (size_t)b * W * a.stride : nullptr;
 
-    // a node per lane (every wave for itself: the refused tokens are looked up by lane later on)
-    int up = -1, token = -1;
-    float u = 0.f;
-    if (lane < nd) {
-        up = a.parent[(size_t)b * W + lane];
-        token = a.token[(size_t)b * W + lane];
-        u = a.u_accept[(size_t)b * W + lane];
-    }
+    if (lane >= nd) up = token = -1;
     const bool bad = lane < nd && (up < -1 || up >= lane || (lane > 0 && (token < 0 || token >= V)));
     const uint64_t bad_nodes = __ballot(bad);
     if (counts && lane == 0 && bad_nodes) atomicAdd(&a.status[NGC_STATUS_BAD_TREE], __popcll(bad_nodes));
@@ -323,7 +321,6 @@ __global__ __launch_bounds__(VF_THREADS) void verify_kernel(VerifyArgs a)
         if (!is_last) return;
     }
     __asm__ volatile("" ::: "memory");
-    const double us = (double)a.u_sample[b];
     int token_out = draw_token(res, sums, a.chunks, us);     // (every wave the same)
     if (token_out < 0) {                                     // nothing left: p itself
         __syncthreads();
