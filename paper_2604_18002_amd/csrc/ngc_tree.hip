@@ -12,9 +12,12 @@
 // S^T = K Q^T and O^T = V^T P by 32x32x16 matrix instructions: one query row per lane % 32, so all soft-max state is lane
 // local and crosses lanes once, between the two halves; one pass over the keys with a running maximum and sum.  K and V go
 // from memory straight into LDS, V is read transposed from there.  Two kernels:
-//   tree_narrow_kernel  R <= 32: every wave has all query rows and walks key tiles of its own, without a barrier;
-//   tree_attn_kernel    beyond: 4 waves share tiles of 64 keys, wave (wq, wk) has row block wq of WQ = 2 or 4 and part wk of
-//                       the keys; more than 128 rows are several workgroups.
+//   tree_narrow_kernel  a workgroup has 32 query rows; every wave has all of them and walks key tiles of its own, without a
+//                       barrier;
+//   tree_attn_kernel    4 waves share tiles of 64 keys, wave (wq, wk) has row block wq of WQ = 2 or 4 and part wk of the keys;
+//                       more than 128 rows are several workgroups.
+// The first reads a segment's keys once for every 32 rows, from L2 while all of them are at work at the same time, and is the
+// faster one where little else goes on (tree_shape() has the rule and its figures).
 // The drafted rows are one more tile behind those of the cache, masked by a word of ancestor bits per lane.
 //
 // P enters the second product as three bf16 parts (24 bits): with two (2^-17 of an entry lost at most) the output would be
@@ -529,11 +532,11 @@ void tree_attn_kernel(TreeArgs a)
     }
 }
 
-// Up to 32 query rows.  Every wave walks key tiles of its own, 32 keys each (tile t belongs to wave t % 4 of workgroup
+// 32 query rows.  Every wave walks key tiles of its own, 32 keys each (tile t belongs to wave t % 4 of workgroup
 // (t / 4) % S), through its own part of LDS: no barrier until the end.  A tile's K and V have one buffer each; the next
 // tile's K is requested as soon as this one's has been read into registers, its V likewise, so that 8 to 16 KB of every
 // wave are on their way, two workgroups a CU.  The drafted rows are the last one or two tiles.
-template <int D, bool PAGED>
+template <int D, bool ONCE, bool PAGED>
 __global__ __launch_bounds__(TREE_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void tree_narrow_kernel(TreeArgs a)
 {
@@ -550,13 +553,13 @@ void tree_narrow_kernel(TreeArgs a)
 
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
     const int li = lane & 31, half = lane >> 5;
-    const int split = (int)blockIdx.y;
+    const int split = (int)blockIdx.y, block = (int)blockIdx.z, row_base = block * TREE_QW;
     const int G = a.G, Hq = a.G * a.Hkv;
     TreeSegment s(a);
 
     // ---- asked for before the lengths have arrived: parents, queries and the wave's first tile ----
     const int up = a.parent[(size_t)s.b * a.W + (lane < a.W ? lane : a.W - 1)];      // (of lanes that are no node it is not looked at)
-    const int my_row = li < a.W * G ? li : a.W * G - 1;
+    const int my_row = row_base + li < a.W * G ? row_base + li : a.W * G - 1;
     const int node = my_row / G;
     bf16x8 qop[KCH];
     {
@@ -577,6 +580,10 @@ void tree_narrow_kernel(TreeArgs a)
     constexpr int SWZ = PIECES - 1;
     auto v_swizzle = [](int r) { return (2 * r) & (PIECES < 16 ? SWZ : 7); };
     auto k_swizzle = [](int r) { return r & SWZ; };
+    auto load_piece = [](const unsigned char *from, unsigned char *to) {
+        if constexpr (ONCE) load_once_to_lds16(from, to);
+        else load_to_lds16(from, to);
+    };
     const int lrow = lane / PIECES, lslot = lane % PIECES;
     unsigned char *const wk = lds_k + wv * TILE_LDS, *const wvl = lds_v + wv * TILE_LDS;
     const int step = a.S * TREE_WAVES;
@@ -590,8 +597,7 @@ void tree_narrow_kernel(TreeArgs a)
 #pragma unroll
             for (int r = 0; r < LOADS; ++r) {
                 const int slot_row = r * LOAD_ROWS + lrow, row = slot_row < most ? slot_row : most;
-                load_once_to_lds16(rows + base0 + (uint32_t)row * ROW_BYTES + (uint32_t)(lslot ^ swizzle(slot_row)) * 16u,
-                                   to + r * LOAD_ROWS * ROW_BYTES);
+                load_piece(rows + base0 + (uint32_t)row * ROW_BYTES + (uint32_t)(lslot ^ swizzle(slot_row)) * 16u, to + r * LOAD_ROWS * ROW_BYTES);
             }
         };
         whole(kseg, wk, k_swizzle);
@@ -599,12 +605,13 @@ void tree_narrow_kernel(TreeArgs a)
         whole(vseg, wvl, v_swizzle);
         __asm__ volatile("" ::: "memory");
     }
-    s.clamp(a, threadIdx.x == 0 && split == 0);
-    const int n = s.n, nd = s.nd, R = nd * G;
+    s.clamp(a, threadIdx.x == 0 && split == 0 && block == 0);
+    const int n = s.n, nd = s.nd;
+    const int rows_left = nd * G - row_base, R = rows_left < TREE_QW ? rows_left : TREE_QW;      // query rows of the block
     const int cache_tiles = (n + TREE_MT - 1) / TREE_MT;
     const int tiles = cache_tiles + (nd + TREE_MT - 1) / TREE_MT;
     const int parts = (tiles + TREE_WAVES - 1) / TREE_WAVES < a.S ? (tiles + TREE_WAVES - 1) / TREE_WAVES : a.S;   // with tiles
-    if (nd == 0 || split >= parts) {
+    if (R <= 0 || split >= parts) {
         __builtin_amdgcn_s_waitcnt(0x0F70);                // nothing may be on its way to LDS that is not this workgroup's any more
         return;
     }
@@ -625,7 +632,7 @@ void tree_narrow_kernel(TreeArgs a)
         for (int r = 0; r < LOADS; ++r) {
             const int slot_row = r * LOAD_ROWS + lrow;
             const int row = slot_row < last ? slot_row : last;
-            load_once_to_lds16(src + ((uint32_t)row * stride + (uint32_t)(lslot ^ swizzle(slot_row)) * 16u), to + r * LOAD_ROWS * ROW_BYTES);
+            load_piece(src + ((uint32_t)row * stride + (uint32_t)(lslot ^ swizzle(slot_row)) * 16u), to + r * LOAD_ROWS * ROW_BYTES);
         }
     };
     auto load_k = [&](int t, size_t base) { load(t, base, kseg, a.k_draft, wk, k_swizzle); };
@@ -648,7 +655,7 @@ void tree_narrow_kernel(TreeArgs a)
     }
     uint32_t sees_lo, sees_hi;             // drafted nodes that this lane's row sees
     {
-        const uint64_t anc = tree_ancestors(a, up, nd, wv == 0 && split == 0 && s.h == 0);
+        const uint64_t anc = tree_ancestors(a, up, nd, wv == 0 && split == 0 && block == 0 && s.h == 0);
         sees_lo = (uint32_t)__shfl((int)(uint32_t)anc, node);
         sees_hi = (uint32_t)__shfl((int)(uint32_t)(anc >> 32), node);
     }
@@ -851,11 +858,11 @@ void tree_narrow_kernel(TreeArgs a)
     if (parts == 1) {
         for (int row = threadIdx.x / OP; row < R; row += ROWS) {
             const f32x4 o = joined(row, m_all, l_all);
-            write(row, o, m_all, l_all);
+            write(row_base + row, o, m_all, l_all);
         }
         return;
     }
-    const size_t first = ((size_t)s.seg_local * a.S + split) * (size_t)(a.W * G);
+    const size_t first = ((size_t)s.seg_local * a.S + split) * (size_t)(a.W * G) + row_base;
     for (int row = threadIdx.x / OP; row < R; row += ROWS) {           // a second launch joins the partials
         const f32x4 o = joined(row, m_all, l_all);
         *(reinterpret_cast<f32x4 *>(a.part_o + (first + row) * D) + piece) = o;
@@ -941,12 +948,13 @@ int tree_most_splits(int nseg, int blocks, int groups)
     return most > 1 ? (int)most : 1;
 }
 
-// How many workgroups share a segment's keys.  A workgroup works through rounds of tiles, 256 keys of four waves' (narrow) or 64
-// of one tile: 1.2 us (narrow, and two row blocks) or 1.6 us (four) a round at D = 128, half of that at D = 64.  Two workgroups on
-// a CU take 1.3 times as long as one (narrow) or no longer.  The rows come at 4.5 TB/s while it lasts, less where the last
-// workgroups have a CU to themselves; of the two the longer counts whole, the other by 0.64.  Sharing costs a launch that
-// joins the partials and their way to memory and back.  Microseconds per launch at S workgroups (HIP graph), best in brackets,
-// * what the rule takes (1.01 times the best on average):
+// How many workgroups share a segment's keys.  A workgroup works through rounds of tiles, 128 keys (narrow, 32 a wave) or 64: 1.2 us
+// (narrow, and two row blocks) or 1.6 us (four) a round at D = 128, half of that at D = 64.  Two workgroups on a CU take 1.3 times
+// as long as one (narrow) or no longer.  The rows come at 4.5 TB/s while it lasts, less where several workgroups read them for
+// row blocks of their own, or where the last workgroups have a CU to themselves; of work and rows the longer counts whole, the
+// other by 0.64.  Sharing costs a launch that joins the partials and their way to memory and back.  Microseconds per launch at S
+// workgroups (HIP graph; beyond 32 query rows those of 64 or 128), best in brackets, * what the rule takes (1.01 times the best on
+// average):
 //     segments x rows, query rows     S=1     2      3      4       6      8      12     16     24     32     48
 //         8 x 4000,  32              42.4   27.1   21.5   18.4    16.1   14.0   13.6  [12.6]* 13.4   12.7
 //        64 x  800,  24              15.1   14.1   13.4  [12.6]*  13.1   13.2
@@ -958,11 +966,12 @@ int tree_most_splits(int nseg, int blocks, int groups)
 //         8 x 6000, 112             175.0   94.3   67.0   53.2    39.3   32.5   26.5   23.3  [21.2]* 22.0   25.9
 //       128 x 2000, 128             117.5   74.1   70.6  [64.7]*  75.8   76.6
 //       512 x 2713,  28 and 63    [113, 131]* 126, 152
-int tree_splits(int nseg, int rows, int blocks, int row_bytes, int max_len, int groups, int wq)
+int tree_splits(int nseg, int rows, int blocks, int row_bytes, int max_len, int groups, int wq, float *us_out)
 {
     const int most = tree_most_splits(nseg, blocks, groups);
     const float round = (wq == 4 ? 1.6f : 1.2f) * (row_bytes == 256 ? 1.f : 0.5f);
-    const float read = (float)nseg * (float)max_len * 2.f * (float)row_bytes / 4.5e6f;
+    const float again = 1.f + 0.08f * (float)(blocks - 1);
+    const float read = (float)nseg * (float)max_len * 2.f * (float)row_bytes / 4.5e6f * again;
     int best = 1;
     float best_us = 3.0e38f;
     for (int s = 1; s <= most; ++s) {
@@ -975,19 +984,45 @@ int tree_splits(int nseg, int rows, int blocks, int row_bytes, int max_len, int 
         const float us = (work > wait ? work + 0.64f * wait : wait + 0.64f * work) + shared;
         if (us < best_us) { best_us = us; best = s; }
     }
+    *us_out = best_us;
     return best;
 }
 
+// wq row blocks of 32 in a workgroup, and how long the rule says it takes
+TreeShape tree_shape_of(const ngc_cache *c, int nseg, int W, int max_len, int wq, float *us)
+{
+    const int R = W * (c->Hq / c->Hkv), rows = wq * TREE_QW;
+    TreeShape s;
+    s.wq = wq;
+    s.blocks = (R + rows - 1) / rows;
+    s.tiles = wq == 1 ? TreeTiles{TREE_MT, TREE_WAVES} : TreeTiles{64, 1};
+    s.splits = tree_splits(nseg, R < rows ? R : rows, s.blocks, c->D * 2, max_len, s.tiles.groups(max_len, W), wq, us);
+    return s;
+}
+
+int tree_widest(int R) { return R <= TREE_QW ? 1 : R <= 2 * TREE_QW ? 2 : 4; }
+
+// Row blocks of 32 in workgroups of their own, or several in one: whichever the rule says is faster, as long as the chip holds all of
+// the former at once (beyond, the later ones would find the rows gone from L2).  Microseconds, * what is taken:
+//     segments x rows, query rows   32     64     128 in a workgroup
+//        32 x  525,  96            14.0*  15.5   16.1
+//        32 x 1500,  48            14.5*  15.5   17.0
+//        64 x 1500, 112            22.3*  34.2   29.8
+//       128 x 1493,  48            27.0*  29.1   33.0
+//        60 x 2000, 256            44.2*  51.0   49.2
+//         4 x 16000, 140           26.2*  31.9   31.1
+//       120 x 2000,  80            44.5   56.8   45.3*
+//        64 x 3000, 128            43.7   45.1   40.6*
+//       128 x 4096, 112            96.7  101.2   84.2*
+//       512 x 2713,  63           252    128*
 TreeShape tree_shape(const ngc_cache *c, int nseg, int W, int max_len)
 {
-    const int R = W * (c->Hq / c->Hkv);
-    TreeShape s;
-    s.wq = R <= TREE_QW ? 1 : R <= 2 * TREE_QW ? 2 : 4;
-    const int rows = s.wq * TREE_QW;
-    s.blocks = (R + rows - 1) / rows;
-    s.tiles = s.wq == 1 ? TreeTiles{TREE_MT, TREE_WAVES} : TreeTiles{64, 1};
-    s.splits = tree_splits(nseg, R < rows ? R : rows, s.blocks, c->D * 2, max_len, s.tiles.groups(max_len, W), s.wq);
-    return s;
+    const int R = W * (c->Hq / c->Hkv), wq = tree_widest(R);
+    float us, us_narrow;
+    const TreeShape s = tree_shape_of(c, nseg, W, max_len, wq, &us);
+    if (wq == 1 || (long long)nseg * ((R + TREE_QW - 1) / TREE_QW) > TREE_RESIDENT) return s;
+    const TreeShape narrow = tree_shape_of(c, nseg, W, max_len, 1, &us_narrow);
+    return us_narrow < us ? narrow : s;
 }
 
 bool tree_geometry_ok(const ngc_cache *c, int32_t W)
@@ -1046,7 +1081,7 @@ int launch_tree(const ngc_cache *c, const ngc_paged_cache *pc, int32_t layer, co
     hipStream_t st = (hipStream_t)stream;
 #define NGC_TREE(KERNEL, ...) (pc ? reinterpret_cast<const void *>(&KERNEL<__VA_ARGS__, true>) \
                                   : reinterpret_cast<const void *>(&KERNEL<__VA_ARGS__, false>))
-#define NGC_TREE_D(D) (shape.wq == 1 ? NGC_TREE(tree_narrow_kernel, D) : shape.wq == 2 ? NGC_TREE(tree_attn_kernel, D, 2, true) \
+#define NGC_TREE_D(D) (shape.wq == 1 ? (shape.blocks == 1 ? NGC_TREE(tree_narrow_kernel, D, true) : NGC_TREE(tree_narrow_kernel, D, false)) : shape.wq == 2 ? NGC_TREE(tree_attn_kernel, D, 2, true) \
                        : shape.blocks == 1 ? NGC_TREE(tree_attn_kernel, D, 4, true) : NGC_TREE(tree_attn_kernel, D, 4, false))
     const void *fn = c->D == 128 ? NGC_TREE_D(128) : NGC_TREE_D(64);
 #undef NGC_TREE_D
@@ -1068,7 +1103,8 @@ extern "C" size_t ngc_tree_workspace_bytes(const ngc_cache *c, int32_t W)
     const int per_layer = c->B * c->Hkv;
     // one layer or all layers, any length hint: the most workgroups a segment can be shared by
     auto most = [&](int nseg) {
-        const TreeShape s = tree_shape(c, nseg, W, c->cap);
+        float us;
+        const TreeShape s = tree_shape_of(c, nseg, W, c->cap, tree_widest(W * (c->Hq / c->Hkv)), &us);
         return tree_partial_bytes(c, nseg, W, tree_most_splits(nseg, s.blocks, s.tiles.groups(c->cap, W)));
     };
     const size_t one = most(per_layer), all = most(per_layer * c->L);

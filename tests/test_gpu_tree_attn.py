@@ -288,3 +288,77 @@ def test_the_workspace_serves_decode_in_between():
         ngc.ngc_decode_attn(c.cache, 0, q, c.D ** -0.5, 0, b, c.ws)
         assert torch.equal(a, b)
     c.check()
+
+
+# More row blocks of 32 than workgroups that the chip holds at once: workgroups of several row blocks
+MANY = [(130, 2, 1, 33, 128), (260, 1, 4, 16, 64), (88, 2, 2, 64, 128), (176, 1, 7, 10, 64), (66, 1, 4, 64, 128), (30, 2, 5, 57, 64)]
+
+
+@pytest.mark.parametrize("page", [0, 32, 128])
+@pytest.mark.parametrize("B,H,G,W,D", MANY)
+def test_many_segments(B, H, G, W, D, page):
+    nd = np.random.default_rng(B).integers(0, W + 1, size=B)
+    nd[:4] = (0, 1, W, W - 1)
+    c = Case(B=B, H=H, G=G, D=D, W=W, cap=256, lens=EDGES, page=page, nd=nd, seed=B + W + page)
+    c.run()
+    c.check()
+    assert c.ngc.read_status(c.ws)[:8] == [0] * 8
+
+
+@pytest.mark.parametrize("B,H,G,W,D", MANY)
+def test_many_segments_shared_by_workgroups(B, H, G, W, D):
+    c = Case(B=B, H=H, G=G, D=D, W=W, cap=900, lens=(0, 890, 64, 300, 449), seed=B + W)
+    for hint in (0, 200):
+        c.out.fill_(77.0)
+        c.run(hint=hint)
+        c.check()
+
+
+@pytest.mark.parametrize("B,H,G,W,D", MANY[::2] + MANY[-1:])
+def test_many_segments_with_values_that_are_not_seen(B, H, G, W, D):
+    from _drafts import ancestors
+    for bad in (float("nan"), float("inf")):
+        c = Case(B=B, H=H, G=G, D=D, W=W, lens=(40, 0), seed=3)
+        c.run()
+        c.torch.cuda.synchronize()
+        clean = c.out.clone()
+        node = W // 2
+        c.vd[0, :, node] = bad
+        c.kd[0, :, node] = bad if bad != bad else 3.0e38
+        c.run()
+        c.torch.cuda.synchronize()
+        for b in range(0, B, 7):
+            sees = ancestors(c.parent[b])[:, node]
+            assert 0 < sees.sum() < W
+            assert c.torch.allclose(c.out[0, b][~sees], clean[0, b][~sees], atol=OUT_TOL)
+            assert not c.torch.isfinite(c.out[0, b][sees]).any()
+
+
+def test_many_segments_with_parents_counts_and_lengths_out_of_range():
+    c = Case(B=264, H=1, G=2, W=17, cap=50, lens=(50, 0, 20), nd=[17] * 262 + [40, -1], seed=1)
+    c.parents[0, :5] = c.torch.tensor([-1, 0, 2, 99, -7])
+    c.parent[0, :5] = [-1, 0, -1, -1, -1]
+    c.nd[262:] = (17, 0)
+    c.kd[:, 262:], c.vd[:, 262:] = c.kd[:, :2], c.vd[:, :2]
+    c.cache.len[0, 0, 0] = 51
+    c.cache.len[0, 1, 0] = -1
+    c.run()
+    c.check()
+    s = c.ngc.read_status(c.ws)
+    assert s[c.ngc.STATUS_BAD_TREE] == 2 + 3 and s[c.ngc.STATUS_LEN_CLAMPED] == 2
+
+
+def test_many_segments_captured():
+    c = Case(B=88, H=2, G=2, W=64, lens=(700, 70, 899), cap=1000, seed=31)
+    torch = c.torch
+    c.run()
+    c.check()
+    want = c.out.clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.run()
+    for _ in range(3):
+        c.out.fill_(77.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c.out, want)
