@@ -70,7 +70,7 @@ struct TreeArgs {
     float *part_o;                      // [segments of the launch][S][R][D]
     float *part_ml;                     // [segments of the launch][S][R][2]
     int32_t *status;
-    int seg0, S, W, G, B, Hkv, cap;
+    int seg0, nseg, blocks, S, W, G, B, Hkv, cap;
     float scale_log2e;
     const int32_t *table;               // paged layout only
     int max_pages, num_pages, page_shift;
@@ -99,8 +99,8 @@ struct TreeSegment {
     int b;
     int n, nd;                          // rows in the cache, drafted nodes; as they are in memory until clamp()
 
-    __device__ __forceinline__ TreeSegment(const TreeArgs &a)
-        : seg_local((int)blockIdx.x), h(seg_local % a.Hkv), seq((size_t)(seg_local / a.Hkv)),
+    __device__ __forceinline__ TreeSegment(const TreeArgs &a, int seg_local)
+        : seg_local(seg_local), h(seg_local % a.Hkv), seq((size_t)(seg_local / a.Hkv)),
           b((int)(seq % a.B)), n(constant_word(a.len + a.seg0 + seg_local)),
           nd(a.n_draft ? constant_word(a.n_draft + b) : a.W)
     {
@@ -115,6 +115,21 @@ struct TreeSegment {
             if (counts && h == 0) atomicAdd(&a.status[NGC_STATUS_BAD_TREE], 1);
             nd = nd < 0 ? 0 : a.W;
         }
+    }
+};
+
+// A workgroup's segment and row block.  Workgroups go round-robin to the 8 XCDs: the row blocks of a segment follow one another on
+// one of them, so that its rows come from memory once, while they are at work together (with the row block as the slowest
+// coordinate instead, 100 segments x 3000 rows in 6 blocks of 32 take 119 us in place of 87; 128 x 4096 in 4 of 128 248, not 245).
+struct TreePlace {
+    int seg, block;
+    __device__ __forceinline__ TreePlace(const TreeArgs &a) : seg((int)blockIdx.x), block(0)
+    {
+        if (a.blocks == 1) return;
+        const int first = (int)(blockIdx.x / (8u * (unsigned)a.blocks)) * 8, at = (int)blockIdx.x - first * a.blocks;
+        const int here = a.nseg - first < 8 ? a.nseg - first : 8;
+        block = at / here;
+        seg = first + at - block * here;
     }
 };
 
@@ -163,8 +178,9 @@ void tree_attn_kernel(TreeArgs a)
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
     const int wq = wv % WQ, wk = wv / WQ;
     const int li = lane & 31, half = lane >> 5;
-    const int split = (int)blockIdx.y, block = (int)blockIdx.z;
-    TreeSegment s(a);
+    const TreePlace place(a);
+    const int split = (int)blockIdx.y, block = place.block;
+    TreeSegment s(a, place.seg);
     const int G = a.G, Hq = a.G * a.Hkv;
     const int row_base = block * RB, wave_row0 = row_base + wq * TREE_QW;
 
@@ -553,9 +569,10 @@ void tree_narrow_kernel(TreeArgs a)
 
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
     const int li = lane & 31, half = lane >> 5;
-    const int split = (int)blockIdx.y, block = (int)blockIdx.z, row_base = block * TREE_QW;
+    const TreePlace place(a);
+    const int split = (int)blockIdx.y, block = place.block, row_base = block * TREE_QW;
     const int G = a.G, Hq = a.G * a.Hkv;
-    TreeSegment s(a);
+    TreeSegment s(a, place.seg);
 
     // ---- asked for before the lengths have arrived: parents, queries and the wave's first tile ----
     const int up = a.parent[(size_t)s.b * a.W + (lane < a.W ? lane : a.W - 1)];      // (of lanes that are no node it is not looked at)
@@ -876,7 +893,7 @@ template <int D>
 __global__ __launch_bounds__(TREE_MERGE_THREADS) void tree_merge_kernel(TreeArgs a, TreeTiles tl)
 {
     constexpr int OP = D / 4;
-    TreeSegment s(a);
+    TreeSegment s(a, (int)blockIdx.x);
     s.clamp(a, false);
     const int row = (int)blockIdx.y * (TREE_MERGE_THREADS / OP) + (int)threadIdx.x / OP;
     const int piece = (int)threadIdx.x % OP;
@@ -970,7 +987,7 @@ int tree_splits(int nseg, int rows, int blocks, int row_bytes, int max_len, int 
 {
     const int most = tree_most_splits(nseg, blocks, groups);
     const float round = (wq == 4 ? 1.6f : 1.2f) * (row_bytes == 256 ? 1.f : 0.5f);
-    const float again = 1.f + 0.08f * (float)(blocks - 1);
+    const float again = 1.f + 0.05f * (float)(blocks - 1);
     const float read = (float)nseg * (float)max_len * 2.f * (float)row_bytes / 4.5e6f * again;
     int best = 1;
     float best_us = 3.0e38f;
@@ -1003,18 +1020,19 @@ TreeShape tree_shape_of(const ngc_cache *c, int nseg, int W, int max_len, int wq
 int tree_widest(int R) { return R <= TREE_QW ? 1 : R <= 2 * TREE_QW ? 2 : 4; }
 
 // Row blocks of 32 in workgroups of their own, or several in one: whichever the rule says is faster, as long as the chip holds all of
-// the former at once (beyond, the later ones would find the rows gone from L2).  Microseconds, * what is taken:
+// the former at once.  (1.02 times the best of the three on average over 120 drawn geometries.)  Microseconds, * what is taken:
 //     segments x rows, query rows   32     64     128 in a workgroup
-//        32 x  525,  96            14.0*  15.5   16.1
-//        32 x 1500,  48            14.5*  15.5   17.0
-//        64 x 1500, 112            22.3*  34.2   29.8
-//       128 x 1493,  48            27.0*  29.1   33.0
-//        60 x 2000, 256            44.2*  51.0   49.2
-//         4 x 16000, 140           26.2*  31.9   31.1
-//       120 x 2000,  80            44.5   56.8   45.3*
-//        64 x 3000, 128            43.7   45.1   40.6*
-//       128 x 4096, 112            96.7  101.2   84.2*
-//       512 x 2713,  63           252    128*
+//        32 x  525,  96            14.3*  15.8   16.2
+//        32 x 1500,  48            14.6*  15.5   17.1
+//        64 x 1500, 112            22.9*  30.8   30.5
+//       128 x 1493,  48            27.7*  29.9   33.5
+//        60 x 2000, 256            43.1*  51.8   49.0
+//         4 x 16000, 140           26.1*  32.7   34.1
+//       120 x 2000,  80            46.6   48.3   45.5*
+//        64 x 3000, 128            45.4   42.8   41.9*
+//       200 x 1000, 120            52.1   44.2   43.2*
+//       226 x   38,  84            19.8   15.2   13.5*
+//       512 x 2713,  56           169    143*   165
 TreeShape tree_shape(const ngc_cache *c, int nseg, int W, int max_len)
 {
     const int R = W * (c->Hq / c->Hkv), wq = tree_widest(R);
@@ -1072,7 +1090,7 @@ int launch_tree(const ngc_cache *c, const ngc_paged_cache *pc, int32_t layer, co
                                           align256((size_t)nseg * S * W * G * c->D * sizeof(float)));
     a.status = reinterpret_cast<int32_t *>(ws);
     a.seg0 = layer < 0 ? 0 : layer * per_layer;
-    a.S = S; a.W = W; a.G = G; a.B = c->B; a.Hkv = c->Hkv; a.cap = c->cap;
+    a.nseg = nseg; a.blocks = shape.blocks; a.S = S; a.W = W; a.G = G; a.B = c->B; a.Hkv = c->Hkv; a.cap = c->cap;
     a.scale_log2e = scale * 1.4426950408889634f;
     if (pc) {
         a.table = pc->table; a.max_pages = pc->max_pages; a.num_pages = pc->num_pages;
@@ -1086,7 +1104,7 @@ int launch_tree(const ngc_cache *c, const ngc_paged_cache *pc, int32_t layer, co
     const void *fn = c->D == 128 ? NGC_TREE_D(128) : NGC_TREE_D(64);
 #undef NGC_TREE_D
 #undef NGC_TREE
-    const int rc = launch(fn, dim3(nseg, S, shape.blocks), dim3(TREE_WAVES * 64), 0, st, a);
+    const int rc = launch(fn, dim3(nseg * shape.blocks, S), dim3(TREE_WAVES * 64), 0, st, a);
     if (rc || S == 1) return rc;
     const int rows_per = TREE_MERGE_THREADS / (c->D / 4);
     const dim3 grid(nseg, (W * G + rows_per - 1) / rows_per);
