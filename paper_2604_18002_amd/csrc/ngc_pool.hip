@@ -14,7 +14,7 @@
 // plan of a fork of 3584 segments 10).  Forks of 28 x 2 segments of 300-500 rows (256 bytes each), all launches: 15 copies of 48 MB
 // 163 us (715 MB written; a fill runs at 5.7 TB/s: 125), one copy of 360 MB 168 us; packing a pool after half of 64 sequences have
 // ended (611 MB moved) 138 us, the copy of it at 5.4 TB/s, the best copy shape of this card 5.9.  Rows appended to 3584 dense segments
-// (4.5 each on average) 5.9 us, to 896 paged ones 6.4 (two launches).
+// (4.5 each on average) 5.3-5.8 us, to 896 paged ones 6.4 (two launches).
 // Measured and not kept: tiles of 64 KB, 256 or 1024 workgroups for the moves (0.98-1.02); plain stores (1.1); 8 or 16 copies from one
 // read (15 copies 181-188 us without caching the reads, four copies 163 with).
 #include <hip/hip_runtime.h>
