@@ -965,40 +965,40 @@ int tree_most_splits(int nseg, int blocks, int groups)
     return most > 1 ? (int)most : 1;
 }
 
-// How many workgroups share a segment's keys.  A workgroup works through rounds of tiles, 128 keys (narrow, 32 a wave) or 64: 1.2 us
-// (narrow, and two row blocks) or 1.6 us (four) a round at D = 128, half of that at D = 64.  Two workgroups on a CU take 1.3 times
-// as long as one (narrow) or no longer.  The rows come at 4.5 TB/s while it lasts, less where several workgroups read them for
-// row blocks of their own, or where the last workgroups have a CU to themselves; of work and rows the longer counts whole, the
-// other by 0.64.  Sharing costs a launch that joins the partials and their way to memory and back.  Microseconds per launch at S
-// workgroups (HIP graph; beyond 32 query rows those of 64 or 128), best in brackets, * what the rule takes (1.01 times the best on
-// average):
-//     segments x rows, query rows     S=1     2      3      4       6      8      12     16     24     32     48
-//         8 x 4000,  32              42.4   27.1   21.5   18.4    16.1   14.0   13.6  [12.6]* 13.4   12.7
-//        64 x  800,  24              15.1   14.1   13.4  [12.6]*  13.1   13.2
-//        80 x 4000,  30              48.9   37.3  [36.1]* 42.7    38.7   40.5
-//       128 x 1493,  48              35.9   33.7   32.2  [30.7]*  39.6   40.2
-//        16 x  700,  56              20.8   16.4   14.5   14.2    12.5   12.6  [11.9]*
-//        32 x  525,  96              32.9   23.4   19.6   18.7   [16.4]  16.9                              (* 5: 18.6)
-//        32 x 2000, 128              67.7   43.2   33.2   30.0   [25.4]* 28.0   28.6   29.0
-//         8 x 6000, 112             175.0   94.3   67.0   53.2    39.3   32.5   26.5   23.3  [21.2]* 22.0   25.9
-//       128 x 2000, 128             117.5   74.1   70.6  [64.7]*  75.8   76.6
-//       512 x 2713,  28 and 63    [113, 131]* 126, 152
+// How many workgroups share a segment's keys, and how long that takes: a model whose numbers were fitted to 325 geometries, each
+// at up to 11 splits in workgroups of 32, 64 and 128 query rows.  A workgroup works through rounds of tiles, 128 keys (32 rows: 32 a
+// wave) or 64, of `round` us; several on a CU take `crowd` of their sum.  Rows come from memory at 6.2 TB/s, less where the last
+// workgroups have a CU to themselves, and again for every row block from L2, 13.6 TB/s in all.  Of work and rows the longer counts
+// whole, the other by 0.3.  Sharing costs a launch that joins the partials and their way to memory and back.  Microseconds at S workgroups
+// (HIP graph), best in brackets, * what the rule takes (over 80 other drawn geometries 1.02 times the best of all):
+//     segments x rows, query rows     S=1     2      3      4       6      8      12     16     24
+//         8 x 4000,  32              42.5   27.1   21.6   18.5    16.5   14.0   13.7  [12.6]* 13.4
+//        64 x  800,  24              15.0   14.2   13.5  [12.6]*  13.5   14.5
+//       256 x 2000,  16 (D = 64)    [25.5]* 28.6   28.3   28.9    29.5   32.0
+//        16 x 8000,  63, in 32       77.1   46.4   34.0   28.7    23.4  [21.6]* 23.9   23.8
+//       128 x 1493,  48, in 32      [27.3]* 32.2   34.1   36.7    42.5
+//                        in 64       35.9   33.5*  33.7  [32.2]
+//        32 x  525,  96, in 32       14.3  [14.3]* 15.1   14.6    18.6
+//                        in 128      29.0   21.5   18.6   17.9   [16.1]* 16.7   18.9
+//       128 x 4096, 112, in 128     124.9   89.3   93.2  [86.0]*
 int tree_splits(int nseg, int rows, int blocks, int row_bytes, int max_len, int groups, int wq, float *us_out)
 {
     const int most = tree_most_splits(nseg, blocks, groups);
-    const float round = (wq == 4 ? 1.6f : 1.2f) * (row_bytes == 256 ? 1.f : 0.5f);
-    const float again = 1.f + 0.05f * (float)(blocks - 1);
-    const float read = (float)nseg * (float)max_len * 2.f * (float)row_bytes / 4.5e6f * again;
+    const bool d128 = row_bytes == 256;
+    const float round = wq == 1 ? (d128 ? 1.2f : 0.78f) : wq == 2 ? (d128 ? 1.f : 0.85f) : (d128 ? 2.3f : 1.5f);
+    const float crowd = wq == 1 ? 0.62f : wq == 2 ? 0.3f : 0.8f;
+    const float bytes = (float)nseg * (float)max_len * 2.f * (float)row_bytes;
+    const float read = fmaxf(bytes / 6.2e6f, bytes * (float)blocks / 13.6e6f);
     int best = 1;
     float best_us = 3.0e38f;
     for (int s = 1; s <= most; ++s) {
         const int rounds = (groups + s - 1) / s;
         if (s > 1 && (groups + s - 2) / (s - 1) == rounds) continue;       // one fewer does as well
         const int wg = nseg * blocks * s, per_cu = (wg + TREE_CUS - 1) / TREE_CUS;
-        const float work = round * (float)rounds * (per_cu == 1 ? 1.f : (float)per_cu * (wq == 1 ? 0.66f : 0.5f));
+        const float work = round * (float)rounds * (per_cu == 1 ? 1.f : (float)per_cu * crowd);
         const float wait = read * (per_cu == 1 ? 1.f : sqrtf((float)(per_cu * TREE_CUS) / (float)wg));
-        const float shared = s == 1 ? 0.f : 1.27f * (float)per_cu + (float)wg * (float)rows * (float)row_bytes * 4.f / 5.0e6f;
-        const float us = (work > wait ? work + 0.64f * wait : wait + 0.64f * work) + shared;
+        const float shared = s == 1 ? 0.f : 2.4f * (float)per_cu + (float)wg * (float)rows * (float)row_bytes * 4.f / 6.4e6f;
+        const float us = (work > wait ? work + 0.3f * wait : wait + 0.3f * work) + shared;
         if (us < best_us) { best_us = us; best = s; }
     }
     *us_out = best_us;
@@ -1019,26 +1019,27 @@ TreeShape tree_shape_of(const ngc_cache *c, int nseg, int W, int max_len, int wq
 
 int tree_widest(int R) { return R <= TREE_QW ? 1 : R <= 2 * TREE_QW ? 2 : 4; }
 
-// Row blocks of 32 in workgroups of their own, or several in one: whichever the rule says is faster, as long as the chip holds all of
-// the former at once.  (1.02 times the best of the three on average over 120 drawn geometries.)  Microseconds, * what is taken:
+// Row blocks of 32 in workgroups of their own, or several in one: whichever the rule says is faster, as long as not many more than the
+// chip holds at once are at work on the former.  Microseconds at the best split of each, * what is taken:
 //     segments x rows, query rows   32     64     128 in a workgroup
-//        32 x  525,  96            14.3*  15.8   16.2
-//        32 x 1500,  48            14.6*  15.5   17.1
-//        64 x 1500, 112            22.9*  30.8   30.5
-//       128 x 1493,  48            27.7*  29.9   33.5
-//        60 x 2000, 256            43.1*  51.8   49.0
-//         4 x 16000, 140           26.1*  32.7   34.1
-//       120 x 2000,  80            46.6   48.3   45.5*
-//        64 x 3000, 128            45.4   42.8   41.9*
-//       200 x 1000, 120            52.1   44.2   43.2*
+//        32 x  525,  96            14.3*  15.4   16.1
+//        32 x 1500,  48            14.1*  15.3   16.8
+//        64 x 1500, 112            22.5*  29.7   31.2
+//       128 x 1493,  48            27.3*  32.2   32.8
+//        60 x 2000, 256            42.1*  46.7   48.7
+//         4 x 16000, 140           24.6*  30.1   36.4
+//       120 x 2000,  80            46.2*  47.1   45.7
+//        64 x 3000, 128            40.8*  42.4   41.7
+//       128 x 4096, 112            88.8   88.4   86.0*
+//       200 x 1000, 120            52.5   44.8   42.4*
 //       226 x   38,  84            19.8   15.2   13.5*
-//       512 x 2713,  56           169    143*   165
+//       512 x 2713,  56           167    143*   166
 TreeShape tree_shape(const ngc_cache *c, int nseg, int W, int max_len)
 {
     const int R = W * (c->Hq / c->Hkv), wq = tree_widest(R);
     float us, us_narrow;
     const TreeShape s = tree_shape_of(c, nseg, W, max_len, wq, &us);
-    if (wq == 1 || (long long)nseg * ((R + TREE_QW - 1) / TREE_QW) > TREE_RESIDENT) return s;
+    if (wq == 1 || (long long)nseg * ((R + TREE_QW - 1) / TREE_QW) > (c->D == 128 ? TREE_RESIDENT : 3 * TREE_RESIDENT)) return s;
     const TreeShape narrow = tree_shape_of(c, nseg, W, max_len, 1, &us_narrow);
     return us_narrow < us ? narrow : s;
 }

@@ -290,8 +290,9 @@ def test_the_workspace_serves_decode_in_between():
     c.check()
 
 
-# More row blocks of 32 than workgroups that the chip holds at once: workgroups of several row blocks
-MANY = [(130, 2, 1, 33, 128), (260, 1, 4, 16, 64), (88, 2, 2, 64, 128), (176, 1, 7, 10, 64), (66, 1, 4, 64, 128), (30, 2, 5, 57, 64)]
+# More row blocks of 32 than workgroups that the chip holds at once (the last three: three times as many): workgroups of several row blocks
+MANY = [(130, 2, 1, 33, 128), (260, 1, 4, 16, 64), (88, 2, 2, 64, 128), (176, 1, 7, 10, 64), (66, 1, 4, 64, 128), (30, 2, 5, 57, 64),
+        (400, 2, 4, 16, 64), (260, 2, 5, 14, 64), (100, 2, 4, 64, 64)]
 
 
 @pytest.mark.parametrize("page", [0, 32, 128])
@@ -314,7 +315,7 @@ def test_many_segments_shared_by_workgroups(B, H, G, W, D):
         c.check()
 
 
-@pytest.mark.parametrize("B,H,G,W,D", MANY[::2] + MANY[-1:])
+@pytest.mark.parametrize("B,H,G,W,D", MANY)
 def test_many_segments_with_values_that_are_not_seen(B, H, G, W, D):
     from _drafts import ancestors
     for bad in (float("nan"), float("inf")):
