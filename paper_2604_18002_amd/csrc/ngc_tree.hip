@@ -36,7 +36,8 @@
 // Measured and not kept: the exponentials of 16 keys between the products of the 16 before (no change, see above); the
 // remainders of P by a bf16 dot product (3 instead of 5 instructions a pair: 4 % slower); 64 rows in a wave of tree_narrow_kernel
 // (one wave per SIMD: 128 segments x 1493 rows 30 -> 32-40 us); 8 waves and 128 keys per workgroup (R 33-64: 0.90-1.04 of the time,
-// R 65-128: 0.96-1.12); joining the partials in the same launch by tickets (as fast or slower, and state to keep).
+// R 65-128: 0.96-1.12); joining the partials in the same launch by tickets (as fast or slower, and state to keep); 8 waves with 32 rows (one workgroup on a CU
+// gets its rows at ~50 KB a microsecond however many waves ask: 0.82-1.12, 0.98 at the best choice of each geometry).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -991,9 +992,8 @@ int tree_splits(int nseg, int rows, int blocks, int row_bytes, int max_len, int 
     const float read = fmaxf(bytes / 6.2e6f, bytes * (float)blocks / 13.6e6f);
     int best = 1;
     float best_us = 3.0e38f;
-    for (int s = 1; s <= most; ++s) {
-        const int rounds = (groups + s - 1) / s;
-        if (s > 1 && (groups + s - 2) / (s - 1) == rounds) continue;       // one fewer does as well
+    for (int s = 1, rounds; s <= most; s = rounds > 1 ? (groups + rounds - 2) / (rounds - 1) : most + 1) {     // the next with fewer rounds
+        rounds = (groups + s - 1) / s;
         const int wg = nseg * blocks * s, per_cu = (wg + TREE_CUS - 1) / TREE_CUS;
         const float work = round * (float)rounds * (per_cu == 1 ? 1.f : (float)per_cu * crowd);
         const float wait = read * (per_cu == 1 ? 1.f : sqrtf((float)(per_cu * TREE_CUS) / (float)wg));
