@@ -156,6 +156,45 @@ __device__ __forceinline__ uint64_t tree_ancestors(const TreeArgs &a, int up, in
     return (uint64_t)hi << 32 | lo;
 }
 
+// Values of drafted V rows that are not finite would reach rows that do not see them, through a product with P = 0.  They become 0 in
+// LDS, in every slot of the tile that is multiplied (behind the last drafted row stand copies of it), and are added, by themselves, to
+// the rows that see them.
+__device__ __forceinline__ bool take_out_odd_values(unsigned char *piece)      // of 16 bytes; whether it had any
+{
+    u32x4 x = *reinterpret_cast<const u32x4 *>(piece);
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if ((x[e] & 0x7F80u) == 0x7F80u) { odd = true; x[e] &= 0xFFFF0000u; }
+        if ((x[e] & 0x7F800000u) == 0x7F800000u) { odd = true; x[e] &= 0xFFFFu; }
+    }
+    if (odd) *reinterpret_cast<u32x4 *>(piece) = x;
+    return odd;
+}
+// Those of up to 32 drafted rows, `stride` bytes apart in memory, that `sees` has a bit for.
+template <int DT>
+__device__ __forceinline__ void add_odd_values(const unsigned char *rows, uint32_t stride, int count, uint32_t sees, f32x16 (&oacc)[DT])
+{
+    const int half = lane_id() >> 5;
+    for (int j = 0; j < count; ++j) {
+        const bool seen = ((sees >> j) & 1u) != 0;
+        // of lane half: d = 32 c + 8 g + 4 half + i.  (The address is made opaque: nothing of it is kept over the loop.)
+        const unsigned char *row = rows + (size_t)j * stride + half * 8;
+        __asm__ volatile("" : "+v"(row));
+#pragma unroll
+        for (int c = 0; c < DT; ++c)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const u32x2 x = *reinterpret_cast<const u32x2 *>(row + (32 * c + 8 * g) * 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t bits = i & 1 ? x[i / 2] & 0xFFFF0000u : x[i / 2] << 16;
+                    if (seen && (bits & 0x7F800000u) == 0x7F800000u) oacc[c][4 * g + i] += __uint_as_float(bits);
+                }
+            }
+    }
+}
+
 template <int D, int WQ, bool ONCE, bool PAGED>
 __global__ __launch_bounds__(TREE_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void tree_attn_kernel(TreeArgs a)
@@ -383,43 +422,6 @@ void tree_attn_kernel(TreeArgs a)
         }
     };
 
-    // The drafted V rows: values that are not finite would reach rows that do not see them, through a product with P = 0.  They
-    // become 0 in LDS and are added, by themselves, to the rows that see them.  Returns whether there are any.
-    auto take_out_odd_values = [&](unsigned char *lv) {
-        bool any = false;
-        for (int i = threadIdx.x; i < nd * PIECES; i += TREE_WAVES * 64) {
-            u32x4 x = *reinterpret_cast<const u32x4 *>(lv + i * 16);
-            bool odd = false;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if ((x[e] & 0x7F80u) == 0x7F80u) { odd = true; x[e] &= 0xFFFF0000u; }
-                if ((x[e] & 0x7F800000u) == 0x7F800000u) { odd = true; x[e] &= 0xFFFFu; }
-            }
-            if (odd) *reinterpret_cast<u32x4 *>(lv + i * 16) = x;
-            any |= odd;
-        }
-        return __syncthreads_or(any) != 0;
-    };
-    auto add_odd_values = [&]() {
-        for (int j = 0; j < nd; ++j) {
-            const bool seen = ((j < 32 ? sees_lo >> j : sees_hi >> (j - 32)) & 1u) != 0;
-            // of lane half: d = 32 c + 8 g + 4 half + i.  (The address is made opaque: nothing of it is kept over the loop.)
-            const unsigned char *row = a.v_draft + draft_at + (size_t)j * draft_row + half * 8;
-            __asm__ volatile("" : "+v"(row));
-#pragma unroll
-            for (int c = 0; c < DT; ++c)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const u32x2 x = *reinterpret_cast<const u32x2 *>(row + (32 * c + 8 * g) * 2);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t bits = i & 1 ? x[i / 2] & 0xFFFF0000u : x[i / 2] << 16;
-                        if (seen && (bits & 0x7F800000u) == 0x7F800000u) oacc[c][4 * g + i] += __uint_as_float(bits);
-                    }
-                }
-        }
-    };
-
     // One tile, in two parts with a barrier in front of each.  In front of the first: everybody's K rows are there, and the V
     // buffer of the tile before is read out, so the next tile's V is asked for.  In front of the second: everybody's V rows
     // are there, and the K buffer is read out, so K of the tile after the next is asked for.  Each wait is for all but the
@@ -458,7 +460,13 @@ void tree_attn_kernel(TreeArgs a)
         if (MAIN || t + 2 * S < tiles) load_k(t + 2 * S, base2, lk);
         base1 = base2;
         base2 = tile_base(t + 3 * S);
-        if (drafted) odd = take_out_odd_values(lv);
+        if (drafted) {
+            bool any = false;
+#pragma unroll
+            for (int i = 0; i < KT * PIECES / (TREE_WAVES * 64); ++i)
+                any |= take_out_odd_values(lv + (i * TREE_WAVES * 64 + (int)threadIdx.x) * 16);
+            odd = __syncthreads_or(any) != 0;
+        }
         if (!active || steps == 0) return;
         __builtin_amdgcn_sched_barrier(0);
         float top = -INFINITY;
@@ -481,7 +489,11 @@ void tree_attn_kernel(TreeArgs a)
             if (!MAIN && st >= steps) break;
             add_values(lv + (wk * STEPS + st) * TREE_MT * ROW_BYTES, sc[st]);
         }
-        if (odd && wk == 0) add_odd_values();
+        if (odd && wk == 0) {
+#pragma unroll 1
+            for (int j = 0; j < nd; j += 32)
+                add_odd_values(a.v_draft + draft_at + (size_t)j * draft_row, draft_row, nd - j < 32 ? nd - j : 32, j == 0 ? sees_lo : sees_hi, oacc);
+        }
     };
     // (The compiler keeps account of what is on its way and makes a read of a buffer wait for it: it must find the same order on
     // every way into the loop, or it has everything waited for.  The waits above are its builtin for the same reason.)
@@ -697,42 +709,6 @@ void tree_narrow_kernel(TreeArgs a)
         }
     }
 
-    // as in tree_attn_kernel: values of drafted V rows that are not finite become 0 and are added to the rows that see them
-    auto take_out_odd_values = [&]() {
-        bool any = false;
-#pragma unroll
-        for (int i = 0; i < TILE_LDS / 16 / 64; ++i) {
-            u32x4 x = *reinterpret_cast<const u32x4 *>(wvl + (i * 64 + lane) * 16);
-            bool odd = false;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if ((x[e] & 0x7F80u) == 0x7F80u) { odd = true; x[e] &= 0xFFFF0000u; }
-                if ((x[e] & 0x7F800000u) == 0x7F800000u) { odd = true; x[e] &= 0xFFFFu; }
-            }
-            if (odd) *reinterpret_cast<u32x4 *>(wvl + (i * 64 + lane) * 16) = x;
-            any |= odd;
-        }
-        return __ballot(any) != 0;
-    };
-    auto add_odd_values = [&](int chunk, uint32_t sees) {
-        for (int j = chunk * TREE_MT; j < nd && j < (chunk + 1) * TREE_MT; ++j) {
-            const bool seen = ((sees >> (j - chunk * TREE_MT)) & 1u) != 0;
-            const unsigned char *row = a.v_draft + draft_at + (size_t)j * draft_row + half * 8;
-            __asm__ volatile("" : "+v"(row));
-#pragma unroll
-            for (int c = 0; c < DT; ++c)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const u32x2 x = *reinterpret_cast<const u32x2 *>(row + (32 * c + 8 * g) * 2);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t bits = i & 1 ? x[i / 2] & 0xFFFF0000u : x[i / 2] << 16;
-                        if (seen && (bits & 0x7F800000u) == 0x7F800000u) oacc[c][4 * g + i] += __uint_as_float(bits);
-                    }
-                }
-        }
-    };
-
     constexpr int WAIT_LDS = 0xC07F;                       // lgkmcnt(0)
     constexpr int WAIT_OLDER = 0x0F70 | LOADS;             // vmcnt(LOADS): all but the newest tile half is there
     auto tile_step = [&](int t, auto next) {
@@ -794,7 +770,12 @@ void tree_narrow_kernel(TreeArgs a)
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(NEXT ? WAIT_OLDER : 0x0F70);        // V
         __asm__ volatile("" ::: "memory");
-        const bool odd = drafted && take_out_odd_values();
+        bool odd = false;
+        if (drafted) {
+#pragma unroll
+            for (int i = 0; i < TILE_LDS / 16 / 64; ++i) odd |= take_out_odd_values(wvl + (i * 64 + lane) * 16);
+            odd = __ballot(odd) != 0;
+        }
         u32x2 vop[2][DT][2];
 #pragma unroll
         for (int kc = 0; kc < 2; ++kc)
@@ -824,7 +805,10 @@ void tree_narrow_kernel(TreeArgs a)
                 for (int c = 0; c < DT; ++c) oacc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c], p, oacc[c], 0, 0, 0);
             }
         }
-        if (odd) add_odd_values(chunk, sees);
+        if (odd) {
+            const int first = chunk * TREE_MT, count = nd - first < TREE_MT ? nd - first : TREE_MT;
+            add_odd_values(a.v_draft + draft_at + (size_t)first * draft_row, draft_row, count, sees, oacc);
+        }
     };
     if (t < tiles) {
         while (t + step < tiles) {
