@@ -195,6 +195,58 @@ __device__ __forceinline__ void add_odd_values(const unsigned char *rows, uint32
     }
 }
 
+// Whether one of four values is not finite: 0 x is NaN for those.
+__device__ __forceinline__ bool not_finite(f32x4 o)
+{
+    const float t = __builtin_fmaf(o[0], 0.f, o[1] * 0.f) + __builtin_fmaf(o[2], 0.f, o[3] * 0.f);
+    return t != 0.f;
+}
+
+// Four values of an output row that are not all finite, `sum` being its sum of weights.  By the formula, whose weights are positive, an
+// infinity in a V row that is seen makes the output that infinity; the products gave NaN, because parts of P are 0 or below 0 and
+// weights may be 0 in 32 bits.  So what is not finite in the rows that the output sees is added up by itself: rare, and slow (every
+// thread reads all rows).
+template <int D>
+__device__ __forceinline__ f32x4 seen_infinities(const TreeArgs &a, const TreeSegment &s, int row, int piece, f32x4 o, float sum)
+{
+    if (!(sum > 0.f && sum < INFINITY)) return o;           // scores that are not finite: NaN
+    constexpr int ROW_BYTES = D * 2, BATCH = 8;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](u32x2 x) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t bits = e & 1 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16;
+            if ((bits & 0x7F800000u) == 0x7F800000u) acc[e] += __uint_as_float(bits);
+        }
+    };
+    const size_t seg = (size_t)(a.seg0 + s.seg_local);
+    auto cached = [&](int j) {
+        size_t at = seg * a.cap + j;
+        if (a.table) {
+            int page = a.table[seg * a.max_pages + (j >> a.page_shift)];
+            page = (page < 0 || page >= a.num_pages) ? 0 : page;
+            at = ((size_t)page << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+        }
+        return *reinterpret_cast<const u32x2 *>(a.v + at * ROW_BYTES + piece * 8);
+    };
+    for (int j0 = 0; j0 < s.n; j0 += BATCH) {
+        u32x2 x[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) x[u] = cached(j0 + u < s.n ? j0 + u : s.n - 1);
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) add(x[u]);
+        if (acc[0] != acc[0] && acc[1] != acc[1] && acc[2] != acc[2] && acc[3] != acc[3]) return acc;      // NaN: nothing more to find
+    }
+    for (int j = row / a.G; j >= 0;) {
+        add(*reinterpret_cast<const u32x2 *>(a.v_draft + ((s.seq * a.W + j) * a.Hkv + s.h) * ROW_BYTES + piece * 8));
+        const int up = a.parent[(size_t)s.b * a.W + j];
+        j = up < j ? up : -1;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = acc[e] != 0.f ? acc[e] : o[e];
+    return o;
+}
+
 template <int D, int WQ, bool ONCE, bool PAGED>
 __global__ __launch_bounds__(TREE_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void tree_attn_kernel(TreeArgs a)
@@ -535,11 +587,10 @@ void tree_attn_kernel(TreeArgs a)
     __syncthreads();
     constexpr int ROWS = TREE_WAVES * 64 / OP;             // rows per workgroup-wide store
     const int piece = threadIdx.x % OP;
-    for (int r0 = threadIdx.x / OP; r0 < RB; r0 += ROWS) {
-        const int row = row_base + r0;
-        if (row >= R) break;
+    auto joined = [&](int r0, float &m_all, float &l_all) {
         const int q = r0 / TREE_QW, i = r0 % TREE_QW;
-        float f[WK], m_all = TREE_M_INIT, l_all = 0.f;
+        float f[WK];
+        m_all = TREE_M_INIT, l_all = 0.f;
 #pragma unroll
         for (int w = 0; w < WK; ++w) m_all = fmaxf(m_all, red_m[w * WQ + q][i]);
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -549,16 +600,32 @@ void tree_attn_kernel(TreeArgs a)
             l_all += red_l[w * WQ + q][i] * f[w];
             o += *reinterpret_cast<const f32x4 *>(rows_of(w * WQ + q) + i * (D * 4) + ((piece ^ i) & (OP - 1)) * 16) * f[w];
         }
+        return o;
+    };
+    auto out_row = [&](int row) { return (s.seq * a.W + row / G) * Hq + s.h * G + row % G; };
+    const int rows_here = R - row_base < RB ? R - row_base : RB;
+    bool odd = false;
+    float m_all, l_all;
+    for (int r0 = threadIdx.x / OP; r0 < rows_here; r0 += ROWS) {
+        f32x4 o = joined(r0, m_all, l_all);
         if (a.S == 1 || tiles == 1) {
-            const size_t at = (s.seq * a.W + row / G) * Hq + s.h * G + row % G;
-            __builtin_nontemporal_store(o / l_all, reinterpret_cast<f32x4 *>(a.out + at * D) + piece);
+            const size_t at = out_row(row_base + r0);
+            o /= l_all;
+            odd |= not_finite(o);
+            __builtin_nontemporal_store(o, reinterpret_cast<f32x4 *>(a.out + at * D) + piece);
             if (a.lse_out && piece == 0) a.lse_out[at] = (m_all + __log2f(l_all)) * 0.6931471805599453f;
         } else {
-            const size_t at = ((size_t)s.seg_local * a.S + split) * (size_t)(a.W * G) + row;
+            const size_t at = ((size_t)s.seg_local * a.S + split) * (size_t)(a.W * G) + row_base + r0;
             *(reinterpret_cast<f32x4 *>(a.part_o + at * D) + piece) = o;
             if (piece == 0) *reinterpret_cast<f32x2 *>(a.part_ml + at * 2) = f32x2{m_all, l_all};
         }
     }
+    if (odd)
+        for (int r0 = threadIdx.x / OP; r0 < rows_here; r0 += ROWS) {
+            const f32x4 o = joined(r0, m_all, l_all) / l_all;
+            if (not_finite(o))
+                *(reinterpret_cast<f32x4 *>(a.out + out_row(row_base + r0) * D) + piece) = seen_infinities<D>(a, s, row_base + r0, piece, o, l_all);
+        }
 }
 
 // 32 query rows.  Every wave walks key tiles of its own, 32 keys each (tile t belongs to wave t % 4 of workgroup
@@ -851,17 +918,23 @@ void tree_narrow_kernel(TreeArgs a)
         }
         return o;
     };
-    auto write = [&](int row, f32x4 o, float m_all, float l_all) {
-        const size_t at = (s.seq * a.W + row / G) * Hq + s.h * G + row % G;
-        *(reinterpret_cast<f32x4 *>(a.out + at * D) + piece) = o / l_all;
-        if (a.lse_out && piece == 0) a.lse_out[at] = (m_all + __log2f(l_all)) * 0.6931471805599453f;
-    };
     float m_all, l_all;
     if (parts == 1) {
+        auto out_row = [&](int row) { return (s.seq * a.W + (row_base + row) / G) * Hq + s.h * G + (row_base + row) % G; };
+        bool odd = false;
         for (int row = threadIdx.x / OP; row < R; row += ROWS) {
-            const f32x4 o = joined(row, m_all, l_all);
-            write(row_base + row, o, m_all, l_all);
+            const f32x4 o = joined(row, m_all, l_all) / l_all;
+            const size_t at = out_row(row);
+            odd |= not_finite(o);
+            *(reinterpret_cast<f32x4 *>(a.out + at * D) + piece) = o;
+            if (a.lse_out && piece == 0) a.lse_out[at] = (m_all + __log2f(l_all)) * 0.6931471805599453f;
         }
+        if (odd)
+            for (int row = threadIdx.x / OP; row < R; row += ROWS) {
+                const f32x4 o = joined(row, m_all, l_all) / l_all;
+                if (not_finite(o))
+                    *(reinterpret_cast<f32x4 *>(a.out + out_row(row) * D) + piece) = seen_infinities<D>(a, s, row_base + row, piece, o, l_all);
+            }
         return;
     }
     const size_t first = ((size_t)s.seg_local * a.S + split) * (size_t)(a.W * G) + row_base;
@@ -915,7 +988,9 @@ __global__ __launch_bounds__(TREE_MERGE_THREADS) void tree_merge_kernel(TreeArgs
         }
     }
     const size_t at = (s.seq * a.W + row / a.G) * (a.G * a.Hkv) + s.h * a.G + row % a.G;
-    *(reinterpret_cast<f32x4 *>(a.out + at * D) + piece) = num / den;
+    f32x4 o = num / den;
+    if (not_finite(o)) o = seen_infinities<D>(a, s, row, piece, o, den);
+    *(reinterpret_cast<f32x4 *>(a.out + at * D) + piece) = o;
     if (a.lse_out && piece == 0) a.lse_out[at] = (M + __log2f(den)) * 0.6931471805599453f;
 }
 
