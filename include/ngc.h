@@ -533,8 +533,9 @@ int ngc_paged_score_keys(const ngc_paged_cache *pc, int32_t layer, const void *q
  * ngc_decode_step would, one after the other.  What a node does not see never
  * reaches its output, values that are not finite included.  An infinity in a V row
  * that it sees makes that column of its output the infinity (NaN where both signs
- * or a NaN are seen), however small its weight; finding it takes longer.  Scores,
- * soft-max and accumulation are fp32.
+ * or a NaN are seen), however small its weight.  Scores, soft-max and accumulation
+ * are fp32; scaled scores may have any size below 2e38.  Rows with such values, or
+ * with scores beyond 1e7, are computed key by key and take longer.
  * ws must hold ngc_workspace_bytes(); with ngc_tree_workspace_bytes(), which is
  * not less, few segments are shared by as many workgroups as pays. */
 size_t ngc_tree_workspace_bytes(const ngc_cache *c, int32_t W);

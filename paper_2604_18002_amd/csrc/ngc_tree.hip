@@ -38,6 +38,7 @@
 // (one wave per SIMD: 128 segments x 1493 rows 30 -> 32-40 us); 8 waves and 128 keys per workgroup (R 33-64: 0.90-1.04 of the time,
 // R 65-128: 0.96-1.12); joining the partials in the same launch by tickets (as fast or slower, and state to keep); 8 waves with 32 rows (one workgroup on a CU
 // gets its rows at ~50 KB a microsecond however many waves ask: 0.82-1.12, 0.98 at the best choice of each geometry).
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -54,10 +55,14 @@ constexpr int TREE_WAVES = 4;
 constexpr int TREE_QW = 32;                 // query rows per wave
 constexpr int TREE_MT = 32;                 // keys per step of the math
 constexpr int TREE_PARTS = 3;               // bf16 parts of P
-// Start of the running max: finite and below every real score, so that 2^(x - m) is 0 for x = -inf without a special case.
-constexpr float TREE_M_INIT = -1.0e30f;
+// Start of the running max: the smallest finite number, so that 2^(x - m) is 0 for x = -inf without a special case and every finite
+// score is above it or equal to it.
+constexpr float TREE_M_INIT = -FLT_MAX;
 // The reference of the exponents moves only when a maximum has outgrown it by 2^8.
 constexpr float TREE_LAZY = 8.0f;
+// Rows whose maximum lies beyond this are computed again, key by key (see odd_row()): half a step of the maximum, rounded to 32 bits,
+// is a common factor in all weights, 2 at 2^24, but more than 2^x can hold from 2^31 on.
+constexpr float TREE_FAR = 16777216.0f;
 
 struct TreeArgs {
     const unsigned char *k, *v;         // the cache's rows, or the pools
@@ -156,6 +161,62 @@ __device__ __forceinline__ uint64_t tree_ancestors(const TreeArgs &a, int up, in
     return (uint64_t)hi << 32 | lo;
 }
 
+// The sums are rescaled only when a maximum has outgrown the reference: any reference gives the same quotients, and
+// probabilities up to 2^TREE_LAZY lose nothing in fp32 or in their bf16 parts.  `top`: of the row, in the scaled domain.
+template <int DT>
+__device__ __forceinline__ void raise_reference(float top, float &m_run, float &l_run, f32x16 (&oacc)[DT])
+{
+    if (__ballot(top > m_run + TREE_LAZY)) {
+        const float m_new = max_no_nan(m_run, top);
+        const float alpha = (m_new == m_run) ? 1.0f : fast_exp2(m_run - m_new);
+        l_run *= alpha;
+#pragma unroll
+        for (int c = 0; c < DT; ++c) oacc[c] *= alpha;
+        m_run = m_new;
+    }
+}
+
+// P of 32 keys from their raw scores with this lane's row, in bf16 parts; returns its sum.  The (positive) scale is applied inside the
+// exponent's multiply-add.
+__device__ __forceinline__ float tree_weights(const f32x16 &sc, float scale_log2e, float m_run, uint32_t (&part)[TREE_PARTS][8])
+{
+    const float neg_m = -m_run;
+    float psum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        f32x2 p = {fast_exp2(__builtin_fmaf(sc[2 * e], scale_log2e, neg_m)),       // -inf gives 0
+                   fast_exp2(__builtin_fmaf(sc[2 * e + 1], scale_log2e, neg_m))};
+        psum += p[0] + p[1];
+#pragma unroll
+        for (int i = 0; i < TREE_PARTS; ++i) {        // rounded to bf16; the remainder is exact
+            const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+            part[i][e] = w;
+            if (i + 1 < TREE_PARTS) p = f32x2{p[0] - __uint_as_float(w << 16), p[1] - __uint_as_float(w & 0xFFFF0000u)};
+        }
+    }
+    return psum;
+}
+
+// O += P V for 32 keys.  vop: [16-key chunk][d tile][keys 4 half .. +3, 8 + 4 half .. +3].
+template <int DT>
+__device__ __forceinline__ void add_products(const u32x2 (&vop)[2][DT][2], const uint32_t (&part)[TREE_PARTS][8], f32x16 (&oacc)[DT])
+{
+#pragma unroll
+    for (int kc = 0; kc < 2; ++kc) {
+        bf16x8 v[DT];
+#pragma unroll
+        for (int c = 0; c < DT; ++c)
+            v[c] = __builtin_bit_cast(bf16x8, u32x4{vop[kc][c][0][0], vop[kc][c][0][1], vop[kc][c][1][0], vop[kc][c][1][1]});
+#pragma unroll
+        for (int i = 0; i < TREE_PARTS; ++i) {
+            const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{part[i][4 * kc], part[i][4 * kc + 1], part[i][4 * kc + 2],
+                                                              part[i][4 * kc + 3]});
+#pragma unroll
+            for (int c = 0; c < DT; ++c) oacc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c], p, oacc[c], 0, 0, 0);
+        }
+    }
+}
+
 // Values of drafted V rows that are not finite would reach rows that do not see them, through a product with P = 0.  They become 0 in
 // LDS, in every slot of the tile that is multiplied (behind the last drafted row stand copies of it), and are added, by themselves, to
 // the rows that see them.
@@ -195,56 +256,108 @@ __device__ __forceinline__ void add_odd_values(const unsigned char *rows, uint32
     }
 }
 
-// Whether one of four values is not finite: 0 x is NaN for those.
-__device__ __forceinline__ bool not_finite(f32x4 o)
+// Whether a row has to be looked at again: four of its values are not all finite (0 x is NaN for those; a sum that is not finite though they
+// are is looked at in vain), or its scores are far.
+__device__ __forceinline__ bool is_odd(f32x4 o, float m)
 {
-    const float t = __builtin_fmaf(o[0], 0.f, o[1] * 0.f) + __builtin_fmaf(o[2], 0.f, o[3] * 0.f);
-    return t != 0.f;
+    return 0.f * ((o[0] + o[1]) + (o[2] + o[3])) != 0.f || fabsf(m) > TREE_FAR;
 }
 
-// Four values of an output row that are not all finite, `sum` being its sum of weights.  By the formula, whose weights are positive, an
-// infinity in a V row that is seen makes the output that infinity; the products gave NaN, because parts of P are 0 or below 0 and
-// weights may be 0 in 32 bits.  So what is not finite in the rows that the output sees is added up by itself: rare, and slow (every
-// thread reads all rows).
+// Four values (of D, by D / 4 consecutive lanes that call this together) of an output row that is odd, with its maximum m and sum of weights.
+//   Infinities  By the formula, whose weights are positive, an infinity in a V row that is seen makes the output that infinity; the
+//               products gave NaN, because parts of P are 0 or below 0 and weights may be 0 in 32 bits.  So what is not finite in
+//               the rows that the output sees is added up by itself.
+//   Far scores  A weight's exponent is the difference of two scaled scores that are rounded alike.
+// Rare, and slow, key after key by a quarter of D lanes (32 x 28/4 heads x 4096 rows, trees of 64: an infinity in every segment 12 ms, all
+// scores far 29; 1 x 32/8 x 16000, chains of 8: 3.2 and 8.0).
 template <int D>
-__device__ __forceinline__ f32x4 seen_infinities(const TreeArgs &a, const TreeSegment &s, int row, int piece, f32x4 o, float sum)
+__device__ __forceinline__ f32x4 odd_row(int seg_local, int row, int piece, f32x4 o, float &m, float &sum)
 {
-    if (!(sum > 0.f && sum < INFINITY)) return o;           // scores that are not finite: NaN
-    constexpr int ROW_BYTES = D * 2, BATCH = 8;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    auto add = [&](u32x2 x) {
+#pragma clang fp contract(off)
+    const bool far = fabsf(m) > TREE_FAR;
+    if (!far && !(sum > 0.f && sum < INFINITY)) return o;   // scores that are not finite: NaN
+    // Arguments and segment once more from where they come: nothing of this is kept in registers over the kernel's loop.
+    auto args = __builtin_amdgcn_kernarg_segment_ptr();
+    __asm__ volatile("" : "+s"(args));
+    const TreeArgs &a = *reinterpret_cast<const TreeArgs *>((uintptr_t)args);
+    TreeSegment s(a, seg_local);
+    s.clamp(a, false);
+    constexpr int ROW_BYTES = D * 2;
+    auto value = [](u32x2 x, int e) { return __uint_as_float(e & 1 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16); };
+    const u32x2 q = *reinterpret_cast<const u32x2 *>(a.q + ((s.seq * a.W + row / a.G) * (a.G * a.Hkv) + s.h * a.G + row % a.G) * ROW_BYTES + piece * 8);
+    f32x4 infinities = {0.f, 0.f, 0.f, 0.f}, acc = {0.f, 0.f, 0.f, 0.f};
+    float top = TREE_M_INIT, l = 0.f;
+    auto add = [&](u32x2 k, u32x2 v) {
+        float p = 0.f;
+        if (far) {
+            float score = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) score += value(q, e) * value(k, e);
+#pragma unroll
+            for (int step = 1; step < D / 4; step *= 2) score += __shfl_xor(score, step);
+            score *= a.scale_log2e;
+            if (score > top) {
+                const float alpha = fast_exp2(top - score);
+                l *= alpha;
+                acc *= alpha;
+                top = score;
+            }
+            p = fast_exp2(score - top);
+            l += p;
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint32_t bits = e & 1 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16;
-            if ((bits & 0x7F800000u) == 0x7F800000u) acc[e] += __uint_as_float(bits);
+            const float f = value(v, e);
+            const bool finite = fabsf(f) < INFINITY;
+            infinities[e] += finite ? 0.f : f;
+            acc[e] += finite ? p * f : 0.f;
         }
     };
-    const size_t seg = (size_t)(a.seg0 + s.seg_local);
-    auto cached = [&](int j) {
-        size_t at = seg * a.cap + j;
-        if (a.table) {
-            int page = a.table[seg * a.max_pages + (j >> a.page_shift)];
-            page = (page < 0 || page >= a.num_pages) ? 0 : page;
-            at = ((size_t)page << a.page_shift) + (j & ((1 << a.page_shift) - 1));
-        }
-        return *reinterpret_cast<const u32x2 *>(a.v + at * ROW_BYTES + piece * 8);
-    };
+    auto piece_of = [&](const unsigned char *rows, size_t at) { return *reinterpret_cast<const u32x2 *>(rows + at * ROW_BYTES + piece * 8); };
+    const size_t seg = (size_t)(a.seg0 + seg_local);
+    constexpr int BATCH = 4;                                // asked for together
     for (int j0 = 0; j0 < s.n; j0 += BATCH) {
-        u32x2 x[BATCH];
+        u32x2 k[BATCH] = {}, v[BATCH];
 #pragma unroll
-        for (int u = 0; u < BATCH; ++u) x[u] = cached(j0 + u < s.n ? j0 + u : s.n - 1);
+        for (int u = 0; u < BATCH; ++u) {
+            const int j = j0 + u < s.n ? j0 + u : s.n - 1;
+            size_t at = seg * a.cap + j;
+            if (a.table) {
+                int page = a.table[seg * a.max_pages + (j >> a.page_shift)];
+                page = (page < 0 || page >= a.num_pages) ? 0 : page;
+                at = ((size_t)page << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+            }
+            v[u] = piece_of(a.v, at);
+            if (far) k[u] = piece_of(a.k, at);
+        }
 #pragma unroll
-        for (int u = 0; u < BATCH; ++u) add(x[u]);
-        if (acc[0] != acc[0] && acc[1] != acc[1] && acc[2] != acc[2] && acc[3] != acc[3]) return acc;      // NaN: nothing more to find
+        for (int u = 0; u < BATCH; ++u)
+            if (j0 + u < s.n) add(k[u], v[u]);
+        const f32x4 x = infinities;
+        if (!far && x[0] != x[0] && x[1] != x[1] && x[2] != x[2] && x[3] != x[3]) return x;     // NaN: nothing more to find
     }
     for (int j = row / a.G; j >= 0;) {
-        add(*reinterpret_cast<const u32x2 *>(a.v_draft + ((s.seq * a.W + j) * a.Hkv + s.h) * ROW_BYTES + piece * 8));
+        const size_t at = (s.seq * a.W + j) * a.Hkv + s.h;
+        add(piece_of(a.k_draft, at), piece_of(a.v_draft, at));
         const int up = a.parent[(size_t)s.b * a.W + j];
         j = up < j ? up : -1;
     }
+    if (far) {
+        o = acc / l;
+        m = top;
+        sum = l;
+    }
+    if (!far || l == l)                                     // (NaN among the scores: NaN)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = acc[e] != 0.f ? acc[e] : o[e];
+        for (int e = 0; e < 4; ++e) o[e] = infinities[e] != 0.f ? infinities[e] : o[e];
     return o;
+}
+// The lanes of a row decide together.
+template <int D>
+__device__ __forceinline__ bool row_is_odd(bool mine)
+{
+    const uint64_t lanes = (((uint64_t)1 << (D / 4)) - 1) << (lane_id() / (D / 4) * (D / 4));
+    return (__ballot(mine) & lanes) != 0;
 }
 
 template <int D, int WQ, bool ONCE, bool PAGED>
@@ -263,6 +376,7 @@ void tree_attn_kernel(TreeArgs a)
     constexpr int WAVE_ROWS = KT / TREE_WAVES;             // rows of a tile that a wave loads: inside one page
     constexpr int LOADS = WAVE_ROWS / LOAD_ROWS;
     constexpr int RB = TREE_QW * WQ;                       // query rows of the workgroup
+    static_assert(TREE_MT * PIECES % (TREE_WAVES * 64) == 0, "a step's rows are cleaned by whole workgroups");
 
     __shared__ __align__(16) unsigned char lds_k0[TILE_LDS], lds_k1[TILE_LDS], lds_v0[TILE_LDS], lds_v1[TILE_LDS];
     __shared__ float red_m[TREE_WAVES][TREE_QW], red_l[TREE_WAVES][TREE_QW];
@@ -405,19 +519,6 @@ void tree_attn_kernel(TreeArgs a)
         }
     }
 
-    // The sums are rescaled only when a maximum has outgrown the reference: any reference gives the same quotients, and
-    // probabilities up to 2^TREE_LAZY lose nothing in fp32 or in their bf16 parts.  `top`: of the row, in the scaled domain.
-    auto raise_reference = [&](float top) {
-        if (__ballot(top > m_run + TREE_LAZY)) {
-            const float m_new = max_no_nan(m_run, top);
-            const float alpha = (m_new == m_run) ? 1.0f : fast_exp2(m_run - m_new);
-            l_run *= alpha;
-#pragma unroll
-            for (int c = 0; c < DT; ++c) oacc[c] *= alpha;
-            m_run = m_new;
-        }
-    };
-
     // Raw scores of 32 keys with this lane's row: register r holds key 8 (r / 4) + 4 half + r % 4 of them.
     auto scores = [&](const unsigned char *lk) {
         f32x16 sc;
@@ -431,9 +532,9 @@ void tree_attn_kernel(TreeArgs a)
             sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kop[c]), qop[c], sc, 0, 0, 0);
         return sc;
     };
-    // O += P V for 32 keys and their raw scores; the (positive) scale is applied inside the exponent's multiply-add.
+    // O += P V for 32 keys and their raw scores.
     auto add_values = [&](const unsigned char *lv, const f32x16 &sc) {
-        u32x2 vop[2][DT][2];      // [16-key chunk][d tile][keys 4 half .. +3, 8 + 4 half .. +3]
+        u32x2 vop[2][DT][2];
 #pragma unroll
         for (int kc = 0; kc < 2; ++kc)
 #pragma unroll
@@ -442,36 +543,9 @@ void tree_attn_kernel(TreeArgs a)
                 for (int g = 0; g < 2; ++g)
                     vop[kc][c][g] = read_transposed16(lv + vrd[c] + (16 * kc + 8 * g) * ROW_BYTES);
         __builtin_amdgcn_sched_barrier(0);     // the V rows arrive while the exponentials are made
-        const float neg_m = -m_run;
         uint32_t part[TREE_PARTS][8];
-        float psum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            f32x2 p = {fast_exp2(__builtin_fmaf(sc[2 * e], a.scale_log2e, neg_m)),       // -inf gives 0
-                       fast_exp2(__builtin_fmaf(sc[2 * e + 1], a.scale_log2e, neg_m))};
-            psum += p[0] + p[1];
-#pragma unroll
-            for (int i = 0; i < TREE_PARTS; ++i) {        // rounded to bf16; the remainder is exact
-                const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
-                part[i][e] = w;
-                if (i + 1 < TREE_PARTS) p = f32x2{p[0] - __uint_as_float(w << 16), p[1] - __uint_as_float(w & 0xFFFF0000u)};
-            }
-        }
-        l_run += psum;
-#pragma unroll
-        for (int kc = 0; kc < 2; ++kc) {
-            bf16x8 v[DT];
-#pragma unroll
-            for (int c = 0; c < DT; ++c)
-                v[c] = __builtin_bit_cast(bf16x8, u32x4{vop[kc][c][0][0], vop[kc][c][0][1], vop[kc][c][1][0], vop[kc][c][1][1]});
-#pragma unroll
-            for (int i = 0; i < TREE_PARTS; ++i) {
-                const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{part[i][4 * kc], part[i][4 * kc + 1], part[i][4 * kc + 2],
-                                                                  part[i][4 * kc + 3]});
-#pragma unroll
-                for (int c = 0; c < DT; ++c) oacc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c], p, oacc[c], 0, 0, 0);
-            }
-        }
+        l_run += tree_weights(sc, a.scale_log2e, m_run, part);
+        add_products(vop, part, oacc);
     };
 
     // One tile, in two parts with a barrier in front of each.  In front of the first: everybody's K rows are there, and the V
@@ -514,9 +588,10 @@ void tree_attn_kernel(TreeArgs a)
         base2 = tile_base(t + 3 * S);
         if (drafted) {
             bool any = false;
+            for (int first = 0; first < nd; first += TREE_MT)
 #pragma unroll
-            for (int i = 0; i < KT * PIECES / (TREE_WAVES * 64); ++i)
-                any |= take_out_odd_values(lv + (i * TREE_WAVES * 64 + (int)threadIdx.x) * 16);
+                for (int i = 0; i < TREE_MT * PIECES; i += TREE_WAVES * 64)
+                    any |= take_out_odd_values(lv + (first * PIECES + i + (int)threadIdx.x) * 16);
             odd = __syncthreads_or(any) != 0;
         }
         if (!active || steps == 0) return;
@@ -535,7 +610,7 @@ void tree_attn_kernel(TreeArgs a)
 #pragma unroll
             for (int r = 0; r < 16; r += 2) top = max_or_nan(max_or_nan(top, sc[st][r]), sc[st][r + 1]);
         }
-        raise_reference(half_rows_max(top) * a.scale_log2e);
+        raise_reference(half_rows_max(top) * a.scale_log2e, m_run, l_run, oacc);
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
             if (!MAIN && st >= steps) break;
@@ -602,30 +677,33 @@ void tree_attn_kernel(TreeArgs a)
         }
         return o;
     };
-    auto out_row = [&](int row) { return (s.seq * a.W + row / G) * Hq + s.h * G + row % G; };
-    const int rows_here = R - row_base < RB ? R - row_base : RB;
-    bool odd = false;
     float m_all, l_all;
-    for (int r0 = threadIdx.x / OP; r0 < rows_here; r0 += ROWS) {
+    auto write = [&](int row, f32x4 o, auto store) {
+        const size_t at = (s.seq * a.W + row / G) * Hq + s.h * G + row % G;
+        store(o, reinterpret_cast<f32x4 *>(a.out + at * D) + piece);
+        if (a.lse_out && piece == 0) a.lse_out[at] = (m_all + __log2f(l_all)) * 0.6931471805599453f;
+    };
+    bool odd = false;
+    for (int r0 = threadIdx.x / OP; r0 < RB; r0 += ROWS) {
+        const int row = row_base + r0;
+        if (row >= R) break;
         f32x4 o = joined(r0, m_all, l_all);
         if (a.S == 1 || tiles == 1) {
-            const size_t at = out_row(row_base + r0);
-            o /= l_all;
-            odd |= not_finite(o);
-            __builtin_nontemporal_store(o, reinterpret_cast<f32x4 *>(a.out + at * D) + piece);
-            if (a.lse_out && piece == 0) a.lse_out[at] = (m_all + __log2f(l_all)) * 0.6931471805599453f;
+            o *= 1.0f / l_all;          // (one quotient a row: four of them, a rounding less, made the epilogue a fifth longer)
+            odd |= is_odd(o, m_all);
+            write(row, o, [](f32x4 x, f32x4 *at) { __builtin_nontemporal_store(x, at); });
         } else {
-            const size_t at = ((size_t)s.seg_local * a.S + split) * (size_t)(a.W * G) + row_base + r0;
+            const size_t at = ((size_t)s.seg_local * a.S + split) * (size_t)(a.W * G) + row;
             *(reinterpret_cast<f32x4 *>(a.part_o + at * D) + piece) = o;
             if (piece == 0) *reinterpret_cast<f32x2 *>(a.part_ml + at * 2) = f32x2{m_all, l_all};
         }
     }
-    if (odd)
-        for (int r0 = threadIdx.x / OP; r0 < rows_here; r0 += ROWS) {
-            const f32x4 o = joined(r0, m_all, l_all) / l_all;
-            if (not_finite(o))
-                *(reinterpret_cast<f32x4 *>(a.out + out_row(row_base + r0) * D) + piece) = seen_infinities<D>(a, s, row_base + r0, piece, o, l_all);
-        }
+    if (__ballot(odd) == 0) return;
+    for (int r0 = threadIdx.x / OP; r0 < RB && row_base + r0 < R; r0 += ROWS) {
+        const f32x4 o = joined(r0, m_all, l_all) * (1.0f / l_all);
+        if (row_is_odd<D>(is_odd(o, m_all)))
+            write(row_base + r0, odd_row<D>(s.seg_local, row_base + r0, piece, o, m_all, l_all), [](f32x4 x, f32x4 *at) { *at = x; });
+    }
 }
 
 // 32 query rows.  Every wave walks key tiles of its own, 32 keys each (tile t belongs to wave t % 4 of workgroup
@@ -809,31 +887,9 @@ void tree_narrow_kernel(TreeArgs a)
         float tmx = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 16; r += 2) tmx = max_or_nan(max_or_nan(tmx, sc[r]), sc[r + 1]);
-        tmx = half_rows_max(tmx) * a.scale_log2e;
-        if (__ballot(tmx > m_run + TREE_LAZY)) {
-            const float m_new = max_no_nan(m_run, tmx);
-            const float alpha = (m_new == m_run) ? 1.0f : fast_exp2(m_run - m_new);
-            l_run *= alpha;
-#pragma unroll
-            for (int c = 0; c < DT; ++c) oacc[c] *= alpha;
-            m_run = m_new;
-        }
-        const float neg_m = -m_run;
+        raise_reference(half_rows_max(tmx) * a.scale_log2e, m_run, l_run, oacc);
         uint32_t part[TREE_PARTS][8];
-        float psum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            f32x2 p = {fast_exp2(__builtin_fmaf(sc[2 * e], a.scale_log2e, neg_m)),
-                       fast_exp2(__builtin_fmaf(sc[2 * e + 1], a.scale_log2e, neg_m))};
-            psum += p[0] + p[1];
-#pragma unroll
-            for (int i = 0; i < TREE_PARTS; ++i) {
-                const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
-                part[i][e] = w;
-                if (i + 1 < TREE_PARTS) p = f32x2{p[0] - __uint_as_float(w << 16), p[1] - __uint_as_float(w & 0xFFFF0000u)};
-            }
-        }
-        l_run += psum;
+        l_run += tree_weights(sc, a.scale_log2e, m_run, part);
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(NEXT ? WAIT_OLDER : 0x0F70);        // V
         __asm__ volatile("" ::: "memory");
@@ -858,20 +914,7 @@ void tree_narrow_kernel(TreeArgs a)
             base1 = tile_base(t + 2 * step);
         }
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int kc = 0; kc < 2; ++kc) {
-            bf16x8 v[DT];
-#pragma unroll
-            for (int c = 0; c < DT; ++c)
-                v[c] = __builtin_bit_cast(bf16x8, u32x4{vop[kc][c][0][0], vop[kc][c][0][1], vop[kc][c][1][0], vop[kc][c][1][1]});
-#pragma unroll
-            for (int i = 0; i < TREE_PARTS; ++i) {
-                const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{part[i][4 * kc], part[i][4 * kc + 1], part[i][4 * kc + 2],
-                                                                  part[i][4 * kc + 3]});
-#pragma unroll
-                for (int c = 0; c < DT; ++c) oacc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c], p, oacc[c], 0, 0, 0);
-            }
-        }
+        add_products(vop, part, oacc);
         if (odd) {
             const int first = chunk * TREE_MT, count = nd - first < TREE_MT ? nd - first : TREE_MT;
             add_odd_values(a.v_draft + draft_at + (size_t)first * draft_row, draft_row, count, sees, oacc);
@@ -919,29 +962,30 @@ void tree_narrow_kernel(TreeArgs a)
         return o;
     };
     float m_all, l_all;
-    if (parts == 1) {
-        auto out_row = [&](int row) { return (s.seq * a.W + (row_base + row) / G) * Hq + s.h * G + (row_base + row) % G; };
-        bool odd = false;
+    if (parts > 1) {                                       // a second launch joins the partials
+        const size_t first = ((size_t)s.seg_local * a.S + split) * (size_t)(a.W * G) + row_base;
         for (int row = threadIdx.x / OP; row < R; row += ROWS) {
-            const f32x4 o = joined(row, m_all, l_all) / l_all;
-            const size_t at = out_row(row);
-            odd |= not_finite(o);
-            *(reinterpret_cast<f32x4 *>(a.out + at * D) + piece) = o;
-            if (a.lse_out && piece == 0) a.lse_out[at] = (m_all + __log2f(l_all)) * 0.6931471805599453f;
+            const f32x4 o = joined(row, m_all, l_all);
+            *(reinterpret_cast<f32x4 *>(a.part_o + (first + row) * D) + piece) = o;
+            if (piece == 0) *reinterpret_cast<f32x2 *>(a.part_ml + (first + row) * 2) = f32x2{m_all, l_all};
         }
-        if (odd)
-            for (int row = threadIdx.x / OP; row < R; row += ROWS) {
-                const f32x4 o = joined(row, m_all, l_all) / l_all;
-                if (not_finite(o))
-                    *(reinterpret_cast<f32x4 *>(a.out + out_row(row) * D) + piece) = seen_infinities<D>(a, s, row_base + row, piece, o, l_all);
-            }
         return;
     }
-    const size_t first = ((size_t)s.seg_local * a.S + split) * (size_t)(a.W * G) + row_base;
-    for (int row = threadIdx.x / OP; row < R; row += ROWS) {           // a second launch joins the partials
-        const f32x4 o = joined(row, m_all, l_all);
-        *(reinterpret_cast<f32x4 *>(a.part_o + (first + row) * D) + piece) = o;
-        if (piece == 0) *reinterpret_cast<f32x2 *>(a.part_ml + (first + row) * 2) = f32x2{m_all, l_all};
+    auto write = [&](int row, f32x4 o) {
+        const size_t at = (s.seq * a.W + (row_base + row) / G) * Hq + s.h * G + (row_base + row) % G;
+        *(reinterpret_cast<f32x4 *>(a.out + at * D) + piece) = o;
+        if (a.lse_out && piece == 0) a.lse_out[at] = (m_all + __log2f(l_all)) * 0.6931471805599453f;
+    };
+    bool odd = false;
+    for (int row = threadIdx.x / OP; row < R; row += ROWS) {
+        const f32x4 o = joined(row, m_all, l_all) * (1.0f / l_all);
+        odd |= is_odd(o, m_all);
+        write(row, o);
+    }
+    if (__ballot(odd) == 0) return;
+    for (int row = threadIdx.x / OP; row < R; row += ROWS) {
+        const f32x4 o = joined(row, m_all, l_all) * (1.0f / l_all);
+        if (row_is_odd<D>(is_odd(o, m_all))) write(row, odd_row<D>(s.seg_local, row_base + row, piece, o, m_all, l_all));
     }
 }
 
@@ -988,8 +1032,8 @@ __global__ __launch_bounds__(TREE_MERGE_THREADS) void tree_merge_kernel(TreeArgs
         }
     }
     const size_t at = (s.seq * a.W + row / a.G) * (a.G * a.Hkv) + s.h * a.G + row % a.G;
-    f32x4 o = num / den;
-    if (not_finite(o)) o = seen_infinities<D>(a, s, row, piece, o, den);
+    f32x4 o = num * (1.0f / den);
+    if (row_is_odd<D>(is_odd(o, M))) o = odd_row<D>(s.seg_local, row, piece, o, M, den);
     *(reinterpret_cast<f32x4 *>(a.out + at * D) + piece) = o;
     if (a.lse_out && piece == 0) a.lse_out[at] = (M + __log2f(den)) * 0.6931471805599453f;
 }
