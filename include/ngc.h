@@ -526,7 +526,7 @@ int ngc_paged_score_keys(const ngc_paged_cache *pc, int32_t layer, const void *q
  *   out      fp32, same shape, 16-byte aligned
  *   lse_out  optional fp32 [B][W][Hq] (or [L][B][W][Hq]): the log of the sum of the
  *            exponentials (natural log), as from ngc_decode_attn, or NULL
- *   scale    positive and finite (NGC_EINVAL otherwise)
+ *   scale    positive, at most 2.35e38 (NGC_EINVAL otherwise)
  *   max_len_hint  as in ngc_decode_attn: steers how the work is split, never what
  *            is computed
  * The cache is only read.  A chain (parent[i] = i - 1) gives what W calls of

@@ -1164,7 +1164,8 @@ int launch_tree(const ngc_cache *c, const ngc_paged_cache *pc, int32_t layer, co
     if (c->D != 64 && c->D != 128) return NGC_EINVAL;
     if (c->Hq % c->Hkv != 0 || c->Hq / c->Hkv > 16) return NGC_EINVAL;
     if (layer < -1 || layer >= c->L || max_len_hint < 0) return NGC_EINVAL;
-    if (!(scale > 0.f) || scale > 3.0e38f) return NGC_EINVAL;       // positive and finite: maxima are taken before scaling
+    const float scale_log2e = scale * 1.4426950408889634f;
+    if (!(scale > 0.f) || !(scale_log2e <= FLT_MAX)) return NGC_EINVAL;       // maxima are taken before scaling
     if (W > TREE_MAX_NODES) return NGC_EUNSUPPORTED;
     if ((long long)c->cap * c->D * 2 > 0x7FFFFFFFLL) return NGC_EUNSUPPORTED;                       // 32-bit byte offsets
     if ((long long)W * c->Hkv * c->D * 2 > 0x7FFFFFFFLL) return NGC_EUNSUPPORTED;
@@ -1195,7 +1196,7 @@ int launch_tree(const ngc_cache *c, const ngc_paged_cache *pc, int32_t layer, co
     a.status = reinterpret_cast<int32_t *>(ws);
     a.seg0 = layer < 0 ? 0 : layer * per_layer;
     a.nseg = nseg; a.blocks = shape.blocks; a.S = S; a.W = W; a.G = G; a.B = c->B; a.Hkv = c->Hkv; a.cap = c->cap;
-    a.scale_log2e = scale * 1.4426950408889634f;
+    a.scale_log2e = scale_log2e;
     if (pc) {
         a.table = pc->table; a.max_pages = pc->max_pages; a.num_pages = pc->num_pages;
         a.page_shift = __builtin_ctz((unsigned)pc->page_rows);
