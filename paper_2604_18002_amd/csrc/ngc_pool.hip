@@ -259,7 +259,7 @@ __global__ __launch_bounds__(POOL_THREADS) void pool_plan_kernel(PoolArgs a)
             const int i = i0 + u < hi ? i0 + u : hi - 1, b = (i / a.Hkv) % a.B;
             const int held = pages(n[u] < 0 ? 0 : n[u] > cap ? cap : n[u]);
             p[u].rows = m[u];
-            p[u].clamped = m[u] >= 0 && (n[u] < 0 || n[u] > cap);
+            p[u].clamped = (m[u] >= 0 || (FORK && copies[b] > 0)) && (n[u] < 0 || n[u] > cap);      // given back, or copied
             p[u].back = m[u] >= 0 ? held : 0;
             p[u].take = m[u] > 0 ? pages(m[u]) : 0;
             p[u].work = FORK ? held * ((copies[b] + FORK_COPIES - 1) / FORK_COPIES) : 0;
