@@ -560,8 +560,8 @@ int ngc_tree_attn(const ngc_cache *c, int32_t layer, const void *k_draft, const 
  * refused tokens (p itself if that is zero everywhere):
  *     next = min { t : r(0) + .. + r(t) > u_sample[b] * (r(0) + .. + r(V - 1)) }.
  *   target, draft  fp32, row of node i at [(b * W + i) * prob_stride], V values that
- *            add up to 1 (rows of nodes the walk does not reach are not read); 4-byte
- *            aligned.  Values below 0 and NaN count as 0.  One-hot rows give greedy
+ *            add up to 1 (what rows of nodes that the walk does not reach hold does not
+ *            matter); 4-byte aligned.  Values below 0 and NaN count as 0.  One-hot rows give greedy
  *            verification.
  *   token    int32 [B][W]; token[b][0] is not looked at.  A token outside [0, V)
  *            is counted and never accepted.
@@ -571,7 +571,8 @@ int ngc_tree_attn(const ngc_cache *c, int32_t layer, const void *k_draft, const 
  *   next_out int32 [B]: the token that follows; -1 where n_draft is 0, and, counted,
  *            where p has no positive value
  * Sums are 64-bit, in a fixed order.  ws must hold ngc_verify_workspace_bytes();
- * it may be a workspace of a cache: it is left as it was found. */
+ * it may be a workspace of a cache, whose tickets have to be zero between launches:
+ * what a launch has used behind the status words is zero when it has ended. */
 size_t ngc_verify_workspace_bytes(int32_t B, int32_t V);
 int ngc_tree_verify(const float *target, const float *draft, int64_t prob_stride,
                     const int32_t *token, const int32_t *parent, const int32_t *n_draft,
