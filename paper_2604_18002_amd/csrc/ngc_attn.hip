@@ -112,6 +112,32 @@ struct AttnArgs {
     int B;
 };
 
+// Loads and stores that other workgroups' data travels through: device scope (served by memory, not by an XCD's own
+// L2), 16 bytes wide for the partial O rows (a wave's stores land as whole cache lines instead of one 4-byte
+// write-through per lane): raw buffer accesses with the device-scope bit, bounds-checked by the hardware against
+// `bytes` (a load past the end returns 0, a store past the end is dropped).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t device_span(const void *base, uint32_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x00020000);
+}
+constexpr int AUX_DEVICE_SCOPE = 16;   // sc1
+__device__ __forceinline__ void st_device16(__amdgpu_buffer_rsrc_t r, uint32_t byte_off, f32x4 v)
+{
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, byte_off, 0, AUX_DEVICE_SCOPE);
+}
+__device__ __forceinline__ f32x4 ld_device16(__amdgpu_buffer_rsrc_t r, uint32_t byte_off)
+{
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, byte_off, 0, AUX_DEVICE_SCOPE));
+}
+__device__ __forceinline__ void st_device8(__amdgpu_buffer_rsrc_t r, uint32_t byte_off, f32x2 v)
+{
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), r, byte_off, 0, AUX_DEVICE_SCOPE);
+}
+__device__ __forceinline__ f32x2 ld_device8(__amdgpu_buffer_rsrc_t r, uint32_t byte_off)
+{
+    return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(r, byte_off, 0, AUX_DEVICE_SCOPE));
+}
+
 // EARLY: a wave's first tile is requested before the length has arrived (see first_tile_early()).
 template <int D, bool PAGED, bool APPEND, bool EARLY>
 __global__ __launch_bounds__(ATT_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
@@ -714,6 +740,20 @@ int static_limit_splits(int nseg_launch, int max_len, int row_bytes)
 constexpr size_t FIXED_TICKET_OFFSET = STATUS_BYTES;
 constexpr size_t FIXED_PARTIAL_OFFSET = 4096;
 constexpr size_t FIXED_TICKETS = (FIXED_PARTIAL_OFFSET - FIXED_TICKET_OFFSET) / sizeof(int32_t);
+
+// Words between the tickets of two segments.  Atomics on one cache line are served one after the other, so a launch's
+// tickets lie as far apart as the words at hand allow, up to a line of 128 bytes.  A workspace has a word for every
+// segment of the cache, so the launches of a model of L layers, one layer each, have L words for a segment; a launch
+// over all layers has one, as does a cache of a single layer.  Microseconds per layer from a HIP graph of 28 layers, words
+// next to each other -> 28 apart, D = 128 (no difference below 16 segments, where at most 64 atomics meet):
+//     16 x 1500 rows   8.27 -> 6.69      32 x 1500   8.83 -> 8.11      64 x 1500        11.56 -> 11.06
+//     32 x  300        5.70 -> 5.47      64 x  525   8.06 -> 7.79      128 x 525        10.18 ->  9.55
+//     32 x  525        6.31 -> 5.74      48 x 676-1352 8.91 -> 8.64    64 x 3000-10000  41.18 -> 39.89
+int ticket_step(size_t words, int nseg_launch)
+{
+    const size_t apart = words / (size_t)nseg_launch;
+    return apart > 32 ? 32 : apart > 1 ? (int)apart : 1;
+}
 
 bool fits_static(const ngc_cache *c, int nseg_launch, int S)
 {

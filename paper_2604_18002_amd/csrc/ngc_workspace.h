@@ -22,20 +22,6 @@ inline size_t scratch_offset(const ngc_cache *c)
     return align256(ticket_offset(c) + (size_t)c->L * c->B * c->Hkv * sizeof(int32_t));
 }
 
-// Words between the tickets of two segments.  Atomics on one cache line are served one after the other, so a launch's
-// tickets lie as far apart as the words at hand allow, up to a line of 128 bytes.  A workspace has a word for every
-// segment of the cache, so the launches of a model of L layers, one layer each, have L words for a segment; a launch
-// over all layers has one, as does a cache of a single layer.  Microseconds per layer from a HIP graph of 28 layers, words
-// next to each other -> 28 apart, D = 128 (no difference below 16 segments, where at most 64 atomics meet):
-//     16 x 1500 rows   8.27 -> 6.69      32 x 1500   8.83 -> 8.11      64 x 1500        11.56 -> 11.06
-//     32 x  300        5.70 -> 5.47      64 x  525   8.06 -> 7.79      128 x 525        10.18 ->  9.55
-//     32 x  525        6.31 -> 5.74      48 x 676-1352 8.91 -> 8.64    64 x 3000-10000  41.18 -> 39.89
-inline int ticket_step(size_t words, int nseg_launch)
-{
-    const size_t apart = words / (size_t)nseg_launch;
-    return apart > 32 ? 32 : apart > 1 ? (int)apart : 1;
-}
-
 // The geometry of a paged cache as if its rows were held contiguously.
 inline ngc_cache logical_geometry(const ngc_paged_cache *pc)
 {
