@@ -21,8 +21,8 @@
 // The drafted rows are one more tile behind those of the cache, masked by a word of ancestor bits per lane.
 //
 // P enters the second product as three bf16 parts (24 bits): with two (2^-17 of an entry lost at most) the output would be
-// 2.2e-6 (of its norm) from the 64-bit result, where products in 32 bits are 3e-7 to 1.2e-6 away; with three it is 1.5e-7 to
-// 7e-7.  That is 4 products per 32x32x32 block in place of 3.
+// 2.2e-6 (of its norm) from the 64-bit result, where products in 32 bits are 3e-7 to 1.2e-6 away; with three it is 1.2e-7 to
+// 7.2e-7.  That is 4 products per 32x32x32 block in place of 3.
 //
 // Few segments are shared by S workgroups that take tiles in turn; each leaves an unnormalised partial (max, sum, O) and
 // a second launch joins them (tree_splits() has the rule and its figures).
