@@ -641,6 +641,81 @@ int ngc_paged_free(const ngc_paged_cache *pc, int32_t layer, const int32_t *drop
  * Takes the whole cache; ws must hold ngc_paged_pool_workspace_bytes(). */
 int ngc_paged_compact(const ngc_paged_cache *pc, void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Many new rows at once: prompts, and steps in which sequences grow by different
+ * numbers of tokens.  The tokens of all sequences are packed one behind the
+ * other, sequence after sequence. */
+
+/* Rows for n_new[b] more tokens in every segment of `layer` (-1 = all) of sequence b:
+ * the pages that are missing are granted (segments in ascending id, to each as many
+ * as it needs from the top of the stack downwards; a segment that finds fewer gets
+ * those that are left) and entered in the tables, and len grows.  Says where every
+ * packed token's row is; ngc_paged_fill brings it there.
+ *   n_new      int32 [B], or NULL: one token each
+ *   T          packed tokens that slot_out has room for, at most 1048576
+ *              (NGC_EUNSUPPORTED beyond).  Counts below 0 are taken for 0, and
+ *              tokens beyond T are left out; either is counted once a sequence
+ *              (NGC_STATUS_LEN_CLAMPED).
+ *   slot_out   int32 [Hkv][T] (or [L][Hkv][T] for layer = -1): page * page_rows + row of
+ *              every token, -1 for one without room and behind the last token
+ *   start_out  int32 [B + 1]: where each sequence's tokens begin, and their number
+ * Rows that a segment has no room or no page for are left out, the last first, and
+ * counted one by one (NGC_STATUS_APPEND_FULL); a length out of range leaves its
+ * segment as it is (NGC_STATUS_LEN_CLAMPED), and a row in a page outside the pool has
+ * slot -1 (NGC_STATUS_POOL_BOUNDS).  num_pages * page_rows < 2^31
+ * (NGC_EUNSUPPORTED).  ws must hold ngc_paged_workspace_bytes(). */
+int ngc_paged_extend(const ngc_paged_cache *pc, int32_t layer, const int32_t *n_new, int32_t T,
+                     int32_t *slot_out, int32_t *start_out, void *ws, size_t ws_bytes, void *stream);
+
+/* The rows of packed tokens to their slots in the pools.
+ *   k_new, v_new  bf16 [T][Hkv][D] (or [L][T][Hkv][D] for layer = -1), 16-byte aligned
+ *   new_pos       int32 [T]: what is stored into pos_pool for each token, or NULL
+ *   slot          as ngc_paged_extend writes it.  Negative: the row is left out; beyond
+ *                 the pool: counted too, once a row (NGC_STATUS_POOL_BOUNDS).  No slot
+ *                 may stand twice.
+ * ws needs NGC_STATUS_WORDS * 4 bytes (status only). */
+int ngc_paged_fill(const ngc_paged_cache *pc, int32_t layer, const void *k_new, const void *v_new,
+                   const int32_t *new_pos, const int32_t *slot, int32_t T,
+                   void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Latent caches.  A layer may keep one row a token for all its query heads: a latent
+ * vector of R values, from which keys and values of every head could be expanded, and
+ * a rotary part of E values that all heads share.  Such a cache is an ngc_paged_cache
+ * of one pool:
+ *   k_pool   bf16 [num_pages][page_rows][R + E], latent part first; v_pool is NULL
+ *   Hkv = 1; D = R + E: 576 = 512 + 64 or 288 = 256 + 32; Hq <= 128 (NGC_EUNSUPPORTED)
+ * Calls that deal with pages take it as they take others: ngc_paged_extend,
+ * ngc_paged_fill (v_new NULL), ngc_paged_evict, ngc_paged_free.  All other
+ * ngc_paged_* calls refuse it. */
+
+/* Attention of the newest tokens over a latent cache, in the absorbed form: their
+ * queries have been brought to the latent space (by the matrix that expands keys from
+ * it), and the output is brought from there to the heads' values by the caller's next
+ * matrix product.  For token i < n_new[b] of sequence b and head h,
+ *     out[b][i][h][:] = sum_j softmax_j( scale * <q[b][i][h], c_j> ) c_j[0 .. R)
+ *     over the rows j <= len - n_new[b] + i of the sequence: the last n_new rows are
+ *     those of the new tokens.  One token: attention over all rows.
+ *   n_new    int32 [B], 0 .. W, or NULL: W each.  Others are clamped and counted
+ *            (NGC_STATUS_LEN_CLAMPED).  Nothing is written for tokens from n_new on.
+ *   q        bf16 [B][W][Hq][R + E] (or [L][B][W][Hq][R + E] for layer = -1), 16-byte
+ *            aligned; W <= 1024 (NGC_EUNSUPPORTED)
+ *   out      bf16 [B][W][Hq][R] (or [L]..), 16-byte aligned
+ *   lse_out  optional fp32 [B][W][Hq] (or [L]..): the log of the sum of the
+ *            exponentials (natural log), or NULL
+ *   scale    positive, at most 2.35e38 (NGC_EINVAL otherwise)
+ *   max_len_hint  as in ngc_decode_attn: steers how the work is split, never what is
+ *            computed
+ * A token that sees no row has zeros and -inf (an empty sequence is counted:
+ * NGC_STATUS_EMPTY_ATTN).  Scores, soft-max and accumulation are fp32, weights are rounded
+ * to bf16.  Values that are not finite reach the tokens that see their row, and no other.
+ * ws must hold ngc_latent_workspace_bytes(), which makes every call on such a cache
+ * succeed. */
+size_t ngc_latent_workspace_bytes(const ngc_paged_cache *pc, int32_t W);
+int ngc_latent_attn(const ngc_paged_cache *pc, int32_t layer, const int32_t *n_new, int32_t W,
+                    const void *q, float scale, int32_t max_len_hint, void *out, float *lse_out,
+                    void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

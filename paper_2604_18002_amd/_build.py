@@ -31,6 +31,8 @@ _UNITS = (
     ("ngc_tree.hip", []),
     ("ngc_verify.hip", ["-ffp-contract=off"]),      # what is compared is defined product by product
     ("ngc_pool.hip", []),
+    ("ngc_prompt.hip", []),
+    ("ngc_latent.hip", []),
 )
 _PROBE_UNITS = (("ngc_probe.hip", []),)
 

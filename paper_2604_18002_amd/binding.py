@@ -48,7 +48,8 @@ EXPORTS = ("ngc_version", "ngc_strerror", "ngc_workspace_bytes", "ngc_perturbed_
            "ngc_paged_score_keys", "ngc_lmem", "ngc_keep_counts", "ngc_decode_attn_static", "ngc_decode_step",
            "ngc_tree_workspace_bytes", "ngc_tree_attn", "ngc_verify_workspace_bytes", "ngc_tree_verify", "ngc_tree_commit",
            "ngc_paged_tree_workspace_bytes", "ngc_paged_tree_attn", "ngc_paged_tree_commit",
-           "ngc_paged_pool_workspace_bytes", "ngc_paged_fork", "ngc_paged_free", "ngc_paged_compact")
+           "ngc_paged_pool_workspace_bytes", "ngc_paged_fork", "ngc_paged_free", "ngc_paged_compact",
+           "ngc_paged_extend", "ngc_paged_fill", "ngc_latent_workspace_bytes", "ngc_latent_attn")
 STATIC_SCRATCH_BYTES = 2 << 20
 
 
@@ -162,6 +163,14 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         fn.argtypes, fn.restype = [gp, i32, vp, vp, sz, vp], C.c_int
     lib.ngc_paged_compact.argtypes = [gp, vp, sz, vp]
     lib.ngc_paged_compact.restype = C.c_int
+    lib.ngc_paged_extend.argtypes = [gp, i32, vp, i32, vp, vp, vp, sz, vp]
+    lib.ngc_paged_extend.restype = C.c_int
+    lib.ngc_paged_fill.argtypes = [gp, i32, vp, vp, vp, vp, i32, vp, sz, vp]
+    lib.ngc_paged_fill.restype = C.c_int
+    lib.ngc_latent_workspace_bytes.argtypes = [gp, i32]
+    lib.ngc_latent_workspace_bytes.restype = sz
+    lib.ngc_latent_attn.argtypes = [gp, i32, vp, i32, vp, f32, i32, vp, vp, vp, sz, vp]
+    lib.ngc_latent_attn.restype = C.c_int
     if path == LIB_PATH:
         if not os.path.exists(HOST_LIB_PATH):
             raise RuntimeError(f"{HOST_LIB_PATH} is missing: build it first (python -m paper_2604_18002_amd._build); "
@@ -373,7 +382,8 @@ class PagedCache:
 
     k_pool, v_pool: bf16 [num_pages, page_rows, D]; pos_pool: int32 [num_pages, page_rows] or None;
     table: int32 [L, B, Hkv, max_pages]; len: int32 [L, B, Hkv]; free_stack: int32 [num_pages];
-    free_count: int32 [1]."""
+    free_count: int32 [1].
+    A cache of latent rows has one pool: k_pool bf16 [num_pages, page_rows, 576 or 288], v_pool None, Hkv = 1."""
     k_pool: object
     v_pool: object
     pos_pool: object
@@ -395,7 +405,7 @@ class PagedCache:
         num_pages, P, D = self.k_pool.shape
         L, B, Hkv, max_pages = self.table.shape
         for t in (self.k_pool, self.v_pool, self.table, self.len, self.free_stack, self.free_count):
-            assert t.is_contiguous()
+            assert t is None or t.is_contiguous()
         return ngc_paged_cache(_ptr(self.k_pool), _ptr(self.v_pool), _ptr(self.pos_pool), _ptr(self.table),
                                _ptr(self.len), _ptr(self.free_stack), _ptr(self.free_count),
                                L, B, Hkv, self.Hq, D, P, max_pages, num_pages)
@@ -412,6 +422,14 @@ class PagedCache:
         stack = torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device)
         count = torch.full((1,), num_pages, dtype=torch.int32, device=device)
         return PagedCache(k, v, pos, table, ln, stack, count, Hq)
+
+    @staticmethod
+    def allocate_latent(L, B, Hq, D, page_rows, max_pages, num_pages, device="cuda", with_pos=False) -> "PagedCache":
+        """An empty cache of latent rows of D values (576 or 288), one a token for all heads."""
+        pc = PagedCache.allocate(L, B, 1, Hq, 1, page_rows, max_pages, num_pages, device, with_pos)
+        import torch
+        pc.k_pool, pc.v_pool = torch.zeros(num_pages, page_rows, D, dtype=torch.bfloat16, device=device), None
+        return pc
 
 
 def ngc_paged_workspace_bytes(pc: PagedCache) -> int:
@@ -538,3 +556,30 @@ def ngc_paged_free(pc: PagedCache, layer: int, drop, ws, stream=None):
 
 def ngc_paged_compact(pc: PagedCache, ws, stream=None):
     _check(_front().paged_compact(pc, ws, _stream(stream)), "ngc_paged_compact")
+
+
+# ------------------------------------------------- prompts, latent caches ---
+
+def ngc_paged_extend(pc: PagedCache, layer: int, n_new, T: int, slot_out, start_out, ws, stream=None):
+    _check(_front().paged_extend(pc, layer, n_new, T, slot_out, start_out, ws, _stream(stream)), "ngc_paged_extend")
+
+
+def ngc_paged_fill(pc: PagedCache, layer: int, k_new, v_new, new_pos, slot, T: int, ws, stream=None):
+    _check(_front().paged_fill(pc, layer, k_new, v_new, new_pos, slot, T, ws, _stream(stream)), "ngc_paged_fill")
+
+
+def ngc_latent_workspace_bytes(pc: PagedCache, W: int) -> int:
+    v = pc.view()
+    return int(load_library().ngc_latent_workspace_bytes(C.byref(v), W))
+
+
+def allocate_latent_workspace(pc: PagedCache, W: int = 1):
+    """A zeroed workspace tensor (uint8) for every call on a cache of latent rows, attention of up to W new tokens among them."""
+    import torch
+    return torch.zeros(ngc_latent_workspace_bytes(pc, W), dtype=torch.uint8, device=pc.k_pool.device)
+
+
+def ngc_latent_attn(pc: PagedCache, layer: int, n_new, W: int, q, scale: float, max_len_hint: int, out, ws, stream=None,
+                    lse_out=None):
+    _check(_front().latent_attn(pc, layer, n_new, W, q, scale, max_len_hint, out, lse_out, ws, _stream(stream)),
+           "ngc_latent_attn")

@@ -20,7 +20,7 @@ namespace {
     X(perturbed_keys) X(keep_counts) X(evict) X(subset_logprob) X(subset_logprob_backward) X(lmem) X(cache_append) \
     X(decode_attn) X(decode_step) X(decode_attn_static) X(score_keys) X(replay_attn) X(paged_evict) X(paged_append) \
     X(paged_decode_attn) X(paged_score_keys) X(tree_attn) X(paged_tree_attn) X(tree_verify) X(tree_commit) \
-    X(paged_tree_commit) X(paged_fork) X(paged_free) X(paged_compact)
+    X(paged_tree_commit) X(paged_fork) X(paged_free) X(paged_compact) X(paged_extend) X(paged_fill) X(latent_attn)
 
 // the library's entry points, looked up once by open()
 struct Entries {
@@ -120,7 +120,7 @@ void *attr_ptr(const Object &o, PyObject *name, bool contiguous)
 {
     if (PyErr_Occurred()) return nullptr;
     const Ref t(o.get(name));
-    if (!t.o) return nullptr;
+    if (!t.o || t.o == Py_None) return nullptr;
     ngc_tensor x;
     if (read_tensor && read_tensor(t.o, &x) && (x.contiguous || !contiguous)) return x.data;
     if (contiguous) {
@@ -381,6 +381,22 @@ ENTRY(paged_compact, 3)
     return call(lib.paged_compact, &c, ptr(a[1]), bytes(a[1]), stream(a[2]));
 END
 
+ENTRY(paged_extend, 8)
+    const ngc_paged_cache c = paged_of(a[0]);
+    return call(lib.paged_extend, &c, i32(a[1]), as<int32_t>(a[2]), i32(a[3]), as<int32_t>(a[4]), as<int32_t>(a[5]), ptr(a[6]),
+                bytes(a[6]), stream(a[7]));
+END
+ENTRY(paged_fill, 9)
+    const ngc_paged_cache c = paged_of(a[0]);
+    return call(lib.paged_fill, &c, i32(a[1]), ptr(a[2]), ptr(a[3]), as<int32_t>(a[4]), as<int32_t>(a[5]), i32(a[6]), ptr(a[7]),
+                bytes(a[7]), stream(a[8]));
+END
+ENTRY(latent_attn, 11)
+    const ngc_paged_cache c = paged_of(a[0]);
+    return call(lib.latent_attn, &c, i32(a[1]), as<int32_t>(a[2]), i32(a[3]), ptr(a[4]), f32(a[5]), i32(a[6]), ptr(a[7]),
+                as<float>(a[8]), ptr(a[9]), bytes(a[9]), stream(a[10]));
+END
+
 // open(path): the library the calls go to (already loaded by the binding, so this only finds its entry points)
 PyObject *open_(PyObject *, PyObject *path)
 {
@@ -459,7 +475,7 @@ PyMethodDef methods[] = {
     FAST(cache_append), FAST(decode_attn), FAST(decode_step), FAST(decode_attn_static), FAST(score_keys),
     FAST(replay_attn), FAST(paged_evict), FAST(paged_append), FAST(paged_decode_attn), FAST(paged_score_keys),
     FAST(tree_attn), FAST(paged_tree_attn), FAST(tree_verify), FAST(tree_commit), FAST(paged_tree_commit),
-    FAST(paged_fork), FAST(paged_free), FAST(paged_compact),
+    FAST(paged_fork), FAST(paged_free), FAST(paged_compact), FAST(paged_extend), FAST(paged_fill), FAST(latent_attn),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ngc_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -338,7 +338,7 @@ extern "C" int ngc_paged_evict(const ngc_paged_cache *pc, int32_t layer, const f
                                int32_t max_keep, int32_t *kept_out, int32_t *sigma_out, float *logp_out,
                                void *ws, size_t ws_bytes, void *stream)
 {
-    int rc = check_paged(pc);
+    int rc = check_pages(pc);
     if (rc) return rc;
     if (!logits || !keep || !p || !kept_out || !ws || max_keep < 1) return NGC_EINVAL;
     if (p->block != pc->page_rows || logit_stride < pc->max_pages) return NGC_EINVAL;

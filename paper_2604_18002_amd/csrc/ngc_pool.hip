@@ -672,7 +672,7 @@ extern "C" int ngc_paged_tree_commit(const ngc_paged_cache *pc, int32_t layer, c
 
 extern "C" int ngc_paged_free(const ngc_paged_cache *pc, int32_t layer, const int32_t *drop, void *ws, size_t ws_bytes, void *stream)
 {
-    int rc = check_paged(pc);
+    int rc = check_pages(pc);
     if (rc) return rc;
     if (!drop || !ws || !aligned16(ws)) return NGC_EINVAL;
     int seg0, nseg;

@@ -32,21 +32,45 @@ inline ngc_cache logical_geometry(const ngc_paged_cache *pc)
     return c;
 }
 
-inline int check_paged(const ngc_paged_cache *pc)
+// What paged caches of either kind have to be.
+inline int check_pages_of(const ngc_paged_cache *pc)
 {
-    if (!pc || !pc->k_pool || !pc->v_pool || !pc->table || !pc->len || !pc->free_stack || !pc->free_count)
-        return NGC_EINVAL;
-    if (!aligned16(pc->k_pool) || !aligned16(pc->v_pool)) return NGC_EINVAL;
+    if (!pc || !pc->k_pool || !pc->table || !pc->len || !pc->free_stack || !pc->free_count) return NGC_EINVAL;
+    if (!aligned16(pc->k_pool)) return NGC_EINVAL;
     if (pc->L <= 0 || pc->B <= 0 || pc->Hkv <= 0 || pc->Hq <= 0 || pc->max_pages <= 0 || pc->num_pages <= 0)
         return NGC_EINVAL;
-    if (pc->D != 64 && pc->D != 128) return NGC_EINVAL;
-    if (pc->Hq % pc->Hkv != 0 || pc->Hq / pc->Hkv > 16) return NGC_EINVAL;
     if (pc->L > 65535 || pc->Hkv > 65534) return NGC_EINVAL;
     if (pc->page_rows < 32 || (pc->page_rows & (pc->page_rows - 1)) != 0) return NGC_EINVAL;
+    return NGC_OK;
+}
+inline int check_pages_limits(const ngc_paged_cache *pc)
+{
     if (pc->max_pages > 16384) return NGC_EUNSUPPORTED;
     if ((long long)pc->max_pages * pc->page_rows > 0x7FFFFFFFLL / 256) return NGC_EUNSUPPORTED;
     return NGC_OK;
 }
+
+inline int check_paged(const ngc_paged_cache *pc)
+{
+    if (check_pages_of(pc) != NGC_OK || !pc->v_pool || !aligned16(pc->v_pool)) return NGC_EINVAL;
+    if (pc->D != 64 && pc->D != 128) return NGC_EINVAL;
+    if (pc->Hq % pc->Hkv != 0 || pc->Hq / pc->Hkv > 16) return NGC_EINVAL;
+    return check_pages_limits(pc);
+}
+
+// Latent caches: one pool, one row a token for all heads.
+constexpr int LATENT_MOST_HEADS = 128, LATENT_MOST_TOKENS = 1024;
+inline int latent_width(int D) { return D / 9 * 8; }           // of the latent part of a row of D values
+inline int check_latent(const ngc_paged_cache *pc)
+{
+    if (check_pages_of(pc) != NGC_OK || pc->v_pool || pc->Hkv != 1) return NGC_EINVAL;
+    if (pc->D != 576 && pc->D != 288) return NGC_EINVAL;
+    if (pc->Hq > LATENT_MOST_HEADS) return NGC_EUNSUPPORTED;
+    return check_pages_limits(pc);
+}
+
+// A cache of either kind, for calls that only deal with pages.
+inline int check_pages(const ngc_paged_cache *pc) { return pc && !pc->v_pool ? check_latent(pc) : check_paged(pc); }
 
 inline int paged_layer_range(const ngc_paged_cache *pc, int layer, int *seg0, int *nseg)
 {
