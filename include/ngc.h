@@ -716,6 +716,47 @@ int ngc_latent_attn(const ngc_paged_cache *pc, int32_t layer, const int32_t *n_n
                     const void *q, float scale, int32_t max_len_hint, void *out, float *lse_out,
                     void *ws, size_t ws_bytes, void *stream);
 
+/* Replay attention of a latent layer, in the expanded form: all positions of every
+ * trajectory at once, on keys and values that the caller has expanded from the latent
+ * vectors, each query seeing the keys that were in the cache when its token was
+ * generated (prompts: all before it).  For position i < n[b] and head h, with
+ * E = D / 2, k_j = [ kv[b][j][h][0 .. D), rope_j ] and v_j = kv[b][j][h][D .. 2 D),
+ *     out[b][i][h][:] = sum_j softmax_j( scale * <q[b][i][h], k_j> ) v_j
+ *     over the j with  j <= i < death[b][j].
+ *   q        bf16 [B][T][Hq][D + E], 16-byte aligned; Hq <= 128 (NGC_EUNSUPPORTED)
+ *   kv       bf16 [B][T][Hq][2 D], 16-byte aligned: keys and values of a head side by
+ *            side, as one matrix product expands them
+ *   rope     bf16, 16-byte aligned: E values a position, the same for all heads, those of
+ *            position (b, j) at rope + (b * T + j) * rope_stride.  rope_stride: a multiple
+ *            of 8 from E on (for instance the width of the latent rows they stand in)
+ *   death    int32 [B][T], or NULL: nothing was evicted
+ *   n        int32 [B]: positions of each trajectory, taken for 0 .. T where it lies
+ *            outside; or NULL: T.  What the buffers hold at other positions does not
+ *            matter, and nothing is written there
+ *   out      bf16 [B][T][Hq][D], 16-byte aligned
+ *   lse_out  fp32 [B][Hq][T]: the log of the sum of the exponentials (natural log), or
+ *            NULL; the backward pass needs it
+ *   scale    positive, at most 2.35e38 (NGC_EINVAL otherwise)
+ * D is 64 or 128; T <= 131072 (NGC_EUNSUPPORTED).  A position that sees no key has zeros
+ * and -inf.  Scores, soft-max and accumulation are fp32, weights are rounded to bf16.
+ * Values that are not finite reach the positions that see them, and no other. */
+int ngc_latent_replay_attn(const void *q, const void *kv, const void *rope, int64_t rope_stride,
+                           const int32_t *death, const int32_t *n, int32_t B, int32_t T, int32_t Hq,
+                           int32_t D, float scale, void *out, float *lse_out, void *stream);
+
+/* Its gradient.  out and lse as the forward pass has left them; with dout the gradient
+ * that arrives at out (bf16, same shape):
+ *   dq, dkv  bf16, shapes of q and kv
+ *   drope    bf16 [B][T][E], one position behind the other: summed over the heads
+ * all written over, up to n[b] positions; 16-byte aligned.  Sums are fp32 and have one
+ * owner each: the same inputs give the same bits.  ws must hold
+ * ngc_latent_replay_workspace_bytes(); nothing in it has to be zero. */
+size_t ngc_latent_replay_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t D);
+int ngc_latent_replay_attn_backward(const void *q, const void *kv, const void *rope, int64_t rope_stride,
+                                    const int32_t *death, const int32_t *n, const void *out, const float *lse,
+                                    const void *dout, int32_t B, int32_t T, int32_t Hq, int32_t D, float scale,
+                                    void *dq, void *dkv, void *drope, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,6 +33,7 @@ _UNITS = (
     ("ngc_pool.hip", []),
     ("ngc_prompt.hip", []),
     ("ngc_latent.hip", []),
+    ("ngc_latent_replay.hip", []),
 )
 _PROBE_UNITS = (("ngc_probe.hip", []),)
 

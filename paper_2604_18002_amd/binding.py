@@ -49,7 +49,8 @@ EXPORTS = ("ngc_version", "ngc_strerror", "ngc_workspace_bytes", "ngc_perturbed_
            "ngc_tree_workspace_bytes", "ngc_tree_attn", "ngc_verify_workspace_bytes", "ngc_tree_verify", "ngc_tree_commit",
            "ngc_paged_tree_workspace_bytes", "ngc_paged_tree_attn", "ngc_paged_tree_commit",
            "ngc_paged_pool_workspace_bytes", "ngc_paged_fork", "ngc_paged_free", "ngc_paged_compact",
-           "ngc_paged_extend", "ngc_paged_fill", "ngc_latent_workspace_bytes", "ngc_latent_attn")
+           "ngc_paged_extend", "ngc_paged_fill", "ngc_latent_workspace_bytes", "ngc_latent_attn",
+           "ngc_latent_replay_workspace_bytes", "ngc_latent_replay_attn", "ngc_latent_replay_attn_backward")
 STATIC_SCRATCH_BYTES = 2 << 20
 
 
@@ -171,6 +172,12 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.ngc_latent_workspace_bytes.restype = sz
     lib.ngc_latent_attn.argtypes = [gp, i32, vp, i32, vp, f32, i32, vp, vp, vp, sz, vp]
     lib.ngc_latent_attn.restype = C.c_int
+    lib.ngc_latent_replay_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.ngc_latent_replay_workspace_bytes.restype = sz
+    lib.ngc_latent_replay_attn.argtypes = [vp, vp, vp, i64, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp]
+    lib.ngc_latent_replay_attn.restype = C.c_int
+    lib.ngc_latent_replay_attn_backward.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp, vp, sz, vp]
+    lib.ngc_latent_replay_attn_backward.restype = C.c_int
     if path == LIB_PATH:
         if not os.path.exists(HOST_LIB_PATH):
             raise RuntimeError(f"{HOST_LIB_PATH} is missing: build it first (python -m paper_2604_18002_amd._build); "
@@ -583,3 +590,20 @@ def ngc_latent_attn(pc: PagedCache, layer: int, n_new, W: int, q, scale: float, 
                     lse_out=None):
     _check(_front().latent_attn(pc, layer, n_new, W, q, scale, max_len_hint, out, lse_out, ws, _stream(stream)),
            "ngc_latent_attn")
+
+
+def ngc_latent_replay_attn(q, kv, rope, rope_stride: int, death, n, B: int, T: int, Hq: int, D: int, scale: float, out, lse_out=None,
+                           stream=None):
+    _check(_front().latent_replay_attn(q, kv, rope, rope_stride, death, n, B, T, Hq, D, scale, out, lse_out, _stream(stream)),
+           "ngc_latent_replay_attn")
+
+
+def ngc_latent_replay_workspace_bytes(B: int, T: int, Hq: int, D: int) -> int:
+    return int(load_library().ngc_latent_replay_workspace_bytes(B, T, Hq, D))
+
+
+def ngc_latent_replay_attn_backward(q, kv, rope, rope_stride: int, death, n, out, lse, dout, B: int, T: int, Hq: int, D: int,
+                                    scale: float, dq, dkv, drope, ws, stream=None):
+    _check(_front().latent_replay_attn_backward(q, kv, rope, rope_stride, death, n, out, lse, dout, B, T, Hq, D, scale, dq, dkv, drope,
+                                                ws, _stream(stream)),
+           "ngc_latent_replay_attn_backward")

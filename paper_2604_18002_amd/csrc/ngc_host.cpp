@@ -20,7 +20,8 @@ namespace {
     X(perturbed_keys) X(keep_counts) X(evict) X(subset_logprob) X(subset_logprob_backward) X(lmem) X(cache_append) \
     X(decode_attn) X(decode_step) X(decode_attn_static) X(score_keys) X(replay_attn) X(paged_evict) X(paged_append) \
     X(paged_decode_attn) X(paged_score_keys) X(tree_attn) X(paged_tree_attn) X(tree_verify) X(tree_commit) \
-    X(paged_tree_commit) X(paged_fork) X(paged_free) X(paged_compact) X(paged_extend) X(paged_fill) X(latent_attn)
+    X(paged_tree_commit) X(paged_fork) X(paged_free) X(paged_compact) X(paged_extend) X(paged_fill) \
+    X(latent_attn) X(latent_replay_attn) X(latent_replay_attn_backward)
 
 // the library's entry points, looked up once by open()
 struct Entries {
@@ -397,6 +398,16 @@ ENTRY(latent_attn, 11)
                 as<float>(a[8]), ptr(a[9]), bytes(a[9]), stream(a[10]));
 END
 
+ENTRY(latent_replay_attn, 14)
+    return call(lib.latent_replay_attn, ptr(a[0]), ptr(a[1]), ptr(a[2]), i64(a[3]), as<int32_t>(a[4]), as<int32_t>(a[5]), i32(a[6]),
+                i32(a[7]), i32(a[8]), i32(a[9]), f32(a[10]), ptr(a[11]), as<float>(a[12]), stream(a[13]));
+END
+ENTRY(latent_replay_attn_backward, 19)
+    return call(lib.latent_replay_attn_backward, ptr(a[0]), ptr(a[1]), ptr(a[2]), i64(a[3]), as<int32_t>(a[4]), as<int32_t>(a[5]),
+                ptr(a[6]), as<float>(a[7]), ptr(a[8]), i32(a[9]), i32(a[10]), i32(a[11]), i32(a[12]), f32(a[13]), ptr(a[14]),
+                ptr(a[15]), ptr(a[16]), ptr(a[17]), bytes(a[17]), stream(a[18]));
+END
+
 // open(path): the library the calls go to (already loaded by the binding, so this only finds its entry points)
 PyObject *open_(PyObject *, PyObject *path)
 {
@@ -476,6 +487,7 @@ PyMethodDef methods[] = {
     FAST(replay_attn), FAST(paged_evict), FAST(paged_append), FAST(paged_decode_attn), FAST(paged_score_keys),
     FAST(tree_attn), FAST(paged_tree_attn), FAST(tree_verify), FAST(tree_commit), FAST(paged_tree_commit),
     FAST(paged_fork), FAST(paged_free), FAST(paged_compact), FAST(paged_extend), FAST(paged_fill), FAST(latent_attn),
+    FAST(latent_replay_attn), FAST(latent_replay_attn_backward),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ngc_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

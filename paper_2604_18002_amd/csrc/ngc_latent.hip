@@ -332,8 +332,9 @@ void latent_attn_kernel(LatentArgs a)
 #pragma unroll
         for (int e = 1; e < Math::SCORES; ++e) tmx = max_no_nan(tmx, s_[e]);
         tmx = Math::top(tmx);
-        if (__ballot((tmx - m_run) * a.scale_log2e > LT_LAZY)) {
-            const float m_new = max_no_nan(m_run, tmx);
+        const bool outgrown = (tmx - m_run) * a.scale_log2e > LT_LAZY;     // of each row by itself: its results do not depend on its neighbours'
+        if (__ballot(outgrown)) {
+            const float m_new = outgrown ? tmx : m_run;
             const float alpha = m_new == m_run ? 1.0f : fast_exp2((m_run - m_new) * a.scale_log2e);
             l_run *= alpha;
             scale_all(oacc, alpha);

@@ -1,0 +1,805 @@
+// Replay attention of latent layers, expanded form, forward and backward, on gfx950.
+//
+// All T positions of a trajectory at once.  Head h has keys k_j = [its own part, D values | rotary part, E = D / 2 values that
+// all heads share] and values v_j of D; query i sees key j iff j <= i < death_j:
+//
+//     s_ij = scale <q_i, k_j>,  P_ij = exp(s_ij - lse_i),  o_i = sum_j P_ij v_j.
+//
+// With g_i the gradient that arrives at o_i and delta_i = <g_i, o_i>:
+//
+//     dv_j = sum_i P_ij g_i,   dS_ij = P_ij (<g_i, v_j> - delta_i),   dq_i = scale sum_j dS_ij k_j,   dk_j = scale sum_i dS_ij q_i,
+//
+// and the rotary part's gradient is the sum of the heads'.
+//
+// Three kernels around the same tiles of 32 x 32 pairs by 32x32x16 matrix instructions, four waves a workgroup:
+//   forward      a wave has 32 queries and walks tiles of 64 keys: S^T = K Q^T, O^T += V^T P.
+//   backward, q  the same walk, S^T and (V G^T) again, dQ^T += K^T dS; leaves delta.
+//   backward, kv a wave has 32 keys and walks tiles of 64 queries: S = Q K^T and G V^T, dV^T += G^T P, dK^T += Q^T dS.
+// In each the pairs stand in registers as the first products leave them, which is the order the second products' operand
+// needs if the rows of the other operand are read transposed in the same order: nothing crosses lanes but a row's maximum.
+// The two backward kernels form S twice (7 products in place of 5), so that every sum has one owner: no atomics, the same
+// bits again.
+//
+// A tile of keys that is dead for all of a workgroup's queries is never loaded: pages are evicted whole, so tiles die
+// whole.  Pairs are masked one by one only in tiles on the diagonal, behind the sequence's end, or where keys die midway.
+//
+// P and dS are rounded to bf16 (2^-8 of an entry at most) for their second products, as outputs and gradients are; sums,
+// maxima, lse and delta are fp32.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/ngc.h"
+#include "ngc_device.h"
+#include "ngc_latent.h"
+#include "ngc_workspace.h"
+
+namespace ngc {
+
+constexpr int LR_WAVES = 4;
+constexpr int LR_OWN = 32;                   // queries (keys) of a wave
+constexpr int LR_BLOCK = LR_WAVES * LR_OWN;  // of a workgroup
+constexpr int LR_TILE = 64;                  // keys (queries) of a tile
+constexpr int LR_STEP = 32;                  // of a step of the math
+constexpr int LR_MOST_POSITIONS = 64 * 32 * LR_TILE;       // a bit of a lane's word per tile
+constexpr float LR_LAZY = 8.0f;              // the reference of the exponents moves when a maximum has outgrown it by 2^8
+
+struct LatentReplayArgs {
+    const unsigned char *q;                  // bf16 [B][T][H][D + E]
+    const unsigned char *kv;                 // bf16 [B][T][H][2 D]: keys, then values
+    const unsigned char *rope;               // bf16, E values a position, rope_row bytes apart
+    const int32_t *death;                    // [B][T] or nullptr
+    const int32_t *n;                        // [B] or nullptr
+    unsigned char *out;                      // bf16 [B][T][H][D]
+    float *lse;                              // fp32 [B][H][T] (or nullptr, forward)
+    // backward
+    const unsigned char *dout;               // bf16 [B][T][H][D]
+    unsigned char *dq, *dkv, *drope;         // bf16, as q and kv; [B][T][E]
+    float *delta;                            // workspace, fp32 [B][H][T]
+    float *part;                             // workspace, fp32 [B][H][T][E]: the heads' gradients of the rotary part
+    size_t rope_row;
+    int B, T, H;
+    float scale, scale_log2e;
+};
+
+// Rows of BYTES in LDS, a multiple of 64 of them behind one another: 16-byte piece p of row r at slot p ^ swizzle(r), so that one
+// piece of 8 consecutive rows, and 64 bytes of 8 of them, meet every bank alike.
+template <int BYTES>
+struct LdsRows {
+    static constexpr int PIECES = BYTES / 16, LOAD_ROWS = 64 / PIECES;
+    static_assert(PIECES == 16 || PIECES == 8 || PIECES == 4, "whole rows a load");
+    __device__ static __forceinline__ int swizzle(int r)
+    {
+        return PIECES == 16 ? ((2 * r) & 15) | ((r >> 3) & 1) : PIECES == 8 ? r & 7 : (r >> 1) & 3;
+    }
+    // LR_TILE rows from memory, `stride` bytes apart, straight to LDS; rows behind `last` are that one again
+    __device__ static __forceinline__ void load(const unsigned char *from, uint32_t stride, int last, unsigned char *to, int wv, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < LR_TILE / (LR_WAVES * LOAD_ROWS); ++i) {
+            const int r0 = (i * LR_WAVES + wv) * LOAD_ROWS, r = r0 + lane / PIECES, row = r < last ? r : last;
+            load_to_lds16(from + ((uint32_t)row * stride + (uint32_t)((lane % PIECES) ^ swizzle(r)) * 16u), to + r0 * BYTES);
+        }
+    }
+    // Offset of piece 2 c + half of row `li`: an operand of 16 values c of 32 rows.  (Rows 32 apart: 32 BYTES more.)
+    __device__ static __forceinline__ uint32_t row_piece(int li, int half, int c)
+    {
+        return (uint32_t)(li * BYTES + (((2 * c + half) ^ swizzle(li)) & (PIECES - 1)) * 16);
+    }
+    // Where a lane points in a transposing read of rows 4 half + 8 g .. + 3 (16 more: 16 BYTES more), columns 32 c ..
+    __device__ static __forceinline__ uint32_t column(int lane, int g, int c)
+    {
+        const int r = 4 * (lane >> 5) + (lane & 15) / 4 + 8 * g, col = 32 * c + (lane & 16) + 4 * (lane & 3);
+        return (uint32_t)(r * BYTES + (((col / 8) ^ swizzle(r)) & (PIECES - 1)) * 16 + (col % 8) * 2);
+    }
+};
+
+__device__ __forceinline__ bf16x8 operand(u32x4 x) { return __builtin_bit_cast(bf16x8, x); }
+__device__ __forceinline__ f32x16 product(bf16x8 x, bf16x8 y, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+__device__ __forceinline__ f32x16 zeros16()
+{
+    f32x16 x;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = 0.f;
+    return x;
+}
+// Row of a tile that register r of a lane's half stands for.
+__device__ __forceinline__ int row_of(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
+
+// acc += X^T w for 32 rows of X in LDS and 32 x 32 weights as the first products leave them.  MIXED: some pairs are masked; values
+// that are not finite are taken for 0 then.  Returns whether there were some.
+template <int BYTES, int CT>
+__device__ __forceinline__ bool add_transposed(const unsigned char *x, const uint32_t (&w)[8], const uint32_t (&at)[CT][2], bool mixed,
+                                               f32x16 (&acc)[CT])
+{
+    bool odd = false;
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+        const bf16x8 weights = operand(u32x4{w[4 * st], w[4 * st + 1], w[4 * st + 2], w[4 * st + 3]});
+        u32x2 v[CT][2];
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) v[c][g] = read_transposed16(x + at[c][g] + 16 * st * BYTES);
+        if (mixed) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c) odd |= take_out_odd(v[c][0]) | take_out_odd(v[c][1]);
+        }
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[c] = product(operand(u32x4{v[c][0][0], v[c][0][1], v[c][1][0], v[c][1][1]}), weights, acc[c]);
+    }
+    return odd;
+}
+
+// Which of 32 rows in LDS have a value that is not finite, a bit each (the whole wave).
+template <int BYTES>
+__device__ __forceinline__ uint32_t odd_rows(const unsigned char *rows)
+{
+    uint32_t mask = 0;
+    for (int r = 0; r < 32; ++r) {
+        bool any = false;
+        if (lane_id() * 8 < BYTES) any = has_odd(*reinterpret_cast<const u32x2 *>(rows + r * BYTES + lane_id() * 8));
+        mask |= (uint32_t)(__ballot(any) != 0) << r;
+    }
+    return mask;
+}
+
+// Tiles of LR_TILE keys that some query of first .. last sees, and those that all of them see where causality lets them, as words of
+// 32 tiles in the lanes.
+struct LiveTiles {
+    uint32_t some, all;
+    __device__ __forceinline__ LiveTiles(const int32_t *death, int tiles, int n, int first, int last)
+    {
+        const int lane = lane_id();
+        some = all = tiles >= 32 * (lane + 1) ? 0xFFFFFFFFu : tiles <= 32 * lane ? 0u : (1u << (tiles - 32 * lane)) - 1u;
+        if (!death) return;
+        some = all = 0;
+        constexpr int BATCH = 8;
+        for (int t0 = 0; t0 < tiles; t0 += BATCH) {
+            int d[BATCH];
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                const int j = (t0 + u) * LR_TILE + lane;
+                d[u] = j < n ? death[j] : 0;
+            }
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                const bool inside = t0 + u < tiles && (t0 + u) * LR_TILE + lane < n;
+                const bool any = __ballot(inside && d[u] > first) != 0, every = __ballot(inside && d[u] <= last) == 0;
+                if (lane == (t0 + u) / 32 && t0 + u < tiles) {
+                    some |= (uint32_t)any << ((t0 + u) % 32);
+                    all |= (uint32_t)every << ((t0 + u) % 32);
+                }
+            }
+        }
+    }
+    // The first live tile from t on, or `tiles`.  Uniform.
+    __device__ __forceinline__ int next(int t, int tiles) const
+    {
+        while (t < tiles) {
+            const uint32_t w = (uint32_t)__builtin_amdgcn_readlane((int)some, t / 32) >> (t % 32);
+            if (w) return t + __builtin_ctz(w);
+            t = (t / 32 + 1) * 32;
+        }
+        return tiles;
+    }
+    __device__ __forceinline__ bool whole(int t) const { return ((uint32_t)__builtin_amdgcn_readlane((int)all, t / 32) >> (t % 32)) & 1u; }
+};
+
+// What a workgroup that owns queries (forward, backward q) or keys (backward kv) works on: heaviest first, a (trajectory, head) on
+// one XCD, whose L2 then holds its rows.
+struct LatentReplayPlace {
+    int block, b, h;
+    __device__ __forceinline__ LatentReplayPlace(const LatentReplayArgs &a, int blocks, bool last_first)
+    {
+        const int heads = a.B * a.H;
+        const int i = (int)(blockIdx.x / (unsigned)heads), bh = (int)(blockIdx.x % (unsigned)heads);
+        block = last_first ? blocks - 1 - i : i;
+        b = bh / a.H;
+        h = bh % a.H;
+    }
+    __device__ __forceinline__ int length(const LatentReplayArgs &a) const
+    {
+        const int n = a.n ? constant_word(a.n + b) : a.T;
+        return n < 0 ? 0 : n > a.T ? a.T : n;
+    }
+};
+
+// The tiles of keys in LDS that the two kernels with queries of their own walk.
+template <int D>
+struct KeyTile {
+    static constexpr int E = D / 2, KB = D * 2, RB = E * 2;
+    static constexpr int ROT = LR_TILE * KB, V = ROT + LR_TILE * RB, BYTES = V + LR_TILE * KB;
+    __device__ static __forceinline__ void load(const LatentReplayArgs &a, int b, int h, int t, unsigned char *to, int wv, int lane)
+    {
+        const int first = t * LR_TILE, last = a.T - 1 - first;         // (of the memory; behind the sequence's end nothing is seen)
+        const unsigned char *k = a.kv + (((size_t)b * a.T + first) * a.H + h) * (2 * KB);
+        const uint32_t stride = (uint32_t)a.H * (2 * KB);
+        LdsRows<KB>::load(k, stride, last, to, wv, lane);
+        LdsRows<RB>::load(a.rope + ((size_t)b * a.T + first) * a.rope_row, (uint32_t)a.rope_row, last, to + ROT, wv, lane);
+        LdsRows<KB>::load(k + KB, stride, last, to + V, wv, lane);
+    }
+};
+
+// The bits of 32 keys from key0 that query i sees, of the 16 that stand in a lane's registers: register r, bit r.
+__device__ __forceinline__ uint32_t seen_keys(const int32_t *death, int key0, int n, int i, int half)
+{
+    uint32_t seen = 0;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int j = key0 + row_of(r, half);
+        bool sees = j <= i && j < n;
+        if (death) sees = sees && i < death[j < n ? j : n - 1];
+        seen |= (uint32_t)sees << r;
+    }
+    return seen;
+}
+
+template <int D>
+__global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
+void latent_replay_kernel(LatentReplayArgs a)
+{
+    using Tile = KeyTile<D>;
+    constexpr int E = D / 2, KC = D / 16, RC = E / 16, DT = D / 32;
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
+    const int li = lane & 31, half = lane >> 5;
+    const LatentReplayPlace at(a, (a.T + LR_BLOCK - 1) / LR_BLOCK, true);
+    const int n = at.length(a), i0 = at.block * LR_BLOCK;
+    if (i0 >= n) return;
+    const int wave0 = i0 + wv * LR_OWN, qpos = wave0 + li;
+    const int wave_last = wave0 + LR_OWN - 1 < n ? wave0 + LR_OWN - 1 : n - 1, block_last = i0 + LR_BLOCK - 1 < n ? i0 + LR_BLOCK - 1 : n - 1;
+    const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
+    const int tiles = block_last / LR_TILE + 1;
+    const LiveTiles live(death, tiles, n, i0, block_last);
+    int t = live.next(0, tiles);
+    if (t < tiles) Tile::load(a, at.b, at.h, t, lds, wv, lane);
+
+    bf16x8 q[KC + RC];
+    {
+        const unsigned char *row = a.q + (((size_t)at.b * a.T + (qpos < n ? qpos : n - 1)) * a.H + at.h) * ((D + E) * 2) + half * 16;
+#pragma unroll
+        for (int c = 0; c < KC + RC; ++c) q[c] = operand(*reinterpret_cast<const u32x4 *>(row + c * 32));
+    }
+    uint32_t k_at[KC], r_at[RC], v_at[DT][2];
+#pragma unroll
+    for (int c = 0; c < KC; ++c) k_at[c] = LdsRows<Tile::KB>::row_piece(li, half, c);
+#pragma unroll
+    for (int c = 0; c < RC; ++c) r_at[c] = Tile::ROT + LdsRows<Tile::RB>::row_piece(li, half, c);
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) v_at[c][g] = Tile::V + LdsRows<Tile::KB>::column(lane, g, c);
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int c = 0; c < DT; ++c) o[c] = zeros16();
+    float m_run = -INFINITY, neg_m = 0.f, l_run = 0.f;     // scaled domain; neg_m: -m_run, or 0 as long as nothing has been seen
+
+    auto step = [&](const unsigned char *tile, int st, int key0, bool whole) {
+        const bool mixed = !whole || key0 + LR_STEP - 1 > wave0 || key0 + LR_STEP > n;
+        f32x16 sc = zeros16();
+#pragma unroll
+        for (int c = 0; c < KC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + k_at[c] + st * LR_STEP * Tile::KB)), q[c], sc);
+#pragma unroll
+        for (int c = 0; c < RC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + r_at[c] + st * LR_STEP * Tile::RB)), q[KC + c], sc);
+        uint32_t seen = 0xFFFFu;
+        if (mixed) {
+            seen = seen_keys(death, key0, n, qpos, half);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[r] = (seen >> r) & 1u ? sc[r] : -INFINITY;
+        }
+        float top = sc[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = max_no_nan(top, sc[r]);
+        top = half_rows_max(top) * a.scale_log2e;
+        const bool outgrown = top - m_run > LR_LAZY;        // of each row by itself: its results do not depend on its neighbours'
+        if (__ballot(outgrown)) {
+            const float m_new = outgrown ? top : m_run;
+            const float alpha = m_new == m_run ? 1.0f : fast_exp2(m_run - m_new);
+            l_run *= alpha;
+#pragma unroll
+            for (int c = 0; c < DT; ++c) o[c] *= alpha;
+            m_run = m_new;
+            neg_m = m_new == -INFINITY ? 0.f : -m_new;
+        }
+        uint32_t w[8];
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float p0 = fast_exp2(__builtin_fmaf(sc[2 * e], a.scale_log2e, neg_m)), p1 = fast_exp2(__builtin_fmaf(sc[2 * e + 1], a.scale_log2e, neg_m));
+            sum += p0 + p1;
+            w[e] = pack_bf16(p0, p1);
+        }
+        l_run += sum;
+        const bool odd = add_transposed<Tile::KB>(tile + st * LR_STEP * Tile::KB, w, v_at, mixed, o);
+        if (__ballot(odd)) {
+            // the queries that see a row with such a value, and no others, become NaN
+            const uint32_t rows = odd_rows<Tile::KB>(tile + Tile::V + st * LR_STEP * Tile::KB);
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (((rows >> row_of(r, half)) & 1u) && ((seen >> r) & 1u)) l_run = NAN;
+        }
+    };
+
+    unsigned char *here = lds, *there = lds + Tile::BYTES;
+    while (t < tiles) {
+        lds_loads_done();
+        const int next = live.next(t + 1, tiles);
+        if (next < tiles) Tile::load(a, at.b, at.h, next, there, wv, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        const bool whole = live.whole(t);
+#pragma unroll
+        for (int st = 0; st < LR_TILE / LR_STEP; ++st) {
+            const int key0 = t * LR_TILE + st * LR_STEP;
+            if (wave0 < n && key0 <= wave_last) step(here, st, key0, whole);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        unsigned char *const x = here;
+        here = there;
+        there = x;
+        t = next;
+    }
+
+    // out, through LDS: rows leave as whole lines; 16-byte piece p of row r at slot p ^ r
+    const float l = half_rows_sum(l_run);
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    if (a.lse && half == 0 && qpos < n)
+        a.lse[((size_t)at.b * a.H + at.h) * a.T + qpos] = l == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    __syncthreads();
+    constexpr int OP = D / 8;
+    unsigned char *const mine = lds + wv * LR_OWN * D * 2;
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int col = 32 * c + 8 * g + 4 * half;
+            *reinterpret_cast<u32x2 *>(mine + li * (D * 2) + (((col / 8) ^ li) & (OP - 1)) * 16 + (col % 8) * 2) =
+                u32x2{pack_bf16(o[c][4 * g] * inv, o[c][4 * g + 1] * inv), pack_bf16(o[c][4 * g + 2] * inv, o[c][4 * g + 3] * inv)};
+        }
+    __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt(0): a wave's rows are its own
+    __asm__ volatile("" ::: "memory");
+#pragma unroll
+    for (int r0 = 0; r0 < LR_OWN; r0 += 64 / OP) {
+        const int r = r0 + lane / OP, piece = lane % OP;
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(mine + r * (D * 2) + ((piece ^ r) & (OP - 1)) * 16);
+        if (wave0 + r < n) *reinterpret_cast<u32x4 *>(a.out + ((((size_t)at.b * a.T + wave0 + r) * a.H + at.h) * D + piece * 8) * 2) = x;
+    }
+}
+
+// 32 rows of COLS gradients (a wave's own) from accumulators to bf16 rows in memory, through LDS as above.  `col0`: first column of
+// the first accumulator in a row.
+template <int CT>
+__device__ __forceinline__ void store_rows(unsigned char *lds, const f32x16 (&acc)[CT], float scale, unsigned char *to, size_t stride, int rows)
+{
+    constexpr int PIECES = CT * 4;                         // 16-byte pieces of a row: 4, 8, 12 or 16
+    const int lane = lane_id(), li = lane & 31, half = lane >> 5;
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __asm__ volatile("" ::: "memory");
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int piece = 4 * c + g;
+            *reinterpret_cast<u32x2 *>(lds + li * (PIECES * 16) + (piece ^ (li & 3)) * 16 + half * 8) =
+                u32x2{pack_bf16(acc[c][4 * g] * scale, acc[c][4 * g + 1] * scale), pack_bf16(acc[c][4 * g + 2] * scale, acc[c][4 * g + 3] * scale)};
+        }
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __asm__ volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32 * PIECES / 64; ++i) {
+        const int r = (i * 64 + lane) / PIECES, piece = (i * 64 + lane) % PIECES;
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(lds + r * (PIECES * 16) + (piece ^ (r & 3)) * 16);
+        if (r < rows) *reinterpret_cast<u32x4 *>(to + r * stride + piece * 16) = x;
+    }
+}
+
+// Gradient of the queries, and delta.
+template <int D>
+__global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(1)))
+void latent_replay_dq_kernel(LatentReplayArgs a)
+{
+    using Tile = KeyTile<D>;
+    constexpr int E = D / 2, KC = D / 16, RC = E / 16, DT = D / 32, ET = E / 32;
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
+    const int li = lane & 31, half = lane >> 5;
+    const LatentReplayPlace at(a, (a.T + LR_BLOCK - 1) / LR_BLOCK, true);
+    const int n = at.length(a), i0 = at.block * LR_BLOCK;
+    if (i0 >= n) return;
+    const int wave0 = i0 + wv * LR_OWN, qpos = wave0 + li, q_row = qpos < n ? qpos : n - 1;
+    const int wave_last = wave0 + LR_OWN - 1 < n ? wave0 + LR_OWN - 1 : n - 1, block_last = i0 + LR_BLOCK - 1 < n ? i0 + LR_BLOCK - 1 : n - 1;
+    const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
+    const int tiles = block_last / LR_TILE + 1;
+    const LiveTiles live(death, tiles, n, i0, block_last);
+    int t = live.next(0, tiles);
+    if (t < tiles) Tile::load(a, at.b, at.h, t, lds, wv, lane);
+
+    bf16x8 q[KC + RC], g_[KC];
+    float delta = 0.f;
+    const size_t row = ((size_t)at.b * a.T + q_row) * a.H + at.h;
+    {
+        const unsigned char *qr = a.q + row * ((D + E) * 2) + half * 16, *gr = a.dout + row * (D * 2) + half * 16, *orow = a.out + row * (D * 2) + half * 16;
+#pragma unroll
+        for (int c = 0; c < KC + RC; ++c) q[c] = operand(*reinterpret_cast<const u32x4 *>(qr + c * 32));
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(gr + c * 32), y = *reinterpret_cast<const u32x4 *>(orow + c * 32);
+            g_[c] = operand(x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                delta += __uint_as_float(x[e] << 16) * __uint_as_float(y[e] << 16) + __uint_as_float(x[e] & 0xFFFF0000u) * __uint_as_float(y[e] & 0xFFFF0000u);
+        }
+        delta = half_rows_sum(delta);
+    }
+    const size_t stat = ((size_t)at.b * a.H + at.h) * a.T + q_row;
+    if (half == 0 && qpos < n) a.delta[stat] = delta;
+    const float neg_lse = -a.lse[stat] * 1.4426950408889634f;
+    uint32_t k_at[KC], r_at[RC], v_at[KC], kt_at[DT][2], rt_at[ET][2];
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+        k_at[c] = LdsRows<Tile::KB>::row_piece(li, half, c);
+        v_at[c] = Tile::V + k_at[c];
+    }
+#pragma unroll
+    for (int c = 0; c < RC; ++c) r_at[c] = Tile::ROT + LdsRows<Tile::RB>::row_piece(li, half, c);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+#pragma unroll
+        for (int c = 0; c < DT; ++c) kt_at[c][g] = LdsRows<Tile::KB>::column(lane, g, c);
+#pragma unroll
+        for (int c = 0; c < ET; ++c) rt_at[c][g] = Tile::ROT + LdsRows<Tile::RB>::column(lane, g, c);
+    }
+    f32x16 dk[DT], dr[ET];                                 // dQ^T: of the part that meets the heads' own keys, and of the rotary part
+#pragma unroll
+    for (int c = 0; c < DT; ++c) dk[c] = zeros16();
+#pragma unroll
+    for (int c = 0; c < ET; ++c) dr[c] = zeros16();
+
+    auto step = [&](const unsigned char *tile, int st, int key0, bool whole) {
+        const bool mixed = !whole || key0 + LR_STEP - 1 > wave0 || key0 + LR_STEP > n;
+        f32x16 sc = zeros16(), dp = zeros16();
+#pragma unroll
+        for (int c = 0; c < KC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + k_at[c] + st * LR_STEP * Tile::KB)), q[c], sc);
+#pragma unroll
+        for (int c = 0; c < RC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + r_at[c] + st * LR_STEP * Tile::RB)), q[KC + c], sc);
+#pragma unroll
+        for (int c = 0; c < KC; ++c) dp = product(operand(*reinterpret_cast<const u32x4 *>(tile + v_at[c] + st * LR_STEP * Tile::KB)), g_[c], dp);
+        float ds[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ds[r] = fast_exp2(__builtin_fmaf(sc[r], a.scale_log2e, neg_lse)) * (dp[r] - delta);
+        if (mixed) {
+            const uint32_t seen = seen_keys(death, key0, n, qpos, half);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) ds[r] = (seen >> r) & 1u ? ds[r] : 0.f;
+        }
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = pack_bf16(ds[2 * e], ds[2 * e + 1]);
+        // (a key that is seen and not finite has made dS NaN)
+        (void)add_transposed<Tile::KB>(tile + st * LR_STEP * Tile::KB, w, kt_at, mixed, dk);
+        (void)add_transposed<Tile::RB>(tile + st * LR_STEP * Tile::RB, w, rt_at, mixed, dr);
+    };
+    unsigned char *here = lds, *there = lds + Tile::BYTES;
+    while (t < tiles) {
+        lds_loads_done();
+        const int next = live.next(t + 1, tiles);
+        if (next < tiles) Tile::load(a, at.b, at.h, next, there, wv, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        const bool whole = live.whole(t);
+#pragma unroll
+        for (int st = 0; st < LR_TILE / LR_STEP; ++st) {
+            const int key0 = t * LR_TILE + st * LR_STEP;
+            if (wave0 < n && key0 <= wave_last) step(here, st, key0, whole);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        unsigned char *const x = here;
+        here = there;
+        there = x;
+        t = next;
+    }
+    __syncthreads();
+    unsigned char *const mine = lds + wv * LR_OWN * D * 2;
+    unsigned char *const to = a.dq + (((size_t)at.b * a.T + wave0) * a.H + at.h) * ((D + E) * 2);
+    const size_t stride = (size_t)a.H * ((D + E) * 2);
+    store_rows(mine, dk, a.scale, to, stride, n - wave0);
+    store_rows(mine, dr, a.scale, to + D * 2, stride, n - wave0);
+}
+
+// Gradients of keys and values, and the head's of the rotary part.
+template <int D>
+__global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(1)))
+void latent_replay_dkv_kernel(LatentReplayArgs a)
+{
+    constexpr int E = D / 2, KC = D / 16, RC = E / 16, DT = D / 32, ET = E / 32, KB = D * 2, RB = E * 2;
+    // a tile of queries: their two parts, the gradients that arrive at them, and -lse (in powers of 2) and delta
+    constexpr int ROT = LR_TILE * KB, G = ROT + LR_TILE * RB, BYTES = G + LR_TILE * KB;
+    extern __shared__ __align__(16) unsigned char lds[];
+    float *const stats = reinterpret_cast<float *>(lds + 2 * BYTES);       // [2][2][LR_TILE]
+    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
+    const int li = lane & 31, half = lane >> 5;
+    const LatentReplayPlace at(a, (a.T + LR_BLOCK - 1) / LR_BLOCK, false);
+    const int n = at.length(a), j0 = at.block * LR_BLOCK;
+    if (j0 >= n) return;
+    const int wave0 = j0 + wv * LR_OWN, key = wave0 + li, k_row = key < n ? key : n - 1;
+    const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
+    // queries key .. until - 1 see this lane's key
+    int until = n;
+    if (death) {
+        const int d = death[k_row];
+        until = d < n ? d : n;
+    }
+    if (key >= n) until = 0;
+    auto larger = [](int x, int y) { return x > y ? x : y; };
+    auto smaller = [](int x, int y) { return x < y ? x : y; };
+    const int wave_end = __builtin_amdgcn_readfirstlane(wave_reduce(until, larger));
+    // all of the wave's keys are seen by queries below this one, where causality lets them
+    const int wave_all = __builtin_amdgcn_readfirstlane(wave_reduce(until, smaller));
+    __shared__ int ends[LR_WAVES];
+    if (lane == 0) ends[wv] = wave_end;
+
+    bf16x8 k[KC + RC], v[KC];
+    {
+        const unsigned char *kr = a.kv + (((size_t)at.b * a.T + k_row) * a.H + at.h) * (2 * KB) + half * 16;
+        const unsigned char *rr = a.rope + ((size_t)at.b * a.T + k_row) * a.rope_row + half * 16;
+#pragma unroll
+        for (int c = 0; c < KC; ++c) k[c] = operand(*reinterpret_cast<const u32x4 *>(kr + c * 32));
+#pragma unroll
+        for (int c = 0; c < RC; ++c) k[KC + c] = operand(*reinterpret_cast<const u32x4 *>(rr + c * 32));
+#pragma unroll
+        for (int c = 0; c < KC; ++c) v[c] = operand(*reinterpret_cast<const u32x4 *>(kr + KB + c * 32));
+    }
+    __syncthreads();
+    int end = 0;
+#pragma unroll
+    for (int w = 0; w < LR_WAVES; ++w) end = larger(end, ends[w]);
+    end = __builtin_amdgcn_readfirstlane(end);
+    const int first = j0 / LR_TILE, tiles = (end + LR_TILE - 1) / LR_TILE;
+
+    const size_t stat = ((size_t)at.b * a.H + at.h) * a.T;
+    auto load_tile = [&](int t, unsigned char *to) {
+        const int i = t * LR_TILE, last = a.T - 1 - i;
+        const size_t row = ((size_t)at.b * a.T + i) * a.H + at.h;
+        const uint32_t stride = (uint32_t)a.H * ((D + E) * 2);
+        LdsRows<KB>::load(a.q + row * ((D + E) * 2), stride, last, to, wv, lane);
+        LdsRows<RB>::load(a.q + row * ((D + E) * 2) + KB, stride, last, to + ROT, wv, lane);
+        LdsRows<KB>::load(a.dout + row * KB, (uint32_t)a.H * KB, last, to + G, wv, lane);
+    };
+    auto load_stat = [&](int t) {                          // threads 0 .. 63: lse, the next 64: delta
+        const int i = t * LR_TILE + ((int)threadIdx.x & (LR_TILE - 1));
+        return threadIdx.x < 2 * LR_TILE ? (threadIdx.x < LR_TILE ? a.lse : a.delta)[stat + (i < n ? i : n - 1)] : 0.f;
+    };
+    uint32_t q_at[KC], r_at[RC], g_at[KC], qt_at[DT][2], rt_at[ET][2], gt_at[DT][2];
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+        q_at[c] = LdsRows<KB>::row_piece(li, half, c);
+        g_at[c] = G + q_at[c];
+    }
+#pragma unroll
+    for (int c = 0; c < RC; ++c) r_at[c] = ROT + LdsRows<RB>::row_piece(li, half, c);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+#pragma unroll
+        for (int c = 0; c < DT; ++c) {
+            qt_at[c][g] = LdsRows<KB>::column(lane, g, c);
+            gt_at[c][g] = G + qt_at[c][g];
+        }
+#pragma unroll
+        for (int c = 0; c < ET; ++c) rt_at[c][g] = ROT + LdsRows<RB>::column(lane, g, c);
+    }
+    f32x16 dv[DT], dk[DT], dr[ET];
+#pragma unroll
+    for (int c = 0; c < DT; ++c) dv[c] = dk[c] = zeros16();
+#pragma unroll
+    for (int c = 0; c < ET; ++c) dr[c] = zeros16();
+    float poison = 0.f;                                    // NaN: a gradient that is not finite arrives at a query that sees the key
+
+    auto step = [&](const unsigned char *tile, const float *st_, int st, int query0) {
+        const bool mixed = query0 < wave0 + LR_OWN - 1 || query0 + LR_STEP > wave_all;
+        f32x16 sc = zeros16(), dp = zeros16();
+#pragma unroll
+        for (int c = 0; c < KC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + q_at[c] + st * LR_STEP * KB)), k[c], sc);
+#pragma unroll
+        for (int c = 0; c < RC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + r_at[c] + st * LR_STEP * RB)), k[KC + c], sc);
+#pragma unroll
+        for (int c = 0; c < KC; ++c) dp = product(operand(*reinterpret_cast<const u32x4 *>(tile + g_at[c] + st * LR_STEP * KB)), v[c], dp);
+        float p[16], ds[16];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 neg_lse = *reinterpret_cast<const f32x4 *>(st_ + st * LR_STEP + 8 * g + 4 * half);
+            const f32x4 delta = *reinterpret_cast<const f32x4 *>(st_ + LR_TILE + st * LR_STEP + 8 * g + 4 * half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                p[4 * g + e] = fast_exp2(__builtin_fmaf(sc[4 * g + e], a.scale_log2e, neg_lse[e]));
+                ds[4 * g + e] = p[4 * g + e] * (dp[4 * g + e] - delta[e]);
+            }
+        }
+        uint32_t seen = 0xFFFFu;
+        if (mixed) {
+            seen = 0;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int i = query0 + row_of(r, half);
+                const bool sees = key <= i && i < until;
+                p[r] = sees ? p[r] : 0.f;
+                ds[r] = sees ? ds[r] : 0.f;
+                seen |= (uint32_t)sees << r;
+            }
+        }
+        uint32_t wp[8], ws[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            wp[e] = pack_bf16(p[2 * e], p[2 * e + 1]);
+            ws[e] = pack_bf16(ds[2 * e], ds[2 * e + 1]);
+        }
+        const bool odd = add_transposed<KB>(tile + st * LR_STEP * KB, wp, gt_at, mixed, dv);
+        // (a query that sees the key and is not finite has made dS NaN)
+        (void)add_transposed<KB>(tile + st * LR_STEP * KB, ws, qt_at, mixed, dk);
+        (void)add_transposed<RB>(tile + st * LR_STEP * RB, ws, rt_at, mixed, dr);
+        if (__ballot(odd)) {
+            const uint32_t rows = odd_rows<KB>(tile + G + st * LR_STEP * KB);
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (((rows >> row_of(r, half)) & 1u) && ((seen >> r) & 1u)) poison = NAN;
+        }
+    };
+    float stat_next = 0.f;
+    if (first < tiles) {
+        load_tile(first, lds);
+        stat_next = load_stat(first);
+    }
+    for (int t = first; t < tiles; ++t) {
+        const int cur = (t - first) & 1;
+        unsigned char *const here = lds + cur * BYTES;
+        if (threadIdx.x < 2 * LR_TILE) stats[cur * 2 * LR_TILE + threadIdx.x] = threadIdx.x < LR_TILE ? -stat_next * 1.4426950408889634f : stat_next;
+        lds_loads_done();
+        if (t + 1 < tiles) {
+            load_tile(t + 1, lds + (cur ^ 1) * BYTES);
+            stat_next = load_stat(t + 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int st = 0; st < LR_TILE / LR_STEP; ++st) {
+            const int query0 = t * LR_TILE + st * LR_STEP;
+            if (query0 + LR_STEP > wave0 && query0 < wave_end) step(here, stats + cur * 2 * LR_TILE, st, query0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();
+    poison += __shfl_xor(poison, 32);                      // (NaN in either half of the key's registers)
+#pragma unroll
+    for (int c = 0; c < DT; ++c) dv[c] += poison;
+    unsigned char *const mine = lds + wv * LR_OWN * KB;
+    const size_t stride = (size_t)a.H * (2 * KB);
+    unsigned char *const to = a.dkv + (((size_t)at.b * a.T + wave0) * a.H + at.h) * (2 * KB);
+    store_rows(mine, dk, a.scale, to, stride, n - wave0);
+    store_rows(mine, dv, 1.0f, to + KB, stride, n - wave0);
+    if (key < n) {
+        float *part = a.part + (stat + key) * E;
+#pragma unroll
+        for (int c = 0; c < ET; ++c)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4 *>(part + 32 * c + 8 * g + 4 * half) =
+                    f32x4{dr[c][4 * g] * a.scale, dr[c][4 * g + 1] * a.scale, dr[c][4 * g + 2] * a.scale, dr[c][4 * g + 3] * a.scale};
+    }
+}
+
+// The heads' gradients of the rotary part, added in their order: four values a thread.
+template <int E>
+__global__ __launch_bounds__(256) void latent_replay_rope_kernel(LatentReplayArgs a)
+{
+    constexpr int QUADS = E / 4;
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long pos = i / QUADS;
+    if (pos >= (long long)a.B * a.T) return;
+    const int b = (int)(pos / a.T), t = (int)(pos % a.T), col = (int)(i % QUADS) * 4;
+    int n = a.n ? a.n[b] : a.T;
+    if (t >= n) return;
+    const float *part = a.part + ((size_t)b * a.H * a.T + t) * E + col;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int h = 0; h < a.H; ++h) sum += *reinterpret_cast<const f32x4 *>(part + (size_t)h * a.T * E);
+    *reinterpret_cast<u32x2 *>(a.drope + (pos * E + col) * 2) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
+}
+
+}  // namespace ngc
+
+// ============================================================ host side ====
+
+using namespace ngc;
+
+namespace {
+
+bool latent_replay_sizes(int32_t B, int32_t T, int32_t Hq, int32_t D) { return B > 0 && T > 0 && Hq > 0 && (D == 64 || D == 128); }
+
+int check_latent_replay(const void *q, const void *kv, const void *rope, int64_t rope_stride, int32_t B, int32_t T, int32_t Hq, int32_t D,
+                        float scale, const void *out)
+{
+    if (!q || !kv || !rope || !out || !aligned16(q) || !aligned16(kv) || !aligned16(rope) || !aligned16(out)) return NGC_EINVAL;
+    if (!latent_replay_sizes(B, T, Hq, D) || rope_stride < D / 2 || rope_stride % 8 != 0) return NGC_EINVAL;
+    if (!(scale > 0.f) || !(scale <= 2.35e38f)) return NGC_EINVAL;
+    if (Hq > LATENT_MOST_HEADS || T > LR_MOST_POSITIONS || rope_stride > 1 << 20) return NGC_EUNSUPPORTED;
+    if ((long long)((T + LR_BLOCK - 1) / LR_BLOCK) * B * Hq > 0x7FFFFFFFLL) return NGC_EUNSUPPORTED;
+    return NGC_OK;
+}
+
+LatentReplayArgs latent_replay_args(const void *q, const void *kv, const void *rope, int64_t rope_stride, const int32_t *death, const int32_t *n,
+                                    int32_t B, int32_t T, int32_t Hq, float scale)
+{
+    LatentReplayArgs a{};
+    a.q = reinterpret_cast<const unsigned char *>(q);
+    a.kv = reinterpret_cast<const unsigned char *>(kv);
+    a.rope = reinterpret_cast<const unsigned char *>(rope);
+    a.death = death; a.n = n;
+    a.rope_row = (size_t)rope_stride * 2;
+    a.B = B; a.T = T; a.H = Hq;
+    a.scale = scale;
+    a.scale_log2e = scale * 1.4426950408889634f;
+    return a;
+}
+
+size_t latent_replay_delta_bytes(int32_t B, int32_t T, int32_t Hq) { return align256((size_t)B * Hq * T * sizeof(float)); }
+
+int launch_blocks(const void *fn, const LatentReplayArgs &args, size_t lds, hipStream_t st)
+{
+    LatentReplayArgs a = args;
+    if (lds > 64 * 1024) NGC_HIP_CHECK(hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    return launch(fn, dim3((unsigned)((a.T + LR_BLOCK - 1) / LR_BLOCK * a.B * a.H)), dim3(LR_WAVES * 64), lds, st, a);
+}
+
+}  // namespace
+
+extern "C" size_t ngc_latent_replay_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t D)
+{
+    if (!latent_replay_sizes(B, T, Hq, D)) return 0;
+    return latent_replay_delta_bytes(B, T, Hq) + (size_t)B * Hq * T * (D / 2) * sizeof(float);
+}
+
+extern "C" int ngc_latent_replay_attn(const void *q, const void *kv, const void *rope, int64_t rope_stride, const int32_t *death,
+                                      const int32_t *n, int32_t B, int32_t T, int32_t Hq, int32_t D, float scale, void *out,
+                                      float *lse_out, void *stream)
+{
+    const int rc = check_latent_replay(q, kv, rope, rope_stride, B, T, Hq, D, scale, out);
+    if (rc) return rc;
+    LatentReplayArgs a = latent_replay_args(q, kv, rope, rope_stride, death, n, B, T, Hq, scale);
+    a.out = reinterpret_cast<unsigned char *>(out);
+    a.lse = lse_out;
+    const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_kernel<64>);
+    return launch_blocks(fn, a, 2 * (D == 128 ? KeyTile<128>::BYTES : KeyTile<64>::BYTES), (hipStream_t)stream);
+}
+
+extern "C" int ngc_latent_replay_attn_backward(const void *q, const void *kv, const void *rope, int64_t rope_stride, const int32_t *death,
+                                               const int32_t *n, const void *out, const float *lse, const void *dout, int32_t B,
+                                               int32_t T, int32_t Hq, int32_t D, float scale, void *dq, void *dkv, void *drope, void *ws,
+                                               size_t ws_bytes, void *stream)
+{
+    int rc = check_latent_replay(q, kv, rope, rope_stride, B, T, Hq, D, scale, out);
+    if (rc) return rc;
+    if (!lse || !dout || !dq || !dkv || !drope || !ws) return NGC_EINVAL;
+    if (!aligned16(dout) || !aligned16(dq) || !aligned16(dkv) || !aligned16(drope) || !aligned16(ws)) return NGC_EINVAL;
+    if (ws_bytes < ngc_latent_replay_workspace_bytes(B, T, Hq, D)) return NGC_ENOSPC;
+    LatentReplayArgs a = latent_replay_args(q, kv, rope, rope_stride, death, n, B, T, Hq, scale);
+    a.out = reinterpret_cast<unsigned char *>(const_cast<void *>(out));    // (only read)
+    a.lse = const_cast<float *>(lse);
+    a.dout = reinterpret_cast<const unsigned char *>(dout);
+    a.dq = reinterpret_cast<unsigned char *>(dq);
+    a.dkv = reinterpret_cast<unsigned char *>(dkv);
+    a.drope = reinterpret_cast<unsigned char *>(drope);
+    a.delta = reinterpret_cast<float *>(ws);
+    a.part = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(ws) + latent_replay_delta_bytes(B, T, Hq));
+    hipStream_t st = (hipStream_t)stream;
+    const size_t lds = 2 * (D == 128 ? KeyTile<128>::BYTES : KeyTile<64>::BYTES);
+    rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dq_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dq_kernel<64>), a, lds, st);
+    if (rc) return rc;
+    rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dkv_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dkv_kernel<64>), a,
+                       lds + 4 * LR_TILE * sizeof(float), st);
+    if (rc) return rc;
+    const long long threads = (long long)B * T * (D / 2 / 4);
+    const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_rope_kernel<64>) : reinterpret_cast<const void *>(&latent_replay_rope_kernel<32>);
+    return launch(fn, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, a);
+}

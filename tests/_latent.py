@@ -77,3 +77,51 @@ def attention(rows, q, limits, scale, R):
     tol_out = magnitude * (2.0 ** -8 + slack.unsqueeze(1)) * (1 + 2.0 ** -8) + 2.0 ** -8 * out.abs()
     tol_lse = delta + (n + 64) * 2.0 ** -24 + 2.0 ** -22 * z.abs() + 2.0 ** -21
     return out, lse, tol_out, tol_lse
+
+
+# ------------------------------------------------------------------ replay ---
+
+def replay(q, kv, rope, death, n, scale, dout=None):
+    """One trajectory, all heads, float64 tensors: q [T, H, D + E], kv [T, H, 2 D], rope [T, E], death [T] or None, n positions.
+
+    -> dict of values, and of bounds of the kernels' errors.  The kernels round P and dS to bf16 for their products, and every
+    result: half a step, 2^-8, each.  The scores' products are exact and their sums in 32 bits, so an exponent is off by at
+    most `eps_x`, and so is lse; out enters delta rounded to bf16."""
+    import torch
+    T, H, DE = q.shape
+    D = kv.shape[2] // 2
+    at = torch.arange(n, device=q.device)
+    hidden = at.unsqueeze(0) > at.unsqueeze(1)
+    if death is not None:
+        hidden = hidden | (at.unsqueeze(1) >= death[:n].unsqueeze(0))
+    empty = hidden.all(1)
+    k = torch.cat([kv[:n, :, :D], rope[:n].unsqueeze(1).expand(n, H, DE - D)], -1).transpose(0, 1).contiguous()
+    v, qq = kv[:n, :, D:].transpose(0, 1).contiguous(), q[:n].transpose(0, 1).contiguous()
+    x = (qq @ k.transpose(1, 2).contiguous() * scale).masked_fill(hidden, -math.inf)
+    half, f32 = 2.0 ** -8, 2.0 ** -23
+    eps_x = (qq.abs() @ k.abs().transpose(1, 2).contiguous()).amax(-1, keepdim=True) * scale * (DE + 4) * 2.0 ** -24 * 2 + (n + 64) * f32
+    z = torch.logsumexp(x, -1, keepdim=True)
+    p = torch.exp(x - torch.where(empty.view(1, n, 1), torch.zeros_like(z), z))
+    out, mag = p @ v, p @ v.abs()
+    slack = 2 * torch.expm1(eps_x)
+    r = dict(out=out, lse=z[..., 0], tol_out=mag * (half + slack) * (1 + half) + half * out.abs(),
+             tol_lse=eps_x[..., 0] + (z[..., 0].abs() * 2.0 ** -22).nan_to_num(posinf=0.0) + 2.0 ** -21, empty=empty)
+    if dout is None:
+        return r
+    g = dout[:n].transpose(0, 1).contiguous()
+    t = lambda a: a.transpose(1, 2).contiguous()      # noqa: E731
+    dp, dp_mag = g @ t(v), g.abs() @ t(v.abs())
+    delta = (g * out).sum(-1, keepdim=True)
+    e_delta = (g.abs() * r["tol_out"]).sum(-1, keepdim=True) + (g * out).abs().sum(-1, keepdim=True) * (D + 2) * f32
+    ds = p * (dp - delta)
+    e_p = p * (slack + half)
+    e_ds = p * (dp_mag * (D + 2) * f32 + e_delta) + (dp - delta).abs() * p * slack * 2 + half * ds.abs() * (1 + half)
+    dv = t(p) @ g
+    dq, dk = ds @ k * scale, t(ds) @ qq * scale
+    acc = (n + 64) * f32                              # the long sums' own steps
+    r.update(dv=dv, tol_dv=(t(e_p) @ g.abs() + acc * (t(p) @ g.abs())) * (1 + half) + half * dv.abs(),
+             dq=dq, tol_dq=(e_ds @ k.abs() + acc * (ds.abs() @ k.abs())) * scale * (1 + half) + half * dq.abs())
+    e_k = (t(e_ds) @ qq.abs() + acc * (t(ds.abs()) @ qq.abs())) * scale * (1 + half)
+    drope = dk[..., D:].sum(0)
+    r.update(dk=dk[..., :D], tol_dk=(e_k + half * dk.abs())[..., :D], drope=drope, tol_drope=e_k[..., D:].sum(0) * (1 + H * f32) + half * drope.abs())
+    return r

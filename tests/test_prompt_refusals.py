@@ -99,3 +99,25 @@ def test_calls_that_move_or_read_two_pools_refuse_one(lib):
     assert lib.ngc_paged_fork(p, -1, A, A, WS, None) == EINVAL
     assert lib.ngc_paged_compact(p, A, WS, None) == EINVAL
     assert lib.ngc_paged_free(p, -1, A, A, 16, None) == ENOSPC       # takes either kind
+
+
+def test_replay_arguments(lib):
+    def forward(q=A, kv=A, rope=A, stride=64, B=2, T=100, H=4, D=128, scale=0.1, out=A):
+        return lib.ngc_latent_replay_attn(q, kv, rope, stride, None, None, B, T, H, D, scale, out, None, None)
+
+    def backward(q=A, kv=A, rope=A, stride=64, B=2, T=100, H=4, D=128, scale=0.1, out=A, lse=A, dout=A, dq=A, dkv=A, drope=A, ws=A, ws_bytes=16):
+        return lib.ngc_latent_replay_attn_backward(q, kv, rope, stride, None, None, out, lse, dout, B, T, H, D, scale, dq, dkv, drope, ws,
+                                                   ws_bytes, None)
+    assert backward() == ENOSPC
+    shared = [dict(q=None), dict(q=A + 8), dict(kv=None), dict(kv=A + 2), dict(rope=None), dict(rope=A + 8), dict(out=None), dict(out=A + 8),
+              dict(stride=56), dict(stride=68), dict(stride=0), dict(B=0), dict(T=0), dict(H=0), dict(D=96), dict(D=0), dict(scale=0.0),
+              dict(scale=-0.1), dict(scale=float("nan")), dict(scale=float("inf"))]
+    for bad in shared:
+        assert forward(**bad) == EINVAL and backward(**bad) == EINVAL, bad
+    for bad in (dict(lse=None), dict(dout=None), dict(dout=A + 8), dict(dq=None), dict(dq=A + 4), dict(dkv=None), dict(dkv=A + 8), dict(drope=None),
+                dict(drope=A + 8), dict(ws=None), dict(ws=A + 8)):
+        assert backward(**bad) == EINVAL, bad
+    for bad in (dict(H=129), dict(T=131073), dict(stride=1 << 21), dict(B=2 ** 31 - 1, T=131072)):
+        assert forward(**bad) == EUNSUPPORTED and backward(**bad) == EUNSUPPORTED, bad
+    assert lib.ngc_latent_replay_workspace_bytes(2, 100, 4, 96) == 0
+    assert lib.ngc_latent_replay_workspace_bytes(2, 100, 4, 128) >= 2 * 100 * 4 * (64 + 1) * 4
