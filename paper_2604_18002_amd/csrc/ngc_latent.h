@@ -13,6 +13,20 @@ __device__ __forceinline__ int32_t constant_word(const int32_t *p)
     return *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>((uintptr_t)p);
 }
 
+// 16-byte piece p of row r of a tile in LDS stands at slot p ^ lds_swizzle<PIECES>(r) of its row.  LDS has 64 banks, and what reads
+// together is (measured: pairs of lanes of one bank, one of them after the other)
+//   reads of 16 bytes           lanes 0-3, 12-15, 20-23, 24-27, the other 16 of the lower half, and the same of the upper half;
+//   transposing reads of 8      the lower half and the upper half.
+// With row = lane % 32 and piece p, or row = lane % 16 and piece p + lane / 16, the first meet every bank once; so do the second
+// with 4 rows of 64 bytes (32 columns) or 8 rows of 32 bytes (16 columns) a half.  Written with r = r3 r2 r1 r0: rows of 256 bytes
+// and multiples r1 r0 (r2^r3) r3, of 128 bytes without r0, of 64 without r1 r0, which count the rows of a line of banks there.
+template <int PIECES>
+__device__ __forceinline__ int lds_swizzle(int r)
+{
+    const int low = ((r >> 2) ^ (r >> 3)) % 2 * 2 + (r >> 3) % 2;
+    return PIECES >= 16 ? r % 4 * 4 + low : PIECES == 8 ? (r >> 1) % 2 * 4 + low : low;
+}
+
 // A value that is not finite would reach rows that do not see it, through a product with a weight of 0.  Where some of a tile's
 // pairs are masked such values become 0 in the operand (this: four of them; whether there was one), and are added by
 // themselves to the rows that see them.

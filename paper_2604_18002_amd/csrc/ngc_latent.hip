@@ -73,9 +73,8 @@ struct LatentSegment {
     }
 };
 
-// Where things are in a tile of 32 rows in LDS: the latent parts, 16-byte piece p of row r at slot p ^ (its 4 low bits)
-// swizzle(r), then the rotary parts.  Eight consecutive rows have one piece in eight places, and 32 bytes of 16 consecutive
-// rows (64 of 8) are spread evenly over the banks, so both products read without conflicts.
+// Where things are in a tile of 32 rows in LDS: the latent parts, 16-byte piece p of row r at slot p ^ swizzle(r), then the rotary
+// parts.
 template <int R, int E>
 struct LatentTile {
     static constexpr int ROW = (R + E) * 2, LAT = R * 2, ROT = E * 2;
@@ -85,8 +84,8 @@ struct LatentTile {
     static constexpr int LAT_LOADS = LT_KEYS / LAT_ROWS, ROT_LOADS = LT_KEYS / ROT_ROWS;
     static_assert(LAT_PIECES == 64 || LAT_PIECES == 32, "whole rows a load");
     static_assert(ROT_PIECES == 8 || ROT_PIECES == 4, "whole rows a load");
-    __device__ static __forceinline__ int swizzle(int r) { return ((2 * r) & 15) | ((r >> 3) & 1); }
-    __device__ static __forceinline__ int rot_swizzle(int r) { return ROT_PIECES == 8 ? r & 7 : (r >> 1) & 3; }
+    __device__ static __forceinline__ int swizzle(int r) { return lds_swizzle<LAT_PIECES>(r); }
+    __device__ static __forceinline__ int rot_swizzle(int r) { return lds_swizzle<ROT_PIECES>(r); }
     __device__ static __forceinline__ uint32_t piece(int r, int p)
     {
         if (p < LAT_PIECES) return (uint32_t)(r * LAT + (p ^ swizzle(r)) * 16);
@@ -183,7 +182,7 @@ void latent_attn_kernel(LatentArgs a)
     constexpr int HALVES = LT_WAVES * RT * R * 4 > SLOTS * Tile::BYTES ? 2 : 1;          // the output goes through LDS in so many parts
     static_assert(LT_WAVES * RT * R * 4 / HALVES <= SLOTS * Tile::BYTES, "a part of the output fits");
 
-    extern __shared__ __align__(16) unsigned char lds[];
+    extern __shared__ __align__(256) unsigned char lds[];
     float *const red = reinterpret_cast<float *>(lds + SLOTS * Tile::BYTES);             // [2][waves][RT]
 
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
@@ -229,18 +228,22 @@ void latent_attn_kernel(LatentArgs a)
     unsigned char *const buffers = lds + kg * NB * Tile::BYTES;
     auto load_tile = [&](int t, unsigned char *to) {
         const unsigned char *base = tile_base(t);
-        const int lrow = lane / Tile::LAT_PIECES, lp = lane % Tile::LAT_PIECES;
+        int lane_ = lane;
+        __asm__ volatile("" : "+v"(lane_));                // (offsets are made where they are used, not kept over the loop)
+        // the swizzle is linear in a row's bits: a lane's part of it, and the load's
+        const int lrow = Tile::LAT_ROWS == 1 ? 0 : lane_ / Tile::LAT_PIECES, lp = lane_ % Tile::LAT_PIECES ^ Tile::swizzle(lrow);
+        const uint32_t lat = (uint32_t)(lrow * Tile::ROW);
 #pragma unroll
         for (int i = 0; i < LAT_LOADS; ++i) {
             const int r0 = (i * RG + rg) * Tile::LAT_ROWS;
-            load_to_lds16(base + (uint32_t)((r0 + lrow) * Tile::ROW + (lp ^ Tile::swizzle(r0 + lrow)) * 16), to + r0 * Tile::LAT);
+            load_to_lds16(base + r0 * Tile::ROW + (lat + (uint32_t)(lp ^ Tile::swizzle(r0)) * 16), to + r0 * Tile::LAT);
         }
-        const int rrow = lane / Tile::ROT_PIECES, rp = lane % Tile::ROT_PIECES;
+        const int rrow = lane_ / Tile::ROT_PIECES, rp = lane_ % Tile::ROT_PIECES ^ Tile::rot_swizzle(rrow);
+        const uint32_t rot = (uint32_t)(rrow * Tile::ROW);
 #pragma unroll
         for (int i = 0; i < ROT_LOADS; ++i) {
             const int r0 = (i * RG + rg) % Tile::ROT_LOADS * Tile::ROT_ROWS;             // (what is left over loads a part again)
-            load_to_lds16(base + (uint32_t)((r0 + rrow) * Tile::ROW + Tile::LAT + (rp ^ Tile::rot_swizzle(r0 + rrow)) * 16),
-                          to + Tile::LAT_BYTES + r0 * Tile::ROT);
+            load_to_lds16(base + r0 * Tile::ROW + Tile::LAT + (rot + (uint32_t)(rp ^ Tile::rot_swizzle(r0)) * 16), to + Tile::LAT_BYTES + r0 * Tile::ROT);
         }
     };
 
@@ -251,35 +254,30 @@ void latent_attn_kernel(LatentArgs a)
         for (int e = 0; e < Math::QUADS * 4; ++e) oacc[c][e] = 0.f;
     float m_run = -INFINITY, m_ref = 0.f, l_run = 0.f;     // m_ref: m_run, or 0 as long as nothing has been seen
 
-    // Where this lane's operands are in a tile: pieces 16 apart are 256 bytes apart whatever the swizzle, rows 16 apart have the same one.
-    constexpr int PIECES_A_CHUNK = Math::CHUNK / 8, LAT_VARIANTS = 16 / PIECES_A_CHUNK, ROT_VARIANTS = Tile::ROT_PIECES / PIECES_A_CHUNK;
-    constexpr int LAT_CHUNKS = R / Math::CHUNK;
-    uint32_t lat_off[LAT_VARIANTS], rot_off[ROT_VARIANTS];
-#pragma unroll
-    for (int c = 0; c < LAT_VARIANTS; ++c) lat_off[c] = Tile::piece(row, c * PIECES_A_CHUNK + part);
-#pragma unroll
-    for (int c = 0; c < ROT_VARIANTS; ++c) rot_off[c] = Tile::piece(row, Tile::LAT_PIECES + c * PIECES_A_CHUNK + part);
-    auto row_piece = [&](const unsigned char *tile, int c, int k) {        // of key tile k
-        const uint32_t at = c < LAT_CHUNKS ? lat_off[c % LAT_VARIANTS] + (uint32_t)(c / LAT_VARIANTS * 256 + k * Math::KEYS * Tile::LAT)
-                                           : rot_off[(c - LAT_CHUNKS) % ROT_VARIANTS] + (uint32_t)(k * Math::KEYS * Tile::ROT);
-        return *reinterpret_cast<const u32x4 *>(tile + at);
-    };
-    constexpr int COL_VARIANTS = 128 / Math::COLS, ROW_VARIANTS = RT == 32 ? 2 : 1;      // (rows 8 apart differ by one bit of the swizzle)
-    uint32_t col_off[COL_VARIANTS][ROW_VARIANTS];
-#pragma unroll
-    for (int c = 0; c < COL_VARIANTS; ++c)
-#pragma unroll
-        for (int g = 0; g < ROW_VARIANTS; ++g) {
-            const int r = Math::read_row(lane) + 8 * g, col = Math::read_col(lane) + Math::COLS * c;
-            col_off[c][g] = Tile::piece(r, col / 8) + (uint32_t)(col % 8) * 2;
-        }
-    // keys 16 st + 8 g .. (of 32 query rows), 16 g .. (of 16), of column tile c
-    auto transposed = [&](const unsigned char *tile, int st, int g, int c) {
-        const uint32_t at = col_off[c % COL_VARIANTS][RT == 32 ? g : 0] + (uint32_t)(c / COL_VARIANTS * 256 + (RT == 32 ? st : g) * 16 * Tile::LAT);
-        return read_transposed16(tile + at);
-    };
+    // Where this lane's operands are in a tile.  Pieces 16 apart are 256 bytes apart whatever the swizzle, rows 16 apart have the same one,
+    // those of rows 8 apart differ by 3, and a tile begins at a multiple of 256: the other offsets differ from the first one's by bits.
+    constexpr int PIECES_A_CHUNK = Math::CHUNK / 8, LAT_CHUNKS = R / Math::CHUNK, LAT_VARIANTS = 16 / PIECES_A_CHUNK;
+    constexpr int COL_VARIANTS = 128 / Math::COLS;
+    static_assert(Tile::BYTES % 256 == 0 && Tile::LAT % 256 == 0, "offsets differ by bits");
+    const uint32_t lat0 = Tile::piece(row, part), rot0 = Tile::piece(row, Tile::LAT_PIECES + part);
+    const uint32_t col0 = Tile::piece(Math::read_row(lane), Math::read_col(lane) / 8) + (uint32_t)(Math::read_col(lane) % 8) * 2;
 
     auto compute_tile = [&](int t, const unsigned char *tile) {
+        uint32_t at_lat = lat0, at_rot = rot0, at_col = col0;
+        __asm__ volatile("" : "+v"(at_lat), "+v"(at_rot), "+v"(at_col));
+        const unsigned char __attribute__((address_space(3))) *const tile3 = (const unsigned char __attribute__((address_space(3))) *)tile;
+        const uint32_t tile_at = (uint32_t)(uintptr_t)tile3;
+        auto row_piece = [&](int c, int k) {               // chunk c of the rows of key tile k
+            const uint32_t at = c < LAT_CHUNKS ? ((tile_at + at_lat) ^ (uint32_t)(c % LAT_VARIANTS * PIECES_A_CHUNK * 16)) + (uint32_t)(c / LAT_VARIANTS * 256 + k * Math::KEYS * Tile::LAT)
+                                               : ((tile_at + at_rot) ^ (uint32_t)((c - LAT_CHUNKS) * PIECES_A_CHUNK * 16)) + (uint32_t)(k * Math::KEYS * Tile::ROT);
+            return *(const u32x4 __attribute__((address_space(3))) *)(uintptr_t)at;
+        };
+        // keys 16 st + 8 g .. (of 32 query rows), 16 g .. (of 16), of column tile c
+        auto transposed = [&](int st, int g, int c) {
+            const uint32_t at = ((tile_at + at_col) ^ (uint32_t)(c % COL_VARIANTS * Math::COLS * 2 ^ (RT == 32 ? g * 48 : 0))) +
+                                (uint32_t)(c / COL_VARIANTS * 256 + (RT == 32 ? st * 16 + g * 8 : g * 16) * Tile::LAT);
+            return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)at));
+        };
         const int key0 = t * LT_KEYS;
         const bool edge = key0 + LT_KEYS > all;            // not every query row of the workgroup sees all of the tile's rows
         typename Math::Acc sc[KTILES];
@@ -295,7 +293,7 @@ void latent_attn_kernel(LatentArgs a)
 #pragma unroll
             for (int u = 0; u < GROUP; ++u)
 #pragma unroll
-                for (int k = 0; k < KTILES; ++k) to[u][k] = row_piece(tile, g0 + u, k);
+                for (int k = 0; k < KTILES; ++k) to[u][k] = row_piece(g0 + u, k);
         };
         ask_rows(0, x[0]);
 #pragma unroll
@@ -317,7 +315,7 @@ void latent_attn_kernel(LatentArgs a)
 #pragma unroll
                 for (int st = 0; st < Math::STEPS; ++st)
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) to[u][st][g] = transposed(tile, st, g, c0 + u);
+                    for (int g = 0; g < 2; ++g) to[u][st][g] = transposed(st, g, c0 + u);
         };
         ask_columns(0, v[0]);
         __builtin_amdgcn_sched_barrier(0);
@@ -334,10 +332,11 @@ void latent_attn_kernel(LatentArgs a)
         tmx = Math::top(tmx);
         const bool outgrown = (tmx - m_run) * a.scale_log2e > LT_LAZY;     // of each row by itself: its results do not depend on its neighbours'
         if (__ballot(outgrown)) {
+            const bool some = __ballot(m_run > -INFINITY) != 0;       // (nothing to scale on the first tile)
             const float m_new = outgrown ? tmx : m_run;
             const float alpha = m_new == m_run ? 1.0f : fast_exp2((m_run - m_new) * a.scale_log2e);
             l_run *= alpha;
-            scale_all(oacc, alpha);
+            if (some) scale_all(oacc, alpha);
             m_run = m_new;
             m_ref = m_new == -INFINITY ? 0.f : m_new;
         }
@@ -482,30 +481,54 @@ void latent_attn_kernel(LatentArgs a)
     }
 }
 
-// Partials of a query row joined: R / 4 threads a row.
-constexpr int JOIN_THREADS = 128;
+// Partials of a query row joined, a workgroup (two for R = 256 in one) a row: R / 4 threads.  The shares of all partials first, then the
+// partials, JOIN_BATCH asked for at a time.
+constexpr int JOIN_THREADS = 128, JOIN_BATCH = 8;
+constexpr int LT_MOST_SPLITS = 128;
 template <int R>
 __global__ __launch_bounds__(JOIN_THREADS) void latent_join_kernel(LatentArgs a)
 {
     constexpr int PER_ROW = R / 4, ROWS = JOIN_THREADS / PER_ROW;
-    const int seg = (int)blockIdx.y, r = (int)blockIdx.x * ROWS + (int)threadIdx.x / PER_ROW, col = (int)threadIdx.x % PER_ROW * 4;
+    __shared__ float shares[ROWS][LT_MOST_SPLITS + JOIN_BATCH];
+    const int sub = (int)threadIdx.x / PER_ROW, lane = lane_id();
+    const int seg = (int)blockIdx.y, r = (int)blockIdx.x * ROWS + sub, col = (int)threadIdx.x % PER_ROW * 4;
     const LatentSegment s(a, seg, false);
-    if (r >= s.w * a.Hq) return;
-    const float *ml = a.part_ml + ((size_t)seg * a.S * a.M + r) * 2;
-    const float *po = a.part_o + ((size_t)seg * a.S * a.M + r) * R + col;
-    float m = -INFINITY, l = 0.f;
-    for (int i = 0; i < a.S; ++i) m = max_no_nan(m, ml[(size_t)i * a.M * 2]);
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < a.S; ++i) {
-        const float mi = ml[(size_t)i * a.M * 2], li = ml[(size_t)i * a.M * 2 + 1];
-        if (mi == -INFINITY) continue;                     // saw nothing; its partial may not have been written
-        const float w = fast_exp2((mi - m) * a.scale_log2e);
-        l += w * li;
-        o += w * *reinterpret_cast<const f32x4 *>(po + (size_t)i * a.M * R);
-    }
+    if ((int)blockIdx.x * ROWS >= s.w * a.Hq) return;
+    const bool real = r < s.w * a.Hq;
+    const int row = real ? r : 0;
+    const float *ml = a.part_ml + ((size_t)seg * a.S * a.M + row) * 2;
+    // of partials lane and 64 + lane
+    f32x2 x = {-INFINITY, 0.f}, y = {-INFINITY, 0.f};
+    if (lane < a.S) x = *reinterpret_cast<const f32x2 *>(ml + (size_t)lane * a.M * 2);
+    if (lane + 64 < a.S) y = *reinterpret_cast<const f32x2 *>(ml + (size_t)(lane + 64) * a.M * 2);
+    const float m = wave_max_f(fmaxf(x[0], y[0]));
+    const float wx = x[0] == -INFINITY ? 0.f : fast_exp2((x[0] - m) * a.scale_log2e), wy = y[0] == -INFINITY ? 0.f : fast_exp2((y[0] - m) * a.scale_log2e);
+    const float l = wave_sum_f((wx == 0.f ? 0.f : wx * x[1]) + (wy == 0.f ? 0.f : wy * y[1]));
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    const u32x2 b = {__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{o[0] * inv, o[1] * inv}, bf16x2)),
-                     __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{o[2] * inv, o[3] * inv}, bf16x2))};
+    if (col / 4 < 64) {                                    // a row's first wave
+        shares[sub][lane] = wx * inv;
+        shares[sub][lane + 64] = wy * inv;
+        if (lane < JOIN_BATCH) shares[sub][LT_MOST_SPLITS + lane] = 0.f;
+    }
+    __syncthreads();
+    const float *po = a.part_o + ((size_t)seg * a.S * a.M + row) * R + col;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < a.S; i0 += JOIN_BATCH) {
+        f32x4 v[JOIN_BATCH];
+#pragma unroll
+        for (int u = 0; u < JOIN_BATCH; ++u) {             // (one without a share may not have been written)
+            const int i = i0 + u < a.S ? i0 + u : a.S - 1;
+            v[u] = *reinterpret_cast<const f32x4 *>(po + (size_t)i * a.M * R);
+        }
+#pragma unroll
+        for (int u = 0; u < JOIN_BATCH; ++u) {
+            const float w = i0 + u < a.S ? shares[sub][i0 + u] : 0.f;
+            if (w != 0.f) o += w * v[u];
+        }
+    }
+    if (!real) return;
+    const u32x2 b = {__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{o[0], o[1]}, bf16x2)),
+                     __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{o[2], o[3]}, bf16x2))};
     *reinterpret_cast<u32x2 *>(a.out + (((size_t)seg * a.M + r) * R + col) * 2) = b;
     if (col == 0 && a.lse_out) a.lse_out[(size_t)seg * a.M + r] = l == 0.f ? -INFINITY : m * a.scale + logf(l);
 }
@@ -532,7 +555,6 @@ LatentShape latent_shape(int M)
     return s;
 }
 
-constexpr int LT_MOST_SPLITS = 128;
 // How many workgroups share a sequence's rows.
 int latent_splits(const LatentShape &s, int nseg, int rows)
 {

@@ -20,8 +20,9 @@
 // The two backward kernels form S twice (7 products in place of 5), so that every sum has one owner: no atomics, the same
 // bits again.
 //
-// A tile of keys that is dead for all of a workgroup's queries is never loaded: pages are evicted whole, so tiles die
-// whole.  Pairs are masked one by one only in tiles on the diagonal, behind the sequence's end, or where keys die midway.
+// 32 keys that are dead for all of a workgroup's queries are never loaded: pages are evicted whole.  Tiles of keys are made of two
+// such units that live, wherever they are.  Pairs are masked one by one only on the diagonal, behind the sequence's end, or
+// where keys die midway.
 //
 // P and dS are rounded to bf16 (2^-8 of an entry at most) for their second products, as outputs and gradients are; sums,
 // maxima, lse and delta are fp32.
@@ -41,7 +42,7 @@ constexpr int LR_OWN = 32;                   // queries (keys) of a wave
 constexpr int LR_BLOCK = LR_WAVES * LR_OWN;  // of a workgroup
 constexpr int LR_TILE = 64;                  // keys (queries) of a tile
 constexpr int LR_STEP = 32;                  // of a step of the math
-constexpr int LR_MOST_POSITIONS = 64 * 32 * LR_TILE;       // a bit of a lane's word per tile
+constexpr int LR_MOST_POSITIONS = 64 * 64 * LR_STEP;       // a bit of a lane's words per LR_STEP keys
 constexpr float LR_LAZY = 8.0f;              // the reference of the exponents moves when a maximum has outgrown it by 2^8
 
 struct LatentReplayArgs {
@@ -62,23 +63,25 @@ struct LatentReplayArgs {
     float scale, scale_log2e;
 };
 
-// Rows of BYTES in LDS, a multiple of 64 of them behind one another: 16-byte piece p of row r at slot p ^ swizzle(r), so that one
-// piece of 8 consecutive rows, and 64 bytes of 8 of them, meet every bank alike.
+// Rows of BYTES in LDS behind one another: 16-byte piece p of row r at slot p ^ swizzle(r).
 template <int BYTES>
 struct LdsRows {
     static constexpr int PIECES = BYTES / 16, LOAD_ROWS = 64 / PIECES;
     static_assert(PIECES == 16 || PIECES == 8 || PIECES == 4, "whole rows a load");
     __device__ static __forceinline__ int swizzle(int r)
     {
-        return PIECES == 16 ? ((2 * r) & 15) | ((r >> 3) & 1) : PIECES == 8 ? r & 7 : (r >> 1) & 3;
+        return lds_swizzle<PIECES>(r);
     }
-    // LR_TILE rows from memory, `stride` bytes apart, straight to LDS; rows behind `last` are that one again
-    __device__ static __forceinline__ void load(const unsigned char *from, uint32_t stride, int last, unsigned char *to, int wv, int lane)
+    // Two units of LR_STEP rows from memory straight to LDS, rows `stride` bytes apart; rows behind `last` of a unit are that one again.
+    // (The swizzle is linear in a row's bits: a lane's part of it, and the load's.)
+    __device__ static __forceinline__ void load(const unsigned char *const (&from)[2], uint32_t stride, const int (&last)[2], unsigned char *to,
+                                                int wv, int lane)
     {
+        const int lrow = lane / PIECES, piece = lane % PIECES ^ swizzle(lrow);
 #pragma unroll
         for (int i = 0; i < LR_TILE / (LR_WAVES * LOAD_ROWS); ++i) {
-            const int r0 = (i * LR_WAVES + wv) * LOAD_ROWS, r = r0 + lane / PIECES, row = r < last ? r : last;
-            load_to_lds16(from + ((uint32_t)row * stride + (uint32_t)((lane % PIECES) ^ swizzle(r)) * 16u), to + r0 * BYTES);
+            const int r0 = (i * LR_WAVES + wv) * LOAD_ROWS, unit = r0 / LR_STEP, r = r0 % LR_STEP + lrow, end = unit ? last[1] : last[0];
+            load_to_lds16((unit ? from[1] : from[0]) + ((uint32_t)(r < end ? r : end) * stride + (uint32_t)(piece ^ swizzle(r0)) * 16u), to + r0 * BYTES);
         }
     }
     // Offset of piece 2 c + half of row `li`: an operand of 16 values c of 32 rows.  (Rows 32 apart: 32 BYTES more.)
@@ -148,46 +151,69 @@ __device__ __forceinline__ uint32_t odd_rows(const unsigned char *rows)
     return mask;
 }
 
-// Tiles of LR_TILE keys that some query of first .. last sees, and those that all of them see where causality lets them, as words of
-// 32 tiles in the lanes.
-struct LiveTiles {
-    uint32_t some, all;
-    __device__ __forceinline__ LiveTiles(const int32_t *death, int tiles, int n, int first, int last)
+// Units of LR_STEP keys that some query of first .. last sees, and those that all of them see where causality lets them, as words of
+// 64 units in the lanes.
+struct LiveUnits {
+    uint32_t some_lo, some_hi, all_lo, all_hi;             // of units 64 lane .. + 31, and the 32 behind them
+    int units;
+    __device__ __forceinline__ LiveUnits(const int32_t *death, int units_, int n, int first, int last) : units(units_)
     {
         const int lane = lane_id();
-        some = all = tiles >= 32 * (lane + 1) ? 0xFFFFFFFFu : tiles <= 32 * lane ? 0u : (1u << (tiles - 32 * lane)) - 1u;
+        auto below = [&](int u0) { return units >= u0 + 32 ? 0xFFFFFFFFu : units <= u0 ? 0u : (1u << (units - u0)) - 1u; };
+        some_lo = all_lo = below(64 * lane);
+        some_hi = all_hi = below(64 * lane + 32);
         if (!death) return;
-        some = all = 0;
-        constexpr int BATCH = 8;
-        for (int t0 = 0; t0 < tiles; t0 += BATCH) {
+        some_lo = some_hi = all_lo = all_hi = 0;
+        constexpr int BATCH = 16;            // loads of 64 keys
+        for (int u0 = 0; u0 < units; u0 += 2 * BATCH) {
             int d[BATCH];
 #pragma unroll
-            for (int u = 0; u < BATCH; ++u) {
-                const int j = (t0 + u) * LR_TILE + lane;
-                d[u] = j < n ? death[j] : 0;
+            for (int i = 0; i < BATCH; ++i) {
+                const int j = (u0 + 2 * i) * LR_STEP + lane;
+                d[i] = j < n ? death[j] : 0;
             }
+            // bit 2 i of a word: of the lower half's unit
+            uint32_t seen = 0, whole = 0;
 #pragma unroll
-            for (int u = 0; u < BATCH; ++u) {
-                const bool inside = t0 + u < tiles && (t0 + u) * LR_TILE + lane < n;
-                const bool any = __ballot(inside && d[u] > first) != 0, every = __ballot(inside && d[u] <= last) == 0;
-                if (lane == (t0 + u) / 32 && t0 + u < tiles) {
-                    some |= (uint32_t)any << ((t0 + u) % 32);
-                    all |= (uint32_t)every << ((t0 + u) % 32);
-                }
+            for (int i = 0; i < BATCH; ++i) {
+                const bool inside = (u0 + 2 * i) * LR_STEP + lane < n;
+                const uint64_t any = __ballot(inside && d[i] > first), not_all = __ballot(inside && d[i] <= last);
+                seen |= ((uint32_t)any != 0 ? 1u : 0u) << (2 * i) | ((uint32_t)(any >> 32) != 0 ? 2u : 0u) << (2 * i);
+                whole |= ((uint32_t)not_all == 0 ? 1u : 0u) << (2 * i) | ((uint32_t)(not_all >> 32) == 0 ? 2u : 0u) << (2 * i);
             }
+            const bool mine = lane == u0 / 64, second = u0 / 32 % 2 != 0;
+            some_lo = mine && !second ? seen : some_lo;
+            some_hi = mine && second ? seen : some_hi;
+            all_lo = mine && !second ? whole : all_lo;
+            all_hi = mine && second ? whole : all_hi;
         }
     }
-    // The first live tile from t on, or `tiles`.  Uniform.
-    __device__ __forceinline__ int next(int t, int tiles) const
+    __device__ static __forceinline__ uint32_t word(uint32_t lo, uint32_t hi, int u)
     {
-        while (t < tiles) {
-            const uint32_t w = (uint32_t)__builtin_amdgcn_readlane((int)some, t / 32) >> (t % 32);
-            if (w) return t + __builtin_ctz(w);
-            t = (t / 32 + 1) * 32;
-        }
-        return tiles;
+        const uint32_t a = (uint32_t)__builtin_amdgcn_readlane((int)lo, u / 64), b = (uint32_t)__builtin_amdgcn_readlane((int)hi, u / 64);
+        return u / 32 % 2 ? b : a;
     }
-    __device__ __forceinline__ bool whole(int t) const { return ((uint32_t)__builtin_amdgcn_readlane((int)all, t / 32) >> (t % 32)) & 1u; }
+    // The first live unit from u on, or `units`.  Uniform.
+    __device__ __forceinline__ int next(int u) const
+    {
+        while (u < units) {
+            const uint32_t w = word(some_lo, some_hi, u) >> (u % 32);
+            if (w) return u + __builtin_ctz(w) < units ? u + __builtin_ctz(w) : units;
+            u = (u / 32 + 1) * 32;
+        }
+        return units;
+    }
+    __device__ __forceinline__ bool whole(int u) const { return (word(all_lo, all_hi, u) >> (u % 32)) & 1u; }
+};
+
+// Two live units that make a tile; the second may be none (`units`).
+struct UnitPair {
+    int u[2];
+    __device__ __forceinline__ UnitPair(const LiveUnits &live, int from)
+    {
+        u[0] = live.next(from);
+        u[1] = live.next(u[0] + 1);
+    }
 };
 
 // What a workgroup that owns queries (forward, backward q) or keys (backward kv) works on: heaviest first, a (trajectory, head) on
@@ -214,14 +240,23 @@ template <int D>
 struct KeyTile {
     static constexpr int E = D / 2, KB = D * 2, RB = E * 2;
     static constexpr int ROT = LR_TILE * KB, V = ROT + LR_TILE * RB, BYTES = V + LR_TILE * KB;
-    __device__ static __forceinline__ void load(const LatentReplayArgs &a, int b, int h, int t, unsigned char *to, int wv, int lane)
+    __device__ static __forceinline__ void load(const LatentReplayArgs &a, int b, int h, const LiveUnits &live, const UnitPair &t, unsigned char *to,
+                                                int wv, int lane)
     {
-        const int first = t * LR_TILE, last = a.T - 1 - first;         // (of the memory; behind the sequence's end nothing is seen)
-        const unsigned char *k = a.kv + (((size_t)b * a.T + first) * a.H + h) * (2 * KB);
+        const unsigned char *k[2], *v[2], *r[2];
+        int last[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int first = (t.u[i] < live.units ? t.u[i] : t.u[0]) * LR_STEP;       // (none: the first again)
+            last[i] = a.T - 1 - first;                     // of the memory; behind the sequence's end nothing is seen
+            k[i] = a.kv + (((size_t)b * a.T + first) * a.H + h) * (2 * KB);
+            v[i] = k[i] + KB;
+            r[i] = a.rope + ((size_t)b * a.T + first) * a.rope_row;
+        }
         const uint32_t stride = (uint32_t)a.H * (2 * KB);
         LdsRows<KB>::load(k, stride, last, to, wv, lane);
-        LdsRows<RB>::load(a.rope + ((size_t)b * a.T + first) * a.rope_row, (uint32_t)a.rope_row, last, to + ROT, wv, lane);
-        LdsRows<KB>::load(k + KB, stride, last, to + V, wv, lane);
+        LdsRows<RB>::load(r, (uint32_t)a.rope_row, last, to + ROT, wv, lane);
+        LdsRows<KB>::load(v, stride, last, to + V, wv, lane);
     }
 };
 
@@ -254,10 +289,9 @@ void latent_replay_kernel(LatentReplayArgs a)
     const int wave0 = i0 + wv * LR_OWN, qpos = wave0 + li;
     const int wave_last = wave0 + LR_OWN - 1 < n ? wave0 + LR_OWN - 1 : n - 1, block_last = i0 + LR_BLOCK - 1 < n ? i0 + LR_BLOCK - 1 : n - 1;
     const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
-    const int tiles = block_last / LR_TILE + 1;
-    const LiveTiles live(death, tiles, n, i0, block_last);
-    int t = live.next(0, tiles);
-    if (t < tiles) Tile::load(a, at.b, at.h, t, lds, wv, lane);
+    const LiveUnits live(death, block_last / LR_STEP + 1, n, i0, block_last);
+    UnitPair t(live, 0);
+    if (t.u[0] < live.units) Tile::load(a, at.b, at.h, live, t, lds, wv, lane);
 
     bf16x8 q[KC + RC];
     {
@@ -327,16 +361,15 @@ void latent_replay_kernel(LatentReplayArgs a)
     };
 
     unsigned char *here = lds, *there = lds + Tile::BYTES;
-    while (t < tiles) {
+    while (t.u[0] < live.units) {
         lds_loads_done();
-        const int next = live.next(t + 1, tiles);
-        if (next < tiles) Tile::load(a, at.b, at.h, next, there, wv, lane);
+        const UnitPair next(live, t.u[1] + 1);
+        if (next.u[0] < live.units) Tile::load(a, at.b, at.h, live, next, there, wv, lane);
         __builtin_amdgcn_sched_barrier(0);
-        const bool whole = live.whole(t);
 #pragma unroll
         for (int st = 0; st < LR_TILE / LR_STEP; ++st) {
-            const int key0 = t * LR_TILE + st * LR_STEP;
-            if (wave0 < n && key0 <= wave_last) step(here, st, key0, whole);
+            const int key0 = t.u[st] * LR_STEP;
+            if (t.u[st] < live.units && wave0 < n && key0 <= wave_last) step(here, st, key0, live.whole(t.u[st]));
         }
         __builtin_amdgcn_sched_barrier(0);
         unsigned char *const x = here;
@@ -400,7 +433,7 @@ __device__ __forceinline__ void store_rows(unsigned char *lds, const f32x16 (&ac
 
 // Gradient of the queries, and delta.
 template <int D>
-__global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(1)))
+__global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void latent_replay_dq_kernel(LatentReplayArgs a)
 {
     using Tile = KeyTile<D>;
@@ -414,10 +447,9 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
     const int wave0 = i0 + wv * LR_OWN, qpos = wave0 + li, q_row = qpos < n ? qpos : n - 1;
     const int wave_last = wave0 + LR_OWN - 1 < n ? wave0 + LR_OWN - 1 : n - 1, block_last = i0 + LR_BLOCK - 1 < n ? i0 + LR_BLOCK - 1 : n - 1;
     const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
-    const int tiles = block_last / LR_TILE + 1;
-    const LiveTiles live(death, tiles, n, i0, block_last);
-    int t = live.next(0, tiles);
-    if (t < tiles) Tile::load(a, at.b, at.h, t, lds, wv, lane);
+    const LiveUnits live(death, block_last / LR_STEP + 1, n, i0, block_last);
+    UnitPair t(live, 0);
+    if (t.u[0] < live.units) Tile::load(a, at.b, at.h, live, t, lds, wv, lane);
 
     bf16x8 q[KC + RC], g_[KC];
     float delta = 0.f;
@@ -485,16 +517,15 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
         (void)add_transposed<Tile::RB>(tile + st * LR_STEP * Tile::RB, w, rt_at, mixed, dr);
     };
     unsigned char *here = lds, *there = lds + Tile::BYTES;
-    while (t < tiles) {
+    while (t.u[0] < live.units) {
         lds_loads_done();
-        const int next = live.next(t + 1, tiles);
-        if (next < tiles) Tile::load(a, at.b, at.h, next, there, wv, lane);
+        const UnitPair next(live, t.u[1] + 1);
+        if (next.u[0] < live.units) Tile::load(a, at.b, at.h, live, next, there, wv, lane);
         __builtin_amdgcn_sched_barrier(0);
-        const bool whole = live.whole(t);
 #pragma unroll
         for (int st = 0; st < LR_TILE / LR_STEP; ++st) {
-            const int key0 = t * LR_TILE + st * LR_STEP;
-            if (wave0 < n && key0 <= wave_last) step(here, st, key0, whole);
+            const int key0 = t.u[st] * LR_STEP;
+            if (t.u[st] < live.units && wave0 < n && key0 <= wave_last) step(here, st, key0, live.whole(t.u[st]));
         }
         __builtin_amdgcn_sched_barrier(0);
         unsigned char *const x = here;
@@ -512,7 +543,7 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
 
 // Gradients of keys and values, and the head's of the rotary part.
 template <int D>
-__global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(1)))
+__global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(D == 128 ? 1 : 2)))
 void latent_replay_dkv_kernel(LatentReplayArgs a)
 {
     constexpr int E = D / 2, KC = D / 16, RC = E / 16, DT = D / 32, ET = E / 32, KB = D * 2, RB = E * 2;
@@ -564,10 +595,14 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
     auto load_tile = [&](int t, unsigned char *to) {
         const int i = t * LR_TILE, last = a.T - 1 - i;
         const size_t row = ((size_t)at.b * a.T + i) * a.H + at.h;
-        const uint32_t stride = (uint32_t)a.H * ((D + E) * 2);
-        LdsRows<KB>::load(a.q + row * ((D + E) * 2), stride, last, to, wv, lane);
-        LdsRows<RB>::load(a.q + row * ((D + E) * 2) + KB, stride, last, to + ROT, wv, lane);
-        LdsRows<KB>::load(a.dout + row * KB, (uint32_t)a.H * KB, last, to + G, wv, lane);
+        const uint32_t stride = (uint32_t)a.H * ((D + E) * 2), g_stride = (uint32_t)a.H * KB;
+        const int second = last < LR_STEP ? last : LR_STEP;                // row of the tile where the second unit begins
+        const int lasts[2] = {last, last - second};
+        const unsigned char *const q = a.q + row * ((D + E) * 2), *const g = a.dout + row * KB;
+        const unsigned char *const q2[2] = {q, q + second * (size_t)stride}, *const r2[2] = {q2[0] + KB, q2[1] + KB}, *const g2[2] = {g, g + second * (size_t)g_stride};
+        LdsRows<KB>::load(q2, stride, lasts, to, wv, lane);
+        LdsRows<RB>::load(r2, stride, lasts, to + ROT, wv, lane);
+        LdsRows<KB>::load(g2, g_stride, lasts, to + G, wv, lane);
     };
     auto load_stat = [&](int t) {                          // threads 0 .. 63: lse, the next 64: delta
         const int i = t * LR_TILE + ((int)threadIdx.x & (LR_TILE - 1));
