@@ -13,6 +13,26 @@ __device__ __forceinline__ int32_t constant_word(const int32_t *p)
     return *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>((uintptr_t)p);
 }
 
+// 16 bytes per lane from `base` (uniform) + offset straight into LDS, lane l to lds + 16 l (uniform), without the compiler's knowledge:
+// of a load that it knows of it assumes that any transposing read may meet it, and waits for all that is on its way, the tiles that
+// are asked for ahead included.  Here nothing waits but wait_for_loads(); no register is written.  (A barrier behind the last reads
+// of what the load overwrites, wait_for_loads() and a barrier before the first reads of what it brings are the caller's.)
+__device__ __forceinline__ void start_load_to_lds16(const unsigned char *base, uint32_t offset, const unsigned char *lds)
+{
+    const uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char *)lds;
+    __asm__ volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(at) : "memory");
+}
+// Until at most N of this wave's loads are on their way, and no read of LDS.
+template <int N>
+__device__ __forceinline__ void wait_for_loads()
+{
+    __asm__ volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ void workgroup_barrier()
+{
+    __asm__ volatile("s_barrier" : : : "memory");
+}
+
 // 16-byte piece p of row r of a tile in LDS stands at slot p ^ lds_swizzle<PIECES>(r) of its row.  LDS has 64 banks, and what reads
 // together is (measured: pairs of lanes of one bank, one of them after the other)
 //   reads of 16 bytes           lanes 0-3, 12-15, 20-23, 24-27, the other 16 of the lower half, and the same of the upper half;

@@ -8,14 +8,13 @@
 // 2 (R + E) + 2 R flops a pair for 2 (R + E) bytes a row: M = W Hq query rows share every row that is read, so few heads
 // are bound by the memory and 128 of them are about as much bound by the products (242 flops a byte).
 //
-// S^T = C Q^T and O^T = C^T P by matrix instructions, 32x32x16 for 32 query rows a wave and 16x16x32 for 16: one query row
-// per lane % 32 (16), so all soft-max state is lane local; one pass over the rows with a running maximum and sum.  A tile of
-// 32 rows is contiguous in a page and goes from memory straight into LDS, once: the first product reads its rows, the second
-// one the same rows transposed.  Queries and output stay in registers (32 rows: 144 and 256 of the 512 of a lane).
+// S^T = C Q^T and O^T = C^T P by 16x16x32 matrix instructions, 16 query rows a wave, one per lane % 16, so all soft-max state is lane
+// local; one pass over the rows with a running maximum and sum.  A tile of 32 rows is contiguous in a page and goes from
+// memory straight into LDS, once: the first product reads its rows, the second one the same rows transposed.  Queries and
+// output stay in registers (72 and 128 of a lane's, for R = 512).
 //
-// A workgroup's 4 waves are RG row groups x 4 / RG key groups: waves of one key group share tiles, the key groups take
-// tiles in turn and are joined in LDS at the end.  Few sequences are shared by S workgroups, whose partials a second launch
-// joins.
+// A workgroup's waves are RG row groups x KG key groups: waves of one key group share tiles, the key groups take tiles in
+// turn and are joined in LDS at the end.  Few sequences are shared by S workgroups, whose partials a second launch joins.
 //
 // P is rounded to bf16 for the second product (2^-9 of an entry at most), as the output is: it is the operand of the
 // product that brings the latent vectors to the heads' values.  Sums and soft-max state are fp32.
@@ -30,8 +29,11 @@
 
 namespace ngc {
 
-constexpr int LT_WAVES = 4;
-constexpr int LT_KEYS = 32;                 // rows of a tile
+constexpr int LT_ROWS = 16;                 // query rows of a wave
+// Rows of a tile.  One row group is bound by the memory: its waves have tiles of their own, small ones, the next on its way while one is
+// worked on.  More of them are as much bound by the products, whose full rate takes 32.
+constexpr int latent_keys(int RG) { return RG == 1 ? 16 : 32; }
+constexpr int LT_LDS_KEYS = 128;            // rows in LDS: those of R = 512 fill a CU's
 
 struct LatentArgs {
     const unsigned char *rows;              // bf16 [num_pages][page_rows][R + E]
@@ -73,15 +75,15 @@ struct LatentSegment {
     }
 };
 
-// Where things are in a tile of 32 rows in LDS: the latent parts, 16-byte piece p of row r at slot p ^ swizzle(r), then the rotary
+// Where things are in a tile of KEYS rows in LDS: the latent parts, 16-byte piece p of row r at slot p ^ swizzle(r), then the rotary
 // parts.
-template <int R, int E>
+template <int R, int E, int KEYS>
 struct LatentTile {
     static constexpr int ROW = (R + E) * 2, LAT = R * 2, ROT = E * 2;
-    static constexpr int LAT_BYTES = LT_KEYS * LAT, BYTES = LT_KEYS * ROW;
+    static constexpr int LAT_BYTES = KEYS * LAT, BYTES = KEYS * ROW;
     static constexpr int LAT_PIECES = LAT / 16, ROT_PIECES = ROT / 16;
     static constexpr int LAT_ROWS = 64 / LAT_PIECES, ROT_ROWS = 64 / ROT_PIECES;         // rows a wave-wide load brings
-    static constexpr int LAT_LOADS = LT_KEYS / LAT_ROWS, ROT_LOADS = LT_KEYS / ROT_ROWS;
+    static constexpr int LAT_LOADS = KEYS / LAT_ROWS, ROT_LOADS = KEYS / ROT_ROWS;
     static_assert(LAT_PIECES == 64 || LAT_PIECES == 32, "whole rows a load");
     static_assert(ROT_PIECES == 8 || ROT_PIECES == 4, "whole rows a load");
     __device__ static __forceinline__ int swizzle(int r) { return lds_swizzle<LAT_PIECES>(r); }
@@ -93,101 +95,47 @@ struct LatentTile {
     }
 };
 
-// A wave's matrix tiles, for 32 and for 16 query rows.  `row`: of the lane.  A score register e of a lane is the score of key
-// key_of(e); eight consecutive ones are an operand of the second product.
-template <int RT>
-struct LatentMath;
-template <>
-struct LatentMath<32> {
-    typedef f32x16 Acc;
-    static constexpr int ROWS = 32, CHUNK = 16, KEYS = 32, COLS = 32, SCORES = 16, STEPS = 2;      // of 16 keys
-    __device__ static __forceinline__ int row(int lane) { return lane & 31; }
-    __device__ static __forceinline__ int part(int lane) { return lane >> 5; }
-    __device__ static __forceinline__ int key_of(int e, int part) { return 8 * (e / 4) + 4 * part + e % 4; }
-    __device__ static __forceinline__ Acc product(bf16x8 x, bf16x8 y, Acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0); }
-    // first row and column of what a lane names in a transposing read: for keys 16 step + 8 g .. of columns 32 c ..
-    __device__ static __forceinline__ int read_row(int lane) { return 4 * (lane >> 5) + (lane & 15) / 4; }
-    __device__ static __forceinline__ int read_col(int lane) { return (lane & 16) + 4 * (lane & 3); }
-    static constexpr int step_rows(int step, int g) { return 16 * step + 8 * g; }
-    __device__ static __forceinline__ float top(float v) { return half_rows_max(v); }
-    __device__ static __forceinline__ float sum(float v) { return half_rows_sum(v); }
-    // registers 4 q .. 4 q + 3 of accumulator c hold columns col(c, q) .. + 3
-    static constexpr int QUADS = 4;
-    __device__ static __forceinline__ int col(int c, int q, int part) { return 32 * c + 8 * q + 4 * part; }
-};
-template <>
-struct LatentMath<16> {
-    typedef f32x4 Acc;
-    static constexpr int ROWS = 16, CHUNK = 32, KEYS = 16, COLS = 16, SCORES = 8, STEPS = 1;       // of 32 keys
-    __device__ static __forceinline__ int row(int lane) { return lane & 15; }
-    __device__ static __forceinline__ int part(int lane) { return lane >> 4; }
-    __device__ static __forceinline__ int key_of(int e, int part) { return 16 * (e / 4) + 4 * part + e % 4; }
-    __device__ static __forceinline__ Acc product(bf16x8 x, bf16x8 y, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); }
-    __device__ static __forceinline__ int read_row(int lane) { return 4 * (lane >> 4) + (lane & 15) / 4; }
-    __device__ static __forceinline__ int read_col(int lane) { return 4 * (lane & 3); }
-    static constexpr int step_rows(int, int g) { return 16 * g; }
-    __device__ static __forceinline__ float top(float v) { return quad_rows_max(v); }
-    __device__ static __forceinline__ float sum(float v) { return quad_rows_sum(v); }
-    static constexpr int QUADS = 1;
-    __device__ static __forceinline__ int col(int c, int, int part) { return 16 * c + 4 * part; }
-};
-
-// For s_waitcnt: at most `n` loads are still on their way, and no LDS operation.
-constexpr int wait_loads(int n) { return 0x0070 | (n & 15) | (n >> 4 << 14); }
+__device__ __forceinline__ f32x4 product16(bf16x8 x, bf16x8 y, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); }
+// Over the 32 (16) rows of a tile: columns (rows read transposed) by weights.
+__device__ __forceinline__ f32x4 add_rows(const u32x2 (&v)[2], const uint32_t (&w)[4], f32x4 c)
+{
+    return product16(__builtin_bit_cast(bf16x8, u32x4{v[0][0], v[0][1], v[1][0], v[1][1]}), __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]}), c);
+}
+__device__ __forceinline__ f32x4 add_rows(const u32x2 (&v)[1], const uint32_t (&w)[2], f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, v[0]), __builtin_bit_cast(s16x4, u32x2{w[0], w[1]}), c, 0, 0, 0);
+}
+// Row of a tile that score register e of a lane's quarter stands for: the scores of rows 0 .. 15, then (of 32) of 16 .. 31.
+__device__ __forceinline__ int latent_key(int e, int quarter) { return 16 * (e / 4) + 4 * quarter + e % 4; }
 
 // 2^8: the reference of the exponents moves only when a maximum has outgrown it by that.
 constexpr float LT_LAZY = 8.0f;
 
-// Waves per SIMD (by registers: queries and output are (2 R + E) RT / 128 of a lane's), and tiles in LDS: four of R = 512 fill a CU's.
-constexpr int latent_waves(int R, int RT) { return R == 256 && RT == 16 ? 2 : 1; }
-constexpr int latent_slots(int R, int RT) { return R == 256 && RT == 32 ? 8 : 4; }
+// Waves per SIMD: what LDS leaves room for.
+constexpr int latent_waves(int R, int NW) { return R == 512 ? NW / 4 : 2; }
 
-// The accumulators times alpha, where they are: left to itself the compiler keeps a second copy of them for the branch around this.
-// (A matrix instruction's result may be read 18 cycles after its issue at the earliest.)
-template <int CT, class Acc>
-__device__ __forceinline__ void scale_all(Acc (&o)[CT], float alpha)
-{
-    if constexpr (CT * sizeof(Acc) <= 512) {
-#pragma unroll
-        for (int c = 0; c < CT; ++c) o[c] *= alpha;
-    } else {
-        __asm__ volatile("s_nop 15\n\ts_nop 7");
-#pragma unroll
-        for (int c = 0; c < CT; ++c)
-#pragma unroll
-            for (int e = 0; e < (int)(sizeof(Acc) / 4); ++e) {
-                float x;
-                __asm__ volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %1, %2\n\tv_accvgpr_write_b32 %0, %1"
-                                 : "+a"(o[c][e]), "=&v"(x) : "v"(alpha));
-            }
-        __asm__ volatile("s_nop 3");
-    }
-}
-
-// RT query rows a wave, RG row groups.
-template <int R, int E, int RT, int RG>
-__global__ __launch_bounds__(LT_WAVES * 64) __attribute__((amdgpu_waves_per_eu(latent_waves(R, RT))))
+// NW waves, RG row groups.
+template <int R, int E, int NW, int RG>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(latent_waves(R, NW))))
 void latent_attn_kernel(LatentArgs a)
 {
-    using Tile = LatentTile<R, E>;
-    using Math = LatentMath<RT>;
-    constexpr int KG = LT_WAVES / RG;
-    constexpr int SLOTS = latent_slots(R, RT);             // tiles in LDS
+    constexpr int KEYS = latent_keys(RG), HALVES = KEYS / 16, SLOTS = LT_LDS_KEYS / KEYS;
+    using Tile = LatentTile<R, E, KEYS>;
+    constexpr int KG = NW / RG;
     constexpr int NB = SLOTS / KG;                         // buffers of a key group
-    constexpr int CHUNKS = (R + E) / Math::CHUNK;          // of the first product
-    constexpr int KTILES = LT_KEYS / Math::KEYS;           // score tiles per tile of rows
-    constexpr int CT = R / Math::COLS;                     // column tiles of the second product
+    static_assert(NB >= 2, "a tile is on its way while one is worked on");
+    constexpr int CHUNKS = (R + E) / 32, LAT_CHUNKS = R / 32, CT = R / 16;               // of the first product; column tiles of the second
     constexpr int LAT_LOADS = (Tile::LAT_LOADS + RG - 1) / RG, ROT_LOADS = (Tile::ROT_LOADS + RG - 1) / RG;      // of a wave, per tile
     constexpr int LOADS = LAT_LOADS + ROT_LOADS;
-    constexpr int HALVES = LT_WAVES * RT * R * 4 > SLOTS * Tile::BYTES ? 2 : 1;          // the output goes through LDS in so many parts
-    static_assert(LT_WAVES * RT * R * 4 / HALVES <= SLOTS * Tile::BYTES, "a part of the output fits");
+    constexpr int PARTS = (NW * LT_ROWS * R * 4 + SLOTS * Tile::BYTES - 1) / (SLOTS * Tile::BYTES);       // the output goes through LDS in
 
     extern __shared__ __align__(256) unsigned char lds[];
-    float *const red = reinterpret_cast<float *>(lds + SLOTS * Tile::BYTES);             // [2][waves][RT]
+    float *const red = reinterpret_cast<float *>(lds + SLOTS * Tile::BYTES);             // [2][waves][rows]
+    uint32_t *const odd_rows = reinterpret_cast<uint32_t *>(red + 2 * NW * LT_ROWS);     // [slots][RG]
 
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
     const int rg = wv % RG, kg = wv / RG;
-    const int row = Math::row(lane), part = Math::part(lane);
+    const int row = lane & 15, quarter = lane >> 4;
     // the row blocks of a sequence follow one another on one XCD
     int seg = (int)blockIdx.x, block = 0;
     if (a.blocks > 1) {
@@ -197,246 +145,238 @@ void latent_attn_kernel(LatentArgs a)
         seg = first + at - block * here;
     }
     const int split = (int)blockIdx.y;
-    const LatentSegment s(a, seg, threadIdx.x == 0 && split == 0 && block == 0);
-    const int real_rows = s.w * a.Hq;                      // query rows of the sequence
-    const int block_row0 = block * RG * RT;
-    if (block_row0 >= real_rows) return;
-    const int my_row = block_row0 + rg * RT + row;
-    const int q_row = my_row < real_rows ? my_row : real_rows - 1;
-
-    bf16x8 qop[CHUNKS];
-    {
-        const unsigned char *q = a.q + ((size_t)seg * a.M + q_row) * Tile::ROW + part * 16;
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) qop[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(q + c * Math::CHUNK * 2));
-    }
-    const int limit = s.limit(a, q_row);
-    // rows below `all` are seen by every query row of the workgroup, rows from `end` on by none
-    const int all = s.limit(a, block_row0);
-    const int last_row = block_row0 + RG * RT - 1;
-    const int end = s.limit(a, last_row < real_rows ? last_row : real_rows - 1);
-    const int tiles = (end + LT_KEYS - 1) / LT_KEYS;
-    const int32_t *tab = a.table + (size_t)(a.seg0 + seg) * a.max_pages;
     const int stride = a.S * KG, first_tile = split * KG + kg;
-
+    const int32_t *tab = a.table + (size_t)(a.seg0 + seg) * a.max_pages;
     auto tile_base = [&](int t) -> const unsigned char * {
-        const int r0 = t * LT_KEYS;
+        const int r0 = t * KEYS;
         int page = constant_word(tab + (r0 >> a.page_shift));
         page = (page < 0 || page >= a.num_pages) ? 0 : page;          // never leave the pool
         return a.rows + (((size_t)page << a.page_shift) + (r0 & ((1 << a.page_shift) - 1))) * Tile::ROW;
     };
+    // ---- asked for before the lengths have arrived: queries (of rows that are none too) and the first tile (or the last there is room
+    // for) ----
+    const int block_row0 = block * RG * LT_ROWS;
+    const int my_row = block_row0 + rg * LT_ROWS + row, q_row = my_row < a.M ? my_row : a.M - 1;
+    const unsigned char *const first_base = tile_base(first_tile < a.cap / KEYS ? first_tile : a.cap / KEYS - 1);
+    const LatentSegment s(a, seg, threadIdx.x == 0 && split == 0 && block == 0);
+
     unsigned char *const buffers = lds + kg * NB * Tile::BYTES;
-    auto load_tile = [&](int t, unsigned char *to) {
-        const unsigned char *base = tile_base(t);
+    auto load_tile = [&](const unsigned char *base, unsigned char *to) {
         int lane_ = lane;
         __asm__ volatile("" : "+v"(lane_));                // (offsets are made where they are used, not kept over the loop)
         // the swizzle is linear in a row's bits: a lane's part of it, and the load's
         const int lrow = Tile::LAT_ROWS == 1 ? 0 : lane_ / Tile::LAT_PIECES, lp = lane_ % Tile::LAT_PIECES ^ Tile::swizzle(lrow);
-        const uint32_t lat = (uint32_t)(lrow * Tile::ROW);
 #pragma unroll
         for (int i = 0; i < LAT_LOADS; ++i) {
             const int r0 = (i * RG + rg) * Tile::LAT_ROWS;
-            load_to_lds16(base + r0 * Tile::ROW + (lat + (uint32_t)(lp ^ Tile::swizzle(r0)) * 16), to + r0 * Tile::LAT);
+            start_load_to_lds16(base + r0 * Tile::ROW, (uint32_t)(lrow * Tile::ROW) + (uint32_t)(lp ^ Tile::swizzle(r0)) * 16, to + r0 * Tile::LAT);
         }
         const int rrow = lane_ / Tile::ROT_PIECES, rp = lane_ % Tile::ROT_PIECES ^ Tile::rot_swizzle(rrow);
-        const uint32_t rot = (uint32_t)(rrow * Tile::ROW);
 #pragma unroll
         for (int i = 0; i < ROT_LOADS; ++i) {
             const int r0 = (i * RG + rg) % Tile::ROT_LOADS * Tile::ROT_ROWS;             // (what is left over loads a part again)
-            load_to_lds16(base + r0 * Tile::ROW + Tile::LAT + (rot + (uint32_t)(rp ^ Tile::rot_swizzle(r0)) * 16), to + Tile::LAT_BYTES + r0 * Tile::ROT);
+            start_load_to_lds16(base + r0 * Tile::ROW + Tile::LAT, (uint32_t)(rrow * Tile::ROW) + (uint32_t)(rp ^ Tile::rot_swizzle(r0)) * 16,
+                                to + Tile::LAT_BYTES + r0 * Tile::ROT);
         }
     };
+    load_tile(first_base, buffers);
+    bf16x8 qop[CHUNKS];
+    {
+        const unsigned char *q = a.q + ((size_t)seg * a.M + q_row) * Tile::ROW + quarter * 16;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) qop[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(q + c * 64));
+    }
 
-    typename Math::Acc oacc[CT];
+    const int real_rows = s.w * a.Hq;                      // query rows of the sequence
+    if (block_row0 >= real_rows) {
+        wait_for_loads<0>();                               // nothing may be on its way to LDS that is not this workgroup's any more
+        return;
+    }
+    const int limit = s.limit(a, q_row);
+    // rows below `all` are seen by every query row of the workgroup, rows from `end` on by none
+    const int all = s.limit(a, block_row0);
+    const int last_row = block_row0 + RG * LT_ROWS - 1;
+    const int end = s.limit(a, last_row < real_rows ? last_row : real_rows - 1);
+    const int tiles = (end + KEYS - 1) / KEYS;
+    // Values of a tile that are not finite, where some query row does not see all of its rows: a weight of 0 would make NaN of them.  Every
+    // wave looks at what it has loaded itself: they become 0, and `odd_rows` says which rows had some.
+    auto take_out = [&](unsigned char *tile, uint32_t *word) {
+        uint32_t rows = 0;
+        auto look = [&](unsigned char *part, int r) {
+            u32x4 *const at = reinterpret_cast<u32x4 *>(part + lane * 16);
+            u32x2 lo = {(*at)[0], (*at)[1]}, hi = {(*at)[2], (*at)[3]};
+            const bool lo_odd = take_out_odd(lo), hi_odd = take_out_odd(hi);
+            if (lo_odd | hi_odd) {
+                *at = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                rows |= 1u << r;
+            }
+        };
+#pragma unroll 1
+        for (int i = 0; i < LAT_LOADS; ++i) {
+            const int r0 = (i * RG + rg) * Tile::LAT_ROWS;
+            look(tile + r0 * Tile::LAT, r0 + lane / Tile::LAT_PIECES);
+        }
+#pragma unroll 1
+        for (int i = 0; i < ROT_LOADS; ++i) {
+            const int r0 = (i * RG + rg) % Tile::ROT_LOADS * Tile::ROT_ROWS;
+            look(tile + Tile::LAT_BYTES + r0 * Tile::ROT, r0 + lane / Tile::ROT_PIECES);
+        }
+        rows = wave_reduce(rows, [](uint32_t x, uint32_t y) { return x | y; });
+        if (lane == 0) word[rg] = rows;
+    };
+
+    f32x4 oacc[CT];                                        // registers e of column tile c: columns 16 c + 4 quarter + e
 #pragma unroll
-    for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int e = 0; e < Math::QUADS * 4; ++e) oacc[c][e] = 0.f;
+    for (int c = 0; c < CT; ++c) oacc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_run = -INFINITY, m_ref = 0.f, l_run = 0.f;     // m_ref: m_run, or 0 as long as nothing has been seen
 
     // Where this lane's operands are in a tile.  Pieces 16 apart are 256 bytes apart whatever the swizzle, rows 16 apart have the same one,
-    // those of rows 8 apart differ by 3, and a tile begins at a multiple of 256: the other offsets differ from the first one's by bits.
-    constexpr int PIECES_A_CHUNK = Math::CHUNK / 8, LAT_CHUNKS = R / Math::CHUNK, LAT_VARIANTS = 16 / PIECES_A_CHUNK;
-    constexpr int COL_VARIANTS = 128 / Math::COLS;
+    // and a tile begins at a multiple of 256: the other offsets differ from the first one's by bits.
     static_assert(Tile::BYTES % 256 == 0 && Tile::LAT % 256 == 0, "offsets differ by bits");
-    const uint32_t lat0 = Tile::piece(row, part), rot0 = Tile::piece(row, Tile::LAT_PIECES + part);
-    const uint32_t col0 = Tile::piece(Math::read_row(lane), Math::read_col(lane) / 8) + (uint32_t)(Math::read_col(lane) % 8) * 2;
-
-    auto compute_tile = [&](int t, const unsigned char *tile) {
-        uint32_t at_lat = lat0, at_rot = rot0, at_col = col0;
-        __asm__ volatile("" : "+v"(at_lat), "+v"(at_rot), "+v"(at_col));
-        const unsigned char __attribute__((address_space(3))) *const tile3 = (const unsigned char __attribute__((address_space(3))) *)tile;
-        const uint32_t tile_at = (uint32_t)(uintptr_t)tile3;
-        auto row_piece = [&](int c, int k) {               // chunk c of the rows of key tile k
-            const uint32_t at = c < LAT_CHUNKS ? ((tile_at + at_lat) ^ (uint32_t)(c % LAT_VARIANTS * PIECES_A_CHUNK * 16)) + (uint32_t)(c / LAT_VARIANTS * 256 + k * Math::KEYS * Tile::LAT)
-                                               : ((tile_at + at_rot) ^ (uint32_t)((c - LAT_CHUNKS) * PIECES_A_CHUNK * 16)) + (uint32_t)(k * Math::KEYS * Tile::ROT);
+    const int read_row = 4 * quarter + row / 4, read_col = 4 * (row % 4);                // of the transposing reads
+    const uint32_t lat0 = Tile::piece(row, quarter), rot0 = Tile::piece(row, Tile::LAT_PIECES + quarter);
+    const uint32_t col0 = Tile::piece(read_row, read_col / 8) + (uint32_t)(read_col % 8) * 2;
+    auto compute_tile = [&](int t, const unsigned char *tile, const uint32_t *odd) {
+        const uint32_t tile_at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char *)tile;
+        auto row_piece = [&](int c, int k) {               // chunk c of rows 16 k ..
+            const uint32_t at = c < LAT_CHUNKS ? ((tile_at + lat0) ^ (uint32_t)(c % 4 * 64)) + (uint32_t)(c / 4 * 256 + k * 16 * Tile::LAT)
+                                               : ((tile_at + rot0) ^ (uint32_t)((c - LAT_CHUNKS) * 64)) + (uint32_t)(k * 16 * Tile::ROT);
             return *(const u32x4 __attribute__((address_space(3))) *)(uintptr_t)at;
         };
-        // keys 16 st + 8 g .. (of 32 query rows), 16 g .. (of 16), of column tile c
-        auto transposed = [&](int st, int g, int c) {
-            const uint32_t at = ((tile_at + at_col) ^ (uint32_t)(c % COL_VARIANTS * Math::COLS * 2 ^ (RT == 32 ? g * 48 : 0))) +
-                                (uint32_t)(c / COL_VARIANTS * 256 + (RT == 32 ? st * 16 + g * 8 : g * 16) * Tile::LAT);
+        auto transposed = [&](int g, int c) {              // rows 16 g + 4 quarter .. + 3 of column tile c
+            const uint32_t at = ((tile_at + col0) ^ (uint32_t)(c % 8 * 32)) + (uint32_t)(c / 8 * 256 + g * 16 * Tile::LAT);
             return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)at));
         };
-        const int key0 = t * LT_KEYS;
-        const bool edge = key0 + LT_KEYS > all;            // not every query row of the workgroup sees all of the tile's rows
-        typename Math::Acc sc[KTILES];
+        const int key0 = t * KEYS;
+        constexpr int SCORES = 4 * HALVES;
+        // GROUP chunks' rows (column tiles) are asked for while the products of those before run
+        constexpr int GROUP = NW == 4 && HALVES == 1 ? (CHUNKS % 6 == 0 ? 6 : 9) : NW == 8 && R == 512 ? 1 : 3, VGROUP = NW == 4 ? 8 : 4;
+        static_assert(CHUNKS % GROUP == 0 && CT % VGROUP == 0, "whole groups");
+        f32x4 sc[HALVES];
 #pragma unroll
-        for (int k = 0; k < KTILES; ++k)
-#pragma unroll
-            for (int e = 0; e < Math::QUADS * 4; ++e) sc[k][e] = 0.f;
-        // GROUP chunks' rows are asked for while the products of those before run
-        constexpr int GROUP = CHUNKS % 4 == 0 ? 4 : 3;
-        static_assert(CHUNKS % GROUP == 0, "whole groups");
-        u32x4 x[2][GROUP][KTILES];
-        auto ask_rows = [&](int g0, u32x4 (&to)[GROUP][KTILES]) {
+        for (int k = 0; k < HALVES; ++k) sc[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+        u32x4 x[2][GROUP][HALVES];
+        auto ask_rows = [&](int g) {
 #pragma unroll
             for (int u = 0; u < GROUP; ++u)
 #pragma unroll
-                for (int k = 0; k < KTILES; ++k) to[u][k] = row_piece(g0 + u, k);
+                for (int k = 0; k < HALVES; ++k) x[g & 1][u][k] = row_piece(g * GROUP + u, k);
         };
-        ask_rows(0, x[0]);
-#pragma unroll
-        for (int g = 0; g < CHUNKS / GROUP; ++g) {
-            if (g + 1 < CHUNKS / GROUP) ask_rows((g + 1) * GROUP, x[(g + 1) & 1]);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int u = 0; u < GROUP; ++u)
-#pragma unroll
-                for (int k = 0; k < KTILES; ++k) sc[k] = Math::product(__builtin_bit_cast(bf16x8, x[g & 1][u][k]), qop[g * GROUP + u], sc[k]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        // the first columns, while the weights are made
-        constexpr int VGROUP = RT == 32 ? 2 : 4;
-        u32x2 v[2][VGROUP][Math::STEPS][2];
-        auto ask_columns = [&](int c0, u32x2 (&to)[VGROUP][Math::STEPS][2]) {
+        u32x2 v[2][VGROUP][HALVES];
+        auto ask_columns = [&](int g) {
 #pragma unroll
             for (int u = 0; u < VGROUP; ++u)
 #pragma unroll
-                for (int st = 0; st < Math::STEPS; ++st)
-#pragma unroll
-                    for (int g = 0; g < 2; ++g) to[u][st][g] = transposed(st, g, c0 + u);
+                for (int h = 0; h < HALVES; ++h) v[g & 1][u][h] = transposed(h, g * VGROUP + u);
         };
-        ask_columns(0, v[0]);
+        ask_rows(0);
+#pragma unroll
+        for (int g = 0; g < CHUNKS / GROUP; ++g) {
+            if (g + 1 < CHUNKS / GROUP) ask_rows(g + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < GROUP; ++u)
+#pragma unroll
+                for (int k = 0; k < HALVES; ++k) sc[k] = product16(__builtin_bit_cast(bf16x8, x[g & 1][u][k]), qop[g * GROUP + u], sc[k]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        ask_columns(0);                                    // (there when the weights are)
         __builtin_amdgcn_sched_barrier(0);
-        float s_[Math::SCORES];
+        float s_[SCORES];
 #pragma unroll
-        for (int e = 0; e < Math::SCORES; ++e) s_[e] = KTILES == 1 ? sc[0][e % 16] : sc[e / 4 % KTILES][e % 4];
-        if (edge) {
+        for (int e = 0; e < SCORES; ++e) s_[e] = sc[e / 4][e % 4];
+        if (key0 + KEYS > all) {                        // not every query row of the workgroup sees all of the tile's rows
 #pragma unroll
-            for (int e = 0; e < Math::SCORES; ++e) s_[e] = key0 + Math::key_of(e, part) < limit ? s_[e] : -INFINITY;
+            for (int e = 0; e < SCORES; ++e) s_[e] = key0 + latent_key(e, quarter) < limit ? s_[e] : -INFINITY;
+            uint32_t rows = 0;
+#pragma unroll
+            for (int i = 0; i < RG; ++i) rows |= odd[i];
+            if (rows)                                      // who sees such a row becomes NaN
+#pragma unroll
+                for (int e = 0; e < SCORES; ++e)
+                    if ((rows >> latent_key(e, quarter)) & 1u) s_[e] = key0 + latent_key(e, quarter) < limit ? NAN : -INFINITY;
         }
         float tmx = s_[0];
 #pragma unroll
-        for (int e = 1; e < Math::SCORES; ++e) tmx = max_no_nan(tmx, s_[e]);
-        tmx = Math::top(tmx);
+        for (int e = 1; e < SCORES; ++e) tmx = max_no_nan(tmx, s_[e]);
+        tmx = quad_rows_max(tmx);
         const bool outgrown = (tmx - m_run) * a.scale_log2e > LT_LAZY;     // of each row by itself: its results do not depend on its neighbours'
         if (__ballot(outgrown)) {
-            const bool some = __ballot(m_run > -INFINITY) != 0;       // (nothing to scale on the first tile)
+            const bool some = __ballot(m_run > -INFINITY) != 0;            // (nothing to scale on the first tile)
             const float m_new = outgrown ? tmx : m_run;
             const float alpha = m_new == m_run ? 1.0f : fast_exp2((m_run - m_new) * a.scale_log2e);
             l_run *= alpha;
-            if (some) scale_all(oacc, alpha);
+            if (some) {
+#pragma unroll
+                for (int c = 0; c < CT; ++c) oacc[c] *= alpha;
+            }
             m_run = m_new;
             m_ref = m_new == -INFINITY ? 0.f : m_new;
         }
-        uint32_t p[Math::SCORES / 2];
+        uint32_t p[SCORES / 2];
         float psum = 0.f;
 #pragma unroll
-        for (int e = 0; e < Math::SCORES / 2; ++e) {
+        for (int e = 0; e < SCORES / 2; ++e) {
             // the difference first: scores of any size
             const f32x2 w = {fast_exp2((s_[2 * e] - m_ref) * a.scale_log2e), fast_exp2((s_[2 * e + 1] - m_ref) * a.scale_log2e)};
             psum += w[0] + w[1];
             p[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(w, bf16x2));
         }
         l_run += psum;
-        bool odd = false;
 #pragma unroll
         for (int g = 0; g < CT / VGROUP; ++g) {
-            if (g + 1 < CT / VGROUP) ask_columns((g + 1) * VGROUP, v[(g + 1) & 1]);
+            if (g + 1 < CT / VGROUP) ask_columns(g + 1);
             __builtin_amdgcn_sched_barrier(0);
-            if (edge) {
 #pragma unroll
-                for (int u = 0; u < VGROUP; ++u)
-#pragma unroll
-                    for (int st = 0; st < Math::STEPS; ++st) odd |= take_out_odd(v[g & 1][u][st][0]) | take_out_odd(v[g & 1][u][st][1]);
-            }
-#pragma unroll
-            for (int st = 0; st < Math::STEPS; ++st)
-#pragma unroll
-                for (int u = 0; u < VGROUP; ++u) {
-                    const u32x2 lo = v[g & 1][u][st][0], hi = v[g & 1][u][st][1];
-                    const bf16x8 vt = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
-                    const bf16x8 w = __builtin_bit_cast(bf16x8, u32x4{p[4 * st], p[4 * st + 1], p[4 * st + 2], p[4 * st + 3]});
-                    oacc[g * VGROUP + u] = Math::product(vt, w, oacc[g * VGROUP + u]);
-                }
+            for (int u = 0; u < VGROUP; ++u) oacc[g * VGROUP + u] = add_rows(v[g & 1][u], p, oacc[g * VGROUP + u]);
             __builtin_amdgcn_sched_barrier(0);
-        }
-        if (__ballot(odd)) {
-            // the query rows that see one of the rows with such values, and no others, become NaN
-            for (int k = 0; k < LT_KEYS && key0 + k < end; ++k) {
-                bool any = false;
-#pragma unroll
-                for (int i = 0; i < Tile::LAT; i += 512) any |= has_odd(*reinterpret_cast<const u32x2 *>(tile + k * Tile::LAT + i + lane * 8));
-                if (__ballot(any) && key0 + k < limit) l_run = NAN;
-            }
         }
     };
 
     // ---- the tiles ----
-    constexpr int WAIT_LDS = 0xC07F;                       // lgkmcnt(0)
     const int mine = first_tile < tiles ? (tiles - first_tile + stride - 1) / stride : 0;
     // how many rounds the workgroup takes (key group 0 has the most tiles)
     const int rounds = split * KG < tiles ? (tiles - split * KG + stride - 1) / stride : 0;
-    if constexpr (NB == 1) {
-        static_assert(RG == 1, "no barrier");
-        // a wave's tiles are its own
-        for (int i = 0; i < mine; ++i) {
-            load_tile(first_tile + i * stride, buffers);
-            __builtin_amdgcn_s_waitcnt(0x0F70);            // vmcnt(0)
-            __asm__ volatile("" ::: "memory");
-            compute_tile(first_tile + i * stride, buffers);
-            __builtin_amdgcn_s_waitcnt(WAIT_LDS);
-            __builtin_amdgcn_sched_barrier(0);
+    int issued = 1;                                        // (that one in any case)
+    for (; issued < NB - 1 && issued < mine; ++issued) load_tile(tile_base(first_tile + issued * stride), buffers + issued * Tile::BYTES);
+    for (int i = 0; i < (RG == 1 ? mine : rounds); ++i) {
+        const int t = first_tile + i * stride, slot = i % NB;
+        if (issued == i + NB - 1) wait_for_loads<(NB - 2) * LOADS>();
+        else wait_for_loads<0>();
+        unsigned char *const tile = buffers + slot * Tile::BYTES;
+        uint32_t *const odd = odd_rows + (kg * NB + slot) * RG;
+        if ((t + 1) * KEYS > all) {                        // (or LDS that holds anything)
+            take_out(tile, odd);
+            wait_for_loads<(NB - 2) * LOADS>();
         }
-    } else {
-        int issued = 0;
-        for (; issued < NB - 1 && issued < mine; ++issued) load_tile(first_tile + issued * stride, buffers + issued * Tile::BYTES);
-        for (int i = 0; i < rounds; ++i) {
-            const int ahead = issued - i - 1;              // tiles on their way behind this one
-            // the tile has arrived, and what this wave has read
-            if (ahead == NB - 2 && i < mine) __builtin_amdgcn_s_waitcnt(wait_loads((NB - 2) * LOADS));
-            else __builtin_amdgcn_s_waitcnt(wait_loads(0));
-            __asm__ volatile("" ::: "memory");
-            if constexpr (RG > 1) __builtin_amdgcn_s_barrier();      // (or a wave's tiles are its own)
-            __asm__ volatile("" ::: "memory");
-            if (issued < mine) {
-                load_tile(first_tile + issued * stride, buffers + issued % NB * Tile::BYTES);
-                ++issued;
-            }
-            // (a key group without a tile in the last round computes one that nobody sees)
-            compute_tile(first_tile + i * stride, buffers + i % NB * Tile::BYTES);
+        if constexpr (RG > 1) workgroup_barrier();         // (or a wave's tiles are its own)
+        if (issued < mine) {
+            load_tile(tile_base(first_tile + issued * stride), buffers + issued % NB * Tile::BYTES);
+            ++issued;
         }
+        // (a key group without a tile in the last round computes one that nobody sees)
+        compute_tile(t, tile, odd);
     }
+    wait_for_loads<0>();
 
     // ---- join the key groups, and out: through LDS, 16-byte piece p of query row r at slot p ^ r ----
-    const float l = Math::sum(l_run);
-    if (part == 0) {
-        red[wv * RT + row] = m_run;
-        red[(LT_WAVES + wv) * RT + row] = l;
+    const float l = quad_rows_sum(l_run);
+    if (quarter == 0) {
+        red[wv * LT_ROWS + row] = m_run;
+        red[(NW + wv) * LT_ROWS + row] = l;
     }
     __syncthreads();
     float m_all = -INFINITY, l_all = 0.f;
 #pragma unroll
-    for (int k = 0; k < KG; ++k) m_all = max_no_nan(m_all, red[(k * RG + rg) * RT + row]);
+    for (int k = 0; k < KG; ++k) m_all = max_no_nan(m_all, red[(k * RG + rg) * LT_ROWS + row]);
 #pragma unroll
     for (int k = 0; k < KG; ++k) {
-        const float mk = red[(k * RG + rg) * RT + row];
-        if (mk > -INFINITY || mk != mk) l_all += red[(LT_WAVES + k * RG + rg) * RT + row] * fast_exp2((mk - m_all) * a.scale_log2e);
+        const float mk = red[(k * RG + rg) * LT_ROWS + row];
+        if (mk != -INFINITY) l_all += red[(NW + k * RG + rg) * LT_ROWS + row] * fast_exp2((mk - m_all) * a.scale_log2e);
     }
     float share = m_run == -INFINITY ? 0.f : fast_exp2((m_run - m_all) * a.scale_log2e);
     if (a.S == 1) share = l_all == 0.f ? 0.f : share / l_all;
-    if (kg == 0 && part == 0 && my_row < real_rows) {
+    if (kg == 0 && quarter == 0 && my_row < real_rows) {
         if (a.S == 1) {
             if (a.lse_out) a.lse_out[(size_t)seg * a.M + my_row] = l_all == 0.f ? -INFINITY : m_all * a.scale + logf(l_all);
         } else {
@@ -446,28 +386,27 @@ void latent_attn_kernel(LatentArgs a)
         }
     }
     if (a.S > 1 && rounds == 0) return;                    // (nothing was seen: the join does not look at it)
-    constexpr int COLS = R / HALVES, PIECES = COLS / 4;
-    float *const mine_o = reinterpret_cast<float *>(lds) + wv * RT * COLS;
+    constexpr int COLS = R / PARTS, PIECES = COLS / 4;
+    float *const mine_o = reinterpret_cast<float *>(lds) + wv * LT_ROWS * COLS;
     const float *const all_o = reinterpret_cast<const float *>(lds);
 #pragma unroll
-    for (int h = 0; h < HALVES; ++h) {
+    for (int h = 0; h < PARTS; ++h) {
         if (h) __syncthreads();
 #pragma unroll
-        for (int c = h * CT / HALVES; c < (h + 1) * CT / HALVES; ++c)
-#pragma unroll
-            for (int qd = 0; qd < Math::QUADS; ++qd) {
-                const int piece = (Math::col(c, qd, part) - h * COLS) / 4;
-                f32x4 o = {oacc[c][4 * qd], oacc[c][4 * qd + 1], oacc[c][4 * qd + 2], oacc[c][4 * qd + 3]};
-                o = share == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * share;
-                *reinterpret_cast<f32x4 *>(mine_o + row * COLS + ((piece ^ row) & (PIECES - 1)) * 4) = o;
-            }
+        for (int c = h * CT / PARTS; c < (h + 1) * CT / PARTS; ++c) {
+            const int piece = (16 * c - h * COLS) / 4 + quarter;
+            *reinterpret_cast<f32x4 *>(mine_o + row * COLS + ((piece ^ row) & (PIECES - 1)) * 4) = oacc[c] * share;
+        }
         __syncthreads();
-        for (int i = threadIdx.x; i < RG * RT * PIECES; i += LT_WAVES * 64) {
-            const int piece = i % PIECES, rr = i / PIECES, g = rr / RT, r = rr % RT;
+        static_assert(RG * LT_ROWS * PIECES % (NW * 64) == 0, "whole rounds");
+#pragma unroll
+        for (int n = 0; n < RG * LT_ROWS * PIECES / (NW * 64); ++n) {
+            const int i = n * NW * 64 + (int)threadIdx.x;
+            const int piece = i % PIECES, rr = i / PIECES, g = rr / LT_ROWS, r = rr % LT_ROWS;
             f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < KG; ++k)
-                o += *reinterpret_cast<const f32x4 *>(all_o + ((k * RG + g) * RT + r) * COLS + ((piece ^ r) & (PIECES - 1)) * 4);
+                o += *reinterpret_cast<const f32x4 *>(all_o + ((k * RG + g) * LT_ROWS + r) * COLS + ((piece ^ r) & (PIECES - 1)) * 4);
             const int to = block_row0 + rr, col = h * COLS + piece * 4;
             if (to >= real_rows) continue;
             if (a.S == 1) {
@@ -484,42 +423,37 @@ void latent_attn_kernel(LatentArgs a)
 // Partials of a query row joined, a workgroup (two for R = 256 in one) a row: R / 4 threads.  The shares of all partials first, then the
 // partials, JOIN_BATCH asked for at a time.
 constexpr int JOIN_THREADS = 128, JOIN_BATCH = 8;
-constexpr int LT_MOST_SPLITS = 128;
+constexpr int LT_MOST_SPLITS = 64;          // a lane each
 template <int R>
 __global__ __launch_bounds__(JOIN_THREADS) void latent_join_kernel(LatentArgs a)
 {
     constexpr int PER_ROW = R / 4, ROWS = JOIN_THREADS / PER_ROW;
-    __shared__ float shares[ROWS][LT_MOST_SPLITS + JOIN_BATCH];
+    __shared__ float shares[ROWS][LT_MOST_SPLITS];
     const int sub = (int)threadIdx.x / PER_ROW, lane = lane_id();
     const int seg = (int)blockIdx.y, r = (int)blockIdx.x * ROWS + sub, col = (int)threadIdx.x % PER_ROW * 4;
-    const LatentSegment s(a, seg, false);
-    if ((int)blockIdx.x * ROWS >= s.w * a.Hq) return;
-    const bool real = r < s.w * a.Hq;
-    const int row = real ? r : 0;
+    const int row = r < a.M ? r : a.M - 1;
     const float *ml = a.part_ml + ((size_t)seg * a.S * a.M + row) * 2;
-    // of partials lane and 64 + lane
-    f32x2 x = {-INFINITY, 0.f}, y = {-INFINITY, 0.f};
-    if (lane < a.S) x = *reinterpret_cast<const f32x2 *>(ml + (size_t)lane * a.M * 2);
-    if (lane + 64 < a.S) y = *reinterpret_cast<const f32x2 *>(ml + (size_t)(lane + 64) * a.M * 2);
-    const float m = wave_max_f(fmaxf(x[0], y[0]));
-    const float wx = x[0] == -INFINITY ? 0.f : fast_exp2((x[0] - m) * a.scale_log2e), wy = y[0] == -INFINITY ? 0.f : fast_exp2((y[0] - m) * a.scale_log2e);
-    const float l = wave_sum_f((wx == 0.f ? 0.f : wx * x[1]) + (wy == 0.f ? 0.f : wy * y[1]));
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    if (col / 4 < 64) {                                    // a row's first wave
-        shares[sub][lane] = wx * inv;
-        shares[sub][lane + 64] = wy * inv;
-        if (lane < JOIN_BATCH) shares[sub][LT_MOST_SPLITS + lane] = 0.f;
-    }
-    __syncthreads();
     const float *po = a.part_o + ((size_t)seg * a.S * a.M + row) * R + col;
+    f32x4 v[JOIN_BATCH];
+    auto ask = [&](int i0) {                               // (what nobody has written is not looked at)
+#pragma unroll
+        for (int u = 0; u < JOIN_BATCH; ++u) v[u] = *reinterpret_cast<const f32x4 *>(po + (size_t)(i0 + u < a.S ? i0 + u : a.S - 1) * a.M * R);
+    };
+    ask(0);
+    f32x2 x = {-INFINITY, 0.f};                            // of partial `lane`
+    if (lane < a.S) x = *reinterpret_cast<const f32x2 *>(ml + (size_t)lane * a.M * 2);
+    int tokens = a.n_new ? a.n_new[seg % a.B] : a.W;
+    tokens = tokens < 0 ? 0 : tokens > a.W ? a.W : tokens;
+    const bool real = r < tokens * a.Hq;
+    const float m = wave_max_f(x[0]);
+    const float wx = x[0] == -INFINITY ? 0.f : fast_exp2((x[0] - m) * a.scale_log2e);
+    const float l = wave_sum_f(wx == 0.f ? 0.f : wx * x[1]);
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    if (col / 4 < 64) shares[sub][lane] = wx * inv;        // a row's first wave
+    __syncthreads();
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int i0 = 0; i0 < a.S; i0 += JOIN_BATCH) {
-        f32x4 v[JOIN_BATCH];
-#pragma unroll
-        for (int u = 0; u < JOIN_BATCH; ++u) {             // (one without a share may not have been written)
-            const int i = i0 + u < a.S ? i0 + u : a.S - 1;
-            v[u] = *reinterpret_cast<const f32x4 *>(po + (size_t)i * a.M * R);
-        }
+        if (i0) ask(i0);
 #pragma unroll
         for (int u = 0; u < JOIN_BATCH; ++u) {
             const float w = i0 + u < a.S ? shares[sub][i0 + u] : 0.f;
@@ -543,15 +477,15 @@ namespace {
 
 // How M query rows are dealt to waves and workgroups.
 struct LatentShape {
-    int rows, groups, blocks, key_groups;
+    int waves, groups, blocks, key_groups;
 };
 LatentShape latent_shape(int M)
 {
     LatentShape s;
-    s.rows = M <= 16 ? 16 : 32;
-    s.groups = M <= 32 ? 1 : M <= 64 ? 2 : 4;
-    s.blocks = (M + s.rows * s.groups - 1) / (s.rows * s.groups);
-    s.key_groups = LT_WAVES / s.groups;
+    s.groups = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+    s.waves = s.groups <= 2 ? 4 : 8;
+    s.blocks = (M + LT_ROWS * s.groups - 1) / (LT_ROWS * s.groups);
+    s.key_groups = s.waves / s.groups;
     return s;
 }
 
@@ -559,9 +493,9 @@ LatentShape latent_shape(int M)
 int latent_splits(const LatentShape &s, int nseg, int rows)
 {
     const long long groups = (long long)nseg * s.blocks;
-    const int rounds = (rows + LT_KEYS * s.key_groups - 1) / (LT_KEYS * s.key_groups);
+    const int keys = latent_keys(s.groups) * s.key_groups, rounds = (rows + keys - 1) / keys;
     long long S = 256 / groups;
-    if (S > rounds / 2) S = rounds / 2;
+    if (S > rounds) S = rounds;
     if (S > LT_MOST_SPLITS) S = LT_MOST_SPLITS;
     return S < 1 ? 1 : (int)S;
 }
@@ -624,16 +558,15 @@ extern "C" int ngc_latent_attn(const ngc_paged_cache *pc, int32_t layer, const i
     const void *fn;
     size_t lds;
 #define NGC_PICK_LATENT(R_, E_) \
-    lds = latent_slots(R_, shape.rows) * LatentTile<R_, E_>::BYTES + 2 * LT_WAVES * 32 * sizeof(float); \
-    fn = shape.rows == 16   ? reinterpret_cast<const void *>(&latent_attn_kernel<R_, E_, 16, 1>) \
-       : shape.groups == 1  ? reinterpret_cast<const void *>(&latent_attn_kernel<R_, E_, 32, 1>) \
-       : shape.groups == 2  ? reinterpret_cast<const void *>(&latent_attn_kernel<R_, E_, 32, 2>) \
-                            : reinterpret_cast<const void *>(&latent_attn_kernel<R_, E_, 32, 4>)
+    lds = LT_LDS_KEYS * (R_ + E_) * 2 + (2 * 8 * LT_ROWS + 32) * sizeof(float); \
+    fn = shape.groups == 1   ? reinterpret_cast<const void *>(&latent_attn_kernel<R_, E_, 4, 1>) \
+         : shape.groups == 2 ? reinterpret_cast<const void *>(&latent_attn_kernel<R_, E_, 4, 2>) \
+                             : reinterpret_cast<const void *>(&latent_attn_kernel<R_, E_, 8, 4>)
     if (R == 512) { NGC_PICK_LATENT(512, 64); }
     else { NGC_PICK_LATENT(256, 32); }
 #undef NGC_PICK_LATENT
     if (lds > 64 * 1024) NGC_HIP_CHECK(hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    rc = launch(fn, dim3((unsigned)(nseg * shape.blocks), (unsigned)S), dim3(LT_WAVES * 64), lds, st, a);
+    rc = launch(fn, dim3((unsigned)(nseg * shape.blocks), (unsigned)S), dim3(shape.waves * 64), lds, st, a);
     if (rc || S == 1) return rc;
     const int rows_a_group = JOIN_THREADS / (R / 4);
     fn = R == 512 ? reinterpret_cast<const void *>(&latent_join_kernel<512>) : reinterpret_cast<const void *>(&latent_join_kernel<256>);

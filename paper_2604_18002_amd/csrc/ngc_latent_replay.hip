@@ -81,7 +81,7 @@ struct LdsRows {
 #pragma unroll
         for (int i = 0; i < LR_TILE / (LR_WAVES * LOAD_ROWS); ++i) {
             const int r0 = (i * LR_WAVES + wv) * LOAD_ROWS, unit = r0 / LR_STEP, r = r0 % LR_STEP + lrow, end = unit ? last[1] : last[0];
-            load_to_lds16((unit ? from[1] : from[0]) + ((uint32_t)(r < end ? r : end) * stride + (uint32_t)(piece ^ swizzle(r0)) * 16u), to + r0 * BYTES);
+            start_load_to_lds16(unit ? from[1] : from[0], (uint32_t)(r < end ? r : end) * stride + (uint32_t)(piece ^ swizzle(r0)) * 16u, to + r0 * BYTES);
         }
     }
     // Offset of piece 2 c + half of row `li`: an operand of 16 values c of 32 rows.  (Rows 32 apart: 32 BYTES more.)
@@ -113,27 +113,39 @@ __device__ __forceinline__ f32x16 zeros16()
 // Row of a tile that register r of a lane's half stands for.
 __device__ __forceinline__ int row_of(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
 
-// acc += X^T w for 32 rows of X in LDS and 32 x 32 weights as the first products leave them.  MIXED: some pairs are masked; values
-// that are not finite are taken for 0 then.  Returns whether there were some.
+// acc += X^T w for 32 rows of X in LDS and 32 x 32 weights as the first products leave them, two of X's column tiles at a time, whose rows
+// are asked for while the products of the two before run.
+struct Columns {
+    u32x2 v[2][2][2];                        // [column tile][16 rows][8 of them]
+};
+// Column tile c of CT, rows BYTES: from x; `at`: where a lane points for the first column tile of a pair (of 64 columns: 128 bytes on).
 template <int BYTES, int CT>
-__device__ __forceinline__ bool add_transposed(const unsigned char *x, const uint32_t (&w)[8], const uint32_t (&at)[CT][2], bool mixed,
-                                               f32x16 (&acc)[CT])
+__device__ __forceinline__ void ask_columns(const unsigned char *x, const uint32_t (&at)[CT][2], int pair, Columns &to)
+{
+#pragma unroll
+    for (int u = 0; u < 2 && 2 * pair + u < CT; ++u)
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) to.v[u][st][g] = read_transposed16(x + at[2 * pair + u][g] + 16 * st * BYTES);
+}
+// `mixed`: some pairs are masked; values that are not finite are taken for 0 then.  Returns whether there were some.
+template <int CT>
+__device__ __forceinline__ bool add_columns(Columns &x, int pair, const uint32_t (&w)[8], bool mixed, f32x16 (&acc)[CT])
 {
     bool odd = false;
+    if (mixed) {
+#pragma unroll
+        for (int u = 0; u < 2 && 2 * pair + u < CT; ++u)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) odd |= take_out_odd(x.v[u][st][0]) | take_out_odd(x.v[u][st][1]);
+    }
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
         const bf16x8 weights = operand(u32x4{w[4 * st], w[4 * st + 1], w[4 * st + 2], w[4 * st + 3]});
-        u32x2 v[CT][2];
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
-#pragma unroll
-            for (int g = 0; g < 2; ++g) v[c][g] = read_transposed16(x + at[c][g] + 16 * st * BYTES);
-        if (mixed) {
-#pragma unroll
-            for (int c = 0; c < CT; ++c) odd |= take_out_odd(v[c][0]) | take_out_odd(v[c][1]);
-        }
-#pragma unroll
-        for (int c = 0; c < CT; ++c) acc[c] = product(operand(u32x4{v[c][0][0], v[c][0][1], v[c][1][0], v[c][1][1]}), weights, acc[c]);
+        for (int u = 0; u < 2 && 2 * pair + u < CT; ++u)
+            acc[2 * pair + u] = product(operand(u32x4{x.v[u][st][0][0], x.v[u][st][0][1], x.v[u][st][1][0], x.v[u][st][1][1]}), weights, acc[2 * pair + u]);
     }
     return odd;
 }
@@ -321,6 +333,9 @@ void latent_replay_kernel(LatentReplayArgs a)
         for (int c = 0; c < KC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + k_at[c] + st * LR_STEP * Tile::KB)), q[c], sc);
 #pragma unroll
         for (int c = 0; c < RC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + r_at[c] + st * LR_STEP * Tile::RB)), q[KC + c], sc);
+        const unsigned char *const values = tile + st * LR_STEP * Tile::KB;
+        Columns x[2];
+        ask_columns<Tile::KB>(values, v_at, 0, x[0]);      // (there when the weights are)
         uint32_t seen = 0xFFFFu;
         if (mixed) {
             seen = seen_keys(death, key0, n, qpos, half);
@@ -350,7 +365,12 @@ void latent_replay_kernel(LatentReplayArgs a)
             w[e] = pack_bf16(p0, p1);
         }
         l_run += sum;
-        const bool odd = add_transposed<Tile::KB>(tile + st * LR_STEP * Tile::KB, w, v_at, mixed, o);
+        bool odd = false;
+#pragma unroll
+        for (int pair = 0; pair < DT / 2; ++pair) {
+            if (pair + 1 < DT / 2) ask_columns<Tile::KB>(values, v_at, pair + 1, x[(pair + 1) & 1]);
+            odd |= add_columns(x[pair & 1], pair, w, mixed, o);
+        }
         if (__ballot(odd)) {
             // the queries that see a row with such a value, and no others, become NaN
             const uint32_t rows = odd_rows<Tile::KB>(tile + Tile::V + st * LR_STEP * Tile::KB);
@@ -501,6 +521,9 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
         for (int c = 0; c < RC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + r_at[c] + st * LR_STEP * Tile::RB)), q[KC + c], sc);
 #pragma unroll
         for (int c = 0; c < KC; ++c) dp = product(operand(*reinterpret_cast<const u32x4 *>(tile + v_at[c] + st * LR_STEP * Tile::KB)), g_[c], dp);
+        const unsigned char *const own = tile + st * LR_STEP * Tile::KB;
+        Columns x[2];
+        ask_columns<Tile::KB>(own, kt_at, 0, x[0]);
         float ds[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] = fast_exp2(__builtin_fmaf(sc[r], a.scale_log2e, neg_lse)) * (dp[r] - delta);
@@ -513,8 +536,13 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = pack_bf16(ds[2 * e], ds[2 * e + 1]);
         // (a key that is seen and not finite has made dS NaN)
-        (void)add_transposed<Tile::KB>(tile + st * LR_STEP * Tile::KB, w, kt_at, mixed, dk);
-        (void)add_transposed<Tile::RB>(tile + st * LR_STEP * Tile::RB, w, rt_at, mixed, dr);
+#pragma unroll
+        for (int pair = 0; pair < DT / 2; ++pair) {
+            if (pair + 1 < DT / 2) ask_columns<Tile::KB>(own, kt_at, pair + 1, x[(pair + 1) & 1]);
+            else ask_columns<Tile::RB>(tile + st * LR_STEP * Tile::RB, rt_at, 0, x[(pair + 1) & 1]);
+            (void)add_columns(x[pair & 1], pair, w, mixed, dk);
+        }
+        (void)add_columns(x[DT / 2 & 1], 0, w, mixed, dr);
     };
     unsigned char *here = lds, *there = lds + Tile::BYTES;
     while (t.u[0] < live.units) {
@@ -541,6 +569,80 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
     store_rows(mine, dr, a.scale, to + D * 2, stride, n - wave0);
 }
 
+// The unit of 32 keys that has place `rank` when they are ordered by the query that sees a key of theirs last, the latest first, and by
+// position among those: the keys of a workgroup's waves then live about as long.  Whole workgroup; `scratch`: LDS of LR_ORDER_BYTES.
+// (A counting sort: how many units end in each stretch of 32 queries, where each stretch begins, then the units in their order.)
+constexpr int LR_MOST_UNITS = LR_MOST_POSITIONS / LR_STEP;
+constexpr int LR_ORDER_BYTES = (LR_MOST_UNITS + LR_MOST_UNITS / 2 + 8 + 32) * 4;
+__device__ __forceinline__ int unit_by_end(const int32_t *death, int n, int rank, int *scratch)
+{
+    constexpr int THREADS = LR_WAVES * 64;
+    int *const count = scratch, *const tmp = scratch + LR_MOST_UNITS + 8;  // count[s]: of units that end in stretch s from the back
+    uint16_t *const end_of = reinterpret_cast<uint16_t *>(scratch + LR_MOST_UNITS + 8 + 32);
+    const int units = (n + LR_STEP - 1) / LR_STEP, lane = lane_id();
+    for (int i = threadIdx.x; i <= units; i += THREADS) count[i] = 0;
+    __syncthreads();
+    constexpr int BATCH = 8;
+    for (int u0 = 2 * wave_id(); u0 < units; u0 += 2 * LR_WAVES * BATCH) {
+        int d[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int j = (u0 + 2 * LR_WAVES * i) * LR_STEP + lane;
+            d[i] = j < n ? death[j] : 0;
+            d[i] = d[i] < n ? d[i] : n;
+            d[i] = d[i] > j ? d[i] : 0;                    // seen by nobody
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int u = u0 + 2 * LR_WAVES * i + lane / 32;
+            int last = d[i];
+#pragma unroll
+            for (int step = 1; step < 32; step *= 2) {
+                const int other = __shfl_xor(last, step);
+                last = last > other ? last : other;
+            }
+            if ((lane & 31) == 0 && u < units) {
+                const int s = units - (last + LR_STEP - 1) / LR_STEP;      // 0: sees the last query's stretch; units: nobody's
+                end_of[u] = (uint16_t)s;
+                atomicAdd(&count[s], 1);
+            }
+        }
+    }
+    __syncthreads();
+    // the stretch of this wave's unit, and its place there
+    const int per = (units + THREADS) / THREADS;           // of units + 1 stretches
+    const int lo = (int)threadIdx.x * per, hi = lo + per < units + 1 ? lo + per : units + 1;
+    int mine = 0;
+    for (int i = lo; i < hi; ++i) mine += count[i];
+    int total;
+    int before = block_excl_scan_i<THREADS>(mine, tmp, &total);
+    for (int i = lo; i < hi; ++i) {
+        const int c = count[i];
+        count[i] = before;
+        before += c;
+    }
+    __syncthreads();
+    int s_lo = 0, s_hi = units;                            // the last stretch that begins at or before rank
+    while (s_lo < s_hi) {
+        const int mid = (s_lo + s_hi + 1) / 2;
+        if (count[mid] <= rank) s_lo = mid;
+        else s_hi = mid - 1;
+    }
+    int left = rank - count[s_lo], found = units;          // (beyond the last unit: none)
+    for (int u0 = 0; u0 < units && found == units; u0 += 64) {
+        const uint64_t here = __ballot(u0 + lane < units && end_of[u0 + lane < units ? u0 + lane : 0] == s_lo);
+        const int some = __popcll(here);
+        if (left < some) {
+            uint64_t w = here;
+            for (int i = 0; i < left; ++i) w &= w - 1;
+            found = u0 + __builtin_ctzll(w);
+        }
+        left -= some;
+    }
+    __syncthreads();                                       // scratch is free again
+    return __builtin_amdgcn_readfirstlane(found);
+}
+
 // Gradients of keys and values, and the head's of the rotary part.
 template <int D>
 __global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(D == 128 ? 1 : 2)))
@@ -550,14 +652,15 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
     // a tile of queries: their two parts, the gradients that arrive at them, and -lse (in powers of 2) and delta
     constexpr int ROT = LR_TILE * KB, G = ROT + LR_TILE * RB, BYTES = G + LR_TILE * KB;
     extern __shared__ __align__(16) unsigned char lds[];
-    float *const stats = reinterpret_cast<float *>(lds + 2 * BYTES);       // [2][2][LR_TILE]
+    float *const stats = reinterpret_cast<float *>(lds + 3 * BYTES);       // [3][2][LR_TILE]
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
     const int li = lane & 31, half = lane >> 5;
     const LatentReplayPlace at(a, (a.T + LR_BLOCK - 1) / LR_BLOCK, false);
-    const int n = at.length(a), j0 = at.block * LR_BLOCK;
-    if (j0 >= n) return;
-    const int wave0 = j0 + wv * LR_OWN, key = wave0 + li, k_row = key < n ? key : n - 1;
+    const int n = at.length(a);
+    if (at.block * LR_BLOCK >= n) return;
     const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
+    const int unit = death ? unit_by_end(death, n, at.block * LR_WAVES + wv, reinterpret_cast<int *>(lds)) : at.block * LR_WAVES + wv;
+    const int wave0 = unit * LR_OWN, key = wave0 + li, k_row = key < n ? key : n - 1;
     // queries key .. until - 1 see this lane's key
     int until = n;
     if (death) {
@@ -570,8 +673,11 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
     const int wave_end = __builtin_amdgcn_readfirstlane(wave_reduce(until, larger));
     // all of the wave's keys are seen by queries below this one, where causality lets them
     const int wave_all = __builtin_amdgcn_readfirstlane(wave_reduce(until, smaller));
-    __shared__ int ends[LR_WAVES];
-    if (lane == 0) ends[wv] = wave_end;
+    __shared__ int begins[LR_WAVES], ends[LR_WAVES];
+    if (lane == 0) {
+        begins[wv] = wave0;
+        ends[wv] = wave_end;
+    }
 
     bf16x8 k[KC + RC], v[KC];
     {
@@ -585,11 +691,13 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
         for (int c = 0; c < KC; ++c) v[c] = operand(*reinterpret_cast<const u32x4 *>(kr + KB + c * 32));
     }
     __syncthreads();
-    int end = 0;
+    int begin = n, end = 0;
 #pragma unroll
-    for (int w = 0; w < LR_WAVES; ++w) end = larger(end, ends[w]);
-    end = __builtin_amdgcn_readfirstlane(end);
-    const int first = j0 / LR_TILE, tiles = (end + LR_TILE - 1) / LR_TILE;
+    for (int w = 0; w < LR_WAVES; ++w) {
+        begin = smaller(begin, begins[w]);
+        end = larger(end, ends[w]);
+    }
+    const int first = __builtin_amdgcn_readfirstlane(begin) / LR_TILE, tiles = (__builtin_amdgcn_readfirstlane(end) + LR_TILE - 1) / LR_TILE;
 
     const size_t stat = ((size_t)at.b * a.H + at.h) * a.T;
     auto load_tile = [&](int t, unsigned char *to) {
@@ -633,76 +741,127 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
     for (int c = 0; c < ET; ++c) dr[c] = zeros16();
     float poison = 0.f;                                    // NaN: a gradient that is not finite arrives at a query that sees the key
 
-    auto step = [&](const unsigned char *tile, const float *st_, int st, int query0) {
-        const bool mixed = query0 < wave0 + LR_OWN - 1 || query0 + LR_STEP > wave_all;
-        f32x16 sc = zeros16(), dp = zeros16();
+    struct Pairs {
+        f32x16 s, dp;                                      // scores and <g, v>
+    };
+    auto scores = [&](const unsigned char *tile, int st, Pairs &x) {
+        x.s = x.dp = zeros16();
 #pragma unroll
-        for (int c = 0; c < KC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + q_at[c] + st * LR_STEP * KB)), k[c], sc);
+        for (int c = 0; c < KC; ++c) x.s = product(operand(*reinterpret_cast<const u32x4 *>(tile + q_at[c] + st * LR_STEP * KB)), k[c], x.s);
 #pragma unroll
-        for (int c = 0; c < RC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + r_at[c] + st * LR_STEP * RB)), k[KC + c], sc);
+        for (int c = 0; c < RC; ++c) x.s = product(operand(*reinterpret_cast<const u32x4 *>(tile + r_at[c] + st * LR_STEP * RB)), k[KC + c], x.s);
 #pragma unroll
-        for (int c = 0; c < KC; ++c) dp = product(operand(*reinterpret_cast<const u32x4 *>(tile + g_at[c] + st * LR_STEP * KB)), v[c], dp);
-        float p[16], ds[16];
+        for (int c = 0; c < KC; ++c) x.dp = product(operand(*reinterpret_cast<const u32x4 *>(tile + g_at[c] + st * LR_STEP * KB)), v[c], x.dp);
+    };
+    struct Weights {
+        uint32_t p[8], ds[8];
+    };
+    auto weights = [&](const float *st_, int st, const Pairs &x, Weights &w) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const f32x4 neg_lse = *reinterpret_cast<const f32x4 *>(st_ + st * LR_STEP + 8 * g + 4 * half);
             const f32x4 delta = *reinterpret_cast<const f32x4 *>(st_ + LR_TILE + st * LR_STEP + 8 * g + 4 * half);
+            float p[4], ds[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                p[4 * g + e] = fast_exp2(__builtin_fmaf(sc[4 * g + e], a.scale_log2e, neg_lse[e]));
-                ds[4 * g + e] = p[4 * g + e] * (dp[4 * g + e] - delta[e]);
+                p[e] = fast_exp2(__builtin_fmaf(x.s[4 * g + e], a.scale_log2e, neg_lse[e]));
+                ds[e] = p[e] * (x.dp[4 * g + e] - delta[e]);
             }
+            w.p[2 * g] = pack_bf16(p[0], p[1]);
+            w.p[2 * g + 1] = pack_bf16(p[2], p[3]);
+            w.ds[2 * g] = pack_bf16(ds[0], ds[1]);
+            w.ds[2 * g + 1] = pack_bf16(ds[2], ds[3]);
         }
-        uint32_t seen = 0xFFFFu;
-        if (mixed) {
-            seen = 0;
+    };
+    // Weights of 0 for the pairs of a step that are masked.
+    auto mask = [&](int query0, Weights &w) {
+        uint32_t keep[8];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int i = query0 + row_of(r, half);
+            const uint32_t bits = key <= i && i < until ? 0xFFFFu : 0u;
+            keep[r / 2] = r % 2 ? keep[r / 2] | bits << 16 : bits;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            w.p[e] &= keep[e];
+            w.ds[e] &= keep[e];
+        }
+    };
+    constexpr int PAIRS = DT / 2;
+    auto ask = [&](const unsigned char *tile, int st, int pair, Columns &to) {
+        if (pair < PAIRS) ask_columns<KB>(tile + st * LR_STEP * KB, gt_at, pair, to);
+        else if (pair < 2 * PAIRS) ask_columns<KB>(tile + st * LR_STEP * KB, qt_at, pair - PAIRS, to);
+        else ask_columns<RB>(tile + st * LR_STEP * RB, rt_at, 0, to);
+    };
+    auto gradients = [&](const unsigned char *tile, int st, const Weights &w, bool mixed, Columns (&x)[2]) {
+        bool odd = false;
+#pragma unroll
+        for (int pair = 0; pair <= 2 * PAIRS; ++pair) {
+            if (pair < 2 * PAIRS) ask(tile, st, pair + 1, x[(pair + 1) & 1]);
+            // (a query that sees the key and is not finite has made dS NaN)
+            if (pair < PAIRS) odd |= add_columns(x[pair & 1], pair, w.p, mixed, dv);
+            else if (pair < 2 * PAIRS) (void)add_columns(x[pair & 1], pair - PAIRS, w.ds, mixed, dk);
+            else (void)add_columns(x[pair & 1], 0, w.ds, mixed, dr);
+        }
+        return odd;
+    };
+    // A step's weights, while the scores of the next one are made (whether anybody needs them or not), and its gradients.
+    auto step = [&](const unsigned char *tile, const float *st_, int st, int query0, Pairs &x, const unsigned char *next_tile, int next_st) {
+        const bool mixed = query0 < wave0 + LR_OWN - 1 || query0 + LR_STEP > wave_all;
+        Pairs y;
+        Weights w;
+        Columns columns[2];
+        scores(next_tile, next_st, y);
+        ask(tile, st, 0, columns[0]);
+        weights(st_, st, x, w);
+        x = y;
+        if (mixed) mask(query0, w);
+        if (__ballot(gradients(tile, st, w, mixed, columns))) {
+            const uint32_t rows = odd_rows<KB>(tile + G + st * LR_STEP * KB);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int i = query0 + row_of(r, half);
-                const bool sees = key <= i && i < until;
-                p[r] = sees ? p[r] : 0.f;
-                ds[r] = sees ? ds[r] : 0.f;
-                seen |= (uint32_t)sees << r;
+                if (((rows >> row_of(r, half)) & 1u) && key <= i && i < until) poison = NAN;
             }
         }
-        uint32_t wp[8], ws[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            wp[e] = pack_bf16(p[2 * e], p[2 * e + 1]);
-            ws[e] = pack_bf16(ds[2 * e], ds[2 * e + 1]);
-        }
-        const bool odd = add_transposed<KB>(tile + st * LR_STEP * KB, wp, gt_at, mixed, dv);
-        // (a query that sees the key and is not finite has made dS NaN)
-        (void)add_transposed<KB>(tile + st * LR_STEP * KB, ws, qt_at, mixed, dk);
-        (void)add_transposed<RB>(tile + st * LR_STEP * RB, ws, rt_at, mixed, dr);
-        if (__ballot(odd)) {
-            const uint32_t rows = odd_rows<KB>(tile + G + st * LR_STEP * KB);
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (((rows >> row_of(r, half)) & 1u) && ((seen >> r) & 1u)) poison = NAN;
-        }
     };
-    float stat_next = 0.f;
+    // Three tiles in LDS: the one whose gradients are made, the next one, whose scores follow, and the one behind it, on its way.
+    auto stage_stat = [&](int slot, float x) {
+        if (threadIdx.x < 2 * LR_TILE) stats[slot * 2 * LR_TILE + threadIdx.x] = threadIdx.x < LR_TILE ? -x * 1.4426950408889634f : x;
+    };
+    auto needed = [&](int query0) { return query0 + LR_STEP > wave0 && query0 < wave_end; };
     if (first < tiles) {
+        Pairs x;
         load_tile(first, lds);
-        stat_next = load_stat(first);
-    }
-    for (int t = first; t < tiles; ++t) {
-        const int cur = (t - first) & 1;
-        unsigned char *const here = lds + cur * BYTES;
-        if (threadIdx.x < 2 * LR_TILE) stats[cur * 2 * LR_TILE + threadIdx.x] = threadIdx.x < LR_TILE ? -stat_next * 1.4426950408889634f : stat_next;
+        stage_stat(0, load_stat(first));
         lds_loads_done();
-        if (t + 1 < tiles) {
-            load_tile(t + 1, lds + (cur ^ 1) * BYTES);
-            stat_next = load_stat(t + 1);
+        float stat_next = 0.f;
+        if (first + 1 < tiles) {
+            load_tile(first + 1, lds + BYTES);
+            stat_next = load_stat(first + 1);
         }
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int st = 0; st < LR_TILE / LR_STEP; ++st) {
-            const int query0 = t * LR_TILE + st * LR_STEP;
-            if (query0 + LR_STEP > wave0 && query0 < wave_end) step(here, stats + cur * 2 * LR_TILE, st, query0);
+        if (needed(first * LR_TILE)) scores(lds, 0, x);
+        int cur = 0;
+        for (int t = first; t < tiles; ++t) {
+            const int next = cur == 2 ? 0 : cur + 1, after = next == 2 ? 0 : next + 1;
+            const unsigned char *const here = lds + cur * BYTES, *const there = lds + next * BYTES;
+            stage_stat(next, stat_next);
+            lds_loads_done();                              // tile t + 1 is there, and everybody has left tile t - 1
+            if (t + 2 < tiles) {
+                load_tile(t + 2, lds + after * BYTES);
+                stat_next = load_stat(t + 2);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            const float *const st_ = stats + cur * 2 * LR_TILE;
+            const int query0 = t * LR_TILE;
+            if (needed(query0)) step(here, st_, 0, query0, x, here, 1);
+            else if (needed(query0 + LR_STEP)) scores(here, 1, x);
+            if (needed(query0 + LR_STEP)) step(here, st_, 1, query0 + LR_STEP, x, there, 0);
+            else if (needed(query0 + 2 * LR_STEP)) scores(there, 0, x);
+            __builtin_amdgcn_sched_barrier(0);
+            cur = next;
         }
-        __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();
     poison += __shfl_xor(poison, 32);                      // (NaN in either half of the key's registers)
@@ -832,7 +991,7 @@ extern "C" int ngc_latent_replay_attn_backward(const void *q, const void *kv, co
     rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dq_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dq_kernel<64>), a, lds, st);
     if (rc) return rc;
     rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dkv_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dkv_kernel<64>), a,
-                       lds + 4 * LR_TILE * sizeof(float), st);
+                       lds / 2 * 3 + 6 * LR_TILE * sizeof(float), st);
     if (rc) return rc;
     const long long threads = (long long)B * T * (D / 2 / 4);
     const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_rope_kernel<64>) : reinterpret_cast<const void *>(&latent_replay_rope_kernel<32>);
