@@ -22,6 +22,12 @@ __device__ __forceinline__ void start_load_to_lds16(const unsigned char *base, u
     const uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char *)lds;
     __asm__ volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(at) : "memory");
 }
+// The same for 4 bytes per lane, lane l to lds + 4 l.
+__device__ __forceinline__ void start_load_to_lds4(const unsigned char *base, uint32_t offset, const unsigned char *lds)
+{
+    const uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char *)lds;
+    __asm__ volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(offset), "s"(base), "s"(at) : "memory");
+}
 // Until at most N of this wave's loads are on their way, and no read of LDS.
 template <int N>
 __device__ __forceinline__ void wait_for_loads()

@@ -13,7 +13,7 @@
 //
 // Three kernels around the same tiles of 32 x 32 pairs by 32x32x16 matrix instructions, four waves a workgroup:
 //   forward      a wave has 32 queries and walks tiles of 64 keys: S^T = K Q^T, O^T += V^T P.
-//   backward, q  the same walk, S^T and (V G^T) again, dQ^T += K^T dS; leaves delta.
+//   backward, q  the same walk, S^T and (V G^T) again, dQ^T += K^T dS; leaves delta and lse as the next one wants them.
 //   backward, kv a wave has 32 keys and walks tiles of 64 queries: S = Q K^T and G V^T, dV^T += G^T P, dK^T += Q^T dS.
 // In each the pairs stand in registers as the first products leave them, which is the order the second products' operand
 // needs if the rows of the other operand are read transposed in the same order: nothing crosses lanes but a row's maximum.
@@ -43,6 +43,7 @@ constexpr int LR_BLOCK = LR_WAVES * LR_OWN;  // of a workgroup
 constexpr int LR_TILE = 64;                  // keys (queries) of a tile
 constexpr int LR_STEP = 32;                  // of a step of the math
 constexpr int LR_MOST_POSITIONS = 64 * 64 * LR_STEP;       // a bit of a lane's words per LR_STEP keys
+constexpr int LR_SLOTS = 6;                  // units of queries in LDS: the most of D = 128
 constexpr float LR_LAZY = 8.0f;              // the reference of the exponents moves when a maximum has outgrown it by 2^8
 
 struct LatentReplayArgs {
@@ -56,7 +57,7 @@ struct LatentReplayArgs {
     // backward
     const unsigned char *dout;               // bf16 [B][T][H][D]
     unsigned char *dq, *dkv, *drope;         // bf16, as q and kv; [B][T][E]
-    float *delta;                            // workspace, fp32 [B][H][T]
+    float *stats;                            // workspace, fp32 [B][H][2][T]: -lse in powers of 2, and delta
     float *part;                             // workspace, fp32 [B][H][T][E]: the heads' gradients of the rotary part
     size_t rope_row;
     int B, T, H;
@@ -73,15 +74,30 @@ struct LdsRows {
         return lds_swizzle<PIECES>(r);
     }
     // Two units of LR_STEP rows from memory straight to LDS, rows `stride` bytes apart; rows behind `last` of a unit are that one again.
-    // (The swizzle is linear in a row's bits: a lane's part of it, and the load's.)
+    // In LOADS parts, of all waves together.  (The swizzle is linear in a row's bits: a lane's part of it, and the load's.)
+    static constexpr int LOADS = LR_TILE / (LR_WAVES * LOAD_ROWS);
+    __device__ static __forceinline__ void load_part(const unsigned char *const (&from)[2], uint32_t stride, const int (&last)[2], unsigned char *to,
+                                                     int i, int wv, int lane)
+    {
+        const int lrow = lane / PIECES, piece = lane % PIECES ^ swizzle(lrow);
+        const int r0 = (i * LR_WAVES + wv) * LOAD_ROWS, unit = r0 / LR_STEP, r = r0 % LR_STEP + lrow, end = unit ? last[1] : last[0];
+        start_load_to_lds16(unit ? from[1] : from[0], (uint32_t)(r < end ? r : end) * stride + (uint32_t)(piece ^ swizzle(r0)) * 16u, to + r0 * BYTES);
+    }
     __device__ static __forceinline__ void load(const unsigned char *const (&from)[2], uint32_t stride, const int (&last)[2], unsigned char *to,
                                                 int wv, int lane)
     {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load_part(from, stride, last, to, i, wv, lane);
+    }
+    // One unit, by all waves; where there are more waves than loads, some load again what others do.
+    static constexpr int UNIT_LOADS = (LR_STEP / LOAD_ROWS + LR_WAVES - 1) / LR_WAVES;
+    __device__ static __forceinline__ void load_unit(const unsigned char *from, uint32_t stride, int last, unsigned char *to, int wv, int lane)
+    {
         const int lrow = lane / PIECES, piece = lane % PIECES ^ swizzle(lrow);
 #pragma unroll
-        for (int i = 0; i < LR_TILE / (LR_WAVES * LOAD_ROWS); ++i) {
-            const int r0 = (i * LR_WAVES + wv) * LOAD_ROWS, unit = r0 / LR_STEP, r = r0 % LR_STEP + lrow, end = unit ? last[1] : last[0];
-            start_load_to_lds16(unit ? from[1] : from[0], (uint32_t)(r < end ? r : end) * stride + (uint32_t)(piece ^ swizzle(r0)) * 16u, to + r0 * BYTES);
+        for (int i = 0; i < UNIT_LOADS; ++i) {
+            const int r0 = (i * LR_WAVES + wv) * LOAD_ROWS % LR_STEP, r = r0 + lrow;
+            start_load_to_lds16(from, (uint32_t)(r < last ? r : last) * stride + (uint32_t)(piece ^ swizzle(r0)) * 16u, to + r0 * BYTES);
         }
     }
     // Offset of piece 2 c + half of row `li`: an operand of 16 values c of 32 rows.  (Rows 32 apart: 32 BYTES more.)
@@ -119,6 +135,16 @@ struct Columns {
     u32x2 v[2][2][2];                        // [column tile][16 rows][8 of them]
 };
 // Column tile c of CT, rows BYTES: from x; `at`: where a lane points for the first column tile of a pair (of 64 columns: 128 bytes on).
+template <int BYTES, int CT>
+__device__ __forceinline__ void ask_columns(const unsigned char *x, const uint32_t (&first)[2], int pair, Columns &to)
+{
+#pragma unroll
+    for (int u = 0; u < 2 && 2 * pair + u < CT; ++u)
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) to.v[u][st][g] = read_transposed16(x + (first[g] ^ (2 * pair + u) * 64) + 16 * st * BYTES);
+}
 template <int BYTES, int CT>
 __device__ __forceinline__ void ask_columns(const unsigned char *x, const uint32_t (&at)[CT][2], int pair, Columns &to)
 {
@@ -489,8 +515,12 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
         delta = half_rows_sum(delta);
     }
     const size_t stat = ((size_t)at.b * a.H + at.h) * a.T + q_row;
-    if (half == 0 && qpos < n) a.delta[stat] = delta;
     const float neg_lse = -a.lse[stat] * 1.4426950408889634f;
+    if (half == 0 && qpos < n) {
+        float *const stats = a.stats + ((size_t)at.b * a.H + at.h) * 2 * a.T + qpos;
+        stats[0] = neg_lse;
+        stats[a.T] = delta;
+    }
     uint32_t k_at[KC], r_at[RC], v_at[KC], kt_at[DT][2], rt_at[ET][2];
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
@@ -574,27 +604,28 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
 // (A counting sort: how many units end in each stretch of 32 queries, where each stretch begins, then the units in their order.)
 constexpr int LR_MOST_UNITS = LR_MOST_POSITIONS / LR_STEP;
 constexpr int LR_ORDER_BYTES = (LR_MOST_UNITS + LR_MOST_UNITS / 2 + 8 + 32) * 4;
+template <int WAVES>
 __device__ __forceinline__ int unit_by_end(const int32_t *death, int n, int rank, int *scratch)
 {
-    constexpr int THREADS = LR_WAVES * 64;
+    constexpr int THREADS = WAVES * 64;
     int *const count = scratch, *const tmp = scratch + LR_MOST_UNITS + 8;  // count[s]: of units that end in stretch s from the back
     uint16_t *const end_of = reinterpret_cast<uint16_t *>(scratch + LR_MOST_UNITS + 8 + 32);
     const int units = (n + LR_STEP - 1) / LR_STEP, lane = lane_id();
     for (int i = threadIdx.x; i <= units; i += THREADS) count[i] = 0;
     __syncthreads();
     constexpr int BATCH = 8;
-    for (int u0 = 2 * wave_id(); u0 < units; u0 += 2 * LR_WAVES * BATCH) {
+    for (int u0 = 2 * wave_id(); u0 < units; u0 += 2 * WAVES * BATCH) {
         int d[BATCH];
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const int j = (u0 + 2 * LR_WAVES * i) * LR_STEP + lane;
+            const int j = (u0 + 2 * WAVES * i) * LR_STEP + lane;
             d[i] = j < n ? death[j] : 0;
             d[i] = d[i] < n ? d[i] : n;
             d[i] = d[i] > j ? d[i] : 0;                    // seen by nobody
         }
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const int u = u0 + 2 * LR_WAVES * i + lane / 32;
+            const int u = u0 + 2 * WAVES * i + lane / 32;
             int last = d[i];
 #pragma unroll
             for (int step = 1; step < 32; step *= 2) {
@@ -643,23 +674,23 @@ __device__ __forceinline__ int unit_by_end(const int32_t *death, int n, int rank
     return __builtin_amdgcn_readfirstlane(found);
 }
 
-// Gradients of keys and values, and the head's of the rotary part.
+// Gradients of keys and values, and the head's of the rotary part.  Two waves for 32 keys: the first makes P of 32 queries, and with
+// it dV; the second makes dS of it and of <g, v>, and with it dK and the rotary part's.
 template <int D>
-__global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(D == 128 ? 1 : 2)))
+__global__ __launch_bounds__(2 * LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void latent_replay_dkv_kernel(LatentReplayArgs a)
 {
-    constexpr int E = D / 2, KC = D / 16, RC = E / 16, DT = D / 32, ET = E / 32, KB = D * 2, RB = E * 2;
-    // a tile of queries: their two parts, the gradients that arrive at them, and -lse (in powers of 2) and delta
-    constexpr int ROT = LR_TILE * KB, G = ROT + LR_TILE * RB, BYTES = G + LR_TILE * KB;
+    constexpr int E = D / 2, KC = D / 16, RC = E / 16, DT = D / 32, ET = E / 32, KB = D * 2, RB = E * 2, PAIRS = DT / 2;
+    // 32 queries in LDS: their two parts, the gradients that arrive at them, and their statistics
+    constexpr int ROT = LR_STEP * KB, G = ROT + LR_STEP * RB, STATS = G + LR_STEP * KB, BYTES = STATS + 2 * LR_STEP * 4;
     extern __shared__ __align__(16) unsigned char lds[];
-    float *const stats = reinterpret_cast<float *>(lds + 3 * BYTES);       // [3][2][LR_TILE]
-    const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), wv = wave % LR_WAVES, second = wave / LR_WAVES;
     const int li = lane & 31, half = lane >> 5;
     const LatentReplayPlace at(a, (a.T + LR_BLOCK - 1) / LR_BLOCK, false);
     const int n = at.length(a);
     if (at.block * LR_BLOCK >= n) return;
     const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
-    const int unit = death ? unit_by_end(death, n, at.block * LR_WAVES + wv, reinterpret_cast<int *>(lds)) : at.block * LR_WAVES + wv;
+    const int unit = death ? unit_by_end<2 * LR_WAVES>(death, n, at.block * LR_WAVES + wv, reinterpret_cast<int *>(lds)) : at.block * LR_WAVES + wv;
     const int wave0 = unit * LR_OWN, key = wave0 + li, k_row = key < n ? key : n - 1;
     // queries key .. until - 1 see this lane's key
     int until = n;
@@ -678,18 +709,6 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
         begins[wv] = wave0;
         ends[wv] = wave_end;
     }
-
-    bf16x8 k[KC + RC], v[KC];
-    {
-        const unsigned char *kr = a.kv + (((size_t)at.b * a.T + k_row) * a.H + at.h) * (2 * KB) + half * 16;
-        const unsigned char *rr = a.rope + ((size_t)at.b * a.T + k_row) * a.rope_row + half * 16;
-#pragma unroll
-        for (int c = 0; c < KC; ++c) k[c] = operand(*reinterpret_cast<const u32x4 *>(kr + c * 32));
-#pragma unroll
-        for (int c = 0; c < RC; ++c) k[KC + c] = operand(*reinterpret_cast<const u32x4 *>(rr + c * 32));
-#pragma unroll
-        for (int c = 0; c < KC; ++c) v[c] = operand(*reinterpret_cast<const u32x4 *>(kr + KB + c * 32));
-    }
     __syncthreads();
     int begin = n, end = 0;
 #pragma unroll
@@ -697,189 +716,200 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
         begin = smaller(begin, begins[w]);
         end = larger(end, ends[w]);
     }
-    const int first = __builtin_amdgcn_readfirstlane(begin) / LR_TILE, tiles = (__builtin_amdgcn_readfirstlane(end) + LR_TILE - 1) / LR_TILE;
+    const int first = __builtin_amdgcn_readfirstlane(begin) / LR_STEP, units = (__builtin_amdgcn_readfirstlane(end) + LR_STEP - 1) / LR_STEP;
 
+    const bool some = first < units;                       // (no query sees any of the keys: no unit to read)
     const size_t stat = ((size_t)at.b * a.H + at.h) * a.T;
-    auto load_tile = [&](int t, unsigned char *to) {
-        const int i = t * LR_TILE, last = a.T - 1 - i;
+    const uint32_t q_stride = (uint32_t)a.H * ((D + E) * 2), g_stride = (uint32_t)a.H * KB;
+    // A unit: the first waves bring the queries, the second ones the gradients and (each of them, they count alike) the statistics.
+    constexpr int LOADS = LdsRows<KB>::UNIT_LOADS + 1;     // of a wave
+    static_assert(LdsRows<RB>::UNIT_LOADS == 1, "the same number for all waves");
+    auto slot = [&](int u) { return lds + (u - first) % LR_SLOTS * BYTES; };
+    auto load_ahead = [&](int u_) {
+        const int u = u_ < units ? u_ : units - 1;         // (the last one again into a free place)
+        const int i = u * LR_STEP, last = a.T - 1 - i;
+        unsigned char *const to = slot(u_);
         const size_t row = ((size_t)at.b * a.T + i) * a.H + at.h;
-        const uint32_t stride = (uint32_t)a.H * ((D + E) * 2), g_stride = (uint32_t)a.H * KB;
-        const int second = last < LR_STEP ? last : LR_STEP;                // row of the tile where the second unit begins
-        const int lasts[2] = {last, last - second};
-        const unsigned char *const q = a.q + row * ((D + E) * 2), *const g = a.dout + row * KB;
-        const unsigned char *const q2[2] = {q, q + second * (size_t)stride}, *const r2[2] = {q2[0] + KB, q2[1] + KB}, *const g2[2] = {g, g + second * (size_t)g_stride};
-        LdsRows<KB>::load(q2, stride, lasts, to, wv, lane);
-        LdsRows<RB>::load(r2, stride, lasts, to + ROT, wv, lane);
-        LdsRows<KB>::load(g2, g_stride, lasts, to + G, wv, lane);
-    };
-    auto load_stat = [&](int t) {                          // threads 0 .. 63: lse, the next 64: delta
-        const int i = t * LR_TILE + ((int)threadIdx.x & (LR_TILE - 1));
-        return threadIdx.x < 2 * LR_TILE ? (threadIdx.x < LR_TILE ? a.lse : a.delta)[stat + (i < n ? i : n - 1)] : 0.f;
-    };
-    uint32_t q_at[KC], r_at[RC], g_at[KC], qt_at[DT][2], rt_at[ET][2], gt_at[DT][2];
-#pragma unroll
-    for (int c = 0; c < KC; ++c) {
-        q_at[c] = LdsRows<KB>::row_piece(li, half, c);
-        g_at[c] = G + q_at[c];
-    }
-#pragma unroll
-    for (int c = 0; c < RC; ++c) r_at[c] = ROT + LdsRows<RB>::row_piece(li, half, c);
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-#pragma unroll
-        for (int c = 0; c < DT; ++c) {
-            qt_at[c][g] = LdsRows<KB>::column(lane, g, c);
-            gt_at[c][g] = G + qt_at[c][g];
-        }
-#pragma unroll
-        for (int c = 0; c < ET; ++c) rt_at[c][g] = ROT + LdsRows<RB>::column(lane, g, c);
-    }
-    f32x16 dv[DT], dk[DT], dr[ET];
-#pragma unroll
-    for (int c = 0; c < DT; ++c) dv[c] = dk[c] = zeros16();
-#pragma unroll
-    for (int c = 0; c < ET; ++c) dr[c] = zeros16();
-    float poison = 0.f;                                    // NaN: a gradient that is not finite arrives at a query that sees the key
-
-    struct Pairs {
-        f32x16 s, dp;                                      // scores and <g, v>
-    };
-    auto scores = [&](const unsigned char *tile, int st, Pairs &x) {
-        x.s = x.dp = zeros16();
-#pragma unroll
-        for (int c = 0; c < KC; ++c) x.s = product(operand(*reinterpret_cast<const u32x4 *>(tile + q_at[c] + st * LR_STEP * KB)), k[c], x.s);
-#pragma unroll
-        for (int c = 0; c < RC; ++c) x.s = product(operand(*reinterpret_cast<const u32x4 *>(tile + r_at[c] + st * LR_STEP * RB)), k[KC + c], x.s);
-#pragma unroll
-        for (int c = 0; c < KC; ++c) x.dp = product(operand(*reinterpret_cast<const u32x4 *>(tile + g_at[c] + st * LR_STEP * KB)), v[c], x.dp);
-    };
-    struct Weights {
-        uint32_t p[8], ds[8];
-    };
-    auto weights = [&](const float *st_, int st, const Pairs &x, Weights &w) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x4 neg_lse = *reinterpret_cast<const f32x4 *>(st_ + st * LR_STEP + 8 * g + 4 * half);
-            const f32x4 delta = *reinterpret_cast<const f32x4 *>(st_ + LR_TILE + st * LR_STEP + 8 * g + 4 * half);
-            float p[4], ds[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                p[e] = fast_exp2(__builtin_fmaf(x.s[4 * g + e], a.scale_log2e, neg_lse[e]));
-                ds[e] = p[e] * (x.dp[4 * g + e] - delta[e]);
-            }
-            w.p[2 * g] = pack_bf16(p[0], p[1]);
-            w.p[2 * g + 1] = pack_bf16(p[2], p[3]);
-            w.ds[2 * g] = pack_bf16(ds[0], ds[1]);
-            w.ds[2 * g + 1] = pack_bf16(ds[2], ds[3]);
+        int lane_ = lane;
+        __asm__ volatile("" : "+v"(lane_));                // (offsets are made where they are used)
+        if (!second) {
+            const unsigned char *const q = a.q + row * ((D + E) * 2);
+            LdsRows<KB>::load_unit(q, q_stride, last, to, wv, lane_);
+            LdsRows<RB>::load_unit(q + KB, q_stride, last, to + ROT, wv, lane_);
+        } else {
+            LdsRows<KB>::load_unit(a.dout + row * KB, g_stride, last, to + G, wv, lane_);
+            const int r = lane_ & 31;
+            start_load_to_lds4(reinterpret_cast<const unsigned char *>(a.stats + stat * 2 + i), (uint32_t)((r < last ? r : last) + (lane_ >> 5) * a.T) * 4u, to + STATS);
         }
     };
-    // Weights of 0 for the pairs of a step that are masked.
-    auto mask = [&](int query0, Weights &w) {
-        uint32_t keep[8];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int i = query0 + row_of(r, half);
-            const uint32_t bits = key <= i && i < until ? 0xFFFFu : 0u;
-            keep[r / 2] = r % 2 ? keep[r / 2] | bits << 16 : bits;
-        }
+    // P of a unit, from the first wave to the second: two places, fp32 as the products leave it.
+    unsigned char *const exchange = lds + LR_SLOTS * BYTES + wv * (2 * 4096) + lane * 16;
+    auto place = [&](int u) { return exchange + (u & 1) * 4096; };
+    // units mine_first .. mine_end - 1 have queries that see keys of this wave (a loop of their own: with a branch in it the sums would be
+    // kept twice)
+    const int mine_first = unit < units ? unit : units, mine_end = larger(mine_first, (wave_end + LR_STEP - 1) / LR_STEP);
+    auto mixed_at = [&](int u) { return u * LR_STEP < wave0 + LR_OWN - 1 || (u + 1) * LR_STEP > wave_all; };
+    // Weights of 0 for the pairs of a unit that are masked.
+    auto mask = [&](int query0, uint32_t (&w)[8]) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            w.p[e] &= keep[e];
-            w.ds[e] &= keep[e];
+            const int i = query0 + row_of(2 * e, half);
+            w[e] &= (key <= i && i < until ? 0xFFFFu : 0u) | (key <= i + 1 && i + 1 < until ? 0xFFFF0000u : 0u);
         }
     };
-    constexpr int PAIRS = DT / 2;
-    auto ask = [&](const unsigned char *tile, int st, int pair, Columns &to) {
-        if (pair < PAIRS) ask_columns<KB>(tile + st * LR_STEP * KB, gt_at, pair, to);
-        else if (pair < 2 * PAIRS) ask_columns<KB>(tile + st * LR_STEP * KB, qt_at, pair - PAIRS, to);
-        else ask_columns<RB>(tile + st * LR_STEP * RB, rt_at, 0, to);
-    };
-    auto gradients = [&](const unsigned char *tile, int st, const Weights &w, bool mixed, Columns (&x)[2]) {
-        bool odd = false;
+    // acc += X y for a unit's rows: COUNT operands, at(c) in the unit and y(c), GROUP of them asked for while the products of those before run.
+    auto rows_product = [&](auto count, const unsigned char *from, auto at_, auto y, f32x16 acc) {
+        constexpr int COUNT = decltype(count)::value, GROUP = COUNT % 4 ? 3 : 4, GROUPS = COUNT / GROUP;
+        static_assert(COUNT % GROUP == 0, "whole groups");
+        u32x4 rows[2][GROUP];
+        auto ask = [&](int g) {
 #pragma unroll
-        for (int pair = 0; pair <= 2 * PAIRS; ++pair) {
-            if (pair < 2 * PAIRS) ask(tile, st, pair + 1, x[(pair + 1) & 1]);
-            // (a query that sees the key and is not finite has made dS NaN)
-            if (pair < PAIRS) odd |= add_columns(x[pair & 1], pair, w.p, mixed, dv);
-            else if (pair < 2 * PAIRS) (void)add_columns(x[pair & 1], pair - PAIRS, w.ds, mixed, dk);
-            else (void)add_columns(x[pair & 1], 0, w.ds, mixed, dr);
-        }
-        return odd;
-    };
-    // A step's weights, while the scores of the next one are made (whether anybody needs them or not), and its gradients.
-    auto step = [&](const unsigned char *tile, const float *st_, int st, int query0, Pairs &x, const unsigned char *next_tile, int next_st) {
-        const bool mixed = query0 < wave0 + LR_OWN - 1 || query0 + LR_STEP > wave_all;
-        Pairs y;
-        Weights w;
-        Columns columns[2];
-        scores(next_tile, next_st, y);
-        ask(tile, st, 0, columns[0]);
-        weights(st_, st, x, w);
-        x = y;
-        if (mixed) mask(query0, w);
-        if (__ballot(gradients(tile, st, w, mixed, columns))) {
-            const uint32_t rows = odd_rows<KB>(tile + G + st * LR_STEP * KB);
+            for (int u = 0; u < GROUP; ++u) rows[g & 1][u] = *reinterpret_cast<const u32x4 *>(from + at_(g * GROUP + u));
+        };
+        ask(0);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int i = query0 + row_of(r, half);
-                if (((rows >> row_of(r, half)) & 1u) && key <= i && i < until) poison = NAN;
-            }
-        }
-    };
-    // Three tiles in LDS: the one whose gradients are made, the next one, whose scores follow, and the one behind it, on its way.
-    auto stage_stat = [&](int slot, float x) {
-        if (threadIdx.x < 2 * LR_TILE) stats[slot * 2 * LR_TILE + threadIdx.x] = threadIdx.x < LR_TILE ? -x * 1.4426950408889634f : x;
-    };
-    auto needed = [&](int query0) { return query0 + LR_STEP > wave0 && query0 < wave_end; };
-    if (first < tiles) {
-        Pairs x;
-        load_tile(first, lds);
-        stage_stat(0, load_stat(first));
-        lds_loads_done();
-        float stat_next = 0.f;
-        if (first + 1 < tiles) {
-            load_tile(first + 1, lds + BYTES);
-            stat_next = load_stat(first + 1);
-        }
-        if (needed(first * LR_TILE)) scores(lds, 0, x);
-        int cur = 0;
-        for (int t = first; t < tiles; ++t) {
-            const int next = cur == 2 ? 0 : cur + 1, after = next == 2 ? 0 : next + 1;
-            const unsigned char *const here = lds + cur * BYTES, *const there = lds + next * BYTES;
-            stage_stat(next, stat_next);
-            lds_loads_done();                              // tile t + 1 is there, and everybody has left tile t - 1
-            if (t + 2 < tiles) {
-                load_tile(t + 2, lds + after * BYTES);
-                stat_next = load_stat(t + 2);
-            }
+        for (int g = 0; g < GROUPS; ++g) {
+            if (g + 1 < GROUPS) ask(g + 1);
             __builtin_amdgcn_sched_barrier(0);
-            const float *const st_ = stats + cur * 2 * LR_TILE;
-            const int query0 = t * LR_TILE;
-            if (needed(query0)) step(here, st_, 0, query0, x, here, 1);
-            else if (needed(query0 + LR_STEP)) scores(here, 1, x);
-            if (needed(query0 + LR_STEP)) step(here, st_, 1, query0 + LR_STEP, x, there, 0);
-            else if (needed(query0 + 2 * LR_STEP)) scores(there, 0, x);
-            __builtin_amdgcn_sched_barrier(0);
-            cur = next;
-        }
-    }
-    __syncthreads();
-    poison += __shfl_xor(poison, 32);                      // (NaN in either half of the key's registers)
 #pragma unroll
-    for (int c = 0; c < DT; ++c) dv[c] += poison;
-    unsigned char *const mine = lds + wv * LR_OWN * KB;
+            for (int u = 0; u < GROUP; ++u) acc = product(operand(rows[g & 1][u]), y(g * GROUP + u), acc);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        return acc;
+    };
+    // (addresses are made where they are used: kept, they would cost registers that the sums need)
+    auto fresh = [](uint32_t x) {
+        __asm__ volatile("" : "+v"(x));
+        return x;
+    };
+    auto round_begins = [&](int u) {
+        wait_for_loads<(LR_SLOTS - 3) * LOADS>();          // unit u is there, P of the one before too
+        workgroup_barrier();                               // and everybody has left unit u - 2
+        load_ahead(u + LR_SLOTS - 2);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const unsigned char *const kr = a.kv + (((size_t)at.b * a.T + k_row) * a.H + at.h) * (2 * KB) + half * 16;
+    unsigned char *const mine = lds + wave * LR_OWN * KB;
     const size_t stride = (size_t)a.H * (2 * KB);
     unsigned char *const to = a.dkv + (((size_t)at.b * a.T + wave0) * a.H + at.h) * (2 * KB);
-    store_rows(mine, dk, a.scale, to, stride, n - wave0);
-    store_rows(mine, dv, 1.0f, to + KB, stride, n - wave0);
-    if (key < n) {
-        float *part = a.part + (stat + key) * E;
+    if (!second) {
+        bf16x8 k[KC + RC];
+        const unsigned char *const rr = a.rope + ((size_t)at.b * a.T + k_row) * a.rope_row + half * 16;
 #pragma unroll
-        for (int c = 0; c < ET; ++c)
+        for (int c = 0; c < KC; ++c) k[c] = operand(*reinterpret_cast<const u32x4 *>(kr + c * 32));
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<f32x4 *>(part + 32 * c + 8 * g + 4 * half) =
-                    f32x4{dr[c][4 * g] * a.scale, dr[c][4 * g + 1] * a.scale, dr[c][4 * g + 2] * a.scale, dr[c][4 * g + 3] * a.scale};
+        for (int c = 0; c < RC; ++c) k[KC + c] = operand(*reinterpret_cast<const u32x4 *>(rr + c * 32));
+        const uint32_t q_first = LdsRows<KB>::row_piece(li, half, 0), r_first = LdsRows<RB>::row_piece(li, half, 0);
+        const uint32_t gt_first[2] = {LdsRows<KB>::column(lane, 0, 0), LdsRows<KB>::column(lane, 1, 0)};
+        f32x16 dv[DT];
+#pragma unroll
+        for (int c = 0; c < DT; ++c) dv[c] = zeros16();
+        float poison = 0.f;                                // NaN: a gradient that is not finite arrives at a query that sees the key
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+        for (int u = first; some && u < first + LR_SLOTS - 2; ++u) load_ahead(u);
+        for (int u = first; u < mine_first; ++u) round_begins(u);
+        for (int u = mine_first; u < mine_end; ++u) {
+            round_begins(u);
+            const unsigned char *const here = slot(u);
+            const bool mixed = mixed_at(u);
+            const uint32_t q_0 = fresh(q_first), r_0 = fresh(r_first);
+            const f32x16 s = rows_product(std::integral_constant<int, KC + RC>{}, here, [&](int c) { return c < KC ? q_0 ^ c * 32 : ROT + (r_0 ^ (c - KC) * 32); },
+                                          [&](int c) { return k[c]; }, zeros16());
+            uint32_t w[8];
+            Columns x[2];
+            const uint32_t gt_0[2] = {fresh(gt_first[0]), fresh(gt_first[1])};
+            ask_columns<KB, DT>(here + G, gt_0, 0, x[0]);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 neg_lse = *reinterpret_cast<const f32x4 *>(here + STATS + (8 * g + 4 * half) * 4);
+                f32x4 p;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[e] = fast_exp2(__builtin_fmaf(s[4 * g + e], a.scale_log2e, neg_lse[e]));
+                *reinterpret_cast<f32x4 *>(place(u) + g * 1024) = p;
+                w[2 * g] = pack_bf16(p[0], p[1]);
+                w[2 * g + 1] = pack_bf16(p[2], p[3]);
+            }
+            if (mixed) mask(u * LR_STEP, w);
+            bool odd = false;
+#pragma unroll
+            for (int pair = 0; pair < PAIRS; ++pair) {
+                if (pair + 1 < PAIRS) ask_columns<KB, DT>(here + G, gt_0, pair + 1, x[(pair + 1) & 1]);
+                __builtin_amdgcn_sched_barrier(0);
+                odd |= add_columns(x[pair & 1], pair, w, mixed, dv);
+            }
+            if (__ballot(odd)) {
+                const uint32_t rows = odd_rows<KB>(here + G);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int i = u * LR_STEP + row_of(r, half);
+                    if (((rows >> row_of(r, half)) & 1u) && key <= i && i < until) poison = NAN;
+                }
+            }
+        }
+        for (int u = mine_end; some && u <= units; ++u) round_begins(u);
+        lds_loads_done();
+        poison += __shfl_xor(poison, 32);                  // (NaN in either half of the key's registers)
+#pragma unroll
+        for (int c = 0; c < DT; ++c) dv[c] += poison;
+        store_rows(mine, dv, 1.0f, to + KB, stride, n - wave0);
+    } else {
+        bf16x8 v[KC];
+#pragma unroll
+        for (int c = 0; c < KC; ++c) v[c] = operand(*reinterpret_cast<const u32x4 *>(kr + KB + c * 32));
+        const uint32_t g_first = LdsRows<KB>::row_piece(li, half, 0);
+        const uint32_t qt_first[2] = {LdsRows<KB>::column(lane, 0, 0), LdsRows<KB>::column(lane, 1, 0)};
+        const uint32_t rt_first[2] = {LdsRows<RB>::column(lane, 0, 0), LdsRows<RB>::column(lane, 1, 0)};
+        f32x16 dk[DT], dr[ET];
+#pragma unroll
+        for (int c = 0; c < DT; ++c) dk[c] = zeros16();
+#pragma unroll
+        for (int c = 0; c < ET; ++c) dr[c] = zeros16();
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+        for (int u = first; some && u < first + LR_SLOTS - 2; ++u) load_ahead(u);
+        for (int u = first - 1; some && u < mine_first; ++u) round_begins(u + 1);
+        for (int u = mine_first; u < mine_end; ++u) {
+            round_begins(u + 1);
+            const unsigned char *const here = slot(u);
+            const bool mixed = mixed_at(u);
+            const uint32_t g_0 = fresh(g_first);
+            const f32x16 dp = rows_product(std::integral_constant<int, KC>{}, here, [&](int c) { return G + (g_0 ^ c * 32); }, [&](int c) { return v[c]; }, zeros16());
+            uint32_t w[8];
+            Columns x[2];
+            const uint32_t qt_0[2] = {fresh(qt_first[0]), fresh(qt_first[1])};
+            ask_columns<KB, DT>(here, qt_0, 0, x[0]);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 delta = *reinterpret_cast<const f32x4 *>(here + STATS + (LR_STEP + 8 * g + 4 * half) * 4);
+                const f32x4 p = *reinterpret_cast<const f32x4 *>(place(u) + g * 1024);
+                float ds[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ds[e] = p[e] * (dp[4 * g + e] - delta[e]);
+                w[2 * g] = pack_bf16(ds[0], ds[1]);
+                w[2 * g + 1] = pack_bf16(ds[2], ds[3]);
+            }
+            if (mixed) mask(u * LR_STEP, w);
+#pragma unroll
+            for (int pair = 0; pair <= PAIRS; ++pair) {
+                if (pair + 1 < PAIRS) ask_columns<KB, DT>(here, qt_0, pair + 1, x[(pair + 1) & 1]);
+                else if (pair + 1 == PAIRS) ask_columns<RB, ET>(here + ROT, rt_first, 0, x[(pair + 1) & 1]);
+                __builtin_amdgcn_sched_barrier(0);
+                // (a query that sees the key and is not finite has made dS NaN)
+                if (pair < PAIRS) (void)add_columns(x[pair & 1], pair, w, mixed, dk);
+                else (void)add_columns(x[pair & 1], 0, w, mixed, dr);
+            }
+        }
+        for (int u = mine_end; some && u < units; ++u) round_begins(u + 1);
+        lds_loads_done();
+        store_rows(mine, dk, a.scale, to, stride, n - wave0);
+        if (key < n) {
+            float *part = a.part + (stat + key) * E;
+#pragma unroll
+            for (int c = 0; c < ET; ++c)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<f32x4 *>(part + 32 * c + 8 * g + 4 * half) =
+                        f32x4{dr[c][4 * g] * a.scale, dr[c][4 * g + 1] * a.scale, dr[c][4 * g + 2] * a.scale, dr[c][4 * g + 3] * a.scale};
+        }
     }
 }
 
@@ -937,13 +967,13 @@ LatentReplayArgs latent_replay_args(const void *q, const void *kv, const void *r
     return a;
 }
 
-size_t latent_replay_delta_bytes(int32_t B, int32_t T, int32_t Hq) { return align256((size_t)B * Hq * T * sizeof(float)); }
+size_t latent_replay_stats_bytes(int32_t B, int32_t T, int32_t Hq) { return align256((size_t)B * Hq * T * 2 * sizeof(float)); }
 
-int launch_blocks(const void *fn, const LatentReplayArgs &args, size_t lds, hipStream_t st)
+int launch_blocks(const void *fn, const LatentReplayArgs &args, int waves, size_t lds, hipStream_t st)
 {
     LatentReplayArgs a = args;
     if (lds > 64 * 1024) NGC_HIP_CHECK(hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    return launch(fn, dim3((unsigned)((a.T + LR_BLOCK - 1) / LR_BLOCK * a.B * a.H)), dim3(LR_WAVES * 64), lds, st, a);
+    return launch(fn, dim3((unsigned)((a.T + LR_BLOCK - 1) / LR_BLOCK * a.B * a.H)), dim3(waves * 64), lds, st, a);
 }
 
 }  // namespace
@@ -951,7 +981,7 @@ int launch_blocks(const void *fn, const LatentReplayArgs &args, size_t lds, hipS
 extern "C" size_t ngc_latent_replay_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t D)
 {
     if (!latent_replay_sizes(B, T, Hq, D)) return 0;
-    return latent_replay_delta_bytes(B, T, Hq) + (size_t)B * Hq * T * (D / 2) * sizeof(float);
+    return latent_replay_stats_bytes(B, T, Hq) + (size_t)B * Hq * T * (D / 2) * sizeof(float);
 }
 
 extern "C" int ngc_latent_replay_attn(const void *q, const void *kv, const void *rope, int64_t rope_stride, const int32_t *death,
@@ -964,7 +994,7 @@ extern "C" int ngc_latent_replay_attn(const void *q, const void *kv, const void 
     a.out = reinterpret_cast<unsigned char *>(out);
     a.lse = lse_out;
     const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_kernel<64>);
-    return launch_blocks(fn, a, 2 * (D == 128 ? KeyTile<128>::BYTES : KeyTile<64>::BYTES), (hipStream_t)stream);
+    return launch_blocks(fn, a, LR_WAVES, 2 * (D == 128 ? KeyTile<128>::BYTES : KeyTile<64>::BYTES), (hipStream_t)stream);
 }
 
 extern "C" int ngc_latent_replay_attn_backward(const void *q, const void *kv, const void *rope, int64_t rope_stride, const int32_t *death,
@@ -984,14 +1014,14 @@ extern "C" int ngc_latent_replay_attn_backward(const void *q, const void *kv, co
     a.dq = reinterpret_cast<unsigned char *>(dq);
     a.dkv = reinterpret_cast<unsigned char *>(dkv);
     a.drope = reinterpret_cast<unsigned char *>(drope);
-    a.delta = reinterpret_cast<float *>(ws);
-    a.part = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(ws) + latent_replay_delta_bytes(B, T, Hq));
+    a.stats = reinterpret_cast<float *>(ws);
+    a.part = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(ws) + latent_replay_stats_bytes(B, T, Hq));
     hipStream_t st = (hipStream_t)stream;
     const size_t lds = 2 * (D == 128 ? KeyTile<128>::BYTES : KeyTile<64>::BYTES);
-    rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dq_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dq_kernel<64>), a, lds, st);
+    rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dq_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dq_kernel<64>), a, LR_WAVES, lds, st);
     if (rc) return rc;
     rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dkv_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dkv_kernel<64>), a,
-                       lds / 2 * 3 + 6 * LR_TILE * sizeof(float), st);
+                       2 * LR_WAVES, LR_SLOTS * (lds / 4 + 2 * LR_STEP * sizeof(float)) + LR_WAVES * 2 * 4096, st);
     if (rc) return rc;
     const long long threads = (long long)B * T * (D / 2 / 4);
     const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_rope_kernel<64>) : reinterpret_cast<const void *>(&latent_replay_rope_kernel<32>);
