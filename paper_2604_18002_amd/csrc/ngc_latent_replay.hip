@@ -40,8 +40,7 @@ namespace ngc {
 constexpr int LR_WAVES = 4;
 constexpr int LR_OWN = 32;                   // queries (keys) of a wave
 constexpr int LR_BLOCK = LR_WAVES * LR_OWN;  // of a workgroup
-constexpr int LR_TILE = 64;                  // keys (queries) of a tile
-constexpr int LR_STEP = 32;                  // of a step of the math
+constexpr int LR_STEP = 32;                  // keys (queries) of a unit: a step of the math
 constexpr int LR_MOST_POSITIONS = 64 * 64 * LR_STEP;       // a bit of a lane's words per LR_STEP keys
 constexpr int LR_SLOTS = 6;                  // units of queries in LDS: the most of D = 128
 constexpr float LR_LAZY = 8.0f;              // the reference of the exponents moves when a maximum has outgrown it by 2^8
@@ -73,23 +72,9 @@ struct LdsRows {
     {
         return lds_swizzle<PIECES>(r);
     }
-    // Two units of LR_STEP rows from memory straight to LDS, rows `stride` bytes apart; rows behind `last` of a unit are that one again.
-    // In LOADS parts, of all waves together.  (The swizzle is linear in a row's bits: a lane's part of it, and the load's.)
-    static constexpr int LOADS = LR_TILE / (LR_WAVES * LOAD_ROWS);
-    __device__ static __forceinline__ void load_part(const unsigned char *const (&from)[2], uint32_t stride, const int (&last)[2], unsigned char *to,
-                                                     int i, int wv, int lane)
-    {
-        const int lrow = lane / PIECES, piece = lane % PIECES ^ swizzle(lrow);
-        const int r0 = (i * LR_WAVES + wv) * LOAD_ROWS, unit = r0 / LR_STEP, r = r0 % LR_STEP + lrow, end = unit ? last[1] : last[0];
-        start_load_to_lds16(unit ? from[1] : from[0], (uint32_t)(r < end ? r : end) * stride + (uint32_t)(piece ^ swizzle(r0)) * 16u, to + r0 * BYTES);
-    }
-    __device__ static __forceinline__ void load(const unsigned char *const (&from)[2], uint32_t stride, const int (&last)[2], unsigned char *to,
-                                                int wv, int lane)
-    {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) load_part(from, stride, last, to, i, wv, lane);
-    }
-    // One unit, by all waves; where there are more waves than loads, some load again what others do.
+    // LR_STEP rows from memory straight to LDS, rows `stride` bytes apart, by LR_WAVES waves; rows behind `last` are that one again, and
+    // where there are more waves than loads, some load again what others do.  (The swizzle is linear in a row's bits: a lane's part of
+    // it, and the load's.)
     static constexpr int UNIT_LOADS = (LR_STEP / LOAD_ROWS + LR_WAVES - 1) / LR_WAVES;
     __device__ static __forceinline__ void load_unit(const unsigned char *from, uint32_t stride, int last, unsigned char *to, int wv, int lane)
     {
@@ -126,6 +111,12 @@ __device__ __forceinline__ f32x16 zeros16()
     for (int r = 0; r < 16; ++r) x[r] = 0.f;
     return x;
 }
+// (A value of the loop's own: what is made of it is made where it is used, not kept in registers that the sums need.)
+__device__ __forceinline__ uint32_t fresh(uint32_t x)
+{
+    __asm__ volatile("" : "+v"(x));
+    return x;
+}
 // Row of a tile that register r of a lane's half stands for.
 __device__ __forceinline__ int row_of(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
 
@@ -134,7 +125,8 @@ __device__ __forceinline__ int row_of(int r, int half) { return 8 * (r / 4) + 4 
 struct Columns {
     u32x2 v[2][2][2];                        // [column tile][16 rows][8 of them]
 };
-// Column tile c of CT, rows BYTES: from x; `at`: where a lane points for the first column tile of a pair (of 64 columns: 128 bytes on).
+// Two column tiles of CT, rows of BYTES from x; `first`: where a lane points for column tile 0.  (Offsets of the others differ in a bit
+// of their own: no register is kept for them.)
 template <int BYTES, int CT>
 __device__ __forceinline__ void ask_columns(const unsigned char *x, const uint32_t (&first)[2], int pair, Columns &to)
 {
@@ -144,16 +136,6 @@ __device__ __forceinline__ void ask_columns(const unsigned char *x, const uint32
         for (int st = 0; st < 2; ++st)
 #pragma unroll
             for (int g = 0; g < 2; ++g) to.v[u][st][g] = read_transposed16(x + (first[g] ^ (2 * pair + u) * 64) + 16 * st * BYTES);
-}
-template <int BYTES, int CT>
-__device__ __forceinline__ void ask_columns(const unsigned char *x, const uint32_t (&at)[CT][2], int pair, Columns &to)
-{
-#pragma unroll
-    for (int u = 0; u < 2 && 2 * pair + u < CT; ++u)
-#pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-            for (int g = 0; g < 2; ++g) to.v[u][st][g] = read_transposed16(x + at[2 * pair + u][g] + 16 * st * BYTES);
 }
 // `mixed`: some pairs are masked; values that are not finite are taken for 0 then.  Returns whether there were some.
 template <int CT>
@@ -244,16 +226,6 @@ struct LiveUnits {
     __device__ __forceinline__ bool whole(int u) const { return (word(all_lo, all_hi, u) >> (u % 32)) & 1u; }
 };
 
-// Two live units that make a tile; the second may be none (`units`).
-struct UnitPair {
-    int u[2];
-    __device__ __forceinline__ UnitPair(const LiveUnits &live, int from)
-    {
-        u[0] = live.next(from);
-        u[1] = live.next(u[0] + 1);
-    }
-};
-
 // What a workgroup that owns queries (forward, backward q) or keys (backward kv) works on: heaviest first, a (trajectory, head) on
 // one XCD, whose L2 then holds its rows.
 struct LatentReplayPlace {
@@ -273,28 +245,51 @@ struct LatentReplayPlace {
     }
 };
 
-// The tiles of keys in LDS that the two kernels with queries of their own walk.
+// Live units of keys, two at a time, through two places in LDS, for the two kernels with queries of their own.
 template <int D>
-struct KeyTile {
-    static constexpr int E = D / 2, KB = D * 2, RB = E * 2;
-    static constexpr int ROT = LR_TILE * KB, V = ROT + LR_TILE * RB, BYTES = V + LR_TILE * KB;
-    __device__ static __forceinline__ void load(const LatentReplayArgs &a, int b, int h, const LiveUnits &live, const UnitPair &t, unsigned char *to,
-                                                int wv, int lane)
+struct KeyTiles {
+    static constexpr int KB = D * 2, RB = D, ROT = LR_STEP * KB, V = ROT + LR_STEP * RB, UNIT = V + LR_STEP * KB, BYTES = 4 * UNIT;
+    const LatentReplayArgs &a;
+    const LiveUnits &live;
+    unsigned char *here, *there;
+    int b, h, wv, lane;
+    int unit[2];                             // of the next tile, on its way (`units`: none)
+    __device__ __forceinline__ KeyTiles(const LatentReplayArgs &a_, const LiveUnits &live_, unsigned char *lds, int b_, int h_, int wv_, int lane_)
+        : a(a_), live(live_), here(lds), there(lds + 2 * UNIT), b(b_), h(h_), wv(wv_), lane(lane_)
     {
-        const unsigned char *k[2], *v[2], *r[2];
-        int last[2];
+        ask(0);
+    }
+    __device__ __forceinline__ bool more() const { return unit[0] < live.units; }
+    __device__ __forceinline__ void ask(int from)
+    {
+        unit[0] = live.next(from);
+        unit[1] = live.next(unit[0] + 1);
+        if (!more()) return;
+        const int lane = (int)fresh((uint32_t)this->lane);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int first = (t.u[i] < live.units ? t.u[i] : t.u[0]) * LR_STEP;       // (none: the first again)
-            last[i] = a.T - 1 - first;                     // of the memory; behind the sequence's end nothing is seen
-            k[i] = a.kv + (((size_t)b * a.T + first) * a.H + h) * (2 * KB);
-            v[i] = k[i] + KB;
-            r[i] = a.rope + ((size_t)b * a.T + first) * a.rope_row;
+            const int first = unit[unit[i] < live.units ? i : 0] * LR_STEP;        // (none: the first again)
+            const int last = a.T - 1 - first;              // of the memory; behind the sequence's end nothing is seen
+            unsigned char *const to = there + i * UNIT;
+            const unsigned char *const k = a.kv + (((size_t)b * a.T + first) * a.H + h) * (2 * KB);
+            const uint32_t stride = (uint32_t)a.H * (2 * KB);
+            LdsRows<KB>::load_unit(k, stride, last, to, wv, lane);
+            LdsRows<RB>::load_unit(a.rope + ((size_t)b * a.T + first) * a.rope_row, (uint32_t)a.rope_row, last, to + ROT, wv, lane);
+            LdsRows<KB>::load_unit(k + KB, stride, last, to + V, wv, lane);
         }
-        const uint32_t stride = (uint32_t)a.H * (2 * KB);
-        LdsRows<KB>::load(k, stride, last, to, wv, lane);
-        LdsRows<RB>::load(r, (uint32_t)a.rope_row, last, to + ROT, wv, lane);
-        LdsRows<KB>::load(v, stride, last, to + V, wv, lane);
+    }
+    // The next tile, in LDS until the next call; u: its units.  By all waves.
+    __device__ __forceinline__ const unsigned char *take(int (&u)[2])
+    {
+        u[0] = unit[0];
+        u[1] = unit[1];
+        unsigned char *const x = here;
+        here = there;
+        there = x;
+        lds_loads_done();
+        ask(u[1] + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        return here;
     }
 };
 
@@ -316,7 +311,7 @@ template <int D>
 __global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void latent_replay_kernel(LatentReplayArgs a)
 {
-    using Tile = KeyTile<D>;
+    using Tiles = KeyTiles<D>;
     constexpr int E = D / 2, KC = D / 16, RC = E / 16, DT = D / 32;
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
@@ -328,8 +323,7 @@ void latent_replay_kernel(LatentReplayArgs a)
     const int wave_last = wave0 + LR_OWN - 1 < n ? wave0 + LR_OWN - 1 : n - 1, block_last = i0 + LR_BLOCK - 1 < n ? i0 + LR_BLOCK - 1 : n - 1;
     const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
     const LiveUnits live(death, block_last / LR_STEP + 1, n, i0, block_last);
-    UnitPair t(live, 0);
-    if (t.u[0] < live.units) Tile::load(a, at.b, at.h, live, t, lds, wv, lane);
+    Tiles tiles(a, live, lds, at.b, at.h, wv, lane);
 
     bf16x8 q[KC + RC];
     {
@@ -337,31 +331,23 @@ void latent_replay_kernel(LatentReplayArgs a)
 #pragma unroll
         for (int c = 0; c < KC + RC; ++c) q[c] = operand(*reinterpret_cast<const u32x4 *>(row + c * 32));
     }
-    uint32_t k_at[KC], r_at[RC], v_at[DT][2];
-#pragma unroll
-    for (int c = 0; c < KC; ++c) k_at[c] = LdsRows<Tile::KB>::row_piece(li, half, c);
-#pragma unroll
-    for (int c = 0; c < RC; ++c) r_at[c] = Tile::ROT + LdsRows<Tile::RB>::row_piece(li, half, c);
-#pragma unroll
-    for (int c = 0; c < DT; ++c)
-#pragma unroll
-        for (int g = 0; g < 2; ++g) v_at[c][g] = Tile::V + LdsRows<Tile::KB>::column(lane, g, c);
-
+    const uint32_t k_first = LdsRows<Tiles::KB>::row_piece(li, half, 0), r_first = LdsRows<Tiles::RB>::row_piece(li, half, 0);
+    const uint32_t v_first[2] = {LdsRows<Tiles::KB>::column(lane, 0, 0), LdsRows<Tiles::KB>::column(lane, 1, 0)};
     f32x16 o[DT];
 #pragma unroll
     for (int c = 0; c < DT; ++c) o[c] = zeros16();
     float m_run = -INFINITY, neg_m = 0.f, l_run = 0.f;     // scaled domain; neg_m: -m_run, or 0 as long as nothing has been seen
 
-    auto step = [&](const unsigned char *tile, int st, int key0, bool whole) {
+    auto step = [&](const unsigned char *unit, int key0, bool whole) {
         const bool mixed = !whole || key0 + LR_STEP - 1 > wave0 || key0 + LR_STEP > n;
         f32x16 sc = zeros16();
 #pragma unroll
-        for (int c = 0; c < KC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + k_at[c] + st * LR_STEP * Tile::KB)), q[c], sc);
+        for (int c = 0; c < KC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(unit + (k_first ^ c * 32))), q[c], sc);
 #pragma unroll
-        for (int c = 0; c < RC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + r_at[c] + st * LR_STEP * Tile::RB)), q[KC + c], sc);
-        const unsigned char *const values = tile + st * LR_STEP * Tile::KB;
+        for (int c = 0; c < RC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(unit + Tiles::ROT + (r_first ^ c * 32))), q[KC + c], sc);
+        const unsigned char *const values = unit + Tiles::V;
         Columns x[2];
-        ask_columns<Tile::KB>(values, v_at, 0, x[0]);      // (there when the weights are)
+        ask_columns<Tiles::KB, DT>(values, v_first, 0, x[0]);   // (there when the weights are)
         uint32_t seen = 0xFFFFu;
         if (mixed) {
             seen = seen_keys(death, key0, n, qpos, half);
@@ -394,42 +380,33 @@ void latent_replay_kernel(LatentReplayArgs a)
         bool odd = false;
 #pragma unroll
         for (int pair = 0; pair < DT / 2; ++pair) {
-            if (pair + 1 < DT / 2) ask_columns<Tile::KB>(values, v_at, pair + 1, x[(pair + 1) & 1]);
+            if (pair + 1 < DT / 2) ask_columns<Tiles::KB, DT>(values, v_first, pair + 1, x[(pair + 1) & 1]);
             odd |= add_columns(x[pair & 1], pair, w, mixed, o);
         }
         if (__ballot(odd)) {
             // the queries that see a row with such a value, and no others, become NaN
-            const uint32_t rows = odd_rows<Tile::KB>(tile + Tile::V + st * LR_STEP * Tile::KB);
+            const uint32_t rows = odd_rows<Tiles::KB>(values);
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (((rows >> row_of(r, half)) & 1u) && ((seen >> r) & 1u)) l_run = NAN;
         }
     };
 
-    unsigned char *here = lds, *there = lds + Tile::BYTES;
-    while (t.u[0] < live.units) {
-        lds_loads_done();
-        const UnitPair next(live, t.u[1] + 1);
-        if (next.u[0] < live.units) Tile::load(a, at.b, at.h, live, next, there, wv, lane);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int st = 0; st < LR_TILE / LR_STEP; ++st) {
-            const int key0 = t.u[st] * LR_STEP;
-            if (t.u[st] < live.units && wave0 < n && key0 <= wave_last) step(here, st, key0, live.whole(t.u[st]));
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        unsigned char *const x = here;
-        here = there;
-        there = x;
-        t = next;
+    // (the tiles that this wave sees first, a loop without branches: with one in it the sums would be kept twice)
+    int u[2];
+    while (tiles.more() && wave0 < n && tiles.unit[0] * LR_STEP <= wave_last) {
+        const unsigned char *const here = tiles.take(u);
+        step(here, u[0] * LR_STEP, live.whole(u[0]));
+        step(here + Tiles::UNIT, u[1] * LR_STEP, live.whole(u[1]));        // (none, or one that only others see: all of it is masked)
     }
+    while (tiles.more()) (void)tiles.take(u);
 
     // out, through LDS: rows leave as whole lines; 16-byte piece p of row r at slot p ^ r
     const float l = half_rows_sum(l_run);
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     if (a.lse && half == 0 && qpos < n)
         a.lse[((size_t)at.b * a.H + at.h) * a.T + qpos] = l == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-    __syncthreads();
+    lds_loads_done();
     constexpr int OP = D / 8;
     unsigned char *const mine = lds + wv * LR_OWN * D * 2;
 #pragma unroll
@@ -482,7 +459,7 @@ template <int D>
 __global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void latent_replay_dq_kernel(LatentReplayArgs a)
 {
-    using Tile = KeyTile<D>;
+    using Tiles = KeyTiles<D>;
     constexpr int E = D / 2, KC = D / 16, RC = E / 16, DT = D / 32, ET = E / 32;
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
@@ -494,8 +471,7 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
     const int wave_last = wave0 + LR_OWN - 1 < n ? wave0 + LR_OWN - 1 : n - 1, block_last = i0 + LR_BLOCK - 1 < n ? i0 + LR_BLOCK - 1 : n - 1;
     const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
     const LiveUnits live(death, block_last / LR_STEP + 1, n, i0, block_last);
-    UnitPair t(live, 0);
-    if (t.u[0] < live.units) Tile::load(a, at.b, at.h, live, t, lds, wv, lane);
+    Tiles tiles(a, live, lds, at.b, at.h, wv, lane);
 
     bf16x8 q[KC + RC], g_[KC];
     float delta = 0.f;
@@ -521,39 +497,28 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
         stats[0] = neg_lse;
         stats[a.T] = delta;
     }
-    uint32_t k_at[KC], r_at[RC], v_at[KC], kt_at[DT][2], rt_at[ET][2];
-#pragma unroll
-    for (int c = 0; c < KC; ++c) {
-        k_at[c] = LdsRows<Tile::KB>::row_piece(li, half, c);
-        v_at[c] = Tile::V + k_at[c];
-    }
-#pragma unroll
-    for (int c = 0; c < RC; ++c) r_at[c] = Tile::ROT + LdsRows<Tile::RB>::row_piece(li, half, c);
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-#pragma unroll
-        for (int c = 0; c < DT; ++c) kt_at[c][g] = LdsRows<Tile::KB>::column(lane, g, c);
-#pragma unroll
-        for (int c = 0; c < ET; ++c) rt_at[c][g] = Tile::ROT + LdsRows<Tile::RB>::column(lane, g, c);
-    }
+    const uint32_t k_first = LdsRows<Tiles::KB>::row_piece(li, half, 0), r_first = LdsRows<Tiles::RB>::row_piece(li, half, 0);
+    const uint32_t kt_first[2] = {LdsRows<Tiles::KB>::column(lane, 0, 0), LdsRows<Tiles::KB>::column(lane, 1, 0)};
+    const uint32_t rt_first[2] = {LdsRows<Tiles::RB>::column(lane, 0, 0), LdsRows<Tiles::RB>::column(lane, 1, 0)};
     f32x16 dk[DT], dr[ET];                                 // dQ^T: of the part that meets the heads' own keys, and of the rotary part
 #pragma unroll
     for (int c = 0; c < DT; ++c) dk[c] = zeros16();
 #pragma unroll
     for (int c = 0; c < ET; ++c) dr[c] = zeros16();
 
-    auto step = [&](const unsigned char *tile, int st, int key0, bool whole) {
+    auto step = [&](const unsigned char *unit, int key0, bool whole) {
         const bool mixed = !whole || key0 + LR_STEP - 1 > wave0 || key0 + LR_STEP > n;
         f32x16 sc = zeros16(), dp = zeros16();
+        const uint32_t k_0 = fresh(k_first), r_0 = fresh(r_first);
 #pragma unroll
-        for (int c = 0; c < KC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + k_at[c] + st * LR_STEP * Tile::KB)), q[c], sc);
+        for (int c = 0; c < KC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(unit + (k_0 ^ c * 32))), q[c], sc);
 #pragma unroll
-        for (int c = 0; c < RC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(tile + r_at[c] + st * LR_STEP * Tile::RB)), q[KC + c], sc);
+        for (int c = 0; c < RC; ++c) sc = product(operand(*reinterpret_cast<const u32x4 *>(unit + Tiles::ROT + (r_0 ^ c * 32))), q[KC + c], sc);
 #pragma unroll
-        for (int c = 0; c < KC; ++c) dp = product(operand(*reinterpret_cast<const u32x4 *>(tile + v_at[c] + st * LR_STEP * Tile::KB)), g_[c], dp);
-        const unsigned char *const own = tile + st * LR_STEP * Tile::KB;
+        for (int c = 0; c < KC; ++c) dp = product(operand(*reinterpret_cast<const u32x4 *>(unit + Tiles::V + (k_0 ^ c * 32))), g_[c], dp);
+        const uint32_t kt_0[2] = {fresh(kt_first[0]), fresh(kt_first[1])}, rt_0[2] = {fresh(rt_first[0]), fresh(rt_first[1])};
         Columns x[2];
-        ask_columns<Tile::KB>(own, kt_at, 0, x[0]);
+        ask_columns<Tiles::KB, DT>(unit, kt_0, 0, x[0]);
         float ds[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] = fast_exp2(__builtin_fmaf(sc[r], a.scale_log2e, neg_lse)) * (dp[r] - delta);
@@ -568,30 +533,21 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
         // (a key that is seen and not finite has made dS NaN)
 #pragma unroll
         for (int pair = 0; pair < DT / 2; ++pair) {
-            if (pair + 1 < DT / 2) ask_columns<Tile::KB>(own, kt_at, pair + 1, x[(pair + 1) & 1]);
-            else ask_columns<Tile::RB>(tile + st * LR_STEP * Tile::RB, rt_at, 0, x[(pair + 1) & 1]);
+            if (pair + 1 < DT / 2) ask_columns<Tiles::KB, DT>(unit, kt_0, pair + 1, x[(pair + 1) & 1]);
+            else ask_columns<Tiles::RB, ET>(unit + Tiles::ROT, rt_0, 0, x[(pair + 1) & 1]);
             (void)add_columns(x[pair & 1], pair, w, mixed, dk);
         }
         (void)add_columns(x[DT / 2 & 1], 0, w, mixed, dr);
     };
-    unsigned char *here = lds, *there = lds + Tile::BYTES;
-    while (t.u[0] < live.units) {
-        lds_loads_done();
-        const UnitPair next(live, t.u[1] + 1);
-        if (next.u[0] < live.units) Tile::load(a, at.b, at.h, live, next, there, wv, lane);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int st = 0; st < LR_TILE / LR_STEP; ++st) {
-            const int key0 = t.u[st] * LR_STEP;
-            if (t.u[st] < live.units && wave0 < n && key0 <= wave_last) step(here, st, key0, live.whole(t.u[st]));
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        unsigned char *const x = here;
-        here = there;
-        there = x;
-        t = next;
+    // (the tiles that this wave sees first, a loop without branches: with one in it the sums would be kept twice)
+    int u[2];
+    while (tiles.more() && wave0 < n && tiles.unit[0] * LR_STEP <= wave_last) {
+        const unsigned char *const here = tiles.take(u);
+        step(here, u[0] * LR_STEP, live.whole(u[0]));
+        step(here + Tiles::UNIT, u[1] * LR_STEP, live.whole(u[1]));        // (none, or one that only others see: all of it is masked)
     }
-    __syncthreads();
+    while (tiles.more()) (void)tiles.take(u);
+    lds_loads_done();
     unsigned char *const mine = lds + wv * LR_OWN * D * 2;
     unsigned char *const to = a.dq + (((size_t)at.b * a.T + wave0) * a.H + at.h) * ((D + E) * 2);
     const size_t stride = (size_t)a.H * ((D + E) * 2);
@@ -776,11 +732,6 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
             __builtin_amdgcn_sched_barrier(0);
         }
         return acc;
-    };
-    // (addresses are made where they are used: kept, they would cost registers that the sums need)
-    auto fresh = [](uint32_t x) {
-        __asm__ volatile("" : "+v"(x));
-        return x;
     };
     auto round_begins = [&](int u) {
         wait_for_loads<(LR_SLOTS - 3) * LOADS>();          // unit u is there, P of the one before too
@@ -994,7 +945,7 @@ extern "C" int ngc_latent_replay_attn(const void *q, const void *kv, const void 
     a.out = reinterpret_cast<unsigned char *>(out);
     a.lse = lse_out;
     const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_kernel<64>);
-    return launch_blocks(fn, a, LR_WAVES, 2 * (D == 128 ? KeyTile<128>::BYTES : KeyTile<64>::BYTES), (hipStream_t)stream);
+    return launch_blocks(fn, a, LR_WAVES, D == 128 ? KeyTiles<128>::BYTES : KeyTiles<64>::BYTES, (hipStream_t)stream);
 }
 
 extern "C" int ngc_latent_replay_attn_backward(const void *q, const void *kv, const void *rope, int64_t rope_stride, const int32_t *death,
@@ -1017,7 +968,7 @@ extern "C" int ngc_latent_replay_attn_backward(const void *q, const void *kv, co
     a.stats = reinterpret_cast<float *>(ws);
     a.part = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(ws) + latent_replay_stats_bytes(B, T, Hq));
     hipStream_t st = (hipStream_t)stream;
-    const size_t lds = 2 * (D == 128 ? KeyTile<128>::BYTES : KeyTile<64>::BYTES);
+    const size_t lds = D == 128 ? KeyTiles<128>::BYTES : KeyTiles<64>::BYTES;
     rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dq_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dq_kernel<64>), a, LR_WAVES, lds, st);
     if (rc) return rc;
     rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dkv_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dkv_kernel<64>), a,
