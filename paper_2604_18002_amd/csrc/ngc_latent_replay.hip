@@ -293,16 +293,27 @@ struct KeyTiles {
     }
 };
 
-// The bits of 32 keys from key0 that query i sees, of the 16 that stand in a lane's registers: register r, bit r.
-__device__ __forceinline__ uint32_t seen_keys(const int32_t *death, int key0, int n, int i, int half)
+// The bits of 32 keys from key0 (uniform) that query i sees, of the 16 that stand in a lane's registers: register r, bit r.  (The keys'
+// ends through the scalar unit: a vector load's result would be waited for behind all the tiles on their way.)
+__device__ __forceinline__ uint32_t seen_keys(const int32_t *death, int key0, int n, int T, int i, int half)
 {
+    const int below = i < n - 1 ? i : n - 1;               // the last key that it may see
     uint32_t seen = 0;
+    if (!death) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const int j = key0 + row_of(r, half);
-        bool sees = j <= i && j < n;
-        if (death) sees = sees && i < death[j < n ? j : n - 1];
-        seen |= (uint32_t)sees << r;
+        for (int r = 0; r < 16; ++r) seen |= (uint32_t)(key0 + row_of(r, half) <= below) << r;
+    } else if (key0 + LR_STEP <= T) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int lower = constant_word(death + key0 + row_of(r, 0)), upper = constant_word(death + key0 + row_of(r, 1));
+            seen |= (uint32_t)(key0 + row_of(r, half) <= below && i < (half ? upper : lower)) << r;
+        }
+    } else {
+#pragma unroll 1
+        for (int r = 0; r < 16; ++r) {
+            const int j = key0 + row_of(r, half);
+            seen |= (uint32_t)(j <= below && i < death[j < T ? j : T - 1]) << r;
+        }
     }
     return seen;
 }
@@ -350,7 +361,7 @@ void latent_replay_kernel(LatentReplayArgs a)
         ask_columns<Tiles::KB, DT>(values, v_first, 0, x[0]);   // (there when the weights are)
         uint32_t seen = 0xFFFFu;
         if (mixed) {
-            seen = seen_keys(death, key0, n, qpos, half);
+            seen = seen_keys(death, key0, n, a.T, qpos, half);
 #pragma unroll
             for (int r = 0; r < 16; ++r) sc[r] = (seen >> r) & 1u ? sc[r] : -INFINITY;
         }
@@ -392,12 +403,17 @@ void latent_replay_kernel(LatentReplayArgs a)
         }
     };
 
-    // (the tiles that this wave sees first, a loop without branches: with one in it the sums would be kept twice)
+    // (the tiles that this wave sees first, in a loop without branches: with one in it the sums would be kept twice)
     int u[2];
-    while (tiles.more() && wave0 < n && tiles.unit[0] * LR_STEP <= wave_last) {
+    auto mine = [&](int unit) { return unit < live.units && wave0 < n && unit * LR_STEP <= wave_last; };
+    while (mine(tiles.unit[1])) {
         const unsigned char *const here = tiles.take(u);
         step(here, u[0] * LR_STEP, live.whole(u[0]));
-        step(here + Tiles::UNIT, u[1] * LR_STEP, live.whole(u[1]));        // (none, or one that only others see: all of it is masked)
+        step(here + Tiles::UNIT, u[1] * LR_STEP, live.whole(u[1]));
+    }
+    if (mine(tiles.unit[0])) {
+        const unsigned char *const here = tiles.take(u);
+        step(here, u[0] * LR_STEP, live.whole(u[0]));
     }
     while (tiles.more()) (void)tiles.take(u);
 
@@ -408,13 +424,13 @@ void latent_replay_kernel(LatentReplayArgs a)
         a.lse[((size_t)at.b * a.H + at.h) * a.T + qpos] = l == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
     lds_loads_done();
     constexpr int OP = D / 8;
-    unsigned char *const mine = lds + wv * LR_OWN * D * 2;
+    unsigned char *const rows = lds + wv * LR_OWN * D * 2;
 #pragma unroll
     for (int c = 0; c < DT; ++c)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int col = 32 * c + 8 * g + 4 * half;
-            *reinterpret_cast<u32x2 *>(mine + li * (D * 2) + (((col / 8) ^ li) & (OP - 1)) * 16 + (col % 8) * 2) =
+            *reinterpret_cast<u32x2 *>(rows + li * (D * 2) + (((col / 8) ^ li) & (OP - 1)) * 16 + (col % 8) * 2) =
                 u32x2{pack_bf16(o[c][4 * g] * inv, o[c][4 * g + 1] * inv), pack_bf16(o[c][4 * g + 2] * inv, o[c][4 * g + 3] * inv)};
         }
     __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt(0): a wave's rows are its own
@@ -422,7 +438,7 @@ void latent_replay_kernel(LatentReplayArgs a)
 #pragma unroll
     for (int r0 = 0; r0 < LR_OWN; r0 += 64 / OP) {
         const int r = r0 + lane / OP, piece = lane % OP;
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(mine + r * (D * 2) + ((piece ^ r) & (OP - 1)) * 16);
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(rows + r * (D * 2) + ((piece ^ r) & (OP - 1)) * 16);
         if (wave0 + r < n) *reinterpret_cast<u32x4 *>(a.out + ((((size_t)at.b * a.T + wave0 + r) * a.H + at.h) * D + piece * 8) * 2) = x;
     }
 }
@@ -523,7 +539,7 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] = fast_exp2(__builtin_fmaf(sc[r], a.scale_log2e, neg_lse)) * (dp[r] - delta);
         if (mixed) {
-            const uint32_t seen = seen_keys(death, key0, n, qpos, half);
+            const uint32_t seen = seen_keys(death, key0, n, a.T, qpos, half);
 #pragma unroll
             for (int r = 0; r < 16; ++r) ds[r] = (seen >> r) & 1u ? ds[r] : 0.f;
         }
@@ -539,20 +555,25 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
         }
         (void)add_columns(x[DT / 2 & 1], 0, w, mixed, dr);
     };
-    // (the tiles that this wave sees first, a loop without branches: with one in it the sums would be kept twice)
+    // (the tiles that this wave sees first, in a loop without branches: with one in it the sums would be kept twice)
     int u[2];
-    while (tiles.more() && wave0 < n && tiles.unit[0] * LR_STEP <= wave_last) {
+    auto mine = [&](int unit) { return unit < live.units && wave0 < n && unit * LR_STEP <= wave_last; };
+    while (mine(tiles.unit[1])) {
         const unsigned char *const here = tiles.take(u);
         step(here, u[0] * LR_STEP, live.whole(u[0]));
-        step(here + Tiles::UNIT, u[1] * LR_STEP, live.whole(u[1]));        // (none, or one that only others see: all of it is masked)
+        step(here + Tiles::UNIT, u[1] * LR_STEP, live.whole(u[1]));
+    }
+    if (mine(tiles.unit[0])) {
+        const unsigned char *const here = tiles.take(u);
+        step(here, u[0] * LR_STEP, live.whole(u[0]));
     }
     while (tiles.more()) (void)tiles.take(u);
     lds_loads_done();
-    unsigned char *const mine = lds + wv * LR_OWN * D * 2;
+    unsigned char *const rows = lds + wv * LR_OWN * D * 2;
     unsigned char *const to = a.dq + (((size_t)at.b * a.T + wave0) * a.H + at.h) * ((D + E) * 2);
     const size_t stride = (size_t)a.H * ((D + E) * 2);
-    store_rows(mine, dk, a.scale, to, stride, n - wave0);
-    store_rows(mine, dr, a.scale, to + D * 2, stride, n - wave0);
+    store_rows(rows, dk, a.scale, to, stride, n - wave0);
+    store_rows(rows, dr, a.scale, to + D * 2, stride, n - wave0);
 }
 
 // The unit of 32 keys that has place `rank` when they are ordered by the query that sees a key of theirs last, the latest first, and by
