@@ -136,15 +136,15 @@ void latent_attn_kernel(LatentArgs a)
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
     const int rg = wv % RG, kg = wv / RG;
     const int row = lane & 15, quarter = lane >> 4;
-    // the row blocks of a sequence follow one another on one XCD
-    int seg = (int)blockIdx.x, block = 0;
+    // the row blocks of a share of a sequence follow one another on one XCD, whose L2 then has the rows for all but the first
+    int share = (int)blockIdx.x, block = 0;
     if (a.blocks > 1) {
         const int first = (int)(blockIdx.x / (8u * (unsigned)a.blocks)) * 8, at = (int)blockIdx.x - first * a.blocks;
-        const int here = a.nseg - first < 8 ? a.nseg - first : 8;
+        const int here = a.nseg * a.S - first < 8 ? a.nseg * a.S - first : 8;
         block = at / here;
-        seg = first + at - block * here;
+        share = first + at - block * here;
     }
-    const int split = (int)blockIdx.y;
+    const int seg = share % a.nseg, split = share / a.nseg;
     const int stride = a.S * KG, first_tile = split * KG + kg;
     const int32_t *tab = a.table + (size_t)(a.seg0 + seg) * a.max_pages;
     auto tile_base = [&](int t) -> const unsigned char * {
@@ -374,8 +374,8 @@ void latent_attn_kernel(LatentArgs a)
         const float mk = red[(k * RG + rg) * LT_ROWS + row];
         if (mk != -INFINITY) l_all += red[(NW + k * RG + rg) * LT_ROWS + row] * fast_exp2((mk - m_all) * a.scale_log2e);
     }
-    float share = m_run == -INFINITY ? 0.f : fast_exp2((m_run - m_all) * a.scale_log2e);
-    if (a.S == 1) share = l_all == 0.f ? 0.f : share / l_all;
+    float part = m_run == -INFINITY ? 0.f : fast_exp2((m_run - m_all) * a.scale_log2e);
+    if (a.S == 1) part = l_all == 0.f ? 0.f : part / l_all;
     if (kg == 0 && quarter == 0 && my_row < real_rows) {
         if (a.S == 1) {
             if (a.lse_out) a.lse_out[(size_t)seg * a.M + my_row] = l_all == 0.f ? -INFINITY : m_all * a.scale + logf(l_all);
@@ -395,7 +395,7 @@ void latent_attn_kernel(LatentArgs a)
 #pragma unroll
         for (int c = h * CT / PARTS; c < (h + 1) * CT / PARTS; ++c) {
             const int piece = (16 * c - h * COLS) / 4 + quarter;
-            *reinterpret_cast<f32x4 *>(mine_o + row * COLS + ((piece ^ row) & (PIECES - 1)) * 4) = oacc[c] * share;
+            *reinterpret_cast<f32x4 *>(mine_o + row * COLS + ((piece ^ row) & (PIECES - 1)) * 4) = oacc[c] * part;
         }
         __syncthreads();
         static_assert(RG * LT_ROWS * PIECES % (NW * 64) == 0, "whole rounds");
@@ -566,7 +566,7 @@ extern "C" int ngc_latent_attn(const ngc_paged_cache *pc, int32_t layer, const i
     else { NGC_PICK_LATENT(256, 32); }
 #undef NGC_PICK_LATENT
     if (lds > 64 * 1024) NGC_HIP_CHECK(hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    rc = launch(fn, dim3((unsigned)(nseg * shape.blocks), (unsigned)S), dim3(shape.waves * 64), lds, st, a);
+    rc = launch(fn, dim3((unsigned)(nseg * shape.blocks * S)), dim3(shape.waves * 64), lds, st, a);
     if (rc || S == 1) return rc;
     const int rows_a_group = JOIN_THREADS / (R / 4);
     fn = R == 512 ? reinterpret_cast<const void *>(&latent_join_kernel<512>) : reinterpret_cast<const void *>(&latent_join_kernel<256>);
