@@ -127,6 +127,9 @@ void latent_attn_kernel(LatentArgs a)
     constexpr int CHUNKS = (R + E) / 32, LAT_CHUNKS = R / 32, CT = R / 16;               // of the first product; column tiles of the second
     constexpr int LAT_LOADS = (Tile::LAT_LOADS + RG - 1) / RG, ROT_LOADS = (Tile::ROT_LOADS + RG - 1) / RG;      // of a wave, per tile
     constexpr int LOADS = LAT_LOADS + ROT_LOADS;
+    // A wave is held up where it asks for a tile, about 100 clocks a load.  The two waves of a SIMD, of different key groups, do it at
+    // different times: 343 us for 380 with 256 sequences of 4096 rows and 128 heads, R = 512.
+    constexpr bool LATER = NW == 8;
     constexpr int PARTS = (NW * LT_ROWS * R * 4 + SLOTS * Tile::BYTES - 1) / (SLOTS * Tile::BYTES);       // the output goes through LDS in
 
     extern __shared__ __align__(256) unsigned char lds[];
@@ -236,7 +239,7 @@ void latent_attn_kernel(LatentArgs a)
     const int read_row = 4 * quarter + row / 4, read_col = 4 * (row % 4);                // of the transposing reads
     const uint32_t lat0 = Tile::piece(row, quarter), rot0 = Tile::piece(row, Tile::LAT_PIECES + quarter);
     const uint32_t col0 = Tile::piece(read_row, read_col / 8) + (uint32_t)(read_col % 8) * 2;
-    auto compute_tile = [&](int t, const unsigned char *tile, const uint32_t *odd) {
+    auto compute_tile = [&](int t, const unsigned char *tile, const uint32_t *odd, auto between) {
         const uint32_t tile_at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char *)tile;
         auto row_piece = [&](int c, int k) {               // chunk c of rows 16 k ..
             const uint32_t at = c < LAT_CHUNKS ? ((tile_at + lat0) ^ (uint32_t)(c % 4 * 64)) + (uint32_t)(c / 4 * 256 + k * 16 * Tile::LAT)
@@ -249,18 +252,18 @@ void latent_attn_kernel(LatentArgs a)
         };
         const int key0 = t * KEYS;
         constexpr int SCORES = 4 * HALVES;
-        // GROUP chunks' rows (column tiles) are asked for while the products of those before run
-        constexpr int GROUP = NW == 4 && HALVES == 1 ? (CHUNKS % 6 == 0 ? 6 : 9) : NW == 8 && R == 512 ? 1 : 3, VGROUP = NW == 4 ? 8 : 4;
+        // GROUP chunks' rows (column tiles) are asked for DEPTH - 1 groups (a group) before their products run
+        constexpr int GROUP = NW == 4 && HALVES == 1 ? (CHUNKS % 6 == 0 ? 6 : 9) : NW == 8 && R == 512 ? 1 : 3, VGROUP = NW == 4 ? 8 : 4, DEPTH = NW == 8 && R == 512 ? 4 : 2;
         static_assert(CHUNKS % GROUP == 0 && CT % VGROUP == 0, "whole groups");
         f32x4 sc[HALVES];
 #pragma unroll
         for (int k = 0; k < HALVES; ++k) sc[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-        u32x4 x[2][GROUP][HALVES];
+        u32x4 x[DEPTH][GROUP][HALVES];
         auto ask_rows = [&](int g) {
 #pragma unroll
             for (int u = 0; u < GROUP; ++u)
 #pragma unroll
-                for (int k = 0; k < HALVES; ++k) x[g & 1][u][k] = row_piece(g * GROUP + u, k);
+                for (int k = 0; k < HALVES; ++k) x[g % DEPTH][u][k] = row_piece(g * GROUP + u, k);
         };
         u32x2 v[2][VGROUP][HALVES];
         auto ask_columns = [&](int g) {
@@ -269,17 +272,19 @@ void latent_attn_kernel(LatentArgs a)
 #pragma unroll
                 for (int h = 0; h < HALVES; ++h) v[g & 1][u][h] = transposed(h, g * VGROUP + u);
         };
-        ask_rows(0);
+#pragma unroll
+        for (int g = 0; g < DEPTH - 1; ++g) ask_rows(g);
 #pragma unroll
         for (int g = 0; g < CHUNKS / GROUP; ++g) {
-            if (g + 1 < CHUNKS / GROUP) ask_rows(g + 1);
+            if (g + DEPTH - 1 < CHUNKS / GROUP) ask_rows(g + DEPTH - 1);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int u = 0; u < GROUP; ++u)
 #pragma unroll
-                for (int k = 0; k < HALVES; ++k) sc[k] = product16(__builtin_bit_cast(bf16x8, x[g & 1][u][k]), qop[g * GROUP + u], sc[k]);
+                for (int k = 0; k < HALVES; ++k) sc[k] = product16(__builtin_bit_cast(bf16x8, x[g % DEPTH][u][k]), qop[g * GROUP + u], sc[k]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        between();
         ask_columns(0);                                    // (there when the weights are)
         __builtin_amdgcn_sched_barrier(0);
         float s_[SCORES];
@@ -350,12 +355,17 @@ void latent_attn_kernel(LatentArgs a)
             wait_for_loads<(NB - 2) * LOADS>();
         }
         if constexpr (RG > 1) workgroup_barrier();         // (or a wave's tiles are its own)
-        if (issued < mine) {
-            load_tile(tile_base(first_tile + issued * stride), buffers + issued % NB * Tile::BYTES);
-            ++issued;
-        }
+        auto load_next = [&] {
+            if (issued < mine) {
+                load_tile(tile_base(first_tile + issued * stride), buffers + issued % NB * Tile::BYTES);
+                ++issued;
+            }
+        };
+        if (!LATER || kg % 2 == 0) load_next();
         // (a key group without a tile in the last round computes one that nobody sees)
-        compute_tile(t, tile, odd);
+        compute_tile(t, tile, odd, [&] {
+            if (LATER && kg % 2) load_next();
+        });
     }
     wait_for_loads<0>();
 
