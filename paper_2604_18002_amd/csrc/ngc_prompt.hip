@@ -26,7 +26,7 @@ struct ExtendArgs {
     int page_rows, page_shift, max_pages, num_pages;
 };
 
-constexpr int EXTEND_THREADS = 1024;
+constexpr int EXTEND_THREADS = 1024, EXTEND_BATCH = 4;
 // Sums over all threads stay in 32 bits when each adds at most this.
 constexpr int EXTEND_MOST_TOKENS = 1 << 20;
 
@@ -63,34 +63,52 @@ __global__ __launch_bounds__(EXTEND_THREADS) void extend_plan_kernel(ExtendArgs 
     const int lo = (int)threadIdx.x * per, hi = lo + per < a.nseg ? lo + per : a.nseg;
     const int cap = a.page_rows * a.max_pages;
     auto pages = [&](int rows) { return (rows + a.page_rows - 1) >> a.page_shift; };
-    // length, rows asked for, rows there is room for, and pages that are missing for them
-    auto wants = [&](int i, int &n, int &w, int &m) {
-        const int b = (i / a.Hkv) % a.B;
-        n = a.len[a.seg0 + i];
-        w = a.start[b + 1] - a.start[b];
-        if (n < 0 || n > cap) { m = -1; return 0; }
-        m = w < cap - n ? w : cap - n;
-        return pages(n + m) - pages(n);
+    // lengths of a batch of segments and rows asked for: all of them on their way together
+    int n[EXTEND_BATCH], w[EXTEND_BATCH];
+    auto load = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < EXTEND_BATCH; ++u) {
+            const int i = i0 + u < a.nseg ? i0 + u : a.nseg - 1, b = (i / a.Hkv) % a.B;
+            n[u] = a.len[a.seg0 + i];
+            w[u] = a.start[b + 1] - a.start[b];
+        }
     };
-    int n, w, m, mine = 0;
-    for (int i = lo; i < hi; ++i) mine += wants(i, n, w, m);
+    // rows there is room for (-1: no length), and pages that are missing for them
+    auto wants = [&](int n_, int w_, int &m) {
+        if (n_ < 0 || n_ > cap) { m = -1; return 0; }
+        m = w_ < cap - n_ ? w_ : cap - n_;
+        return pages(n_ + m) - pages(n_);
+    };
+    int m, mine = 0;
+    for (int i0 = lo; i0 < hi; i0 += EXTEND_BATCH) {
+        load(i0);
+#pragma unroll
+        for (int u = 0; u < EXTEND_BATCH; ++u)
+            if (i0 + u < hi) mine += wants(n[u], w[u], m);
+    }
     int total;
     int rank = block_excl_scan_i<EXTEND_THREADS>(mine, tmp, &total);       // (and everybody has read the height of the stack)
-    for (int i = lo; i < hi; ++i) {
-        const int need = wants(i, n, w, m);
-        int got = count - rank;
-        got = got < 0 ? 0 : got < need ? got : need;
-        if (got < need) m = ((pages(n) + got) << a.page_shift) - n;
-        if (m < 0) {                        // no length
-            atomicAdd(&a.status[NGC_STATUS_LEN_CLAMPED], 1);
-            m = 0;
-        } else if (m > 0) {
-            a.len[a.seg0 + i] = n + m;
+    for (int i0 = lo; i0 < hi; i0 += EXTEND_BATCH) {
+        if (per > EXTEND_BATCH) load(i0);                  // (or they are here still)
+#pragma unroll
+        for (int u = 0; u < EXTEND_BATCH; ++u) {
+            const int i = i0 + u;
+            if (i >= hi) break;
+            const int need = wants(n[u], w[u], m);
+            int got = count - rank;
+            got = got < 0 ? 0 : got < need ? got : need;
+            if (got < need) m = ((pages(n[u]) + got) << a.page_shift) - n[u];
+            if (m < 0) {                    // no length
+                atomicAdd(&a.status[NGC_STATUS_LEN_CLAMPED], 1);
+                m = 0;
+            } else if (m > 0) {
+                a.len[a.seg0 + i] = n[u] + m;
+            }
+            if (w[u] > m) atomicAdd(&a.status[NGC_STATUS_APPEND_FULL], w[u] - m);
+            a.first[a.seg0 + i] = count - 1 - rank;
+            a.rows[a.seg0 + i] = m;
+            rank += need;
         }
-        if (w > m) atomicAdd(&a.status[NGC_STATUS_APPEND_FULL], w - m);
-        a.first[a.seg0 + i] = count - 1 - rank;
-        a.rows[a.seg0 + i] = m;
-        rank += need;
     }
     if (threadIdx.x == 0) {
         if (count != count_raw) atomicAdd(&a.status[NGC_STATUS_POOL_BOUNDS], 1);
@@ -98,7 +116,7 @@ __global__ __launch_bounds__(EXTEND_THREADS) void extend_plan_kernel(ExtendArgs 
     }
 }
 
-constexpr int SLOT_THREADS = 256;
+constexpr int SLOT_THREADS = 256, SLOT_BATCH = 4;
 __global__ __launch_bounds__(SLOT_THREADS) void extend_slots_kernel(ExtendArgs a)
 {
     const int i = (int)blockIdx.x, seg = a.seg0 + i;
@@ -111,19 +129,25 @@ __global__ __launch_bounds__(SLOT_THREADS) void extend_slots_kernel(ExtendArgs a
     if (m > 0)
         for (int j = have + (int)threadIdx.x; j < want; j += SLOT_THREADS) tab[j] = a.free_stack[first - (j - have)];
     int outside = 0;
-    for (int t = threadIdx.x; t < w; t += SLOT_THREADS) {
-        int to = -1;
-        if (t < m) {
-            const int at = n + t, p = at >> a.page_shift;
-            const int page = p < have ? tab[p] : a.free_stack[first - (p - have)];
-            if (page < 0 || page >= a.num_pages) ++outside;
-            else to = (page << a.page_shift) + (at & (a.page_rows - 1));
+    for (int t0 = threadIdx.x; t0 < w; t0 += SLOT_BATCH * SLOT_THREADS) {
+        int page[SLOT_BATCH];               // (all on their way together)
+#pragma unroll
+        for (int u = 0; u < SLOT_BATCH; ++u) {
+            const int t = t0 + u * SLOT_THREADS, p = (n + t) >> a.page_shift;
+            page[u] = t < m ? (p < have ? tab[p] : a.free_stack[first - (p - have)]) : 0;
         }
-        slot[start + t] = to;
+#pragma unroll
+        for (int u = 0; u < SLOT_BATCH; ++u) {
+            const int t = t0 + u * SLOT_THREADS;
+            const bool in_pool = page[u] >= 0 && page[u] < a.num_pages;
+            outside += !in_pool;
+            if (t < w) slot[start + t] = t < m && in_pool ? (page[u] << a.page_shift) + ((n + t) & (a.page_rows - 1)) : -1;
+        }
     }
     if (outside) atomicAdd(&a.status[NGC_STATUS_POOL_BOUNDS], outside);
-    if (b == a.B - 1)                       // behind the last sequence's tokens
-        for (int t = start + w + (int)threadIdx.x; t < a.T; t += SLOT_THREADS) slot[t] = -1;
+    // behind the last sequence's tokens: a part for each
+    const int end = a.start[a.B], per = (a.T - end + a.B - 1) / a.B, lo = end + b * per, hi = lo + per < a.T ? lo + per : a.T;
+    for (int t = lo + (int)threadIdx.x; t < hi; t += SLOT_THREADS) slot[t] = -1;
 }
 
 // ------------------------------------------------------------------ fill ------
