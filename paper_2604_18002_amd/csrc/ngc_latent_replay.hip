@@ -172,20 +172,22 @@ __device__ __forceinline__ uint32_t odd_rows(const unsigned char *rows)
 }
 
 // Units of LR_STEP keys that some query of first .. last sees, and those that all of them see where causality lets them, as words of
-// 64 units in the lanes.
+// 64 units in the lanes.  The workgroup's waves look at a part of the keys each and share their words in `scratch` (LDS, 1 KB, free
+// again behind the next barrier).
 struct LiveUnits {
     uint32_t some_lo, some_hi, all_lo, all_hi;             // of units 64 lane .. + 31, and the 32 behind them
     int units;
-    __device__ __forceinline__ LiveUnits(const int32_t *death, int units_, int n, int first, int last) : units(units_)
+    __device__ __forceinline__ LiveUnits(const int32_t *death, int units_, int n, int first, int last, int wv, uint32_t *scratch) : units(units_)
     {
         const int lane = lane_id();
         auto below = [&](int u0) { return units >= u0 + 32 ? 0xFFFFFFFFu : units <= u0 ? 0u : (1u << (units - u0)) - 1u; };
         some_lo = all_lo = below(64 * lane);
         some_hi = all_hi = below(64 * lane + 32);
         if (!death) return;
-        some_lo = some_hi = all_lo = all_hi = 0;
-        constexpr int BATCH = 16;            // loads of 64 keys
-        for (int u0 = 0; u0 < units; u0 += 2 * BATCH) {
+        constexpr int BATCH = 16;            // loads of 64 keys: a word of units
+        const int words = (units + 2 * BATCH - 1) / (2 * BATCH);
+        for (int at = wv; at < words; at += LR_WAVES) {
+            const int u0 = at * 2 * BATCH;
             int d[BATCH];
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
@@ -201,12 +203,14 @@ struct LiveUnits {
                 seen |= ((uint32_t)any != 0 ? 1u : 0u) << (2 * i) | ((uint32_t)(any >> 32) != 0 ? 2u : 0u) << (2 * i);
                 whole |= ((uint32_t)not_all == 0 ? 1u : 0u) << (2 * i) | ((uint32_t)(not_all >> 32) == 0 ? 2u : 0u) << (2 * i);
             }
-            const bool mine = lane == u0 / 64, second = u0 / 32 % 2 != 0;
-            some_lo = mine && !second ? seen : some_lo;
-            some_hi = mine && second ? seen : some_hi;
-            all_lo = mine && !second ? whole : all_lo;
-            all_hi = mine && second ? whole : all_hi;
+            if (lane < 2) scratch[2 * at + lane] = lane ? whole : seen;
         }
+        __syncthreads();
+        auto mine = [&](int at, int which) { return at < words ? scratch[2 * at + which] : 0u; };
+        some_lo = mine(2 * lane, 0);
+        some_hi = mine(2 * lane + 1, 0);
+        all_lo = mine(2 * lane, 1);
+        all_hi = mine(2 * lane + 1, 1);
     }
     __device__ static __forceinline__ uint32_t word(uint32_t lo, uint32_t hi, int u)
     {
@@ -333,15 +337,14 @@ void latent_replay_kernel(LatentReplayArgs a)
     const int wave0 = i0 + wv * LR_OWN, qpos = wave0 + li;
     const int wave_last = wave0 + LR_OWN - 1 < n ? wave0 + LR_OWN - 1 : n - 1, block_last = i0 + LR_BLOCK - 1 < n ? i0 + LR_BLOCK - 1 : n - 1;
     const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
-    const LiveUnits live(death, block_last / LR_STEP + 1, n, i0, block_last);
-    Tiles tiles(a, live, lds, at.b, at.h, wv, lane);
-
     bf16x8 q[KC + RC];
     {
         const unsigned char *row = a.q + (((size_t)at.b * a.T + (qpos < n ? qpos : n - 1)) * a.H + at.h) * ((D + E) * 2) + half * 16;
 #pragma unroll
         for (int c = 0; c < KC + RC; ++c) q[c] = operand(*reinterpret_cast<const u32x4 *>(row + c * 32));
     }
+    const LiveUnits live(death, block_last / LR_STEP + 1, n, i0, block_last, wv, reinterpret_cast<uint32_t *>(lds));
+    Tiles tiles(a, live, lds, at.b, at.h, wv, lane);       // (its first tile goes behind the words)
     const uint32_t k_first = LdsRows<Tiles::KB>::row_piece(li, half, 0), r_first = LdsRows<Tiles::RB>::row_piece(li, half, 0);
     const uint32_t v_first[2] = {LdsRows<Tiles::KB>::column(lane, 0, 0), LdsRows<Tiles::KB>::column(lane, 1, 0)};
     f32x16 o[DT];
@@ -486,9 +489,6 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
     const int wave0 = i0 + wv * LR_OWN, qpos = wave0 + li, q_row = qpos < n ? qpos : n - 1;
     const int wave_last = wave0 + LR_OWN - 1 < n ? wave0 + LR_OWN - 1 : n - 1, block_last = i0 + LR_BLOCK - 1 < n ? i0 + LR_BLOCK - 1 : n - 1;
     const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
-    const LiveUnits live(death, block_last / LR_STEP + 1, n, i0, block_last);
-    Tiles tiles(a, live, lds, at.b, at.h, wv, lane);
-
     bf16x8 q[KC + RC], g_[KC];
     float delta = 0.f;
     const size_t row = ((size_t)at.b * a.T + q_row) * a.H + at.h;
@@ -506,6 +506,8 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
         }
         delta = half_rows_sum(delta);
     }
+    const LiveUnits live(death, block_last / LR_STEP + 1, n, i0, block_last, wv, reinterpret_cast<uint32_t *>(lds));
+    Tiles tiles(a, live, lds, at.b, at.h, wv, lane);       // (its first tile goes behind the words)
     const size_t stat = ((size_t)at.b * a.H + at.h) * a.T + q_row;
     const float neg_lse = -a.lse[stat] * 1.4426950408889634f;
     if (half == 0 && qpos < n) {
