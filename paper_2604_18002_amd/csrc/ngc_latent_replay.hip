@@ -42,7 +42,9 @@ constexpr int LR_OWN = 32;                   // queries (keys) of a wave
 constexpr int LR_BLOCK = LR_WAVES * LR_OWN;  // of a workgroup
 constexpr int LR_STEP = 32;                  // keys (queries) of a unit: a step of the math
 constexpr int LR_MOST_POSITIONS = 64 * 64 * LR_STEP;       // a bit of a lane's words per LR_STEP keys
-constexpr int LR_SLOTS = 6;                  // units of queries in LDS: the most of D = 128
+constexpr int KV_GROUPS = 2;                 // units of keys of a workgroup of the keys' gradients
+constexpr int KV_BLOCK = KV_GROUPS * LR_OWN;
+constexpr int kv_slots(int D) { return D == 128 ? 3 : 6; }     // units of queries in LDS, for two workgroups a CU
 constexpr float LR_LAZY = 8.0f;              // the reference of the exponents moves when a maximum has outgrown it by 2^8
 
 struct LatentReplayArgs {
@@ -72,16 +74,18 @@ struct LdsRows {
     {
         return lds_swizzle<PIECES>(r);
     }
-    // LR_STEP rows from memory straight to LDS, rows `stride` bytes apart, by LR_WAVES waves; rows behind `last` are that one again, and
-    // where there are more waves than loads, some load again what others do.  (The swizzle is linear in a row's bits: a lane's part of
-    // it, and the load's.)
-    static constexpr int UNIT_LOADS = (LR_STEP / LOAD_ROWS + LR_WAVES - 1) / LR_WAVES;
-    __device__ static __forceinline__ void load_unit(const unsigned char *from, uint32_t stride, int last, unsigned char *to, int wv, int lane)
+    // LR_STEP rows from memory straight to LDS, rows `stride` bytes apart, by WAVES waves (this: wave wv of them); rows behind `last` are
+    // that one again, and where there are more waves than loads, some load again what others do.  (The swizzle is linear in a row's bits:
+    // a lane's part of it, and the load's.)
+    template <int WAVES>
+    static constexpr int LOADS = (LR_STEP / LOAD_ROWS + WAVES - 1) / WAVES;                // of a wave
+    template <int WAVES>
+    __device__ static __forceinline__ void load(const unsigned char *from, uint32_t stride, int last, unsigned char *to, int wv, int lane)
     {
         const int lrow = lane / PIECES, piece = lane % PIECES ^ swizzle(lrow);
 #pragma unroll
-        for (int i = 0; i < UNIT_LOADS; ++i) {
-            const int r0 = (i * LR_WAVES + wv) * LOAD_ROWS % LR_STEP, r = r0 + lrow;
+        for (int i = 0; i < LOADS<WAVES>; ++i) {
+            const int r0 = (i * WAVES + wv) * LOAD_ROWS % LR_STEP, r = r0 + lrow;
             start_load_to_lds16(from, (uint32_t)(r < last ? r : last) * stride + (uint32_t)(piece ^ swizzle(r0)) * 16u, to + r0 * BYTES);
         }
     }
@@ -277,9 +281,9 @@ struct KeyTiles {
             unsigned char *const to = there + i * UNIT;
             const unsigned char *const k = a.kv + (((size_t)b * a.T + first) * a.H + h) * (2 * KB);
             const uint32_t stride = (uint32_t)a.H * (2 * KB);
-            LdsRows<KB>::load_unit(k, stride, last, to, wv, lane);
-            LdsRows<RB>::load_unit(a.rope + ((size_t)b * a.T + first) * a.rope_row, (uint32_t)a.rope_row, last, to + ROT, wv, lane);
-            LdsRows<KB>::load_unit(k + KB, stride, last, to + V, wv, lane);
+            LdsRows<KB>::template load<LR_WAVES>(k, stride, last, to, wv, lane);
+            LdsRows<RB>::template load<LR_WAVES>(a.rope + ((size_t)b * a.T + first) * a.rope_row, (uint32_t)a.rope_row, last, to + ROT, wv, lane);
+            LdsRows<KB>::template load<LR_WAVES>(k + KB, stride, last, to + V, wv, lane);
         }
     }
     // The next tile, in LDS until the next call; u: its units.  By all waves.
@@ -656,20 +660,20 @@ __device__ __forceinline__ int unit_by_end(const int32_t *death, int n, int rank
 // Gradients of keys and values, and the head's of the rotary part.  Two waves for 32 keys: the first makes P of 32 queries, and with
 // it dV; the second makes dS of it and of <g, v>, and with it dK and the rotary part's.
 template <int D>
-__global__ __launch_bounds__(2 * LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(2 * KV_GROUPS * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void latent_replay_dkv_kernel(LatentReplayArgs a)
 {
     constexpr int E = D / 2, KC = D / 16, RC = E / 16, DT = D / 32, ET = E / 32, KB = D * 2, RB = E * 2, PAIRS = DT / 2;
     // 32 queries in LDS: their two parts, the gradients that arrive at them, and their statistics
     constexpr int ROT = LR_STEP * KB, G = ROT + LR_STEP * RB, STATS = G + LR_STEP * KB, BYTES = STATS + 2 * LR_STEP * 4;
     extern __shared__ __align__(16) unsigned char lds[];
-    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), wv = wave % LR_WAVES, second = wave / LR_WAVES;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), wv = wave % KV_GROUPS, second = wave / KV_GROUPS;
     const int li = lane & 31, half = lane >> 5;
-    const LatentReplayPlace at(a, (a.T + LR_BLOCK - 1) / LR_BLOCK, false);
+    const LatentReplayPlace at(a, (a.T + KV_BLOCK - 1) / KV_BLOCK, false);
     const int n = at.length(a);
-    if (at.block * LR_BLOCK >= n) return;
+    if (at.block * KV_BLOCK >= n) return;
     const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
-    const int unit = death ? unit_by_end<2 * LR_WAVES>(death, n, at.block * LR_WAVES + wv, reinterpret_cast<int *>(lds)) : at.block * LR_WAVES + wv;
+    const int unit = death ? unit_by_end<2 * KV_GROUPS>(death, n, at.block * KV_GROUPS + wv, reinterpret_cast<int *>(lds)) : at.block * KV_GROUPS + wv;
     const int wave0 = unit * LR_OWN, key = wave0 + li, k_row = key < n ? key : n - 1;
     // queries key .. until - 1 see this lane's key
     int until = n;
@@ -683,7 +687,7 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
     const int wave_end = __builtin_amdgcn_readfirstlane(wave_reduce(until, larger));
     // all of the wave's keys are seen by queries below this one, where causality lets them
     const int wave_all = __builtin_amdgcn_readfirstlane(wave_reduce(until, smaller));
-    __shared__ int begins[LR_WAVES], ends[LR_WAVES];
+    __shared__ int begins[KV_GROUPS], ends[KV_GROUPS];
     if (lane == 0) {
         begins[wv] = wave0;
         ends[wv] = wave_end;
@@ -691,7 +695,7 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
     __syncthreads();
     int begin = n, end = 0;
 #pragma unroll
-    for (int w = 0; w < LR_WAVES; ++w) {
+    for (int w = 0; w < KV_GROUPS; ++w) {
         begin = smaller(begin, begins[w]);
         end = larger(end, ends[w]);
     }
@@ -700,10 +704,10 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
     const bool some = first < units;                       // (no query sees any of the keys: no unit to read)
     const size_t stat = ((size_t)at.b * a.H + at.h) * a.T;
     const uint32_t q_stride = (uint32_t)a.H * ((D + E) * 2), g_stride = (uint32_t)a.H * KB;
-    // A unit: the first waves bring the queries, the second ones the gradients and (each of them, they count alike) the statistics.
-    constexpr int LOADS = LdsRows<KB>::UNIT_LOADS + 1;     // of a wave
-    static_assert(LdsRows<RB>::UNIT_LOADS == 1, "the same number for all waves");
-    auto slot = [&](int u) { return lds + (u - first) % LR_SLOTS * BYTES; };
+    // A unit: the first waves bring the queries, the second ones the gradients and (each of them) the statistics.
+    constexpr int Q_LOADS = LdsRows<KB>::template LOADS<KV_GROUPS> + LdsRows<RB>::template LOADS<KV_GROUPS>, G_LOADS = LdsRows<KB>::template LOADS<KV_GROUPS> + 1;
+    constexpr int SLOTS = kv_slots(D);
+    auto slot = [&](int u) { return lds + (u - first) % SLOTS * BYTES; };
     auto load_ahead = [&](int u_) {
         const int u = u_ < units ? u_ : units - 1;         // (the last one again into a free place)
         const int i = u * LR_STEP, last = a.T - 1 - i;
@@ -713,16 +717,16 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
         __asm__ volatile("" : "+v"(lane_));                // (offsets are made where they are used)
         if (!second) {
             const unsigned char *const q = a.q + row * ((D + E) * 2);
-            LdsRows<KB>::load_unit(q, q_stride, last, to, wv, lane_);
-            LdsRows<RB>::load_unit(q + KB, q_stride, last, to + ROT, wv, lane_);
+            LdsRows<KB>::template load<KV_GROUPS>(q, q_stride, last, to, wv, lane_);
+            LdsRows<RB>::template load<KV_GROUPS>(q + KB, q_stride, last, to + ROT, wv, lane_);
         } else {
-            LdsRows<KB>::load_unit(a.dout + row * KB, g_stride, last, to + G, wv, lane_);
+            LdsRows<KB>::template load<KV_GROUPS>(a.dout + row * KB, g_stride, last, to + G, wv, lane_);
             const int r = lane_ & 31;
             start_load_to_lds4(reinterpret_cast<const unsigned char *>(a.stats + stat * 2 + i), (uint32_t)((r < last ? r : last) + (lane_ >> 5) * a.T) * 4u, to + STATS);
         }
     };
     // P of a unit, from the first wave to the second: two places, fp32 as the products leave it.
-    unsigned char *const exchange = lds + LR_SLOTS * BYTES + wv * (2 * 4096) + lane * 16;
+    unsigned char *const exchange = lds + SLOTS * BYTES + wv * (2 * 4096) + lane * 16;
     auto place = [&](int u) { return exchange + (u & 1) * 4096; };
     // units mine_first .. mine_end - 1 have queries that see keys of this wave (a loop of their own: with a branch in it the sums would be
     // kept twice)
@@ -757,9 +761,10 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
         return acc;
     };
     auto round_begins = [&](int u) {
-        wait_for_loads<(LR_SLOTS - 3) * LOADS>();          // unit u is there, P of the one before too
+        if (second) wait_for_loads<(SLOTS - 3) * G_LOADS>();   // unit u is there, P of the one before too
+        else wait_for_loads<(SLOTS - 3) * Q_LOADS>();
         workgroup_barrier();                               // and everybody has left unit u - 2
-        load_ahead(u + LR_SLOTS - 2);
+        load_ahead(u + SLOTS - 2);
         __builtin_amdgcn_sched_barrier(0);
     };
     const unsigned char *const kr = a.kv + (((size_t)at.b * a.T + k_row) * a.H + at.h) * (2 * KB) + half * 16;
@@ -780,7 +785,7 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
         for (int c = 0; c < DT; ++c) dv[c] = zeros16();
         float poison = 0.f;                                // NaN: a gradient that is not finite arrives at a query that sees the key
         __builtin_amdgcn_s_waitcnt(0x0F70);
-        for (int u = first; some && u < first + LR_SLOTS - 2; ++u) load_ahead(u);
+        for (int u = first; some && u < first + SLOTS - 2; ++u) load_ahead(u);
         for (int u = first; u < mine_first; ++u) round_begins(u);
         for (int u = mine_first; u < mine_end; ++u) {
             round_begins(u);
@@ -839,7 +844,7 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
 #pragma unroll
         for (int c = 0; c < ET; ++c) dr[c] = zeros16();
         __builtin_amdgcn_s_waitcnt(0x0F70);
-        for (int u = first; some && u < first + LR_SLOTS - 2; ++u) load_ahead(u);
+        for (int u = first; some && u < first + SLOTS - 2; ++u) load_ahead(u);
         for (int u = first - 1; some && u < mine_first; ++u) round_begins(u + 1);
         for (int u = mine_first; u < mine_end; ++u) {
             round_begins(u + 1);
@@ -943,11 +948,11 @@ LatentReplayArgs latent_replay_args(const void *q, const void *kv, const void *r
 
 size_t latent_replay_stats_bytes(int32_t B, int32_t T, int32_t Hq) { return align256((size_t)B * Hq * T * 2 * sizeof(float)); }
 
-int launch_blocks(const void *fn, const LatentReplayArgs &args, int waves, size_t lds, hipStream_t st)
+int launch_blocks(const void *fn, const LatentReplayArgs &args, int block, int threads, size_t lds, hipStream_t st)
 {
     LatentReplayArgs a = args;
     if (lds > 64 * 1024) NGC_HIP_CHECK(hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    return launch(fn, dim3((unsigned)((a.T + LR_BLOCK - 1) / LR_BLOCK * a.B * a.H)), dim3(waves * 64), lds, st, a);
+    return launch(fn, dim3((unsigned)((a.T + block - 1) / block * a.B * a.H)), dim3(threads), lds, st, a);
 }
 
 }  // namespace
@@ -968,7 +973,7 @@ extern "C" int ngc_latent_replay_attn(const void *q, const void *kv, const void 
     a.out = reinterpret_cast<unsigned char *>(out);
     a.lse = lse_out;
     const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_kernel<64>);
-    return launch_blocks(fn, a, LR_WAVES, D == 128 ? KeyTiles<128>::BYTES : KeyTiles<64>::BYTES, (hipStream_t)stream);
+    return launch_blocks(fn, a, LR_BLOCK, LR_WAVES * 64, D == 128 ? KeyTiles<128>::BYTES : KeyTiles<64>::BYTES, (hipStream_t)stream);
 }
 
 extern "C" int ngc_latent_replay_attn_backward(const void *q, const void *kv, const void *rope, int64_t rope_stride, const int32_t *death,
@@ -992,10 +997,10 @@ extern "C" int ngc_latent_replay_attn_backward(const void *q, const void *kv, co
     a.part = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(ws) + latent_replay_stats_bytes(B, T, Hq));
     hipStream_t st = (hipStream_t)stream;
     const size_t lds = D == 128 ? KeyTiles<128>::BYTES : KeyTiles<64>::BYTES;
-    rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dq_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dq_kernel<64>), a, LR_WAVES, lds, st);
+    rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dq_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dq_kernel<64>), a, LR_BLOCK, LR_WAVES * 64, lds, st);
     if (rc) return rc;
     rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dkv_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dkv_kernel<64>), a,
-                       2 * LR_WAVES, LR_SLOTS * (lds / 4 + 2 * LR_STEP * sizeof(float)) + LR_WAVES * 2 * 4096, st);
+                       KV_BLOCK, 2 * KV_GROUPS * 64, kv_slots(D) * (lds / 4 + 2 * LR_STEP * sizeof(float)) + KV_GROUPS * 2 * 4096, st);
     if (rc) return rc;
     const long long threads = (long long)B * T * (D / 2 / 4);
     const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_rope_kernel<64>) : reinterpret_cast<const void *>(&latent_replay_rope_kernel<32>);
