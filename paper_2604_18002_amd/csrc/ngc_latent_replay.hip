@@ -234,14 +234,21 @@ struct LiveUnits {
     __device__ __forceinline__ bool whole(int u) const { return (word(all_lo, all_hi, u) >> (u % 32)) & 1u; }
 };
 
-// What a workgroup that owns queries (forward, backward q) or keys (backward kv) works on: heaviest first, a (trajectory, head) on
-// one XCD, whose L2 then holds its rows.
+// What a workgroup that owns queries (forward, backward q) or keys (backward kv) works on: `at_once` (trajectory, head)s at a time (0:
+// all), the heaviest blocks of each first; their number is a multiple of 8, so that each keeps to one XCD, whose L2 then has its rows.
+// Few at a time read less (backward kv, 16 for all 32 of 2 x 3850 positions, 16 heads: half the misses, 437 us for 451 with
+// backward q); the queries' owners read less in the first place and fare better with the heaviest of all first (16 x 1050 positions:
+// 95 us for 100).
+constexpr int KV_AT_ONCE = 16;
 struct LatentReplayPlace {
     int block, b, h;
-    __device__ __forceinline__ LatentReplayPlace(const LatentReplayArgs &a, int blocks, bool last_first)
+    __device__ __forceinline__ LatentReplayPlace(const LatentReplayArgs &a, int blocks, bool last_first, int at_once)
     {
         const int heads = a.B * a.H;
-        const int i = (int)(blockIdx.x / (unsigned)heads), bh = (int)(blockIdx.x % (unsigned)heads);
+        if (at_once == 0) at_once = heads;
+        const int chunk = (int)(blockIdx.x / (unsigned)(at_once * blocks)), r = (int)blockIdx.x - chunk * at_once * blocks;
+        const int first = chunk * at_once, here = heads - first < at_once ? heads - first : at_once;
+        const int i = r / here, bh = first + r % here;
         block = last_first ? blocks - 1 - i : i;
         b = bh / a.H;
         h = bh % a.H;
@@ -335,7 +342,7 @@ void latent_replay_kernel(LatentReplayArgs a)
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
     const int li = lane & 31, half = lane >> 5;
-    const LatentReplayPlace at(a, (a.T + LR_BLOCK - 1) / LR_BLOCK, true);
+    const LatentReplayPlace at(a, (a.T + LR_BLOCK - 1) / LR_BLOCK, true, 0);
     const int n = at.length(a), i0 = at.block * LR_BLOCK;
     if (i0 >= n) return;
     const int wave0 = i0 + wv * LR_OWN, qpos = wave0 + li;
@@ -487,7 +494,7 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
     const int li = lane & 31, half = lane >> 5;
-    const LatentReplayPlace at(a, (a.T + LR_BLOCK - 1) / LR_BLOCK, true);
+    const LatentReplayPlace at(a, (a.T + LR_BLOCK - 1) / LR_BLOCK, true, 0);
     const int n = at.length(a), i0 = at.block * LR_BLOCK;
     if (i0 >= n) return;
     const int wave0 = i0 + wv * LR_OWN, qpos = wave0 + li, q_row = qpos < n ? qpos : n - 1;
@@ -669,7 +676,7 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), wv = wave % KV_GROUPS, second = wave / KV_GROUPS;
     const int li = lane & 31, half = lane >> 5;
-    const LatentReplayPlace at(a, (a.T + KV_BLOCK - 1) / KV_BLOCK, false);
+    const LatentReplayPlace at(a, (a.T + KV_BLOCK - 1) / KV_BLOCK, false, KV_AT_ONCE);
     const int n = at.length(a);
     if (at.block * KV_BLOCK >= n) return;
     const int32_t *death = a.death ? a.death + (size_t)at.b * a.T : nullptr;
