@@ -546,7 +546,7 @@ extern "C" int ngc_latent_attn(const ngc_paged_cache *pc, int32_t layer, const i
     if (ws_bytes < scratch_offset(&c)) return NGC_ENOSPC;
     const int R = latent_width(pc->D), M = W * pc->Hq;
     const LatentShape shape = latent_shape(M);
-    if ((long long)nseg * shape.blocks > 0x7FFFFFFFLL || nseg > 65535) return NGC_EUNSUPPORTED;
+    if (!launchable((long long)nseg * shape.blocks, shape.waves * 64) || nseg > 65535) return NGC_EUNSUPPORTED;
     const int rows = max_len_hint > 0 && max_len_hint < c.cap ? max_len_hint : c.cap;
     int S = latent_splits(shape, nseg, rows);
     while (S > 1 && scratch_offset(&c) + latent_partial_bytes(nseg, S, M, R) > ws_bytes) S /= 2;

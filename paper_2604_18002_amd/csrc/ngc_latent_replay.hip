@@ -934,7 +934,7 @@ int check_latent_replay(const void *q, const void *kv, const void *rope, int64_t
     if (!latent_replay_sizes(B, T, Hq, D) || rope_stride < D / 2 || rope_stride % 8 != 0) return NGC_EINVAL;
     if (!(scale > 0.f) || !(scale <= 2.35e38f)) return NGC_EINVAL;
     if (Hq > LATENT_MOST_HEADS || T > LR_MOST_POSITIONS || rope_stride > 1 << 20) return NGC_EUNSUPPORTED;
-    if ((long long)((T + LR_BLOCK - 1) / LR_BLOCK) * B * Hq > 0x7FFFFFFFLL) return NGC_EUNSUPPORTED;
+    if (!launchable((long long)((T + KV_BLOCK - 1) / KV_BLOCK) * B * Hq, 2 * KV_GROUPS * 64)) return NGC_EUNSUPPORTED;
     return NGC_OK;
 }
 

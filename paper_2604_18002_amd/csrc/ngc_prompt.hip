@@ -213,6 +213,7 @@ extern "C" int ngc_paged_extend(const ngc_paged_cache *pc, int32_t layer, const 
     int rc = check_pages(pc);
     if (rc) return rc;
     if (!slot_out || !start_out || !ws || !aligned16(ws) || T < 1) return NGC_EINVAL;
+    if ((long long)pc->B * pc->Hkv > MOST_SEGMENTS / pc->L) return NGC_EUNSUPPORTED;
     int seg0, nseg;
     rc = paged_layer_range(pc, layer, &seg0, &nseg);
     if (rc) return rc;
@@ -249,7 +250,7 @@ extern "C" int ngc_paged_fill(const ngc_paged_cache *pc, int32_t layer, const vo
     if (ws_bytes < STATUS_BYTES) return NGC_ENOSPC;
     const int pieces = pc->D * 2 / 16;
     const long long groups = ((long long)T * pc->Hkv * pieces + FILL_THREADS * FILL_BATCH - 1) / (FILL_THREADS * FILL_BATCH);
-    if ((long long)T * pc->Hkv > 0x7FFFFFFFLL || groups > 0x7FFFFFFFLL || (long long)pc->num_pages * pc->page_rows > 0x7FFFFFFFLL)
+    if ((long long)T * pc->Hkv > 0x7FFFFFFFLL || !launchable(groups * (layer < 0 ? pc->L : 1), FILL_THREADS) || (long long)pc->num_pages * pc->page_rows > 0x7FFFFFFFLL)
         return NGC_EUNSUPPORTED;
     FillArgs a{};
     a.k_pool = reinterpret_cast<unsigned char *>(pc->k_pool);

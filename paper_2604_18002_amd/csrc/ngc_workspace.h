@@ -60,12 +60,15 @@ inline int check_paged(const ngc_paged_cache *pc)
 
 // Latent caches: one pool, one row a token for all heads.
 constexpr int LATENT_MOST_HEADS = 128, LATENT_MOST_TOKENS = 1024;
+// A launch has fewer than 2^32 threads: segments, a workgroup of 256 each, and workgroups of any launch.
+constexpr long long MOST_SEGMENTS = (1 << 24) - 1;
+constexpr bool launchable(long long groups, int threads) { return groups * threads <= 0xFFFFFFFFLL; }
 inline int latent_width(int D) { return D / 9 * 8; }           // of the latent part of a row of D values
 inline int check_latent(const ngc_paged_cache *pc)
 {
     if (check_pages_of(pc) != NGC_OK || pc->v_pool || pc->Hkv != 1) return NGC_EINVAL;
     if (pc->D != 576 && pc->D != 288) return NGC_EINVAL;
-    if (pc->Hq > LATENT_MOST_HEADS) return NGC_EUNSUPPORTED;
+    if (pc->Hq > LATENT_MOST_HEADS || (long long)pc->L * pc->B > MOST_SEGMENTS) return NGC_EUNSUPPORTED;
     return check_pages_limits(pc);
 }
 

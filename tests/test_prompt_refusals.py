@@ -121,3 +121,19 @@ def test_replay_arguments(lib):
         assert forward(**bad) == EUNSUPPORTED and backward(**bad) == EUNSUPPORTED, bad
     assert lib.ngc_latent_replay_workspace_bytes(2, 100, 4, 96) == 0
     assert lib.ngc_latent_replay_workspace_bytes(2, 100, 4, 128) >= 2 * 100 * 4 * (64 + 1) * 4
+
+
+def test_launches_beyond_the_number_of_threads(lib):
+    """2^32 threads and more, and numbers of segments that do not fit, are refused before anything is computed from them."""
+    for B, T, H, D in ((100, 131072, 128, 128), (20000, 4096, 128, 64)):
+        args = (A, A, A, 64, None, None)
+        assert lib.ngc_latent_replay_attn(*args, B, T, H, D, 0.1, A, None, None) == EUNSUPPORTED
+        assert lib.ngc_latent_replay_attn_backward(*args, A, A, A, B, T, H, D, 0.1, A, A, A, A, WS, None) == EUNSUPPORTED
+    def attn(layer, **kw):
+        return lib.ngc_latent_attn(C.byref(latent(Hq=128, **kw)), layer, None, 1024, A, 0.1, 0, A, None, A, WS, None)
+    assert attn(0, L=1, B=8192, max_pages=1) == EUNSUPPORTED
+    assert attn(-1, L=2, B=2 ** 31 - 1, max_pages=1) == EUNSUPPORTED
+    for pc in (cache(L=65535, B=2 ** 31 - 1, Hkv=2, max_pages=1), latent(L=65535, B=300, max_pages=1), cache(L=1, B=2 ** 24, Hkv=1, max_pages=1)):
+        assert lib.ngc_paged_extend(C.byref(pc), -1, None, 8, A, A, A, WS, None) == EUNSUPPORTED
+    for pc, v in ((cache(L=65535), A), (latent(L=60000), None)):
+        assert lib.ngc_paged_fill(C.byref(pc), -1, A, v, None, A, 1 << 24, A, WS, None) == EUNSUPPORTED
