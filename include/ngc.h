@@ -36,6 +36,15 @@
  *   ngc_paged_fork, ngc_paged_free, ngc_paged_compact  copies of sequences, ended
  *                        sequences, and a pool with its pages in use at the front
  *
+ * for prompts, and for layers that keep one latent row a token for all heads:
+ *
+ *   ngc_paged_extend     pages, lengths and slots for any number of new tokens of
+ *                        every sequence
+ *   ngc_paged_fill       their rows to those slots
+ *   ngc_latent_attn      attention of new tokens over a paged cache of latent rows
+ *   ngc_latent_replay_attn, ngc_latent_replay_attn_backward  training-time attention
+ *                        of such layers under the replay mask, and its gradient
+ *
  * General conventions
  *   - Every pointer is a DEVICE pointer unless a comment says "host".  The
  *     structs themselves (ngc_cache, ngc_evict_params) live in HOST memory and
@@ -83,7 +92,8 @@ extern "C" {
  * when a launch has ended. */
 #define NGC_STATUS_WORDS        64
 #define NGC_STATUS_KEEP_CLAMPED  0  /* keep[seg] > items (or < 0): clamped                  */
-#define NGC_STATUS_LEN_CLAMPED   1  /* len[seg] > cap (or < 0): clamped                     */
+#define NGC_STATUS_LEN_CLAMPED   1  /* len[seg] > cap (or < 0), or a number of new tokens out
+                                       of range: clamped                                    */
 #define NGC_STATUS_EMPTY_ATTN    2  /* decode attention over an empty segment: zeros        */
 #define NGC_STATUS_APPEND_FULL   3  /* append to a full segment: skipped                    */
 #define NGC_STATUS_BAD_SIGMA     4  /* ngc_subset_logprob: index out of range or repeated   */
@@ -662,8 +672,9 @@ int ngc_paged_compact(const ngc_paged_cache *pc, void *ws, size_t ws_bytes, void
  * Rows that a segment has no room or no page for are left out, the last first, and
  * counted one by one (NGC_STATUS_APPEND_FULL); a length out of range leaves its
  * segment as it is (NGC_STATUS_LEN_CLAMPED), and a row in a page outside the pool has
- * slot -1 (NGC_STATUS_POOL_BOUNDS).  num_pages * page_rows < 2^31
- * (NGC_EUNSUPPORTED).  ws must hold ngc_paged_workspace_bytes(). */
+ * slot -1 (NGC_STATUS_POOL_BOUNDS).  num_pages * page_rows < 2^31,
+ * L * B * Hkv < 2^24 (NGC_EUNSUPPORTED).  ws must hold ngc_paged_workspace_bytes()
+ * (of a latent cache, below, ngc_latent_workspace_bytes()). */
 int ngc_paged_extend(const ngc_paged_cache *pc, int32_t layer, const int32_t *n_new, int32_t T,
                      int32_t *slot_out, int32_t *start_out, void *ws, size_t ws_bytes, void *stream);
 
@@ -684,10 +695,11 @@ int ngc_paged_fill(const ngc_paged_cache *pc, int32_t layer, const void *k_new, 
  * a rotary part of E values that all heads share.  Such a cache is an ngc_paged_cache
  * of one pool:
  *   k_pool   bf16 [num_pages][page_rows][R + E], latent part first; v_pool is NULL
- *   Hkv = 1; D = R + E: 576 = 512 + 64 or 288 = 256 + 32; Hq <= 128 (NGC_EUNSUPPORTED)
+ *   Hkv = 1; D = R + E: 576 = 512 + 64 or 288 = 256 + 32; Hq <= 128, L * B < 2^24
+ *   (NGC_EUNSUPPORTED)
  * Calls that deal with pages take it as they take others: ngc_paged_extend,
- * ngc_paged_fill (v_new NULL), ngc_paged_evict, ngc_paged_free.  All other
- * ngc_paged_* calls refuse it. */
+ * ngc_paged_fill (v_new NULL), ngc_paged_evict, ngc_paged_free, with a workspace of
+ * ngc_latent_workspace_bytes().  All other ngc_paged_* calls refuse it (NGC_EINVAL). */
 
 /* Attention of the newest tokens over a latent cache, in the absorbed form: their
  * queries have been brought to the latent space (by the matrix that expands keys from
@@ -709,8 +721,9 @@ int ngc_paged_fill(const ngc_paged_cache *pc, int32_t layer, const void *k_new, 
  * A token that sees no row has zeros and -inf (an empty sequence is counted:
  * NGC_STATUS_EMPTY_ATTN).  Scores, soft-max and accumulation are fp32, weights are rounded
  * to bf16.  Values that are not finite reach the tokens that see their row, and no other.
- * ws must hold ngc_latent_workspace_bytes(), which makes every call on such a cache
- * succeed. */
+ * ws must hold ngc_latent_workspace_bytes(), which serves every call on such a cache
+ * with up to W new tokens; with less, down to its fixed part, fewer workgroups share
+ * a sequence. */
 size_t ngc_latent_workspace_bytes(const ngc_paged_cache *pc, int32_t W);
 int ngc_latent_attn(const ngc_paged_cache *pc, int32_t layer, const int32_t *n_new, int32_t W,
                     const void *q, float scale, int32_t max_len_hint, void *out, float *lse_out,

@@ -16,6 +16,13 @@
 // A workgroup's waves are RG row groups x KG key groups: waves of one key group share tiles, the key groups take tiles in
 // turn and are joined in LDS at the end.  Few sequences are shared by S workgroups, whose partials a second launch joins.
 //
+// What bounds it, R = 512, per row of every sequence (one long batch minus a shorter one, 256 sequences): 16 heads 6.2 TB/s, what
+// reads alone reach; 64 heads 6.3 TB/s; 128 heads 940 TFLOP/s and 3.9 TB/s, where a large product of matrices reaches 1230.  There a
+// wave's products wait for its own reads of LDS (256 bytes a clock: 30 % of it is used) and for the loads' issue, ~100 clocks each;
+// the other wave of the SIMD covers a part, the matrix units are busy 40 % of the time.  Besides that, a call of 64 sequences x 16 heads x
+// 1000 to 2000 rows (35 us; 18 for the bytes) has ~5 us until the first tile is there, lengths 1.3 times the mean in its longest
+// workgroups, 3 us of partials and a joining launch of 4.7; one of 128 x 128 x 1894 to 3533 (135 us; 78 for the products) its lengths.
+//
 // P is rounded to bf16 for the second product (2^-9 of an entry at most), as the output is: it is the operand of the
 // product that brings the latent vectors to the heads' values.  Sums and soft-max state are fp32.
 #include <hip/hip_runtime.h>
@@ -30,8 +37,8 @@
 namespace ngc {
 
 constexpr int LT_ROWS = 16;                 // query rows of a wave
-// Rows of a tile.  One row group is bound by the memory: its waves have tiles of their own, small ones, the next on its way while one is
-// worked on.  More of them are as much bound by the products, whose full rate takes 32.
+// Rows of a tile.  The waves of one row group are key groups, each with tiles of its own: small ones, the next on its way while one is
+// worked on.  Four row groups are as much bound by the products, whose full rate takes 32.
 constexpr int latent_keys(int RG) { return RG == 1 ? 16 : 32; }
 constexpr int LT_LDS_KEYS = 128;            // rows in LDS: those of R = 512 fill a CU's
 
@@ -129,7 +136,7 @@ void latent_attn_kernel(LatentArgs a)
     constexpr int LOADS = LAT_LOADS + ROT_LOADS;
     // A wave is held up where it asks for a tile, about 100 clocks a load.  The two waves of a SIMD, of different key groups, do it at
     // different times: 343 us for 380 with 256 sequences of 4096 rows and 128 heads, R = 512.
-    constexpr bool LATER = NW == 8;
+    constexpr bool LATER = RG > 1;
     constexpr int PARTS = (NW * LT_ROWS * R * 4 + SLOTS * Tile::BYTES - 1) / (SLOTS * Tile::BYTES);       // the output goes through LDS in
 
     extern __shared__ __align__(256) unsigned char lds[];
@@ -253,7 +260,7 @@ void latent_attn_kernel(LatentArgs a)
         const int key0 = t * KEYS;
         constexpr int SCORES = 4 * HALVES;
         // GROUP chunks' rows (column tiles) are asked for DEPTH - 1 groups (a group) before their products run
-        constexpr int GROUP = NW == 4 && HALVES == 1 ? (CHUNKS % 6 == 0 ? 6 : 9) : NW == 8 && R == 512 ? 1 : 3, VGROUP = NW == 4 ? 8 : 4, DEPTH = NW == 8 && R == 512 ? 4 : 2;
+        constexpr int GROUP = RG == 1 ? (CHUNKS % 6 == 0 ? 6 : 9) : R == 512 ? 1 : 3, VGROUP = RG == 1 ? 8 : 4, DEPTH = RG > 1 && R == 512 ? 4 : 2;
         static_assert(CHUNKS % GROUP == 0 && CT % VGROUP == 0, "whole groups");
         f32x4 sc[HALVES];
 #pragma unroll
@@ -485,18 +492,29 @@ using namespace ngc;
 
 namespace {
 
-// How M query rows are dealt to waves and workgroups.
+// How M query rows are dealt to waves and workgroups: one row group a workgroup, or four.
 struct LatentShape {
     int waves, groups, blocks, key_groups;
 };
-LatentShape latent_shape(int M)
+LatentShape latent_shape(int groups, int M)
 {
     LatentShape s;
-    s.groups = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    s.waves = s.groups <= 2 ? 4 : 8;
-    s.blocks = (M + LT_ROWS * s.groups - 1) / (LT_ROWS * s.groups);
-    s.key_groups = s.waves / s.groups;
+    s.groups = groups;
+    s.waves = groups == 1 ? 4 : 8;
+    s.blocks = (M + LT_ROWS * groups - 1) / (LT_ROWS * groups);
+    s.key_groups = s.waves / groups;
     return s;
+}
+// One row group reads every row once for 16 query rows, four for 64; but its workgroups have more of the matrix units to themselves,
+// start and end sooner, and leave a quarter of the sums to join.  It is taken as long as that leaves a CU at most 640 rows.  Measured
+// with 24 to 256 query rows, R = 512 and 256, the time of one for that of four: at 512 rows a CU 0.68 to 0.96 (32 query rows of 8 sequences
+// of 2000 rows, R = 512, where it is 256: 17 us for 24), at 768 1.0 to 1.3, far beyond up to 2.6 (256 of 64 of 8000).  Two groups were
+// behind the better of these everywhere.
+constexpr long long LT_NARROW_ROWS = 256 * 640;
+LatentShape latent_shape(int M, int nseg, int rows)
+{
+    const LatentShape narrow = latent_shape(1, M);
+    return M <= LT_ROWS || (long long)nseg * narrow.blocks * rows <= LT_NARROW_ROWS ? narrow : latent_shape(4, M);
 }
 
 // How many workgroups share a sequence's rows.
@@ -523,9 +541,11 @@ extern "C" size_t ngc_latent_workspace_bytes(const ngc_paged_cache *pc, int32_t 
     for (int w = 1; w <= W; ++w) {                         // (calls with fewer new tokens may be split more often)
         const int M = w * pc->Hq;
         for (int layers : {1, pc->L}) {
-            const int nseg = layers * pc->B;
-            const size_t bytes = latent_partial_bytes(nseg, latent_splits(latent_shape(M), nseg, c.cap), M, R);
-            most = bytes > most ? bytes : most;
+            for (int groups : {1, 4}) {                    // (or a smaller hint takes the other shape)
+                const int nseg = layers * pc->B;
+                const size_t bytes = latent_partial_bytes(nseg, latent_splits(latent_shape(groups, M), nseg, c.cap), M, R);
+                most = bytes > most ? bytes : most;
+            }
         }
     }
     return scratch_offset(&c) + most;
@@ -545,9 +565,9 @@ extern "C" int ngc_latent_attn(const ngc_paged_cache *pc, int32_t layer, const i
     const ngc_cache c = logical_geometry(pc);
     if (ws_bytes < scratch_offset(&c)) return NGC_ENOSPC;
     const int R = latent_width(pc->D), M = W * pc->Hq;
-    const LatentShape shape = latent_shape(M);
-    if (!launchable((long long)nseg * shape.blocks, shape.waves * 64) || nseg > 65535) return NGC_EUNSUPPORTED;
     const int rows = max_len_hint > 0 && max_len_hint < c.cap ? max_len_hint : c.cap;
+    const LatentShape shape = latent_shape(M, nseg, rows);
+    if (!launchable((long long)nseg * shape.blocks, shape.waves * 64) || nseg > 65535) return NGC_EUNSUPPORTED;
     int S = latent_splits(shape, nseg, rows);
     while (S > 1 && scratch_offset(&c) + latent_partial_bytes(nseg, S, M, R) > ws_bytes) S /= 2;
 
@@ -570,7 +590,6 @@ extern "C" int ngc_latent_attn(const ngc_paged_cache *pc, int32_t layer, const i
 #define NGC_PICK_LATENT(R_, E_) \
     lds = LT_LDS_KEYS * (R_ + E_) * 2 + (2 * 8 * LT_ROWS + 32) * sizeof(float); \
     fn = shape.groups == 1   ? reinterpret_cast<const void *>(&latent_attn_kernel<R_, E_, 4, 1>) \
-         : shape.groups == 2 ? reinterpret_cast<const void *>(&latent_attn_kernel<R_, E_, 4, 2>) \
                              : reinterpret_cast<const void *>(&latent_attn_kernel<R_, E_, 8, 4>)
     if (R == 512) { NGC_PICK_LATENT(512, 64); }
     else { NGC_PICK_LATENT(256, 32); }

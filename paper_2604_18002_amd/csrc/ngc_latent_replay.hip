@@ -11,18 +11,33 @@
 //
 // and the rotary part's gradient is the sum of the heads'.
 //
-// Three kernels around the same tiles of 32 x 32 pairs by 32x32x16 matrix instructions, four waves a workgroup:
-//   forward      a wave has 32 queries and walks tiles of 64 keys: S^T = K Q^T, O^T += V^T P.
+// Kernels around the same units of 32 x 32 pairs by 32x32x16 matrix instructions, two workgroups a CU:
+//   forward      four waves of 32 queries each walk tiles of two units of 32 keys: S^T = K Q^T, O^T += V^T P.
 //   backward, q  the same walk, S^T and (V G^T) again, dQ^T += K^T dS; leaves delta and lse as the next one wants them.
-//   backward, kv a wave has 32 keys and walks tiles of 64 queries: S = Q K^T and G V^T, dV^T += G^T P, dK^T += Q^T dS.
+//   backward, kv two waves for 32 keys (two such pairs in a workgroup) walk units of 32 queries: the first makes S = Q K^T, P and
+//                dV^T += G^T P, the second, a unit behind, G V^T, dS of it and of P, and dK^T += Q^T dS: 20 products of 32 x 32 x 16 each
+//                (D = 128), and the sums of 32 keys, 160 registers of a lane, in two waves.  P goes from one to the other in fp32.
 // In each the pairs stand in registers as the first products leave them, which is the order the second products' operand
 // needs if the rows of the other operand are read transposed in the same order: nothing crosses lanes but a row's maximum.
 // The two backward kernels form S twice (7 products in place of 5), so that every sum has one owner: no atomics, the same
 // bits again.
 //
 // 32 keys that are dead for all of a workgroup's queries are never loaded: pages are evicted whole.  Tiles of keys are made of two
-// such units that live, wherever they are.  Pairs are masked one by one only on the diagonal, behind the sequence's end, or
-// where keys die midway.
+// such units that live, wherever they are; keys are given to workgroups in the order of their ends, so that a workgroup's live about as
+// long.  Pairs are masked one by one only on the diagonal, behind the sequence's end, or where keys die midway.
+//
+// What bounds it.  2 (2 D + E) flops a pair forward, 2 (3 (D + E) + 2 D) + 2 (2 D + E) backward (D = 128: 640 and 1664 with what is formed
+// twice left out) on 16-bit inputs: the products, for more than some hundred positions.  Measured, 16 heads of 128: 8192 positions
+// without evictions 900 to 945 TFLOP/s forward (370 to 385 us) and 690 backward, where a large product of matrices reaches 1230; 2 x 3000
+// to 3850 positions with evictions every 512, 131 us forward, 176 us the queries' and 285 us the keys' gradients.  A wave's products wait
+// for its reads of LDS and its exponentials, which the other wave of its SIMD covers in part: the matrix units are busy 40 % of the time
+// forward without evictions.  With evictions a workgroup has few tiles and its first one, 2.5 us, and the look at the ends, 1.5, count.
+//   Registers decide: two waves a SIMD have 256 each, and one more copy of the sums (a branch around a unit makes the compiler keep
+// one) or offsets kept for every read (they differ in a bit: made where they are used) went to scratch, whose loads wait behind every
+// tile on its way: the queries' gradient 245 us with 23 such registers, 190 without.
+//   Not kept: one wave for 32 keys with all sums (one wave a SIMD, 380 us, nobody covers its waits: 320 with two waves); four pairs of
+// waves a workgroup (317 us with evictions, keys that live for different times; 5 % faster without); units of keys one by one in
+// a ring of four (forward 167 us for 137: a barrier and the offsets for every 32 keys); loads spread between the products.
 //
 // P and dS are rounded to bf16 (2^-8 of an entry at most) for their second products, as outputs and gradients are; sums,
 // maxima, lse and delta are fp32.
