@@ -112,32 +112,6 @@ struct AttnArgs {
     int B;
 };
 
-// Loads and stores that other workgroups' data travels through: device scope (served by memory, not by an XCD's own
-// L2), 16 bytes wide for the partial O rows (a wave's stores land as whole cache lines instead of one 4-byte
-// write-through per lane): raw buffer accesses with the device-scope bit, bounds-checked by the hardware against
-// `bytes` (a load past the end returns 0, a store past the end is dropped).
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t device_span(const void *base, uint32_t bytes)
-{
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x00020000);
-}
-constexpr int AUX_DEVICE_SCOPE = 16;   // sc1
-__device__ __forceinline__ void st_device16(__amdgpu_buffer_rsrc_t r, uint32_t byte_off, f32x4 v)
-{
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, byte_off, 0, AUX_DEVICE_SCOPE);
-}
-__device__ __forceinline__ f32x4 ld_device16(__amdgpu_buffer_rsrc_t r, uint32_t byte_off)
-{
-    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, byte_off, 0, AUX_DEVICE_SCOPE));
-}
-__device__ __forceinline__ void st_device8(__amdgpu_buffer_rsrc_t r, uint32_t byte_off, f32x2 v)
-{
-    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), r, byte_off, 0, AUX_DEVICE_SCOPE);
-}
-__device__ __forceinline__ f32x2 ld_device8(__amdgpu_buffer_rsrc_t r, uint32_t byte_off)
-{
-    return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(r, byte_off, 0, AUX_DEVICE_SCOPE));
-}
-
 // EARLY: a wave's first tile is requested before the length has arrived (see first_tile_early()).
 template <int D, bool PAGED, bool APPEND, bool EARLY>
 __global__ __launch_bounds__(ATT_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))

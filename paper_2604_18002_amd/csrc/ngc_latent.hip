@@ -397,9 +397,7 @@ void latent_attn_kernel(LatentArgs a)
         if (a.S == 1) {
             if (a.lse_out) a.lse_out[(size_t)seg * a.M + my_row] = l_all == 0.f ? -INFINITY : m_all * a.scale + logf(l_all);
         } else {
-            float *ml = a.part_ml + (((size_t)seg * a.S + split) * a.M + my_row) * 2;
-            ml[0] = m_all;
-            ml[1] = l_all;
+            st_device8(device_span(a.part_ml + ((size_t)seg * a.S + split) * a.M * 2, (uint32_t)a.M * 8u), (uint32_t)my_row * 8u, f32x2{m_all, l_all});
         }
     }
     if (a.S > 1 && rounds == 0) return;                    // (nothing was seen: the join does not look at it)
@@ -431,12 +429,15 @@ void latent_attn_kernel(LatentArgs a)
                                  __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{o[2], o[3]}, bf16x2))};
                 *reinterpret_cast<u32x2 *>(a.out + (((size_t)seg * a.M + to) * R + col) * 2) = b;
             } else {
-                *reinterpret_cast<f32x4 *>(a.part_o + (((size_t)seg * a.S + split) * a.M + to) * R + col) = o;
+                st_device16(device_span(a.part_o + ((size_t)seg * a.S + split) * a.M * R, (uint32_t)(a.M * R) * 4u), (uint32_t)(to * R + col) * 4u, o);
             }
         }
     }
 }
 
+// The partials are stored past the L2, which the end of a launch would have to write back before the next one begins (16 x 1000 rows, 32
+// query rows 19.1 -> 16.1 us, 64 x 1500, 16: 29.5 -> 28.6).  A join in the same launch by the last of a segment's workgroups, which a
+// ticket tells, took 2 to 6 us more than this one: a workgroup has to read alone what is read here by 16.
 // Partials of a query row joined, a workgroup (two for R = 256 in one) a row: R / 4 threads.  The shares of all partials first, then the
 // partials, JOIN_BATCH asked for at a time.
 constexpr int JOIN_THREADS = 128, JOIN_BATCH = 8;
