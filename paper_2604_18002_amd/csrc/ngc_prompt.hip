@@ -3,8 +3,11 @@
 //
 // extend   Two prefix sums: over the sequences, where the tokens of each begin among the packed ones, and over the segments, how many
 //          pages are granted before each (the order of every grant of this layout, see ngc.h).  One workgroup makes them, a few
-//          integers per segment; a workgroup per segment then writes its table entries and slots.
-// fill     A copy: row (token, head) to the slot that the map names.  Bound by the memory.
+//          integers per segment; a workgroup per segment then writes its table entries and slots.  Bound by round trips: 28 x 16 x 2
+//          segments that grow by a token 3.9 and 3.5 us (10.4 a call), 28 x 64 x 2 of 300 to 1000 tokens 6.1 and 9.2.  Lengths, pages and
+//          slots go in batches of four, all of a batch on their way together (one by one 8.7 and 14.5).
+// fill     A copy: row (token, head) to the slot that the map names.  Bound by the memory: 64 x 2 x 300 to 1000 rows of 128, K and V
+//          (85 MB), 16.5 us, 5.2 TB/s; 8 x 1000 to 4096 rows of 576 (47 MB) 11.3.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -163,7 +166,9 @@ struct FillArgs {
 };
 
 constexpr int FILL_THREADS = 256;
-constexpr int FILL_BATCH = 4;               // 16-byte pieces of K (and V) per thread
+// 16-byte pieces of K (and V) per thread: 1 17.3 us for those 85 MB, 2 16.5, 4 18.9, 8 41.  The rows are read once, past the caches (through
+// them 20.2); written through the L2 like any others, they are read soon (past it 20.3, with 4).
+constexpr int FILL_BATCH = 2;
 template <int PIECES, bool V>
 __global__ __launch_bounds__(FILL_THREADS) void fill_kernel(FillArgs a)
 {
