@@ -34,6 +34,10 @@ __device__ __forceinline__ void wait_for_loads()
 {
     __asm__ volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(N) : "memory");
 }
+// Everything that this wave has asked for is there, and the compiler knows it.  Needed before a loop that uses what was loaded before it:
+// the compiler would count, inside the loop, the loads that may still be on their way on its first turn, and wait for the tiles asked
+// for ahead of it in their place, on every turn.
+__device__ __forceinline__ void own_rows_loaded() { __builtin_amdgcn_s_waitcnt(0x0F70); }       // vmcnt(0)
 __device__ __forceinline__ void workgroup_barrier()
 {
     __asm__ volatile("s_barrier" : : : "memory");

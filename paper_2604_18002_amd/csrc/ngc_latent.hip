@@ -351,6 +351,8 @@ void latent_attn_kernel(LatentArgs a)
     const int rounds = split * KG < tiles ? (tiles - split * KG + stride - 1) / stride : 0;
     int issued = 1;                                        // (that one in any case)
     for (; issued < NB - 1 && issued < mine; ++issued) load_tile(tile_base(first_tile + issued * stride), buffers + issued * Tile::BYTES);
+    static_assert(NB == 2, "the first tile alone is on its way here");
+    own_rows_loaded();
     for (int i = 0; i < (RG == 1 ? mine : rounds); ++i) {
         const int t = first_tile + i * stride, slot = i % NB;
         if (issued == i + NB - 1) wait_for_loads<(NB - 2) * LOADS>();

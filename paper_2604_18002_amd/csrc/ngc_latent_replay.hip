@@ -95,14 +95,18 @@ struct LdsRows {
     template <int WAVES>
     static constexpr int LOADS = (LR_STEP / LOAD_ROWS + WAVES - 1) / WAVES;                // of a wave
     template <int WAVES>
+    __device__ static __forceinline__ int row(int i, int wv) { return (i * WAVES + wv) * LOAD_ROWS % LR_STEP; }        // load i's first
+    template <int WAVES>
+    __device__ static __forceinline__ uint32_t offset(int i, uint32_t stride, int last, int wv, int lane)
+    {
+        const int lrow = lane / PIECES, piece = lane % PIECES ^ swizzle(lrow), r0 = row<WAVES>(i, wv), r = r0 + lrow;
+        return (uint32_t)(r < last ? r : last) * stride + (uint32_t)(piece ^ swizzle(r0)) * 16u;
+    }
+    template <int WAVES>
     __device__ static __forceinline__ void load(const unsigned char *from, uint32_t stride, int last, unsigned char *to, int wv, int lane)
     {
-        const int lrow = lane / PIECES, piece = lane % PIECES ^ swizzle(lrow);
 #pragma unroll
-        for (int i = 0; i < LOADS<WAVES>; ++i) {
-            const int r0 = (i * WAVES + wv) * LOAD_ROWS % LR_STEP, r = r0 + lrow;
-            start_load_to_lds16(from, (uint32_t)(r < last ? r : last) * stride + (uint32_t)(piece ^ swizzle(r0)) * 16u, to + r0 * BYTES);
-        }
+        for (int i = 0; i < LOADS<WAVES>; ++i) start_load_to_lds16(from, offset<WAVES>(i, stride, last, wv, lane), to + row<WAVES>(i, wv) * BYTES);
     }
     // Offset of piece 2 c + half of row `li`: an operand of 16 values c of 32 rows.  (Rows 32 apart: 32 BYTES more.)
     __device__ static __forceinline__ uint32_t row_piece(int li, int half, int c)
@@ -276,7 +280,7 @@ struct LatentReplayPlace {
 };
 
 // Live units of keys, two at a time, through two places in LDS, for the two kernels with queries of their own.
-template <int D>
+template <int D, bool KEEP>
 struct KeyTiles {
     static constexpr int KB = D * 2, RB = D, ROT = LR_STEP * KB, V = ROT + LR_STEP * RB, UNIT = V + LR_STEP * KB, BYTES = 4 * UNIT;
     const LatentReplayArgs &a;
@@ -284,9 +288,17 @@ struct KeyTiles {
     unsigned char *here, *there;
     int b, h, wv, lane;
     int unit[2];                             // of the next tile, on its way (`units`: none)
+    using Own = LdsRows<KB>;
+    using Rot = LdsRows<RB>;
+    static constexpr int OWN_LOADS = Own::template LOADS<LR_WAVES>, ROT_LOADS = Rot::template LOADS<LR_WAVES>;
+    uint32_t own_at[OWN_LOADS], rot_at[ROT_LOADS];         // this lane's part of a unit that lies whole in memory
     __device__ __forceinline__ KeyTiles(const LatentReplayArgs &a_, const LiveUnits &live_, unsigned char *lds, int b_, int h_, int wv_, int lane_)
         : a(a_), live(live_), here(lds), there(lds + 2 * UNIT), b(b_), h(h_), wv(wv_), lane(lane_)
     {
+#pragma unroll
+        for (int i = 0; i < OWN_LOADS; ++i) own_at[i] = Own::template offset<LR_WAVES>(i, (uint32_t)a.H * (2 * KB), LR_STEP, wv, lane);
+#pragma unroll
+        for (int i = 0; i < ROT_LOADS; ++i) rot_at[i] = Rot::template offset<LR_WAVES>(i, (uint32_t)a.rope_row, LR_STEP, wv, lane);
         ask(0);
     }
     __device__ __forceinline__ bool more() const { return unit[0] < live.units; }
@@ -295,17 +307,26 @@ struct KeyTiles {
         unit[0] = live.next(from);
         unit[1] = live.next(unit[0] + 1);
         if (!more()) return;
-        const int lane = (int)fresh((uint32_t)this->lane);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int first = unit[unit[i] < live.units ? i : 0] * LR_STEP;        // (none: the first again)
             const int last = a.T - 1 - first;              // of the memory; behind the sequence's end nothing is seen
             unsigned char *const to = there + i * UNIT;
-            const unsigned char *const k = a.kv + (((size_t)b * a.T + first) * a.H + h) * (2 * KB);
-            const uint32_t stride = (uint32_t)a.H * (2 * KB);
-            LdsRows<KB>::template load<LR_WAVES>(k, stride, last, to, wv, lane);
-            LdsRows<RB>::template load<LR_WAVES>(a.rope + ((size_t)b * a.T + first) * a.rope_row, (uint32_t)a.rope_row, last, to + ROT, wv, lane);
-            LdsRows<KB>::template load<LR_WAVES>(k + KB, stride, last, to + V, wv, lane);
+            const unsigned char *const k = a.kv + (((size_t)b * a.T + first) * a.H + h) * (2 * KB), *const r = a.rope + ((size_t)b * a.T + first) * a.rope_row;
+            if (KEEP && last >= LR_STEP - 1) {
+#pragma unroll
+                for (int j = 0; j < OWN_LOADS; ++j) start_load_to_lds16(k, own_at[j], to + Own::template row<LR_WAVES>(j, wv) * KB);
+#pragma unroll
+                for (int j = 0; j < ROT_LOADS; ++j) start_load_to_lds16(r, rot_at[j], to + ROT + Rot::template row<LR_WAVES>(j, wv) * RB);
+#pragma unroll
+                for (int j = 0; j < OWN_LOADS; ++j) start_load_to_lds16(k + KB, own_at[j], to + V + Own::template row<LR_WAVES>(j, wv) * KB);
+            } else {
+                const int lane_ = (int)fresh((uint32_t)lane);
+                const uint32_t stride = (uint32_t)a.H * (2 * KB);
+                Own::template load<LR_WAVES>(k, stride, last, to, wv, lane_);
+                Rot::template load<LR_WAVES>(r, (uint32_t)a.rope_row, last, to + ROT, wv, lane_);
+                Own::template load<LR_WAVES>(k + KB, stride, last, to + V, wv, lane_);
+            }
         }
     }
     // The next tile, in LDS until the next call; u: its units.  By all waves.
@@ -352,7 +373,7 @@ template <int D>
 __global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void latent_replay_kernel(LatentReplayArgs a)
 {
-    using Tiles = KeyTiles<D>;
+    using Tiles = KeyTiles<D, true>;
     constexpr int E = D / 2, KC = D / 16, RC = E / 16, DT = D / 32;
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
@@ -432,6 +453,7 @@ void latent_replay_kernel(LatentReplayArgs a)
         }
     };
 
+    own_rows_loaded();
     // (the tiles that this wave sees first, in a loop without branches: with one in it the sums would be kept twice)
     int u[2];
     auto mine = [&](int unit) { return unit < live.units && wave0 < n && unit * LR_STEP <= wave_last; };
@@ -505,7 +527,7 @@ template <int D>
 __global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void latent_replay_dq_kernel(LatentReplayArgs a)
 {
-    using Tiles = KeyTiles<D>;
+    using Tiles = KeyTiles<D, false>;
     constexpr int E = D / 2, KC = D / 16, RC = E / 16, DT = D / 32, ET = E / 32;
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
@@ -584,6 +606,7 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
         }
         (void)add_columns(x[DT / 2 & 1], 0, w, mixed, dr);
     };
+    own_rows_loaded();
     // (the tiles that this wave sees first, in a loop without branches: with one in it the sums would be kept twice)
     int u[2];
     auto mine = [&](int unit) { return unit < live.units && wave0 < n && unit * LR_STEP <= wave_last; };
@@ -807,7 +830,7 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
 #pragma unroll
         for (int c = 0; c < DT; ++c) dv[c] = zeros16();
         float poison = 0.f;                                // NaN: a gradient that is not finite arrives at a query that sees the key
-        __builtin_amdgcn_s_waitcnt(0x0F70);
+        own_rows_loaded();
         for (int u = first; some && u < first + SLOTS - 2; ++u) load_ahead(u);
         for (int u = first; u < mine_first; ++u) round_begins(u);
         for (int u = mine_first; u < mine_end; ++u) {
@@ -866,7 +889,7 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
         for (int c = 0; c < DT; ++c) dk[c] = zeros16();
 #pragma unroll
         for (int c = 0; c < ET; ++c) dr[c] = zeros16();
-        __builtin_amdgcn_s_waitcnt(0x0F70);
+        own_rows_loaded();
         for (int u = first; some && u < first + SLOTS - 2; ++u) load_ahead(u);
         for (int u = first - 1; some && u < mine_first; ++u) round_begins(u + 1);
         for (int u = mine_first; u < mine_end; ++u) {
@@ -996,7 +1019,7 @@ extern "C" int ngc_latent_replay_attn(const void *q, const void *kv, const void 
     a.out = reinterpret_cast<unsigned char *>(out);
     a.lse = lse_out;
     const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_kernel<64>);
-    return launch_blocks(fn, a, LR_BLOCK, LR_WAVES * 64, D == 128 ? KeyTiles<128>::BYTES : KeyTiles<64>::BYTES, (hipStream_t)stream);
+    return launch_blocks(fn, a, LR_BLOCK, LR_WAVES * 64, D == 128 ? KeyTiles<128, true>::BYTES : KeyTiles<64, true>::BYTES, (hipStream_t)stream);
 }
 
 extern "C" int ngc_latent_replay_attn_backward(const void *q, const void *kv, const void *rope, int64_t rope_stride, const int32_t *death,
@@ -1019,7 +1042,7 @@ extern "C" int ngc_latent_replay_attn_backward(const void *q, const void *kv, co
     a.stats = reinterpret_cast<float *>(ws);
     a.part = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(ws) + latent_replay_stats_bytes(B, T, Hq));
     hipStream_t st = (hipStream_t)stream;
-    const size_t lds = D == 128 ? KeyTiles<128>::BYTES : KeyTiles<64>::BYTES;
+    const size_t lds = D == 128 ? KeyTiles<128, true>::BYTES : KeyTiles<64, true>::BYTES;
     rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dq_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dq_kernel<64>), a, LR_BLOCK, LR_WAVES * 64, lds, st);
     if (rc) return rc;
     rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dkv_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dkv_kernel<64>), a,
