@@ -508,27 +508,55 @@ LatentShape latent_shape(int groups, int M)
     s.key_groups = s.waves / groups;
     return s;
 }
-// One row group reads every row once for 16 query rows, four for 64; but its workgroups have more of the matrix units to themselves,
-// start and end sooner, and leave a quarter of the sums to join.  It is taken as long as that leaves a CU at most 640 rows.  Measured
-// with 24 to 256 query rows, R = 512 and 256, the time of one for that of four: at 512 rows a CU 0.68 to 0.96 (32 query rows of 8 sequences
-// of 2000 rows, R = 512, where it is 256: 17 us for 24), at 768 1.0 to 1.3, far beyond up to 2.6 (256 of 64 of 8000).  Two groups were
-// behind the better of these everywhere.
-constexpr long long LT_NARROW_ROWS = 256 * 640;
-LatentShape latent_shape(int M, int nseg, int rows)
-{
-    const LatentShape narrow = latent_shape(1, M);
-    return M <= LT_ROWS || (long long)nseg * narrow.blocks * rows <= LT_NARROW_ROWS ? narrow : latent_shape(4, M);
-}
 
-// How many workgroups share a sequence's rows.
-int latent_splits(const LatentShape &s, int nseg, int rows)
+// Workgroups that the chip holds at once: one a CU, for LDS; two of one row group with R = 256.
+int latent_at_once(const LatentShape &s, int R) { return R == 512 || s.groups > 1 ? 256 : 512; }
+
+// How many workgroups may share a sequence's rows: as many as the chip holds at once, a round of rows for each.
+int latent_most_splits(const LatentShape &s, int nseg, int rows, int R)
 {
-    const long long groups = (long long)nseg * s.blocks;
     const int keys = latent_keys(s.groups) * s.key_groups, rounds = (rows + keys - 1) / keys;
-    long long S = 256 / groups;
+    long long S = latent_at_once(s, R) / ((long long)nseg * s.blocks);
     if (S > rounds) S = rounds;
     if (S > LT_MOST_SPLITS) S = LT_MOST_SPLITS;
     return S < 1 ? 1 : (int)S;
+}
+
+// Microseconds that a call takes, about: what a workgroup needs besides its rounds (64 rows, in either shape), a round (as it is bound by
+// products and LDS, or by the memory), and partials written, read and joined in another launch, by their bytes.  What it chooses, measured
+// with 16 to 256 query rows, 1 to 300 sequences of 60 to 6000 rows, R = 512 and 256, against every other choice: 1.012 times the best one's
+// time in the mean of 476 geometries, 1.24 at most.  Both sides, R = 512, 64 query rows, one row group and four: 32 sequences of 400 rows
+// 17.0 and 23.6 us, 32 of 1500 30.7 and 29.0, 128 of 1000 61.7 and 43.6; shared by one, four and eight: 8 of 400 rows (R = 256) 9.7, 8.8, 9.3.
+float latent_cost(const LatentShape &s, int S, int nseg, int rows, int M, int R)
+{
+    const bool wide = s.groups > 1;
+    const float start = R == 512 ? (wide ? 12.4f : 8.2f) : wide ? 7.2f : 6.3f, products = R == 512 ? (wide ? 2.4f : 1.5f) : wide ? 1.3f : 0.8f;
+    const long long groups = (long long)nseg * s.blocks * S;
+    const int chip = latent_at_once(s, R), rounds = (rows + 63) / 64;
+    const float at_once = (float)(groups < chip ? groups : chip), row_bytes = (float)(R / 8 * 9 * 2);
+    const float memory = at_once / (float)s.blocks * 64.0f * row_bytes / 6.2e6f;
+    const float turns = (float)((groups + chip - 1) / chip), mine = (float)((rounds + S - 1) / S);
+    const float joined = S == 1 ? 0.f : 3.0f + 0.3e-6f * (float)nseg * (float)S * (float)M * (float)R * 4.0f;
+    return turns * (start + mine * (products > memory ? products : memory)) + joined;
+}
+
+// The shape of a call, and how many workgroups share a sequence.  One row group reads every row once for 16 query rows, four for 64; but its
+// workgroups start and end sooner and leave a quarter of the sums to join.
+LatentShape latent_shape(int M, int nseg, int rows, int R, int *splits)
+{
+    LatentShape best{};
+    float least = 0.f;
+    for (int groups = 1; groups <= (M <= LT_ROWS ? 1 : 4); groups += 3) {
+        const LatentShape s = latent_shape(groups, M);
+        for (int S = latent_most_splits(s, nseg, rows, R); S >= 1; --S) {
+            const float cost = latent_cost(s, S, nseg, rows, M, R);
+            if (best.waves && cost >= least) continue;
+            best = s;
+            least = cost;
+            *splits = S;
+        }
+    }
+    return best;
 }
 
 size_t latent_partial_bytes(int nseg, int S, int M, int R) { return S == 1 ? 0 : (size_t)nseg * S * M * (R + 2) * sizeof(float); }
@@ -544,9 +572,9 @@ extern "C" size_t ngc_latent_workspace_bytes(const ngc_paged_cache *pc, int32_t 
     for (int w = 1; w <= W; ++w) {                         // (calls with fewer new tokens may be split more often)
         const int M = w * pc->Hq;
         for (int layers : {1, pc->L}) {
-            for (int groups : {1, 4}) {                    // (or a smaller hint takes the other shape)
+            for (int groups : {1, 4}) {                    // (which of them, and how many splits, is the hint's to say)
                 const int nseg = layers * pc->B;
-                const size_t bytes = latent_partial_bytes(nseg, latent_splits(latent_shape(groups, M), nseg, c.cap), M, R);
+                const size_t bytes = latent_partial_bytes(nseg, latent_most_splits(latent_shape(groups, M), nseg, c.cap, R), M, R);
                 most = bytes > most ? bytes : most;
             }
         }
@@ -569,9 +597,9 @@ extern "C" int ngc_latent_attn(const ngc_paged_cache *pc, int32_t layer, const i
     if (ws_bytes < scratch_offset(&c)) return NGC_ENOSPC;
     const int R = latent_width(pc->D), M = W * pc->Hq;
     const int rows = max_len_hint > 0 && max_len_hint < c.cap ? max_len_hint : c.cap;
-    const LatentShape shape = latent_shape(M, nseg, rows);
+    int S = 1;
+    const LatentShape shape = latent_shape(M, nseg, rows, R, &S);
     if (!launchable((long long)nseg * shape.blocks, shape.waves * 64) || nseg > 65535) return NGC_EUNSUPPORTED;
-    int S = latent_splits(shape, nseg, rows);
     while (S > 1 && scratch_offset(&c) + latent_partial_bytes(nseg, S, M, R) > ws_bytes) S /= 2;
 
     LatentArgs a{};
