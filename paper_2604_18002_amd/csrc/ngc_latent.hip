@@ -523,20 +523,22 @@ int latent_most_splits(const LatentShape &s, int nseg, int rows, int R)
 }
 
 // Microseconds that a call takes, about: what a workgroup needs besides its rounds (64 rows, in either shape), a round (as it is bound by
-// products and LDS, or by the memory), and partials written, read and joined in another launch, by their bytes.  What it chooses, measured
-// with 16 to 256 query rows, 1 to 300 sequences of 60 to 6000 rows, R = 512 and 256, against every other choice: 1.012 times the best one's
-// time in the mean of 476 geometries, 1.24 at most.  Both sides, R = 512, 64 query rows, one row group and four: 32 sequences of 400 rows
-// 17.0 and 23.6 us, 32 of 1500 30.7 and 29.0, 128 of 1000 61.7 and 43.6; shared by one, four and eight: 8 of 400 rows (R = 256) 9.7, 8.8, 9.3.
+// products, LDS and its own loads, or by the memory), and partials written, read and joined in another launch, by their number and bytes.
+// The constants are fitted to calls with 16 to 256 query rows and 1 to 300 sequences of 60 to 6000 rows, R = 512 and 256, layer after
+// layer over more rows than the caches hold, lengths between half the hint and all of it: what they choose takes 1.007 times the best
+// choice's time in the mean of those 180 geometries, 1.10 at most, and 1.012 (1.18) in 174 others.  Both sides, 64 query rows of R = 512, one row group and four, warm:
+// 32 sequences of 400 rows 17.0 and 23.6 us, 32 of 1500 30.7 and 29.0, 128 of 1000 61.7 and 43.6.
 float latent_cost(const LatentShape &s, int S, int nseg, int rows, int M, int R)
 {
     const bool wide = s.groups > 1;
-    const float start = R == 512 ? (wide ? 12.4f : 8.2f) : wide ? 7.2f : 6.3f, products = R == 512 ? (wide ? 2.4f : 1.5f) : wide ? 1.3f : 0.8f;
+    const float start = R == 512 ? (wide ? 8.2f : 7.3f) : wide ? 6.6f : 6.4f;
+    const float products = R == 512 ? (wide ? 2.95f : s.blocks == 1 ? 1.91f : 1.44f) : wide ? 0.91f : 0.85f;      // (rows that nobody shares come late)
     const long long groups = (long long)nseg * s.blocks * S;
     const int chip = latent_at_once(s, R), rounds = (rows + 63) / 64;
     const float at_once = (float)(groups < chip ? groups : chip), row_bytes = (float)(R / 8 * 9 * 2);
-    const float memory = at_once / (float)s.blocks * 64.0f * row_bytes / 6.2e6f;
+    const float memory = at_once / (float)s.blocks * 64.0f * row_bytes / 11.9e6f;
     const float turns = (float)((groups + chip - 1) / chip), mine = (float)((rounds + S - 1) / S);
-    const float joined = S == 1 ? 0.f : 3.0f + 0.3e-6f * (float)nseg * (float)S * (float)M * (float)R * 4.0f;
+    const float joined = S == 1 ? 0.f : 2.4f + 0.54f * (float)((S + 7) / 8) + 0.37e-6f * (float)nseg * (float)S * (float)M * (float)R * 4.0f;
     return turns * (start + mine * (products > memory ? products : memory)) + joined;
 }
 
