@@ -28,10 +28,10 @@
 //
 // What bounds it.  2 (2 D + E) flops a pair forward, 2 (3 (D + E) + 2 D) + 2 (2 D + E) backward (D = 128: 640 and 1664 with what is formed
 // twice left out) on 16-bit inputs: the products, for more than some hundred positions.  Measured, 16 heads of 128: 8192 positions
-// without evictions 900 to 945 TFLOP/s forward (370 to 385 us) and 690 backward, where a large product of matrices reaches 1230; 2 x 3000
-// to 3850 positions with evictions every 512, 131 us forward, 176 us the queries' and 285 us the keys' gradients.  A wave's products wait
-// for its reads of LDS and its exponentials, which the other wave of its SIMD covers in part: the matrix units are busy 40 % of the time
-// forward without evictions.  With evictions a workgroup has few tiles and its first one, 2.5 us, and the look at the ends, 1.5, count.
+// without evictions 920 TFLOP/s forward (373 us; two of them 945) and 670 to 690 backward, where a large product of matrices reaches 1230;
+// 2 x 3000 to 3850 positions with evictions every 512, 117 us forward, 171 us the queries' and 278 us the keys' gradients.  A step of 32 x
+// 32 pairs is 640 clocks of products and some 700 of vector work forward, and two waves overlap little of them: the matrix units are
+// busy 45 % of the time without evictions.  With evictions a workgroup has few tiles and its first one, 2.5 us, and the look at the ends, 1.5, count.
 //   Registers decide: two waves a SIMD have 256 each, and one more copy of the sums (a branch around a unit makes the compiler keep
 // one) or offsets kept for every read (they differ in a bit: made where they are used) went to scratch, whose loads wait behind every
 // tile on its way: the queries' gradient 245 us with 23 such registers, 190 without.
