@@ -106,7 +106,8 @@ struct LdsRows {
     __device__ static __forceinline__ void load(const unsigned char *from, uint32_t stride, int last, unsigned char *to, int wv, int lane)
     {
 #pragma unroll
-        for (int i = 0; i < LOADS<WAVES>; ++i) start_load_to_lds16(from, offset<WAVES>(i, stride, last, wv, lane), to + row<WAVES>(i, wv) * BYTES);
+        for (int i = 0; i < LOADS<WAVES>; ++i)
+            start_load_to_lds16(from, offset<WAVES>(i, stride, last, wv, lane), to + row<WAVES>(i, wv) * BYTES);
     }
     // Offset of piece 2 c + half of row `li`: an operand of 16 values c of 32 rows.  (Rows 32 apart: 32 BYTES more.)
     __device__ static __forceinline__ uint32_t row_piece(int li, int half, int c)
@@ -279,7 +280,8 @@ struct LatentReplayPlace {
     }
 };
 
-// Live units of keys, two at a time, through two places in LDS, for the two kernels with queries of their own.
+// Live units of keys, two at a time, through two places in LDS, for the two kernels with queries of their own.  KEEP: a lane's offsets stay in
+// registers; the forward pass has them left, the queries' gradient would send 8 others to scratch.
 template <int D, bool KEEP>
 struct KeyTiles {
     static constexpr int KB = D * 2, RB = D, ROT = LR_STEP * KB, V = ROT + LR_STEP * RB, UNIT = V + LR_STEP * KB, BYTES = 4 * UNIT;
@@ -312,7 +314,8 @@ struct KeyTiles {
             const int first = unit[unit[i] < live.units ? i : 0] * LR_STEP;        // (none: the first again)
             const int last = a.T - 1 - first;              // of the memory; behind the sequence's end nothing is seen
             unsigned char *const to = there + i * UNIT;
-            const unsigned char *const k = a.kv + (((size_t)b * a.T + first) * a.H + h) * (2 * KB), *const r = a.rope + ((size_t)b * a.T + first) * a.rope_row;
+            const unsigned char *const k = a.kv + (((size_t)b * a.T + first) * a.H + h) * (2 * KB);
+            const unsigned char *const r = a.rope + ((size_t)b * a.T + first) * a.rope_row;
             if (KEEP && last >= LR_STEP - 1) {
 #pragma unroll
                 for (int j = 0; j < OWN_LOADS; ++j) start_load_to_lds16(k, own_at[j], to + Own::template row<LR_WAVES>(j, wv) * KB);
@@ -1018,7 +1021,8 @@ extern "C" int ngc_latent_replay_attn(const void *q, const void *kv, const void 
     LatentReplayArgs a = latent_replay_args(q, kv, rope, rope_stride, death, n, B, T, Hq, scale);
     a.out = reinterpret_cast<unsigned char *>(out);
     a.lse = lse_out;
-    const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_kernel<64>);
+    const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_kernel<128>)
+                              : reinterpret_cast<const void *>(&latent_replay_kernel<64>);
     return launch_blocks(fn, a, LR_BLOCK, LR_WAVES * 64, D == 128 ? KeyTiles<128, true>::BYTES : KeyTiles<64, true>::BYTES, (hipStream_t)stream);
 }
 
@@ -1043,12 +1047,14 @@ extern "C" int ngc_latent_replay_attn_backward(const void *q, const void *kv, co
     a.part = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(ws) + latent_replay_stats_bytes(B, T, Hq));
     hipStream_t st = (hipStream_t)stream;
     const size_t lds = D == 128 ? KeyTiles<128, true>::BYTES : KeyTiles<64, true>::BYTES;
-    rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dq_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dq_kernel<64>), a, LR_BLOCK, LR_WAVES * 64, lds, st);
+    const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_dq_kernel<128>)
+                              : reinterpret_cast<const void *>(&latent_replay_dq_kernel<64>);
+    rc = launch_blocks(fn, a, LR_BLOCK, LR_WAVES * 64, lds, st);
     if (rc) return rc;
-    rc = launch_blocks(D == 128 ? reinterpret_cast<const void *>(&latent_replay_dkv_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dkv_kernel<64>), a,
-                       KV_BLOCK, 2 * KV_GROUPS * 64, kv_slots(D) * (lds / 4 + 2 * LR_STEP * sizeof(float)) + KV_GROUPS * 2 * 4096, st);
+    fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_dkv_kernel<128>) : reinterpret_cast<const void *>(&latent_replay_dkv_kernel<64>);
+    rc = launch_blocks(fn, a, KV_BLOCK, 2 * KV_GROUPS * 64, kv_slots(D) * (lds / 4 + 2 * LR_STEP * sizeof(float)) + KV_GROUPS * 2 * 4096, st);
     if (rc) return rc;
     const long long threads = (long long)B * T * (D / 2 / 4);
-    const void *fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_rope_kernel<64>) : reinterpret_cast<const void *>(&latent_replay_rope_kernel<32>);
+    fn = D == 128 ? reinterpret_cast<const void *>(&latent_replay_rope_kernel<64>) : reinterpret_cast<const void *>(&latent_replay_rope_kernel<32>);
     return launch(fn, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, a);
 }
