@@ -54,6 +54,11 @@ int ngc_probe_copy_shape(const void *src, void *dst, size_t bytes, int32_t threa
 int ngc_probe_compact(void *k, void *v, const int32_t *kept, const int32_t *keep, int32_t nseg, int32_t cap,
                       int32_t max_keep, int32_t threads, int32_t unroll, int32_t mode, void *stream);
 
+/* How ngc_latent_attn deals a call to workgroups whose workspace has room (host only, nothing is launched): `row_groups`
+ * of 16 query rows a workgroup, 1 or 4, and `splits` workgroups for the rows of a sequence.
+ *   D 576 or 288; Hq heads, W new tokens; nseg sequences (of all layers of the call); rows: the hint, or room in a table */
+int ngc_probe_latent_shape(int32_t D, int32_t Hq, int32_t W, int32_t nseg, int32_t rows, int32_t *row_groups, int32_t *splits);
+
 #ifdef __cplusplus
 }
 #endif

@@ -4,10 +4,12 @@
 // with no selection work around it.  The measurement harness runs them beside
 // the library's kernels so that every bandwidth figure can also be read against
 // a ceiling measured in the same job.  Nothing here is part of the method.
+// (And which kernel a call of attention over latent rows takes, for tests that mean one of them.)
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include "../../include/ngc_probe.h"
+#include "ngc_latent_shape.h"
 
 namespace ngc_probe {
 
@@ -263,4 +265,13 @@ extern "C" int ngc_probe_compact(void *k, void *v, const int32_t *kept, const in
     NGC_PROBE_CASE(1024, 2) NGC_PROBE_CASE(1024, 4)
 #undef NGC_PROBE_CASE
     return -1;
+}
+
+extern "C" int ngc_probe_latent_shape(int32_t D, int32_t Hq, int32_t W, int32_t nseg, int32_t rows, int32_t *row_groups, int32_t *splits)
+{
+    if ((D != 576 && D != 288) || Hq < 1 || Hq > 128 || W < 1 || W > 1024 || nseg < 1 || rows < 1 || !row_groups || !splits) return -1;
+    int S = 1;
+    *row_groups = ngc::latent_shape(W * Hq, nseg, rows, D / 9 * 8, &S).groups;
+    *splits = S;
+    return 0;
 }

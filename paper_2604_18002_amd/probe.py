@@ -19,7 +19,7 @@ import numpy as np
 from ._build import PROBE_LIB_PATH
 
 READ, COPY, READ_NT, COPY_NT, FILL_NT = 0, 1, 2, 3, 4
-EXPORTS = ("ngc_probe_stream", "ngc_probe_copy_shape", "ngc_probe_compact")
+EXPORTS = ("ngc_probe_stream", "ngc_probe_copy_shape", "ngc_probe_compact", "ngc_probe_latent_shape")
 
 _lib = None
 
@@ -47,6 +47,8 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.ngc_probe_copy_shape.restype = C.c_int
     lib.ngc_probe_compact.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp]
     lib.ngc_probe_compact.restype = C.c_int
+    lib.ngc_probe_latent_shape.argtypes = [i32, i32, i32, i32, i32, C.POINTER(i32), C.POINTER(i32)]
+    lib.ngc_probe_latent_shape.restype = C.c_int
     if path == PROBE_LIB_PATH:
         _lib = lib
     return lib
@@ -78,6 +80,13 @@ def ngc_probe_compact(k, v, kept, keep, nseg: int, cap: int, max_keep: int, thre
                       stream=None):
     _check(load_library().ngc_probe_compact(k.data_ptr(), v.data_ptr(), kept.data_ptr(), keep.data_ptr(), nseg, cap,
                                             max_keep, threads, unroll, mode, _stream(stream)), "ngc_probe_compact")
+
+
+def ngc_probe_latent_shape(D: int, Hq: int, W: int, nseg: int, rows: int) -> tuple:
+    """(row groups of 16 queries a workgroup, workgroups for a sequence) that ngc_latent_attn takes."""
+    groups, splits = C.c_int32(), C.c_int32()
+    _check(load_library().ngc_probe_latent_shape(D, Hq, W, nseg, rows, C.byref(groups), C.byref(splits)), "ngc_probe_latent_shape")
+    return groups.value, splits.value
 
 
 # ------------------------------------------------------------------ sweep ---
