@@ -387,16 +387,18 @@ void latent_attn_kernel(LatentArgs a)
     for (int k = 0; k < KG; ++k) m_all = max_no_nan(m_all, red[(k * RG + rg) * LT_ROWS + row]);
 #pragma unroll
     for (int k = 0; k < KG; ++k) {
-        const float mk = red[(k * RG + rg) * LT_ROWS + row];
-        if (mk != -INFINITY) l_all += red[(NW + k * RG + rg) * LT_ROWS + row] * fast_exp2((mk - m_all) * a.scale_log2e);
+        // (a group has no weights where its sum is 0; one of NaN counts whatever its maximum, which leaves NaN out)
+        const float mk = red[(k * RG + rg) * LT_ROWS + row], lk = red[(NW + k * RG + rg) * LT_ROWS + row];
+        if (lk != 0.f) l_all += lk * fast_exp2((mk - m_all) * a.scale_log2e);
     }
-    float part = m_run == -INFINITY ? 0.f : fast_exp2((m_run - m_all) * a.scale_log2e);
+    float part = l == 0.f ? 0.f : fast_exp2((m_run - m_all) * a.scale_log2e);
     if (a.S == 1) part = l_all == 0.f ? 0.f : part / l_all;
     if (kg == 0 && quarter == 0 && my_row < real_rows) {
         if (a.S == 1) {
             if (a.lse_out) a.lse_out[(size_t)seg * a.M + my_row] = l_all == 0.f ? -INFINITY : m_all * a.scale + logf(l_all);
         } else {
-            st_device8(device_span(a.part_ml + ((size_t)seg * a.S + split) * a.M * 2, (uint32_t)a.M * 8u), (uint32_t)my_row * 8u, f32x2{m_all, l_all});
+            st_device8(device_span(a.part_ml + ((size_t)seg * a.S + split) * a.M * 2, (uint32_t)a.M * 8u), (uint32_t)my_row * 8u,
+                       f32x2{m_all, rounds == 0 ? -1.0f : l_all});                 // (-1: no partial)
         }
     }
     if (a.S > 1 && rounds == 0) return;                    // (nothing was seen: the join does not look at it)
@@ -456,24 +458,25 @@ __global__ __launch_bounds__(JOIN_THREADS) void latent_join_kernel(LatentArgs a)
         for (int u = 0; u < JOIN_BATCH; ++u) v[u] = *reinterpret_cast<const f32x4 *>(po + (size_t)(i0 + u < a.S ? i0 + u : a.S - 1) * a.M * R);
     };
     ask(0);
-    f32x2 x = {-INFINITY, 0.f};                            // of partial `lane`
+    f32x2 x = {-INFINITY, -1.0f};                          // of partial `lane`; a sum of -1: there is none
     if (lane < a.S) x = *reinterpret_cast<const f32x2 *>(ml + (size_t)lane * a.M * 2);
     int tokens = a.n_new ? a.n_new[seg % a.B] : a.W;
     tokens = tokens < 0 ? 0 : tokens > a.W ? a.W : tokens;
     const bool real = r < tokens * a.Hq;
     const float m = wave_max_f(x[0]);
-    const float wx = x[0] == -INFINITY ? 0.f : fast_exp2((x[0] - m) * a.scale_log2e);
-    const float l = wave_sum_f(wx == 0.f ? 0.f : wx * x[1]);
+    const bool none = x[1] < 0.f, weighs = !none && x[1] != 0.f;       // (NaN weighs, whatever its maximum)
+    const float wx = weighs ? fast_exp2((x[0] - m) * a.scale_log2e) : 0.f;
+    const float l = wave_sum_f(weighs ? wx * x[1] : 0.f);
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    if (col / 4 < 64) shares[sub][lane] = wx * inv;        // a row's first wave
+    if (col / 4 < 64) shares[sub][lane] = none ? -1.0f : wx * inv;     // a row's first wave
     __syncthreads();
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int i0 = 0; i0 < a.S; i0 += JOIN_BATCH) {
         if (i0) ask(i0);
 #pragma unroll
         for (int u = 0; u < JOIN_BATCH; ++u) {
-            const float w = i0 + u < a.S ? shares[sub][i0 + u] : 0.f;
-            if (w != 0.f) o += w * v[u];
+            const float w = i0 + u < a.S ? shares[sub][i0 + u] : -1.0f;
+            if (!(w < 0.f)) o += w * v[u];                 // (a share of 0 too: values that are not finite stay)
         }
     }
     if (!real) return;
