@@ -61,6 +61,10 @@ constexpr int KV_GROUPS = 2;                 // units of keys of a workgroup of 
 constexpr int KV_BLOCK = KV_GROUPS * LR_OWN;
 constexpr int kv_slots(int D) { return D == 128 ? 3 : 6; }     // units of queries in LDS, for two workgroups a CU
 constexpr float LR_LAZY = 8.0f;              // the reference of the exponents moves when a maximum has outgrown it by 2^8
+// Exponents are score * scale - reference in one operation, the reference rounded.  Its rounding is the same for all keys, and lse is of the
+// rounded one; but it would reach 2^7, where weights overflow, at references of 2^31, and count where they move.  From this one on (there half a
+// step is 2^-12, and what has been added up before such a move weighs 2^-8 at most) the scores' difference comes first.
+constexpr float LR_FAR = 4096.0f;
 
 struct LatentReplayArgs {
     const unsigned char *q;                  // bf16 [B][T][H][D + E]
@@ -400,7 +404,7 @@ void latent_replay_kernel(LatentReplayArgs a)
     f32x16 o[DT];
 #pragma unroll
     for (int c = 0; c < DT; ++c) o[c] = zeros16();
-    float m_run = -INFINITY, neg_m = 0.f, l_run = 0.f;     // scaled domain; neg_m: -m_run, or 0 as long as nothing has been seen
+    float m_run = -INFINITY, neg_m = 0.f, l_run = 0.f;     // m_run: a score; neg_m: -m_run scaled, or 0 as long as nothing has been seen
 
     auto step = [&](const unsigned char *unit, int key0, bool whole) {
         const bool mixed = !whole || key0 + LR_STEP - 1 > wave0 || key0 + LR_STEP > n;
@@ -421,22 +425,29 @@ void latent_replay_kernel(LatentReplayArgs a)
         float top = sc[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) top = max_no_nan(top, sc[r]);
-        top = half_rows_max(top) * a.scale_log2e;
-        const bool outgrown = top - m_run > LR_LAZY;        // of each row by itself: its results do not depend on its neighbours'
+        top = half_rows_max(top);
+        const bool outgrown = (top - m_run) * a.scale_log2e > LR_LAZY;     // of each row by itself: its results do not depend on its neighbours'
         if (__ballot(outgrown)) {
             const float m_new = outgrown ? top : m_run;
-            const float alpha = m_new == m_run ? 1.0f : fast_exp2(m_run - m_new);
+            const float alpha = m_new == m_run ? 1.0f : fast_exp2((m_run - m_new) * a.scale_log2e);
             l_run *= alpha;
 #pragma unroll
             for (int c = 0; c < DT; ++c) o[c] *= alpha;
             m_run = m_new;
-            neg_m = m_new == -INFINITY ? 0.f : -m_new;
+            neg_m = m_new == -INFINITY ? 0.f : -(m_new * a.scale_log2e);
+        }
+        float ref = neg_m;
+        const bool far = __builtin_fabsf(neg_m) > LR_FAR;
+        if (__ballot(far)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[r] = far ? sc[r] - m_run : sc[r];
+            ref = far ? 0.f : neg_m;
         }
         uint32_t w[8];
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float p0 = fast_exp2(__builtin_fmaf(sc[2 * e], a.scale_log2e, neg_m)), p1 = fast_exp2(__builtin_fmaf(sc[2 * e + 1], a.scale_log2e, neg_m));
+            const float p0 = fast_exp2(__builtin_fmaf(sc[2 * e], a.scale_log2e, ref)), p1 = fast_exp2(__builtin_fmaf(sc[2 * e + 1], a.scale_log2e, ref));
             sum += p0 + p1;
             w[e] = pack_bf16(p0, p1);
         }
@@ -475,8 +486,11 @@ void latent_replay_kernel(LatentReplayArgs a)
     // row r at slot p ^ r
     const float l = half_rows_sum(l_run);
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    if (a.lse && half == 0 && qpos < n)
-        a.lse[((size_t)at.b * a.H + at.h) * a.T + qpos] = l == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    if (a.lse && half == 0 && qpos < n) {
+        const bool far = __builtin_fabsf(neg_m) > LR_FAR;
+        const float log2_l = __builtin_amdgcn_logf(l), near = (log2_l - neg_m) * 0.6931471805599453f;
+        a.lse[((size_t)at.b * a.H + at.h) * a.T + qpos] = l == 0.f ? -INFINITY : far ? __builtin_fmaf(m_run, a.scale, log2_l * 0.6931471805599453f) : near;
+    }
     lds_loads_done();
     constexpr int OP = D / 8;
     unsigned char *const rows = lds + wv * LR_OWN * D * 2;
