@@ -270,7 +270,7 @@ def _plain_extend(s, L, B, H, P):
     entry = torch.arange(table.shape[1], device=DEV)
     granted = (entry >= have.view(-1, 1)) & (entry < want.view(-1, 1))
     rank = granted.view(-1).cumsum(0).view(granted.shape) - 1
-    table.copy_(torch.where(granted, s.stack[(s.count.long() - 1 - rank).clamp(min=0)], table))
+    table.copy_(torch.where(granted, s.stack[(s.count.long() - 1 - rank).clamp(0, s.stack.numel() - 1)], table))
     s.count.sub_(granted.sum().int())
     start = torch.cat([torch.zeros(1, dtype=torch.int64, device=DEV), new.cumsum(0)])
     token = torch.arange(s.T, device=DEV)
