@@ -13,7 +13,7 @@ def cases(monkeypatch):
     return cases
 
 
-@pytest.mark.parametrize("L,B,H,page,n,new", [(1, 13, 8, 64, (0, 0), (0, 1)), (2, 5, 2, 32, (0, 0), (0, 70)), (3, 4, 2, 32, (0, 50), (0, 40)), (1, 1, 1, 32, (0, 0), (1, 1)),
+@pytest.mark.parametrize("L,B,H,page,n,new", [(1, 13, 8, 64, (0, 0), (0, 1)), (2, 5, 2, 32, (0, 0), (0, 3)), (3, 4, 2, 32, (0, 50), (0, 3)), (3, 4, 2, 32, (0, 50), (1, 70)), (1, 1, 1, 32, (0, 0), (1, 1)),
                                               (2, 7, 1, 64, (10, 200), (1, 1))])
 def test_plain_extend(cases, L, B, H, page, n, new):
     c = dict(kind="extend", L=L, B=B, Hkv=H, page=page, max_pages=-(-(n[1] + new[1]) // page) + 1, n_lo=n[0], n_hi=n[1], new_lo=new[0], new_hi=new[1])
