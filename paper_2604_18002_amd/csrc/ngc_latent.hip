@@ -528,7 +528,8 @@ extern "C" int ngc_latent_attn(const ngc_paged_cache *pc, int32_t layer, const i
     const int rows = max_len_hint > 0 && max_len_hint < c.cap ? max_len_hint : c.cap;
     int S = 1;
     const LatentShape shape = latent_shape(M, nseg, rows, R, &S);
-    if (!launchable((long long)nseg * shape.blocks, shape.waves * 64) || nseg > 65535) return NGC_EUNSUPPORTED;
+    // (workgroups that share sequences are fewer than the chip holds, and so are the sequences that the join counts in its grid's y)
+    if (!launchable((long long)nseg * shape.blocks, shape.waves * 64)) return NGC_EUNSUPPORTED;
     while (S > 1 && scratch_offset(&c) + latent_partial_bytes(nseg, S, M, R) > ws_bytes) S /= 2;
 
     LatentArgs a{};
