@@ -750,10 +750,11 @@ int ngc_latent_attn(const ngc_paged_cache *pc, int32_t layer, const int32_t *n_n
  *   lse_out  fp32 [B][Hq][T]: the log of the sum of the exponentials (natural log), or
  *            NULL; the backward pass needs it
  *   scale    positive, at most 2.35e38 (NGC_EINVAL otherwise)
- * D is 64 or 128; T <= 131072 (NGC_EUNSUPPORTED).  A position that sees no key has zeros
- * and -inf.  Scores, of any size that 32 bits hold, soft-max and accumulation are fp32,
- * weights are rounded to bf16.
- * Values that are not finite reach the positions that see them, and no other. */
+ * D is 64 or 128; T <= 131072 (NGC_EUNSUPPORTED).  A position that sees no key, or none
+ * with a score above minus infinity, has zeros and -inf.  Scores, of any size that 32 bits
+ * hold, soft-max and accumulation are fp32, weights are rounded to bf16.
+ * Values that are not finite reach the positions that see them, and no other: as the formula
+ * has it, an infinite value its column alone (and not lse), a key by its score. */
 int ngc_latent_replay_attn(const void *q, const void *kv, const void *rope, int64_t rope_stride,
                            const int32_t *death, const int32_t *n, int32_t B, int32_t T, int32_t Hq,
                            int32_t D, float scale, void *out, float *lse_out, void *stream);
@@ -765,7 +766,10 @@ int ngc_latent_replay_attn(const void *q, const void *kv, const void *rope, int6
  * all written over, up to n[b] positions; 16-byte aligned.  Sums are fp32 and have one
  * owner each: the same inputs give the same bits.  The weights are formed again from the
  * scores and lse, which is fp32: they are off by up to |lse| 2^-22 of themselves (1.6 %
- * where |lse| is 65536; beyond some 10^8 they may be anything).  ws must hold
+ * where |lse| is 65536; beyond some 10^8 they may be anything).  Weights and their gradients
+ * are rounded to bf16 for the products with other bf16 values, and <dout, out> is of out as
+ * it is stored.  Values that are not finite reach what the formula brings them to (weights of
+ * a position that sees keys, but only with scores of minus infinity, are NaN).  ws must hold
  * ngc_latent_replay_workspace_bytes(); nothing in it has to be zero. */
 size_t ngc_latent_replay_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t D);
 int ngc_latent_replay_attn_backward(const void *q, const void *kv, const void *rope, int64_t rope_stride,

@@ -199,6 +199,39 @@ __device__ __forceinline__ uint32_t odd_rows(const unsigned char *rows)
     return mask;
 }
 
+// What add_columns() has taken for 0 in a unit's rows, times weight(r), to who sees row r: sees(r).  (Both of a lane's column of the products.)
+template <int BYTES, int CT, class Sees, class Weight>
+__device__ __forceinline__ void add_odd_values(const unsigned char *x, Sees sees, Weight weight, f32x16 (&acc)[CT])
+{
+    const int half = lane_id() >> 5;
+    for (uint32_t rows = odd_rows<BYTES>(x); rows; rows &= rows - 1) {
+        const int r = __builtin_ctz(rows);
+        const bool mine = sees(r);
+        const float w = weight(r);
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const u32x2 v = *reinterpret_cast<const u32x2 *>(x + r * BYTES + (((4 * c + g) ^ LdsRows<BYTES>::swizzle(r)) & (LdsRows<BYTES>::PIECES - 1)) * 16 + half * 8);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float f = __uint_as_float(e % 2 ? v[e / 2] & 0xFFFF0000u : v[e / 2] << 16);
+                    if (mine && !(__builtin_fabsf(f) < INFINITY)) acc[c][4 * g + e] += w * f;
+                }
+            }
+    }
+}
+// Weight of row r (uniform) of a unit and this lane's column, of the 32 x 32 as packed for the second product.
+__device__ __forceinline__ float weight_of(const uint32_t (&w)[8], int r)
+{
+    const int at = 4 * (r / 8) + r % 4;                    // register, in the half r / 4 % 2
+    uint32_t x = w[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) x = at / 2 == e ? w[e] : x;
+    x = __shfl(x, (lane_id() & 31) + (r / 4 % 2) * 32);
+    return __uint_as_float(at % 2 ? x & 0xFFFF0000u : x << 16);
+}
+
 // Units of LR_STEP keys that some query of first .. last sees, and those that all of them see where causality lets them, as words of
 // 64 units in the lanes.  The workgroup's waves look at a part of the keys each and share their words in `scratch` (LDS, 1 KB, free
 // again behind the next barrier).
@@ -376,6 +409,12 @@ __device__ __forceinline__ uint32_t seen_keys(const int32_t *death, int key0, in
     return seen;
 }
 
+// Whether this lane's query sees key r (uniform) of a unit, of the bits that its halves have.
+__device__ __forceinline__ bool sees_key(uint32_t seen, int r)
+{
+    return (__shfl(seen, (lane_id() & 31) + (r / 4 % 2) * 32) >> (4 * (r / 8) + r % 4)) & 1u;
+}
+
 template <int D>
 __global__ __launch_bounds__(LR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void latent_replay_kernel(LatentReplayArgs a)
@@ -438,7 +477,7 @@ void latent_replay_kernel(LatentReplayArgs a)
         }
         float ref = neg_m;
         const bool far = __builtin_fabsf(neg_m) > LR_FAR;
-        if (__ballot(far)) {
+        if (__builtin_expect(__ballot(far) != 0, 0)) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) sc[r] = far ? sc[r] - m_run : sc[r];
             ref = far ? 0.f : neg_m;
@@ -458,13 +497,7 @@ void latent_replay_kernel(LatentReplayArgs a)
             if (pair + 1 < DT / 2) ask_columns<Tiles::KB, DT>(values, v_first, pair + 1, x[(pair + 1) & 1]);
             odd |= add_columns(x[pair & 1], pair, w, mixed, o);
         }
-        if (__ballot(odd)) {
-            // the queries that see a row with such a value, and no others, become NaN
-            const uint32_t rows = odd_rows<Tiles::KB>(values);
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (((rows >> row_of(r, half)) & 1u) && ((seen >> r) & 1u)) l_run = NAN;
-        }
+        if (__builtin_expect(__ballot(odd) != 0, 0)) add_odd_values<Tiles::KB>(values, [&](int r) { return sees_key(seen, r); }, [&](int r) { return weight_of(w, r); }, o);
     };
 
     own_rows_loaded();
@@ -614,14 +647,22 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
         uint32_t w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = pack_bf16(ds[2 * e], ds[2 * e + 1]);
-        // (a key that is seen and not finite has made dS NaN)
+        bool odd = false;
 #pragma unroll
         for (int pair = 0; pair < DT / 2; ++pair) {
             if (pair + 1 < DT / 2) ask_columns<Tiles::KB, DT>(unit, kt_0, pair + 1, x[(pair + 1) & 1]);
             else ask_columns<Tiles::RB, ET>(unit + Tiles::ROT, rt_0, 0, x[(pair + 1) & 1]);
-            (void)add_columns(x[pair & 1], pair, w, mixed, dk);
+            odd |= add_columns(x[pair & 1], pair, w, mixed, dk);
         }
-        (void)add_columns(x[DT / 2 & 1], 0, w, mixed, dr);
+        odd |= add_columns(x[DT / 2 & 1], 0, w, mixed, dr);
+        if (__builtin_expect(__ballot(odd) != 0, 0)) {
+            // a key that is seen and not finite has a dS of NaN, or of 0 where its score is minus infinity: NaN times such a value
+            const uint32_t seen = seen_keys(death, key0, n, a.T, qpos, half);          // (again: it would be in the sums' way)
+            auto sees = [&](int r) { return sees_key(seen, r); };
+            auto weight = [](int) { return NAN; };
+            add_odd_values<Tiles::KB>(unit, sees, weight, dk);
+            add_odd_values<Tiles::RB>(unit + Tiles::ROT, sees, weight, dr);
+        }
     };
     own_rows_loaded();
     // (the tiles that this wave sees first, in a loop without branches: with one in it the sums would be kept twice)
@@ -846,7 +887,6 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
         f32x16 dv[DT];
 #pragma unroll
         for (int c = 0; c < DT; ++c) dv[c] = zeros16();
-        float poison = 0.f;                                // NaN: a gradient that is not finite arrives at a query that sees the key
         own_rows_loaded();
         for (int u = first; some && u < first + SLOTS - 2; ++u) load_ahead(u);
         for (int u = first; u < mine_first; ++u) round_begins(u);
@@ -879,20 +919,13 @@ void latent_replay_dkv_kernel(LatentReplayArgs a)
                 __builtin_amdgcn_sched_barrier(0);
                 odd |= add_columns(x[pair & 1], pair, w, mixed, dv);
             }
-            if (__ballot(odd)) {
-                const uint32_t rows = odd_rows<KB>(here + G);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int i = u * LR_STEP + row_of(r, half);
-                    if (((rows >> row_of(r, half)) & 1u) && key <= i && i < until) poison = NAN;
-                }
+            if (__builtin_expect(__ballot(odd) != 0, 0)) {
+                const int i0 = u * LR_STEP;
+                add_odd_values<KB>(here + G, [&](int r) { return key <= i0 + r && i0 + r < until; }, [&](int r) { return weight_of(w, r); }, dv);
             }
         }
         for (int u = mine_end; some && u <= units; ++u) round_begins(u);
         lds_loads_done();
-        poison += __shfl_xor(poison, 32);                  // (NaN in either half of the key's registers)
-#pragma unroll
-        for (int c = 0; c < DT; ++c) dv[c] += poison;
         store_rows(mine, dv, 1.0f, to + KB, stride, n - wave0);
     } else {
         bf16x8 v[KC];
