@@ -718,9 +718,11 @@ int ngc_paged_fill(const ngc_paged_cache *pc, int32_t layer, const void *k_new, 
  *   scale    positive, at most 2.35e38 (NGC_EINVAL otherwise)
  *   max_len_hint  as in ngc_decode_attn: steers how the work is split, never what is
  *            computed
- * A token that sees no row has zeros and -inf (an empty sequence is counted:
- * NGC_STATUS_EMPTY_ATTN).  Scores, soft-max and accumulation are fp32, weights are rounded
- * to bf16.  Values that are not finite reach the tokens that see their row, and no other.
+ * A token that sees no row, or none with a score above minus infinity, has zeros and -inf
+ * (an empty sequence is counted: NGC_STATUS_EMPTY_ATTN).  Scores, soft-max and accumulation
+ * are fp32, weights are rounded to bf16.  Values that are not finite reach the tokens that
+ * see their row, and no other: as the formula has it, by the row's score, and those of its
+ * latent part as NaN in their column.
  * ws must hold ngc_latent_workspace_bytes(), which serves every call on such a cache
  * with up to W new tokens; with less, down to its fixed part, fewer workgroups share
  * a sequence. */

@@ -38,6 +38,8 @@ __device__ __forceinline__ void wait_for_loads()
 // the compiler would count, inside the loop, the loads that may still be on their way on its first turn, and wait for the tiles asked
 // for ahead of it in their place, on every turn.
 __device__ __forceinline__ void own_rows_loaded() { __builtin_amdgcn_s_waitcnt(0x0F70); }       // vmcnt(0)
+// No access to LDS of this wave is on its way.
+__device__ __forceinline__ void lds_accesses_done() { __asm__ volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
 __device__ __forceinline__ void workgroup_barrier()
 {
     __asm__ volatile("s_barrier" : : : "memory");
@@ -72,5 +74,13 @@ __device__ __forceinline__ bool take_out_odd(u32x2 &x)
 }
 
 __device__ __forceinline__ bool has_odd(u32x2 x) { return take_out_odd(x); }
+// 1 where a value is not finite, 0 where it is.
+__device__ __forceinline__ u32x2 odd_ones(u32x2 x)
+{
+    u32x2 ones;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) ones[e] = ((x[e] & 0x7F80u) == 0x7F80u ? 0x3F80u : 0u) | ((x[e] & 0x7F800000u) == 0x7F800000u ? 0x3F800000u : 0u);
+    return ones;
+}
 
 }  // namespace ngc

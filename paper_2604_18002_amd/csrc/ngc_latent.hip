@@ -138,7 +138,7 @@ void latent_attn_kernel(LatentArgs a)
 
     extern __shared__ __align__(256) unsigned char lds[];
     float *const red = reinterpret_cast<float *>(lds + SLOTS * Tile::BYTES);             // [2][waves][rows]
-    uint32_t *const odd_rows = reinterpret_cast<uint32_t *>(red + 2 * NW * LT_ROWS);     // [slots][RG]
+    uint32_t *const odd_waves = reinterpret_cast<uint32_t *>(red + 2 * NW * LT_ROWS);    // [waves]
 
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(wave_id());
     const int rg = wv % RG, kg = wv / RG;
@@ -205,33 +205,6 @@ void latent_attn_kernel(LatentArgs a)
     const int last_row = block_row0 + RG * LT_ROWS - 1;
     const int end = s.limit(a, last_row < real_rows ? last_row : real_rows - 1);
     const int tiles = (end + KEYS - 1) / KEYS;
-    // Values of a tile that are not finite, where some query row does not see all of its rows: a weight of 0 would make NaN of them.  Every
-    // wave looks at what it has loaded itself: they become 0, and `odd_rows` says which rows had some.
-    auto take_out = [&](unsigned char *tile, uint32_t *word) {
-        uint32_t rows = 0;
-        auto look = [&](unsigned char *part, int r) {
-            u32x4 *const at = reinterpret_cast<u32x4 *>(part + lane * 16);
-            u32x2 lo = {(*at)[0], (*at)[1]}, hi = {(*at)[2], (*at)[3]};
-            const bool lo_odd = take_out_odd(lo), hi_odd = take_out_odd(hi);
-            if (lo_odd | hi_odd) {
-                *at = u32x4{lo[0], lo[1], hi[0], hi[1]};
-                rows |= 1u << r;
-            }
-        };
-#pragma unroll 1
-        for (int i = 0; i < LAT_LOADS; ++i) {
-            const int r0 = (i * RG + rg) * Tile::LAT_ROWS;
-            look(tile + r0 * Tile::LAT, r0 + lane / Tile::LAT_PIECES);
-        }
-#pragma unroll 1
-        for (int i = 0; i < ROT_LOADS; ++i) {
-            const int r0 = (i * RG + rg) % Tile::ROT_LOADS * Tile::ROT_ROWS;
-            look(tile + Tile::LAT_BYTES + r0 * Tile::ROT, r0 + lane / Tile::ROT_PIECES);
-        }
-        rows = wave_reduce(rows, [](uint32_t x, uint32_t y) { return x | y; });
-        if (lane == 0) word[rg] = rows;
-    };
-
     f32x4 oacc[CT];                                        // registers e of column tile c: columns 16 c + 4 quarter + e
 #pragma unroll
     for (int c = 0; c < CT; ++c) oacc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -243,7 +216,7 @@ void latent_attn_kernel(LatentArgs a)
     const int read_row = 4 * quarter + row / 4, read_col = 4 * (row % 4);                // of the transposing reads
     const uint32_t lat0 = Tile::piece(row, quarter), rot0 = Tile::piece(row, Tile::LAT_PIECES + quarter);
     const uint32_t col0 = Tile::piece(read_row, read_col / 8) + (uint32_t)(read_col % 8) * 2;
-    auto compute_tile = [&](int t, const unsigned char *tile, const uint32_t *odd, auto between) {
+    auto compute_tile = [&](int t, unsigned char *tile, auto between) {
         const uint32_t tile_at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char *)tile;
         auto row_piece = [&](int c, int k) {               // chunk c of rows 16 k ..
             const uint32_t at = c < LAT_CHUNKS ? ((tile_at + lat0) ^ (uint32_t)(c % 4 * 64)) + (uint32_t)(c / 4 * 256 + k * 16 * Tile::LAT)
@@ -288,22 +261,74 @@ void latent_attn_kernel(LatentArgs a)
                 for (int k = 0; k < HALVES; ++k) sc[k] = product16(__builtin_bit_cast(bf16x8, x[g % DEPTH][u][k]), qop[g * GROUP + u], sc[k]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        const bool mixed = key0 + KEYS > all;              // not every query row of the workgroup sees all of the tile's rows
         between();
+        // Values that are not finite, where some query row does not see their row: a weight of 0 would make NaN of them.  Every wave looks
+        // at what it has loaded itself.  (In a round of several key groups some may have such a tile and some not.)
+        if (RG == 1 ? mixed : (t - kg + KG) * KEYS > all) {
+            unsigned char *const own = tile + (Tile::LAT_ROWS == 2 ? lane / 32 * Tile::LAT + lane % 32 * 16 : lane * 16);
+            auto own_part = [&](auto &&f) {
+#pragma unroll 1
+                for (int k = 0; k < LAT_LOADS; ++k) {
+                    u32x4 *const at = reinterpret_cast<u32x4 *>(own + (k * RG + rg) * Tile::LAT_ROWS * Tile::LAT);
+                    f(at, *at);
+                }
+            };
+            bool odd = false;
+            if (mixed) own_part([&](u32x4 *, u32x4 x) { odd |= has_odd(u32x2{x[0], x[1]}) | has_odd(u32x2{x[2], x[3]}); });
+            bool some = __ballot(odd) != 0;
+            if constexpr (RG > 1) {
+                if (lane == 0) odd_waves[wv] = some;
+                lds_accesses_done();
+                workgroup_barrier();
+                uint32_t any = 0;
+#pragma unroll
+                for (int k = 0; k < NW; ++k) any |= odd_waves[k];
+                some = __builtin_amdgcn_readfirstlane(any) != 0;
+            }
+            if (__builtin_expect(some, 0)) {
+                // They become NaN in the columns of the query rows that see theirs: such a row's score is not finite, its weight NaN, or 0
+                // for minus infinity, and NaN is what either makes of them.  How many of a column a query row sees is another product.
+                // Then they become 0.
+                if (mixed) {
+                    uint32_t sees[SCORES / 2];
+#pragma unroll
+                    for (int e = 0; e < SCORES / 2; ++e)
+                        sees[e] = (key0 + latent_key(2 * e, quarter) < limit ? 0x3F80u : 0u) | (key0 + latent_key(2 * e + 1, quarter) < limit ? 0x3F800000u : 0u);
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) {
+                        u32x2 y[HALVES];
+#pragma unroll
+                        for (int h = 0; h < HALVES; ++h) y[h] = odd_ones(transposed(h, c));
+                        const f32x4 count = add_rows(y, sees, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) oacc[c][e] = count[e] > 0.f ? NAN : oacc[c][e];
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                if constexpr (RG > 1) {
+                    lds_accesses_done();
+                    workgroup_barrier();
+                }
+                if (mixed)
+                    own_part([&](u32x4 *at, u32x4 x) {
+                        u32x2 lo = {x[0], x[1]}, hi = {x[2], x[3]};
+                        take_out_odd(lo);
+                        take_out_odd(hi);
+                        *at = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                    });
+                lds_accesses_done();
+                if constexpr (RG > 1) workgroup_barrier();
+            }
+        }
         ask_columns(0);                                    // (there when the weights are)
         __builtin_amdgcn_sched_barrier(0);
         float s_[SCORES];
 #pragma unroll
         for (int e = 0; e < SCORES; ++e) s_[e] = sc[e / 4][e % 4];
-        if (key0 + KEYS > all) {                        // not every query row of the workgroup sees all of the tile's rows
+        if (mixed) {
 #pragma unroll
             for (int e = 0; e < SCORES; ++e) s_[e] = key0 + latent_key(e, quarter) < limit ? s_[e] : -INFINITY;
-            uint32_t rows = 0;
-#pragma unroll
-            for (int i = 0; i < RG; ++i) rows |= odd[i];
-            if (rows)                                      // who sees such a row becomes NaN
-#pragma unroll
-                for (int e = 0; e < SCORES; ++e)
-                    if ((rows >> latent_key(e, quarter)) & 1u) s_[e] = key0 + latent_key(e, quarter) < limit ? NAN : -INFINITY;
         }
         float tmx = s_[0];
 #pragma unroll
@@ -355,11 +380,6 @@ void latent_attn_kernel(LatentArgs a)
         if (issued == i + NB - 1) wait_for_loads<(NB - 2) * LOADS>();
         else wait_for_loads<0>();
         unsigned char *const tile = buffers + slot * Tile::BYTES;
-        uint32_t *const odd = odd_rows + (kg * NB + slot) * RG;
-        if ((t + 1) * KEYS > all) {                        // (or LDS that holds anything)
-            take_out(tile, odd);
-            wait_for_loads<(NB - 2) * LOADS>();
-        }
         if constexpr (RG > 1) workgroup_barrier();         // (or a wave's tiles are its own)
         auto load_next = [&] {
             if (issued < mine) {
@@ -369,7 +389,7 @@ void latent_attn_kernel(LatentArgs a)
         };
         if (!LATER || kg % 2 == 0) load_next();
         // (a key group without a tile in the last round computes one that nobody sees)
-        compute_tile(t, tile, odd, [&] {
+        compute_tile(t, tile, [&] {
             if (LATER && kg % 2) load_next();
         });
     }
@@ -549,7 +569,7 @@ extern "C" int ngc_latent_attn(const ngc_paged_cache *pc, int32_t layer, const i
     const void *fn;
     size_t lds;
 #define NGC_PICK_LATENT(R_, E_) \
-    lds = LT_LDS_KEYS * (R_ + E_) * 2 + (2 * 8 * LT_ROWS + 32) * sizeof(float); \
+    lds = LT_LDS_KEYS * (R_ + E_) * 2 + (2 * 8 * LT_ROWS + 8) * sizeof(float); \
     fn = shape.groups == 1   ? reinterpret_cast<const void *>(&latent_attn_kernel<R_, E_, 4, 1>) \
                              : reinterpret_cast<const void *>(&latent_attn_kernel<R_, E_, 8, 4>)
     if (R == 512) { NGC_PICK_LATENT(512, 64); }

@@ -69,3 +69,49 @@ def test_a_row_far_below_the_others(D, Hq, B, hint, want):
     out, lse = c.run(hint=hint)
     assert bool(torch.isnan(out[0, 0].float()).all()) and bool(torch.isnan(lse[0, 0]).all())
     assert B == 1 or bool(torch.isfinite(out[0, 1:].float()).all())
+
+
+def formula(rows, q, scale, R):
+    """All rows seen, in 64 bits, term by term: a score of minus infinity is a weight of 0 (and 0 times infinity NaN)."""
+    import torch
+    x = (q.unsqueeze(1) * rows).sum(-1) * scale
+    p = torch.softmax(x, 1)
+    out = torch.stack([(p[h].unsqueeze(1) * rows[:, :R]).sum(0) for h in range(q.shape[0])])
+    return x, out, torch.logsumexp(x, 1)
+
+
+@pytest.mark.parametrize("n", [60, 150])
+@pytest.mark.parametrize("D,Hq,B,hint,want", CALLS + [(576, 40, 32, 257, (4, 1)), (288, 65, 32, 257, (4, 1))])
+def test_as_the_formula_has_it(D, Hq, B, hint, want, n):
+    """Finite where the formula is, whether all of the workgroup's queries see the tile or not; and there within the bounds of the other rows."""
+    import torch
+    from _latent import attention
+    W = 1 if (Hq, B) not in ((40, 32), (65, 32)) else 4
+    c = Case(43, B, Hq, D, 32, [n] * B, W, max_pages=256)
+    assert shape(c, hint) == want
+    clean, clean_lse = c.run(hint=hint)
+    for at in (3, n - 23, n - 21, n - 7, n - 3, n - 1):
+        page, row = int(c.pc.table[0, 0, 0, at // 32]), at % 32
+        kept = c.pc.k_pool[page, row].clone()
+        for col in (7, c.R - 1, c.R, D - 2):
+            for odd in (NAN, INF, -INF):
+                c.pc.k_pool[page, row, col] = odd
+                out, lse = c.run(hint=hint)
+                rows = c.rows(0, 0)
+                c.pc.k_pool[page, row] = kept
+                assert torch.equal(out[0, 1:], clean[0, 1:]) and torch.equal(lse[0, 1:], clean_lse[0, 1:])
+                for i in range(W):
+                    limit = n - W + i + 1
+                    if at >= limit:                      # not seen
+                        assert torch.equal(out[0, 0, i], clean[0, 0, i]) and torch.equal(lse[0, 0, i], clean_lse[0, 0, i])
+                        continue
+                    q = c.q[0, 0, i].double()
+                    x, o, z = formula(rows[:limit], q, c.scale, c.R)
+                    assert torch.equal(torch.isfinite(out[0, 0, i].float()), torch.isfinite(o)), (at, col, odd, i)
+                    assert torch.equal(torch.isfinite(lse[0, 0, i]), torch.isfinite(z)), (at, col, odd, i)
+                    left = x[:, at] == -INF              # heads without this row
+                    others = torch.cat([rows[:at], rows[at + 1:limit]])
+                    o, z, tol, tol_z = attention(others, q[left], torch.full((int(left.sum()),), limit - 1, device="cuda"), c.scale, c.R)
+                    good = (out[0, 0, i, left].double() - o).abs() <= tol
+                    good[:, col:col + 1] |= col < c.R    # (NaN there)
+                    assert bool(good.all()) and bool(((lse[0, 0, i, left].double() - z).abs() <= tol_z).all()), (at, col, odd, i)
