@@ -23,8 +23,9 @@
 // 1000 to 2000 rows (35 us; 18 for the bytes) has ~5 us until the first tile is there, lengths 1.3 times the mean in its longest
 // workgroups, 3 us of partials and a joining launch of 4.7; one of 128 x 128 x 1894 to 3533 (135 us; 78 for the products) its lengths.
 //
-// P is rounded to bf16 for the second product (2^-9 of an entry at most), as the output is: it is the operand of the
-// product that brings the latent vectors to the heads' values.  Sums and soft-max state are fp32.
+// P is rounded to bf16 for the second product (half a step: 2^-8 of an entry at most), since the rows are bf16 and the matrix instructions
+// take operands of one type: in two parts it would be half as many products again, for an error that the output's own rounding (it is
+// the operand of the product that brings the latent vectors to the heads' values) has too.  Sums and soft-max state are fp32.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -127,10 +128,9 @@ void latent_attn_kernel(LatentArgs a)
     using Tile = LatentTile<R, E, KEYS>;
     constexpr int KG = NW / RG;
     constexpr int NB = SLOTS / KG;                         // buffers of a key group
-    static_assert(NB >= 2, "a tile is on its way while one is worked on");
+    static_assert(NB == 2, "a tile is on its way while one is worked on");
     constexpr int CHUNKS = (R + E) / 32, LAT_CHUNKS = R / 32, CT = R / 16;               // of the first product; column tiles of the second
     constexpr int LAT_LOADS = (Tile::LAT_LOADS + RG - 1) / RG, ROT_LOADS = (Tile::ROT_LOADS + RG - 1) / RG;      // of a wave, per tile
-    constexpr int LOADS = LAT_LOADS + ROT_LOADS;
     // A wave is held up where it asks for a tile, about 100 clocks a load.  The two waves of a SIMD, of different key groups, do it at
     // different times: 343 us for 380 with 256 sequences of 4096 rows and 128 heads, R = 512.
     constexpr bool LATER = RG > 1;
@@ -371,21 +371,14 @@ void latent_attn_kernel(LatentArgs a)
     const int mine = first_tile < tiles ? (tiles - first_tile + stride - 1) / stride : 0;
     // how many rounds the workgroup takes (key group 0 has the most tiles)
     const int rounds = split * KG < tiles ? (tiles - split * KG + stride - 1) / stride : 0;
-    int issued = 1;                                        // (that one in any case)
-    for (; issued < NB - 1 && issued < mine; ++issued) load_tile(tile_base(first_tile + issued * stride), buffers + issued * Tile::BYTES);
-    static_assert(NB == 2, "the first tile alone is on its way here");
     own_rows_loaded();
     for (int i = 0; i < (RG == 1 ? mine : rounds); ++i) {
-        const int t = first_tile + i * stride, slot = i % NB;
-        if (issued == i + NB - 1) wait_for_loads<(NB - 2) * LOADS>();
-        else wait_for_loads<0>();
-        unsigned char *const tile = buffers + slot * Tile::BYTES;
+        const int t = first_tile + i * stride;
+        wait_for_loads<0>();
+        unsigned char *const tile = buffers + i % NB * Tile::BYTES;
         if constexpr (RG > 1) workgroup_barrier();         // (or a wave's tiles are its own)
         auto load_next = [&] {
-            if (issued < mine) {
-                load_tile(tile_base(first_tile + issued * stride), buffers + issued % NB * Tile::BYTES);
-                ++issued;
-            }
+            if (i + 1 < mine) load_tile(tile_base(t + stride), buffers + (i + 1) % NB * Tile::BYTES);
         };
         if (!LATER || kg % 2 == 0) load_next();
         // (a key group without a tile in the last round computes one that nobody sees)
