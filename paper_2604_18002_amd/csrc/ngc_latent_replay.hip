@@ -39,8 +39,9 @@
 // waves a workgroup (317 us with evictions, keys that live for different times; 5 % faster without); units of keys one by one in
 // a ring of four (forward 167 us for 137: a barrier and the offsets for every 32 keys); loads spread between the products.
 //
-// P and dS are rounded to bf16 (2^-8 of an entry at most) for their second products, as outputs and gradients are; sums,
-// maxima, lse and delta are fp32.
+// P and dS are rounded to bf16 (half a step: 2^-8 of an entry at most) for their second products, whose other operand is bf16 as it comes
+// (in two parts, half as many products again), as outputs and gradients are; delta is of the output as it is stored, which is what a
+// caller has kept.  Sums, maxima, lse and delta are fp32.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -292,7 +293,7 @@ struct LiveUnits {
 };
 
 // What a workgroup that owns queries (forward, backward q) or keys (backward kv) works on: `at_once` (trajectory, head)s at a time (0:
-// all), the heaviest blocks of each first; their number is a multiple of 8, so that each keeps to one XCD, whose L2 then has its rows.
+// all), the heaviest blocks of each first.  Where their number is a multiple of 8 each keeps to one XCD, whose L2 then has its rows.
 // Few at a time read less (backward kv, 16 for all 32 of 2 x 3850 positions, 16 heads: half the misses, 437 us for 451 with
 // backward q); the queries' owners read less in the first place and fare better with the heaviest of all first (16 x 1050 positions:
 // 95 us for 100).
