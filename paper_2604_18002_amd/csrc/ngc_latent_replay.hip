@@ -222,6 +222,25 @@ __device__ __forceinline__ void add_odd_values(const unsigned char *x, Sees sees
             }
     }
 }
+// NaN in the columns of who sees a value that is not finite: how many of them is another product.
+template <int BYTES, int CT>
+__device__ __forceinline__ void odd_becomes_nan(const unsigned char *x, const uint32_t (&first)[2], const uint32_t (&sees)[8], f32x16 (&acc)[CT])
+{
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        f32x16 count = zeros16();
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            u32x2 y[2];
+#pragma unroll
+            for (int g = 0; g < 2; ++g) y[g] = odd_ones(read_transposed16(x + (first[g] ^ c * 64) + 16 * st * BYTES));
+            count = product(operand(u32x4{y[0][0], y[0][1], y[1][0], y[1][1]}), operand(u32x4{sees[4 * st], sees[4 * st + 1], sees[4 * st + 2], sees[4 * st + 3]}), count);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[c][r] = count[r] > 0.f ? NAN : acc[c][r];
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
 // Weight of row r (uniform) of a unit and this lane's column, of the 32 x 32 as packed for the second product.
 __device__ __forceinline__ float weight_of(const uint32_t (&w)[8], int r)
 {
@@ -659,10 +678,11 @@ void latent_replay_dq_kernel(LatentReplayArgs a)
         if (__builtin_expect(__ballot(odd) != 0, 0)) {
             // a key that is seen and not finite has a dS of NaN, or of 0 where its score is minus infinity: NaN times such a value
             const uint32_t seen = seen_keys(death, key0, n, a.T, qpos, half);          // (again: it would be in the sums' way)
-            auto sees = [&](int r) { return sees_key(seen, r); };
-            auto weight = [](int) { return NAN; };
-            add_odd_values<Tiles::KB>(unit, sees, weight, dk);
-            add_odd_values<Tiles::RB>(unit + Tiles::ROT, sees, weight, dr);
+            uint32_t sees[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sees[e] = ((seen >> 2 * e) & 1u ? 0x3F80u : 0u) | ((seen >> (2 * e + 1)) & 1u ? 0x3F800000u : 0u);
+            odd_becomes_nan<Tiles::KB>(unit, kt_0, sees, dk);
+            odd_becomes_nan<Tiles::RB>(unit + Tiles::ROT, rt_0, sees, dr);
         }
     };
     own_rows_loaded();
