@@ -93,3 +93,11 @@ def test_every_row_is_there_once(D, Hq, lens, hint, want):
         assert bool(((lse - score).abs() < score * 2.0 ** -20).all()), at
         for b in range(len(lens)):
             assert torch.equal(out[0, b, 0], rows[b][j[b]]), (at, b)
+
+
+@pytest.mark.parametrize("D,Hq,W,lens,n_new,groups", [(576, 128, 200, [700, 77], [200, 77], 4), (288, 128, 130, [1000, 129, 400], [130, 1, 70], 4), (576, 40, 1024, [1024], [1024], 4),
+                                                      (288, 20, 300, [2500, 300], [299, 300], 4), (576, 8, 17, [5000], [17], 1), (288, 8, 33, [64, 40], [33, 17], 1)])
+def test_prompts_behind_a_prefix(D, Hq, W, lens, n_new, groups):
+    c = Case(35, len(lens), Hq, D, 32, lens, W, n_new)
+    assert shape(c, c.pc.cap)[0] == groups
+    c.check(*c.run())
