@@ -735,7 +735,7 @@ bool fits_static(const ngc_cache *c, int nseg_launch, int S)
 }
 }  // namespace
 
-extern "C" int ngc_version(void) { return 240; }
+extern "C" int ngc_version(void) { return 241; }
 
 extern "C" const char *ngc_strerror(int code)
 {
