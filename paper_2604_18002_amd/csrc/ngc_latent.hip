@@ -20,7 +20,7 @@
 // reads alone reach; 64 heads 6.3 TB/s; 128 heads 940 TFLOP/s and 3.9 TB/s, where a large product of matrices reaches 1230.  There a
 // wave's products wait for its own reads of LDS (256 bytes a clock: 30 % of it is used) and for the loads' issue, ~100 clocks each;
 // the other wave of the SIMD covers a part, the matrix units are busy 40 % of the time.  Besides that, a call of 64 sequences x 16 heads x
-// 1000 to 2000 rows (35 us; 18 for the bytes) has ~5 us until the first tile is there, lengths 1.3 times the mean in its longest
+// 1000 to 2000 rows (33 us; 18 for the bytes) has ~5 us until the first tile is there, lengths 1.3 times the mean in its longest
 // workgroups, 3 us of partials and a joining launch of 4.7; one of 128 x 128 x 1894 to 3533 (135 us; 78 for the products) its lengths.
 //
 // P is rounded to bf16 for the second product (half a step: 2^-8 of an entry at most), since the rows are bf16 and the matrix instructions

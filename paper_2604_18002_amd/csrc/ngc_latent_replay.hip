@@ -28,8 +28,8 @@
 //
 // What bounds it.  2 (2 D + E) flops a pair forward, 2 (3 (D + E) + 2 D) + 2 (2 D + E) backward (D = 128: 640 and 1664 with what is formed
 // twice left out) on 16-bit inputs: the products, for more than some hundred positions.  Measured, 16 heads of 128: 8192 positions
-// without evictions 920 TFLOP/s forward (373 us; two of them 945) and 670 to 690 backward, where a large product of matrices reaches 1230;
-// 2 x 3000 to 3850 positions with evictions every 512, 117 us forward, 171 us the queries' and 278 us the keys' gradients.  A step of 32 x
+// without evictions 920 TFLOP/s forward (371 us; two of them 945) and 670 to 690 backward, where a large product of matrices reaches 1230;
+// 2 x 3000 to 3850 positions with evictions every 512, 126 us forward, 186 us the queries' and 292 us the keys' gradients.  A step of 32 x
 // 32 pairs is 640 clocks of products and some 700 of vector work forward, and two waves overlap little of them: the matrix units are
 // busy 45 % of the time without evictions.  With evictions a workgroup has few tiles and its first one, 2.5 us, and the look at the ends, 1.5, count.
 //   Registers decide: two waves a SIMD have 256 each, and one more copy of the sums (a branch around a unit makes the compiler keep
